@@ -428,7 +428,8 @@ def _plain_crcs(buf, chunk, tables, out):
 def _plain_policy(s):
     """Sums over the vocabulary in 32 bits; what hangs on a token's log-probability, with the clipping's
     borders, in 64."""
-    z, w, adv = s.logits.float(), s.weights.double(), s.advantages.double()
+    z = s.logits.to(torch.float32, copy=True)  # made the exponentials below
+    w, adv = s.weights.double(), s.advantages.double()
     inside = (s.targets >= 0) & (s.targets < z.shape[1])
     y = torch.where(inside, s.targets, 0)[:, None]
     m = z.amax(1, keepdim=True)
