@@ -300,6 +300,129 @@ int ff_adam_step_chained(const ff_plan *plan, const void *const *grads, const ff
                          float inv_loss_scale, uint64_t *n_nonfinite, const void *prev_chunks,
                          void *chunks, uint32_t *crcs, void *hip_stream);
 
+/* ---- between the loss and the step: gradient norm, clipping, clipped step --------------------- */
+
+/*
+ * A list of gradient tensors: sizes, formats and addresses, laid out once.  segs: HOST array of n
+ * descriptors, copied; FF_BF16, FF_F16 and FF_F32 tensors may be mixed, kind must be FF_KIND_RAW.
+ * Empty tensors and an empty list are allowed.  flags: 0 or FF_PLAN_HOST_ONLY.  The list keeps small device tables
+ * on the device that is current at the time of the call and does not change afterwards; the rules for
+ * calls on one plan hold for calls on one list, every call that is in flight with a workspace of its own.
+ * Addresses may be left out (NULL) if every call brings its own.
+ * Errors as for ff_snapshot_plan, but an empty list is none.
+ */
+typedef struct ff_grad_list ff_grad_list; /* opaque */
+int ff_grad_list_create(const ff_segment *segs, uint64_t n, uint32_t flags, ff_grad_list **out);
+void ff_grad_list_destroy(ff_grad_list *list); /* as ff_plan_destroy */
+uint64_t ff_grad_list_numel(const ff_grad_list *list);           /* elements of all tensors   */
+uint64_t ff_grad_list_workspace_bytes(const ff_grad_list *list); /* what ff_grad_norm is given */
+
+/* What is known about a list of gradients; DEVICE, 8-byte aligned.  Calls read it where it lies, so that
+ * no host waits for a norm before the update can be enqueued. */
+typedef struct {
+    double sumsq;         /* sum of the squares of the elements as stored                      */
+    uint64_t n_nonfinite; /* infinite or NaN elements                                          */
+    double norm;          /* sqrt(sumsq) * inv_loss_scale                                      */
+    float scale;          /* what clipping multiplies a stored element by:
+                             inv_loss_scale * min(1, max_norm / norm); 0 if skip               */
+    uint32_t skip;        /* n_nonfinite > 0: clipping and update are left out                 */
+} ff_grad_stats;
+
+/*
+ * Global L2 norm over all tensors of the list, and what follows from it for clipping.  Squares and
+ * sums are held in 64 bits: no finite element overflows or underflows; the order of the sums depends on the
+ * list alone, so the same values give the same bits.  grads: HOST array of n DEVICE pointers in the list's order, each
+ * aligned to its element (entries of empty tensors are ignored), or NULL for the list's own addresses.
+ * inv_loss_scale: finite and > 0 (1 without a loss scale); max_norm: > 0, INFINITY for no clipping.
+ * stats: DEVICE, 8-byte aligned.  workspace: DEVICE, 16-byte aligned, ff_grad_list_workspace_bytes() bytes,
+ * ZERO before its first use; every call leaves it as the next one needs it.
+ */
+int ff_grad_norm(const ff_grad_list *list, const void *const *grads, double inv_loss_scale,
+                 double max_norm, void *workspace, ff_grad_stats *stats, void *hip_stream);
+
+/*
+ * The same for gradients that are spread over several workers (or several lists): parts: DEVICE array of
+ * n_parts >= 1 stats, one from each worker's ff_grad_norm, gathered in rank order; their sumsq and n_nonfinite
+ * are summed up in that order, so every worker arrives at the same bits.  stats may be one of the
+ * parts.
+ */
+int ff_grad_norm_join(const ff_grad_stats *parts, uint64_t n_parts, double inv_loss_scale,
+                      double max_norm, ff_grad_stats *stats, void *hip_stream);
+
+/*
+ * Clipping in place, for an optimizer other than this library's step: every element g of the list becomes
+ * g * stats->scale, one fp32 multiplication rounded to the tensor's format.  Nothing is touched if
+ * stats->skip is set (what overflowed stays to be looked at) or the scale is exactly 1.  grads as for ff_grad_norm.
+ */
+int ff_grad_clip(const ff_grad_list *list, const void *const *grads, const ff_grad_stats *stats,
+                 void *hip_stream);
+
+/*
+ * The optimizer step with the snapshot in the same pass on clipped gradients: ff_adam_step_snapshot, or for an fp16 plan
+ * ff_adam_step_snapshot_f16, with g = float(grad) * stats->scale (one rounded fp32 multiplication, the
+ * loss scale included); prev_chunks: NULL, or the previous snapshot as for ff_adam_step_chained.  If stats->skip is
+ * set the update is left out: master, m and v keep their bits, the 16-bit weights are rounded from
+ * the master (a NaN to the format's canonical one), and the snapshot holds that state.  stats: DEVICE, read when the
+ * stream gets there.  Gradients, hp, chunks, crcs and errors as for those steps.
+ */
+int ff_adam_step_clipped(const ff_plan *plan, const void *const *grads, const ff_adam_hparams *hp,
+                         const ff_grad_stats *stats, const void *prev_chunks, void *chunks,
+                         uint32_t *crcs, void *hip_stream);
+
+/* ---- clipped policy loss with a KL term, and its gradient ------------------------------------- */
+
+/*
+ * One batch of tokens.  logits: n_tokens rows of `vocab` elements of `dtype`, row_stride >= vocab elements apart
+ * (the last row need not be padded); aligned to the element.  All arrays DEVICE; targets int64, the others fp32,
+ * n_tokens each.  weights: what a token counts in the loss, its share of the mean included; 0 leaves it
+ * out (prompts, padding): its row is not read.
+ */
+typedef struct {
+    const void *logits;
+    uint64_t n_tokens, vocab, row_stride;
+    uint32_t dtype;    /* FF_BF16, FF_F16 or FF_F32 */
+    uint32_t reserved; /* must be 0 */
+    const int64_t *targets;
+    const float *old_logp;   /* log-probability under the policy that made the token */
+    const float *ref_logp;   /* ... under the reference policy, or NULL: no KL term  */
+    const float *advantages;
+    const float *weights;
+    float clip_low, clip_high; /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; 0 <= clip_low <= 1,
+                                  0 <= clip_high                                     */
+    float beta;                /* >= 0, of the KL term; > 0 needs ref_logp           */
+    float loss_scale;          /* finite, > 0: the gradient is that of loss * loss_scale */
+} ff_policy_batch;
+
+/* DEVICE, 8-byte aligned */
+typedef struct {
+    float loss, kl;      /* sums of weight * token loss, and of weight * KL                      */
+    uint64_t n_tokens;   /* that count                                                            */
+    uint64_t n_clipped;  /* of these: the clipped product was the smaller one                    */
+    uint64_t n_invalid;  /* weight not 0 and yet left out: target outside the vocabulary, or every logit -inf */
+} ff_policy_stats;
+
+uint64_t ff_policy_workspace_bytes(uint64_t n_tokens, uint64_t vocab);
+
+/*
+ * For every token with weight w != 0, target y, logits z, advantage A:
+ *     logp  = z_y - log(sum_j exp(z_j))            r = exp(logp - old_logp)
+ *     token = -min(r * A, clip(r) * A) + beta * kl, kl = exp(d) - d - 1 with d = ref_logp - logp
+ *     loss  = sum of w * token
+ *     dlogits_j = loss_scale * w * slope * ([j = y] - exp(z_j) / sum exp),
+ *     slope = (the clipped product is the smaller ? 0 : -r * A) + beta * (1 - exp(d))
+ * Sums over the vocabulary in fp32 against the row's largest logit and joined in fp64, what hangs on logp in
+ * fp64; the gradient is rounded once.  Logits of -inf are probabilities of 0.  A row with a NaN or +inf gives NaN in its outputs and
+ * its whole gradient row (which ff_grad_norm finds downstream).  A token that is left out (weight 0 or invalid) has logp and token
+ * loss 0 and a gradient row of zeros.
+ * logp, token_loss: DEVICE fp32[n_tokens]; logp may be old_logp's array only if that is not needed again, so it may
+ * not alias any input.  dlogits: NULL (no gradient), or DEVICE, of `dtype`, rows grad_stride >= vocab elements apart; it may
+ * be the logits themselves with the same stride, and elements between rows are not touched.
+ * stats: DEVICE.  workspace: DEVICE, 16-byte aligned, ff_policy_workspace_bytes(); nothing is expected in it.
+ * n_tokens = 0 is allowed: the stats become zero.  FF_ERR_INVALID for vocab 0 or above 2^31 - 1.
+ */
+int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss, void *dlogits,
+                   uint64_t grad_stride, ff_policy_stats *stats, void *workspace, void *hip_stream);
+
 /* Test helper: CRC32C of nbytes at dev_buf (DEVICE, 16-byte aligned) into *dev_out (DEVICE),
  * computed by the same tile and combine kernels as ff_pack.  Allocates and frees a small
  * scratch array, so it synchronises the stream before returning. */

@@ -44,7 +44,10 @@ EXPORTS = ["ff_snapshot_plan", "ff_plan_destroy", "ff_plan_payload_bytes", "ff_p
            "ff_plan_num_params", "ff_plan_layout_id", "ff_plan_segment_range",
            "ff_plan_chunk_span", "ff_razor_select", "ff_pack", "ff_pack_to_host", "ff_restore", "ff_restore_checked", "ff_restore_chunks", "ff_adam_step_snapshot",
            "ff_adam_step_snapshot_f16", "ff_adam_step_chained", "ff_crc32c", "ff_crc32c_noalloc",
-           "ff_copy_ceiling", "ff_mix_ceiling", "ff_strerror"]
+           "ff_copy_ceiling", "ff_mix_ceiling", "ff_strerror",
+           "ff_grad_list_create", "ff_grad_list_destroy", "ff_grad_list_numel",
+           "ff_grad_list_workspace_bytes", "ff_grad_norm", "ff_grad_norm_join", "ff_grad_clip",
+           "ff_adam_step_clipped", "ff_policy_workspace_bytes", "ff_policy_loss"]
 
 
 class ff_segment(ctypes.Structure):
@@ -57,6 +60,17 @@ class ff_adam_hparams(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float),
                 ("step", ctypes.c_uint32)]
+
+
+class ff_policy_batch(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
+                ("vocab", ctypes.c_uint64), ("row_stride", ctypes.c_uint64),
+                ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
+                ("targets", ctypes.c_void_p), ("old_logp", ctypes.c_void_p),
+                ("ref_logp", ctypes.c_void_p), ("advantages", ctypes.c_void_p),
+                ("weights", ctypes.c_void_p), ("clip_low", ctypes.c_float),
+                ("clip_high", ctypes.c_float), ("beta", ctypes.c_float),
+                ("loss_scale", ctypes.c_float)]
 
 
 class ff_razor_config(ctypes.Structure):
@@ -126,6 +140,23 @@ def lib():
         L.ff_copy_ceiling.restype, L.ff_copy_ceiling.argtypes = i32, [vp, vp, u64, vp]
         L.ff_mix_ceiling.restype = i32
         L.ff_mix_ceiling.argtypes = [vp, vp, vp, vp, vp]
+        L.ff_grad_list_create.restype = i32
+        L.ff_grad_list_create.argtypes = [ctypes.POINTER(ff_segment), u64, u32, ctypes.POINTER(vp)]
+        L.ff_grad_list_destroy.restype = None
+        L.ff_grad_list_destroy.argtypes = [vp]
+        for name in ("numel", "workspace_bytes"):
+            fn = getattr(L, "ff_grad_list_" + name)
+            fn.restype, fn.argtypes = u64, [vp]
+        f64 = ctypes.c_double
+        L.ff_grad_norm.restype, L.ff_grad_norm.argtypes = i32, [vp, vp, f64, f64, vp, vp, vp]
+        L.ff_grad_norm_join.restype = i32
+        L.ff_grad_norm_join.argtypes = [vp, u64, f64, f64, vp, vp]
+        L.ff_grad_clip.restype, L.ff_grad_clip.argtypes = i32, [vp, vp, vp, vp]
+        L.ff_adam_step_clipped.restype = i32
+        L.ff_adam_step_clipped.argtypes = [vp, vp, ctypes.POINTER(ff_adam_hparams), vp, vp, vp, vp, vp]
+        L.ff_policy_workspace_bytes.restype, L.ff_policy_workspace_bytes.argtypes = u64, [u64, u64]
+        L.ff_policy_loss.restype = i32
+        L.ff_policy_loss.argtypes = [ctypes.POINTER(ff_policy_batch), vp, vp, vp, u64, vp, vp, vp]
         L.ff_strerror.restype, L.ff_strerror.argtypes = ctypes.c_char_p, [i32]
         _lib = L
     return _lib
@@ -342,3 +373,150 @@ def alloc_outputs(plan, device):
     bad = torch.empty(plan.num_chunks, dtype=torch.int32, device=device)
     n_bad = torch.empty(1, dtype=torch.int64, device=device)
     return chunks, crcs, bad, n_bad
+
+
+# ---- between the loss and the step ---------------------------------------------------------------
+
+class GradStats:
+    """Device memory for `n` ff_grad_stats (one per rank for ff_grad_norm_join), and views of the
+    first one's fields: 0-dimensional device tensors, so that looking at one costs no
+    synchronisation until its value is asked for."""
+
+    def __init__(self, device, n=1):
+        self.words = torch.zeros(n, 4, dtype=torch.float64, device=device)
+        first = self.words[0]
+        self.sumsq, self.norm = first[0], first[2]
+        self.n_nonfinite = first.view(torch.int64)[1]
+        self.scale = first.view(torch.float32)[6]
+        self.skip = first.view(torch.int32)[7]
+
+    def data_ptr(self):
+        return self.words.data_ptr()
+
+
+class GradList:
+    """Owns an ff_grad_list handle; keeps the tensors it points at alive."""
+
+    def __init__(self, handle, keepalive):
+        self.handle = handle
+        self._keepalive = keepalive
+
+    def destroy(self):
+        if self.handle:
+            lib().ff_grad_list_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    numel = property(lambda s: int(lib().ff_grad_list_numel(s.handle)))
+    workspace_bytes = property(lambda s: int(lib().ff_grad_list_workspace_bytes(s.handle)))
+
+
+def ff_grad_list(tensors, flags=0):
+    """The list of these gradients (contiguous; bf16, fp16 and fp32 may be mixed)."""
+    out = ctypes.c_void_p()
+    _check(lib().ff_grad_list_create(make_segments(tensors), len(tensors), flags, ctypes.byref(out)))
+    return GradList(out, list(tensors))
+
+
+def alloc_grad_workspace(grad_list, device):
+    return torch.zeros(max(16, grad_list.workspace_bytes), dtype=torch.uint8, device=device)
+
+
+def _list_pointers(grads):
+    """(array to keep alive across the call, its address): none for the list's own addresses."""
+    if grads is None:
+        return None, None
+    ptrs = _grad_pointers(grads)
+    return ptrs, ptrs.buffer_info()[0]
+
+
+def ff_grad_norm(grad_list, stats, workspace, max_norm=float("inf"), inv_loss_scale=1.0, grads=None,
+                 stream=None):
+    """grads: other tensors than the list's own, of the same sizes and formats."""
+    keep, ptrs = _list_pointers(grads)
+    _check(lib().ff_grad_norm(grad_list.handle, ptrs, inv_loss_scale, max_norm, workspace.data_ptr(),
+                              stats.data_ptr(), _stream_ptr(stream)))
+
+
+def ff_grad_norm_join(parts, stats, max_norm=float("inf"), inv_loss_scale=1.0, stream=None):
+    """parts: a GradStats of several (its `words` gathered from the ranks)."""
+    _check(lib().ff_grad_norm_join(parts.data_ptr(), parts.words.shape[0], inv_loss_scale, max_norm,
+                                   stats.data_ptr(), _stream_ptr(stream)))
+
+
+def ff_grad_clip(grad_list, stats, grads=None, stream=None):
+    keep, ptrs = _list_pointers(grads)
+    _check(lib().ff_grad_clip(grad_list.handle, ptrs, stats.data_ptr(), _stream_ptr(stream)))
+
+
+def ff_adam_step_clipped(plan, grads, hparams, stats, chunks, crcs, prev_chunks=None, stream=None):
+    """The step on gradients clipped (and unscaled) by stats.scale; in place, or from the previous
+    snapshot.  grads in the plan's 16-bit format."""
+    ptrs = _grad_pointers(grads)
+    hp = ff_adam_hparams(hparams["lr"], hparams["beta1"], hparams["beta2"], hparams["eps"],
+                         hparams["weight_decay"], hparams["step"])
+    _check(lib().ff_adam_step_clipped(
+        plan.handle, ptrs.buffer_info()[0], ctypes.byref(hp), stats.data_ptr(),
+        prev_chunks.data_ptr() if prev_chunks is not None else None, chunks.data_ptr(),
+        crcs.data_ptr(), _stream_ptr(stream)))
+
+
+class PolicyStats:
+    """Device memory for an ff_policy_stats, and views of its fields (see GradStats)."""
+
+    def __init__(self, device):
+        self.words = torch.zeros(4, dtype=torch.int64, device=device)
+        f = self.words.view(torch.float32)
+        self.loss, self.kl = f[0], f[1]
+        self.n_tokens, self.n_clipped, self.n_invalid = self.words[1], self.words[2], self.words[3]
+
+    def data_ptr(self):
+        return self.words.data_ptr()
+
+
+def alloc_policy_workspace(n_tokens, vocab, device):
+    n = int(lib().ff_policy_workspace_bytes(n_tokens, vocab))
+    return torch.zeros(max(16, n), dtype=torch.uint8, device=device)
+
+
+def policy_batch(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low=0.2,
+                 clip_high=0.2, beta=0.0, loss_scale=1.0):
+    """ff_policy_batch of device tensors: logits [tokens, vocab] (rows may lie apart), targets int64,
+    the others fp32, [tokens] each.  The caller keeps the tensors alive until the stream's work is done."""
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits are rows of contiguous elements")
+    n, vocab = logits.shape
+    for name, t, dtype in (("targets", targets, torch.int64), ("old_logp", old_logp, torch.float32),
+                           ("ref_logp", ref_logp, torch.float32),
+                           ("advantages", advantages, torch.float32),
+                           ("weights", weights, torch.float32)):
+        if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError("%s is a contiguous %s tensor of one entry per token" % (name, dtype))
+    stride = logits.stride(0) if n > 1 else max(vocab, logits.stride(0))
+    return ff_policy_batch(logits.data_ptr(), n, vocab, stride, _DTYPES[logits.dtype], 0,
+                           targets.data_ptr(), old_logp.data_ptr(),
+                           ref_logp.data_ptr() if ref_logp is not None else None,
+                           advantages.data_ptr(), weights.data_ptr(), clip_low, clip_high, beta,
+                           loss_scale)
+
+
+def ff_policy_loss(batch, logp, token_loss, stats, workspace, dlogits=None, stream=None):
+    """dlogits: None (the loss alone), or [tokens, vocab] in the logits' format; may be the logits."""
+    n = batch.n_tokens
+    for t in (logp, token_loss):
+        if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError("logp and token_loss are contiguous fp32 tensors of one entry per token")
+    grad, stride = None, 0
+    if dlogits is not None:
+        if dlogits.shape != (n, batch.vocab) or _DTYPES.get(dlogits.dtype) != batch.dtype or \
+                (batch.vocab > 1 and dlogits.stride(1) != 1):
+            raise ValueError("dlogits has the logits' shape and format")
+        grad = dlogits.data_ptr()
+        stride = dlogits.stride(0) if n > 1 else max(batch.vocab, dlogits.stride(0))
+    _check(lib().ff_policy_loss(ctypes.byref(batch), logp.data_ptr(), token_loss.data_ptr(), grad,
+                                stride, stats.data_ptr(), workspace.data_ptr(), _stream_ptr(stream)))

@@ -15,6 +15,7 @@
 #include "fused.hpp"
 #include "kernels.hpp"
 #include "layout.hpp"
+#include "status.hpp"
 
 using namespace ffsnap;
 
@@ -65,17 +66,15 @@ namespace {
 
 thread_local char g_hip_error[256] = "";
 
-int hip_fail(hipError_t e)
+}  // namespace
+
+int ffsnap::hip_fail(hipError_t e)
 {
     std::snprintf(g_hip_error, sizeof(g_hip_error), "%s", hipGetErrorString(e));
     return FF_ERR_HIP;
 }
 
-#define FF_HIP_TRY(expr)                       \
-    do {                                       \
-        hipError_t e_ = (expr);                \
-        if (e_ != hipSuccess) return hip_fail(e_); \
-    } while (0)
+namespace {
 
 uint64_t align_up(uint64_t v, uint64_t a) { return (v + a - 1) / a * a; }
 
@@ -587,7 +586,7 @@ int check_restore_args(const ff_plan* p, const void* chunks, const uint32_t* crc
 // prev: null for the in-place step; else the snapshot that holds the old master, m and v.
 int adam_impl(const ff_plan* p, const void* const* grads, const ff_adam_hparams* hp,
               uint32_t half_dtype, float inv_scale, uint64_t* n_nonfinite, const void* prev,
-              void* chunks, uint32_t* crcs, hipStream_t s, bool bare = false)
+              void* chunks, uint32_t* crcs, hipStream_t s, bool bare = false, const ff_grad_stats* stats = nullptr)
 {
     int rc = check_device_call(p);
     if (rc != FF_OK) return rc;
@@ -624,6 +623,7 @@ int adam_impl(const ff_plan* p, const void* const* grads, const ff_adam_hparams*
     c.inv_scale = inv_scale;
     c.xcd_group = bare ? p->mix_xcd_group : prev ? p->chained_xcd_group : p->fused_xcd_group;
     c.n_nonfinite = n_nonfinite;
+    c.stats = stats;
     c.prev = static_cast<const uint8_t*>(prev);
     if (!bare && p->work.tally && tally_allowed(s)) {
         c.tally = p->work.tally;
@@ -790,6 +790,17 @@ int ff_adam_step_chained(const ff_plan* p, const void* const* grads, const ff_ad
     if (reinterpret_cast<uint64_t>(n_nonfinite) % 8) return FF_ERR_INVALID;
     return adam_impl(p, grads, hp, half == FF_F16 ? FF_F16 : FF_BF16, inv_loss_scale, n_nonfinite,
                      prev_chunks, chunks, crcs, static_cast<hipStream_t>(hip_stream));
+}
+
+int ff_adam_step_clipped(const ff_plan* p, const void* const* grads, const ff_adam_hparams* hp,
+                         const ff_grad_stats* stats, const void* prev_chunks, void* chunks,
+                         uint32_t* crcs, void* hip_stream)
+{
+    if (!p || !stats) return FF_ERR_NULL;
+    if (reinterpret_cast<uint64_t>(stats) % 8) return FF_ERR_INVALID;
+    const uint32_t half = p->layout.half_dtype == FF_F16 ? FF_F16 : FF_BF16;
+    return adam_impl(p, grads, hp, half, 1.0f, nullptr, prev_chunks, chunks, crcs,
+                     static_cast<hipStream_t>(hip_stream), false, stats);
 }
 
 int ff_mix_ceiling(const ff_plan* p, const void* const* grads, const void* prev_chunks,

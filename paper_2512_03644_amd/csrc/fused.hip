@@ -94,11 +94,12 @@ __device__ __forceinline__ float canonical_nan(float x) { return (x != x) ? bits
 // One element of the update; every operation is a separately rounded fp32 operation (the file
 // is compiled with -ffp-contract=off, division and square root are correctly rounded).
 // F16: the gradient is fp16 of a loss scaled by S and is multiplied by inv_scale = 1/S first.
-// Otherwise it is bf16 and nothing is scaled.  BC2: the second bias correction has not yet rounded
+// Otherwise it is bf16 and nothing is scaled.  CLIP: either is multiplied, by the factor that stands in the gradients'
+// statistics (clipped_kernel).  BC2: the second bias correction has not yet rounded
 // to one (x / 1.0f is x exactly, so the division is left out then; beta2 = 0.95 gets there at step
 // 333).  A NaN in the new m or v makes the new master NaN too, so that one comparison per element
 // finds the rare row whose NaNs have to be put into their stored form.
-template <bool F16, bool BC2>
+template <bool F16, bool BC2, bool CLIP>
 __device__ __forceinline__ void adam_element(const FusedConsts& C, uint32_t g_bits, float& p,
                                              float& m, float& v)
 {
@@ -106,6 +107,8 @@ __device__ __forceinline__ void adam_element(const FusedConsts& C, uint32_t g_bi
     float g;
     if constexpr (F16)
         g = __half2float(__ushort_as_half(static_cast<unsigned short>(g_bits))) * C.inv_scale;
+    else if constexpr (CLIP)
+        g = bits_to_f32(g_bits << 16) * C.inv_scale;
     else
         g = bits_to_f32(g_bits << 16);
     const float pd = p * k.decay;
@@ -400,8 +403,9 @@ __device__ __forceinline__ void store_image(const WorkTile& t, const uint8_t* im
 // three elements at either end that do not fill a lane's slot are updated one per lane, by lanes 0-3
 // (the slot that holds lo) and 4-7 (the slot that holds hi), and handed to the lanes that own those
 // slots.  What is not the tile's counts as zero.
-// WARM: of a short step (fused_kernel_warm).
-template <bool F16, bool CHAINED, bool BC2, bool WHOLE, bool WARM>
+// WARM: of a short step (fused_kernel_warm).  CLIP: with the factor and the decision of the gradients' statistics, keep: the
+// update is left out.
+template <bool F16, bool CHAINED, bool BC2, bool WHOLE, bool WARM, bool CLIP>
 __device__ __forceinline__ void param_sub_block(const WorkTile& t, const uint32_t tile, const uint32_t info,
                                                 const uint32_t run_entry, const int at,
                                                 const int lo, const int hi,
@@ -409,8 +413,10 @@ __device__ __forceinline__ void param_sub_block(const WorkTile& t, const uint32_
                                                 uint8_t* __restrict__ chunks,
                                                 uint32_t* __restrict__ crcs, const FusedConsts& C,
                                                 Lds& lds, uint8_t* img,
-                                                const uint32_t* __restrict__ lane_tab, int wave, int lane)
+                                                const uint32_t* __restrict__ lane_tab, int wave, int lane,
+                                                const bool keep = false)
 {
+    constexpr bool kCount = F16 && !CLIP;  // infinite and NaN gradients
     const int sub = info & 15u;
     // x^(8 * bytes between the end of the lane's column and the end of the block), in the lane's stream
     const uint32_t lane_c0 = lane_tab[(15 - sub) * 64 + lane], lane_c = lane_tab[(16 + 15 - sub) * 64 + lane];
@@ -479,14 +485,17 @@ __device__ __forceinline__ void param_sub_block(const WorkTile& t, const uint32_
     if (!WHOLE) {
         uint32_t wb = 0;
         // (a scalar register: a short step has no other left, and the count went to scratch memory and back)
-        if (F16 && WARM) edge_nonfinite = __popcll(__ballot(f16_nonfinite(eg)));
+        if (kCount && WARM) edge_nonfinite = __popcll(__ballot(f16_nonfinite(eg)));
         if (has_edge) {
-            if constexpr (F16 && !WARM) nonfinite += f16_nonfinite(eg) ? 1u : 0u;
-            adam_element<F16, BC2>(C, eg, ep, em, ev);
-            ep = canonical_nan(ep);
-            em = canonical_nan(em);
-            ev = canonical_nan(ev);
-            wb = (F16 ? f32_to_f16_pair(ep, 0.f) : f32_to_bf16_pair(ep, 0.f)) & 0xFFFFu;
+            if constexpr (kCount && !WARM) nonfinite += f16_nonfinite(eg) ? 1u : 0u;
+            if (!CLIP || !keep) {
+                adam_element<F16, BC2, CLIP>(C, eg, ep, em, ev);
+                ep = canonical_nan(ep);
+                em = canonical_nan(em);
+                ev = canonical_nan(ev);
+            }
+            const float stored = CLIP ? canonical_nan(ep) : ep;
+            wb = (F16 ? f32_to_f16_pair(stored, 0.f) : f32_to_bf16_pair(stored, 0.f)) & 0xFFFFu;
         }
         edge_w = wb;
     }
@@ -497,10 +506,19 @@ __device__ __forceinline__ void param_sub_block(const WorkTile& t, const uint32_
         float p[4] = {bits_to_f32(cur.p.x), bits_to_f32(cur.p.y), bits_to_f32(cur.p.z), bits_to_f32(cur.p.w)};
         float m[4] = {bits_to_f32(cur.m.x), bits_to_f32(cur.m.y), bits_to_f32(cur.m.z), bits_to_f32(cur.m.w)};
         float v[4] = {bits_to_f32(cur.v.x), bits_to_f32(cur.v.y), bits_to_f32(cur.v.z), bits_to_f32(cur.v.w)};
+        uint32_t fw[2], fp[4], fm[4], fv[4];
+        if (CLIP && keep) {  // the state as it is, the weights rounded from it
+#pragma unroll
+            for (int s = 0; s < 4; s++) fp[s] = f32_to_bits(canonical_nan(p[s]));
+            fw[0] = F16 ? f32_to_f16_pair(bits_to_f32(fp[0]), bits_to_f32(fp[1])) : f32_to_bf16_pair(bits_to_f32(fp[0]), bits_to_f32(fp[1]));
+            fw[1] = F16 ? f32_to_f16_pair(bits_to_f32(fp[2]), bits_to_f32(fp[3])) : f32_to_bf16_pair(bits_to_f32(fp[2]), bits_to_f32(fp[3]));
+            q[r].g = u32x2{fw[0], fw[1]};
+            return;
+        }
 #pragma unroll
         for (int s = 0; s < 4; s++) {
-            if constexpr (F16) nonfinite += f16_nonfinite(gb[s]) ? 1u : 0u;
-            adam_element<F16, BC2>(C, gb[s], p[s], m[s], v[s]);
+            if constexpr (kCount) nonfinite += f16_nonfinite(gb[s]) ? 1u : 0u;
+            adam_element<F16, BC2, CLIP>(C, gb[s], p[s], m[s], v[s]);
         }
         if (__any(__builtin_isunordered(p[0], p[1]) | __builtin_isunordered(p[2], p[3]))) {
             asm volatile("");  // a branch, not 24 selections in every row
@@ -511,7 +529,6 @@ __device__ __forceinline__ void param_sub_block(const WorkTile& t, const uint32_
                 v[s] = canonical_nan(v[s]);
             }
         }
-        uint32_t fw[2], fp[4], fm[4], fv[4];
         fw[0] = F16 ? f32_to_f16_pair(p[0], p[1]) : f32_to_bf16_pair(p[0], p[1]);
         fw[1] = F16 ? f32_to_f16_pair(p[2], p[3]) : f32_to_bf16_pair(p[2], p[3]);
 #pragma unroll
@@ -642,7 +659,7 @@ __device__ __forceinline__ void param_sub_block(const WorkTile& t, const uint32_
         store_image(t, img, from, from < 0 ? -from : 0, end < kAll ? end : kAll, chunks, wave, lane);
     }
 
-    if constexpr (F16) {
+    if constexpr (kCount) {
         if (C.n_nonfinite && (__any(nonfinite != 0) || edge_nonfinite)) {
 #pragma unroll
             for (int d = 32; d >= 1; d >>= 1) nonfinite += __shfl_xor(nonfinite, d);
@@ -749,6 +766,55 @@ __device__ __forceinline__ void clear_tail(const FusedConsts& C, uint8_t* __rest
     });
 }
 
+template <bool F16, bool CHAINED, bool BC2, bool TALLY, bool CLIP, class Grads>
+__device__ __forceinline__ void step_body(const WorkWave* __restrict__ waves, const WorkTile* __restrict__ tiles, uint32_t grad_base,
+                                          const uint32_t* __restrict__ tabs, uint8_t* __restrict__ chunks,
+                                          uint32_t* __restrict__ crcs, FusedConsts& C, const Grads& grads, Lds& lds, uint8_t* img)
+{
+    if (!TALLY) C.tally = nullptr;
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const uint32_t group = xcd_order(blockIdx.x, gridDim.x, C.xcd_group);
+    if (C.tally && group >= C.n_groups) {
+        clear_tail(C, chunks, group - C.n_groups);
+        return;
+    }
+    fetch_tables(tabs, lds, wave, lane);
+    const WorkWave e = waves[group * kWavesPerBlock + wave];
+    const uint32_t run_entry = group * kWavesPerBlock + ((e.info >> 4) & 7u);
+    if (e.tile == kNoTile) {
+        tables_ready();
+        return;
+    }
+    // the tile descriptor is uniform and read-only: the loads below go through scalar registers
+    // (a private copy indexed by the stream number would live in scratch memory instead)
+    const WorkTile& t = tiles[e.tile];
+    // (by scalar loads, as the descriptor below)
+    const bool keep = CLIP && table_entry(&C.stats->skip, 0) != 0;
+    if (CLIP) C.inv_scale = table_entry(&C.stats->scale, 0);
+    const int sub = e.info & 15u;
+    const uint32_t* const lane_tab = tabs + kFusedWeightWords;
+    if (t.kind == kWorkRaw) {
+        const int at = sub * int(kSubRawBytes) - static_cast<int>(t.soff[0] % kRawTileBytes);
+        const int lo = at < 0 ? -at : 0;
+        const int left = static_cast<int>(t.n) - at;
+        raw_sub_block<false>(t, e.info, at, lo, left < int(kSubRawBytes) ? left : int(kSubRawBytes), chunks,
+                      crcs, C, run_entry, lds, lane_tab + 32 * 64, wave, lane);
+        return;
+    }
+    const int at = sub * int(kSubElems) - static_cast<int>(t.e0 % kParamTileElems);
+    const int lo = at < 0 ? -at : 0;
+    const int left = static_cast<int>(t.n) - at;
+    const int hi = left < int(kSubElems) ? left : int(kSubElems);
+    const uint8_t* const grad = reinterpret_cast<const uint8_t*>(grads.p[t.grad_index - grad_base]);
+    if (lo == 0 && hi == int(kSubElems) && !(t.head_split && at == 0))
+        param_sub_block<F16, CHAINED, BC2, true, false, CLIP>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
+                                            lane_tab, wave, lane, keep);
+    else
+        param_sub_block<F16, CHAINED, BC2, false, false, CLIP>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
+                                             lane_tab, wave, lane, keep);
+}
+
 // The gradient pointers of the parameter groups [grad_base, grad_base + kGradsPerLaunch) travel by
 // value in the kernel arguments: the step keeps no per-call table in device memory, so calls on
 // one plan may overlap and a captured launch carries its own pointers.
@@ -772,60 +838,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(TALLY 
 {
     __shared__ Lds lds;
     extern __shared__ __attribute__((aligned(16))) uint8_t img[];  // of launches with C.image
-    if (!TALLY) C.tally = nullptr;
-    const int lane = threadIdx.x & (kWaveSize - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
-    const uint32_t group = xcd_order(blockIdx.x, gridDim.x, C.xcd_group);
-    if (C.tally && group >= C.n_groups) {
-        clear_tail(C, chunks, group - C.n_groups);
-        return;
-    }
-    fetch_tables(tabs, lds, wave, lane);
-    const WorkWave e = waves[group * kWavesPerBlock + wave];
-    const uint32_t run_entry = group * kWavesPerBlock + ((e.info >> 4) & 7u);
-    if (e.tile == kNoTile) {
-        tables_ready();
-        return;
-    }
-    // the tile descriptor is uniform and read-only: the loads below go through scalar registers
-    // (a private copy indexed by the stream number would live in scratch memory instead)
-    const WorkTile& t = tiles[e.tile];
-    const int sub = e.info & 15u;
-    const uint32_t* const lane_tab = tabs + kFusedWeightWords;
-    if (t.kind == kWorkRaw) {
-        const int at = sub * int(kSubRawBytes) - static_cast<int>(t.soff[0] % kRawTileBytes);
-        const int lo = at < 0 ? -at : 0;
-        const int left = static_cast<int>(t.n) - at;
-        raw_sub_block<false>(t, e.info, at, lo, left < int(kSubRawBytes) ? left : int(kSubRawBytes), chunks,
-                      crcs, C, run_entry, lds, lane_tab + 32 * 64, wave, lane);
-        return;
-    }
-    const int at = sub * int(kSubElems) - static_cast<int>(t.e0 % kParamTileElems);
-    const int lo = at < 0 ? -at : 0;
-    const int left = static_cast<int>(t.n) - at;
-    const int hi = left < int(kSubElems) ? left : int(kSubElems);
-    const uint8_t* const grad = reinterpret_cast<const uint8_t*>(grads.p[t.grad_index - grad_base]);
-    if (lo == 0 && hi == int(kSubElems) && !(t.head_split && at == 0))
-        param_sub_block<F16, CHAINED, BC2, true, false>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
-                                            lane_tab, wave, lane);
-    else
-        param_sub_block<F16, CHAINED, BC2, false, false>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
-                                             lane_tab, wave, lane);
+    step_body<F16, CHAINED, BC2, TALLY, false>(waves, tiles, grad_base, tabs, chunks, crcs, C, grads, lds, img);
 }
 
-// Steps over small buffers (kWarmStepBytes): they load through the caches; and what the first wavefronts wait for, the
-// arguments' lines, then the descriptor's, the gradient's address and the run's tickets, they ask for at once, and the end of the
-// chain is shorter (deliver_to_tally).  A kernel of its own, as long steps lose by each: the choice of loads by a branch costs
-// lists of 7 million elements and more 3-5 % in place, the earlier start 0.6 % on the 7B shard, chained 0.9 %.
-template <bool F16, bool CHAINED, bool BC2, uint32_t N>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void fused_kernel_warm(
-    const WorkWave* __restrict__ waves, const WorkTile* __restrict__ tiles, uint32_t grid,
+// The step on clipped gradients: the same with the gradients' factor, and the decision whether there is an update at all, read
+// where the norm's kernel has left them, one scalar load a wavefront.  (Always with the division by the second bias
+// correction: it is hidden.)
+template <bool F16, bool CHAINED, uint32_t N, bool TALLY = true>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(TALLY || F16 ? 6 : 7))) void clipped_kernel(
+    const WorkWave* __restrict__ waves, const WorkTile* __restrict__ tiles, uint32_t grad_base,
     const uint32_t* __restrict__ tabs, uint8_t* __restrict__ chunks, uint32_t* __restrict__ crcs,
     FusedConsts C, GradPtrsOf<N> grads)
 {
-    const uint32_t block = block_behind_args<0, 6 * sizeof(void*) + sizeof(FusedConsts)>();  // up to the gradients'
     __shared__ Lds lds;
     extern __shared__ __attribute__((aligned(16))) uint8_t img[];  // of launches with C.image
+    step_body<F16, CHAINED, true, TALLY, true>(waves, tiles, grad_base, tabs, chunks, crcs, C, grads, lds, img);
+}
+
+template <bool F16, bool CHAINED, bool BC2, bool CLIP, class Grads>
+__device__ __forceinline__ void warm_step_body(const uint32_t block, const WorkWave* __restrict__ waves,
+                                               const WorkTile* __restrict__ tiles, uint32_t grid,
+                                               const uint32_t* __restrict__ tabs, uint8_t* __restrict__ chunks,
+                                               uint32_t* __restrict__ crcs, FusedConsts& C, const Grads& grads, Lds& lds, uint8_t* img)
+{
     const int lane = threadIdx.x & (kWaveSize - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     const uint32_t group = xcd_order(block, grid, C.xcd_group);
@@ -850,6 +885,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
         asm("" : "+s"(e.info) : "s"(all), "s"(grad_at));
         __builtin_amdgcn_sched_barrier(0);
     }
+    // (by scalar loads, as the descriptor below)
+    const bool keep = CLIP && table_entry(&C.stats->skip, 0) != 0;
+    if (CLIP) C.inv_scale = table_entry(&C.stats->scale, 0);
     const int sub = e.info & 15u;
     const uint32_t* const lane_tab = tabs + kFusedWeightWords;
     if (t.kind == kWorkRaw) {
@@ -866,11 +904,39 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
     const int hi = left < int(kSubElems) ? left : int(kSubElems);
     const uint8_t* const grad = reinterpret_cast<const uint8_t*>(grad_at);
     if (lo == 0 && hi == int(kSubElems) && !(t.head_split && at == 0))
-        param_sub_block<F16, CHAINED, BC2, true, true>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
-                                                       lane_tab, wave, lane);
+        param_sub_block<F16, CHAINED, BC2, true, true, CLIP>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
+                                                       lane_tab, wave, lane, keep);
     else
-        param_sub_block<F16, CHAINED, BC2, false, true>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
-                                                        lane_tab, wave, lane);
+        param_sub_block<F16, CHAINED, BC2, false, true, CLIP>(t, e.tile, e.info, run_entry, at, lo, hi, grad, chunks, crcs, C, lds, img,
+                                                        lane_tab, wave, lane, keep);
+}
+
+// Steps over small buffers (kWarmStepBytes): they load through the caches; and what the first wavefronts wait for, the
+// arguments' lines, then the descriptor's, the gradient's address and the run's tickets, they ask for at once, and the end of the
+// chain is shorter (deliver_to_tally).  A kernel of its own, as long steps lose by each: the choice of loads by a branch costs
+// lists of 7 million elements and more 3-5 % in place, the earlier start 0.6 % on the 7B shard, chained 0.9 %.
+template <bool F16, bool CHAINED, bool BC2, uint32_t N>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void fused_kernel_warm(
+    const WorkWave* __restrict__ waves, const WorkTile* __restrict__ tiles, uint32_t grid,
+    const uint32_t* __restrict__ tabs, uint8_t* __restrict__ chunks, uint32_t* __restrict__ crcs,
+    FusedConsts C, GradPtrsOf<N> grads)
+{
+    const uint32_t block = block_behind_args<0, 6 * sizeof(void*) + sizeof(FusedConsts)>();  // up to the gradients'
+    __shared__ Lds lds;
+    extern __shared__ __attribute__((aligned(16))) uint8_t img[];  // of launches with C.image
+    warm_step_body<F16, CHAINED, BC2, false>(block, waves, tiles, grid, tabs, chunks, crcs, C, grads, lds, img);
+}
+
+template <bool F16, bool CHAINED, uint32_t N>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void clipped_warm_kernel(
+    const WorkWave* __restrict__ waves, const WorkTile* __restrict__ tiles, uint32_t grid,
+    const uint32_t* __restrict__ tabs, uint8_t* __restrict__ chunks, uint32_t* __restrict__ crcs,
+    FusedConsts C, GradPtrsOf<N> grads)
+{
+    const uint32_t block = block_behind_args<0, 6 * sizeof(void*) + sizeof(FusedConsts)>();  // up to the gradients'
+    __shared__ Lds lds;
+    extern __shared__ __attribute__((aligned(16))) uint8_t img[];  // of launches with C.image
+    warm_step_body<F16, CHAINED, true, true>(block, waves, tiles, grid, tabs, chunks, crcs, C, grads, lds, img);
 }
 
 // ---- the step's traffic alone (bench helper) -------------------------------------------------------
@@ -1121,10 +1187,19 @@ void launch_step(bool f16, const WorkWave* waves, uint32_t n_waves, const WorkTi
     static const Kernel chained[4] = {  // without a tally
         fused_kernel<false, true, false, N, false>, fused_kernel<false, true, true, N, false>,
         fused_kernel<true, true, false, N, false>,  fused_kernel<true, true, true, N, false>};
+    static const Kernel clipped[4] = {clipped_kernel<false, false, N>, clipped_kernel<false, true, N>,
+                                      clipped_kernel<true, false, N>, clipped_kernel<true, true, N>};
+    static const Kernel clipped_warm[4] = {clipped_warm_kernel<false, false, N>, clipped_warm_kernel<false, true, N>,
+                                           clipped_warm_kernel<true, false, N>, clipped_warm_kernel<true, true, N>};
+    static const Kernel clipped_chained[2] = {clipped_kernel<false, true, N, false>, clipped_kernel<true, true, N, false>};
     const bool bc2 = consts.adam.bc2s != 1.0f;
     const int which = (f16 ? 4 : 0) + (consts.prev ? 2 : 0) + (bc2 ? 1 : 0);
-    const Kernel kernel = warm                            ? kernels_warm[which]
-                          : consts.prev && !consts.tally ? chained[(f16 ? 2 : 0) + (bc2 ? 1 : 0)]
+    const bool long_chained = !warm && consts.prev && !consts.tally;
+    const int which_clipped = (f16 ? 2 : 0) + (consts.prev ? 1 : 0);
+    const Kernel kernel = consts.stats && long_chained    ? clipped_chained[f16 ? 1 : 0]
+                          : consts.stats                  ? (warm ? clipped_warm : clipped)[which_clipped]
+                          : warm                            ? kernels_warm[which]
+                          : long_chained                  ? chained[(f16 ? 2 : 0) + (bc2 ? 1 : 0)]
                                                           : kernels[which];
     // The image only pays in launches of several rounds (aligned, in the one round that there is: 64 parameters
     // of 5000 elements 12.0 us from registers, 13.9 through the image; 32 of 32,768 15.6 and 17.2; 64 of 30,011

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/ffsnap.h"
 #include "kernels.hpp"
 #include "layout.hpp"
 
@@ -17,6 +18,7 @@ struct FusedConsts {
     AdamConsts adam;
     float inv_scale = 1.0f;            // fp16 variant: reciprocal of the loss scale
     uint64_t* n_nonfinite = nullptr;   // fp16 variant: device counter of inf/NaN gradients, or null
+    const ff_grad_stats* stats = nullptr;  // clipped step: where the gradients' factor is, and whether to update at all
     uint32_t xcd_group = 0;            // XCD-aware order of the work tiles (see xcd_order.h)
     // Chained step: master, m and v are read from this snapshot buffer (at the segments' stream
     // offsets) instead of their tensors, and those tensors are not written.  Null: in-place step.

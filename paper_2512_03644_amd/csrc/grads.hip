@@ -1,0 +1,376 @@
+// Gradient norm and clipping for gfx950.
+//
+// The norm is one pass over all gradients, which bounds it.  A wavefront takes items of 8 KiB of one tensor
+// (grads.hpp), lane l of a row of 1 KiB taking 16 bytes, and asks for the next item's rows before it sums up
+// those that have come.  Every element is squared and summed in 64 bits: squares of 16- and 32-bit
+// floats are exact there and cannot overflow, and so no finite gradient needs a second look.  An item's sum
+// that is not finite tells that the item holds an infinity or NaN; only then are those counted.  Sums go from lanes to
+// the wavefront to the workgroup to memory in an order that depends on the list alone, and a last workgroup
+// joins them: no atomics, the same bits every time.
+#include "grads.hpp"
+
+#include <hip/hip_fp16.h>
+
+#include "fold.h"
+
+namespace ffsnap {
+
+namespace {
+
+constexpr int kThreads = kGradWaves * kWaveSize;
+constexpr int kRows = kGradItemBytes / 1024;
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+__device__ __forceinline__ float f16_to_f32(uint32_t bits) { return __half2float(__ushort_as_half(static_cast<unsigned short>(bits))); }
+
+// The two elements of a dword (a 32-bit one: itself and zero).
+template <uint32_t FORMAT>
+__device__ __forceinline__ void elements(uint32_t w, float& a, float& b)
+{
+    if constexpr (FORMAT == kGradF32) {
+        a = __uint_as_float(w);
+        b = 0.f;
+    } else if constexpr (FORMAT == kGradBf16) {
+        a = __uint_as_float(w << 16);
+        b = __uint_as_float(w & 0xFFFF0000u);
+    } else {
+        a = f16_to_f32(w & 0xFFFFu);
+        b = f16_to_f32(w >> 16);
+    }
+}
+
+template <uint32_t FORMAT>
+__device__ __forceinline__ void add_squares(double (&sum)[4], const u32x4 w)
+{
+    static_for<4>([&](auto k) {
+        float a, b;
+        elements<FORMAT>(w[int(k)], a, b);
+        sum[int(k)] = fma(static_cast<double>(a), static_cast<double>(a), sum[int(k)]);
+        if constexpr (FORMAT != kGradF32)
+            sum[(k + 2) % 4] = fma(static_cast<double>(b), static_cast<double>(b), sum[(k + 2) % 4]);
+    });
+}
+
+template <uint32_t FORMAT>
+__device__ __forceinline__ uint32_t count_nonfinite(const u32x4 w)
+{
+    uint32_t n = 0;
+    static_for<4>([&](auto k) {
+        float a, b;
+        elements<FORMAT>(w[int(k)], a, b);
+        n += (__builtin_isfinite(a) ? 0u : 1u) + (__builtin_isfinite(b) ? 0u : 1u);
+    });
+    return n;
+}
+
+// The wavefront's part of an item: whole slots of 16 bytes, and what is left behind the last of them, an
+// element for each of the first lanes.  What is not the item's is zero.
+struct Rows {
+    u32x4 slot[kRows];
+    uint32_t rest;
+};
+
+__device__ __forceinline__ GradItem item_at(const GradItem* items, const uint32_t i)
+{
+    const u32x4 w = table_entry(reinterpret_cast<const u32x4*>(items), i);
+    return GradItem{w.x | uint64_t(w.y) << 32, w.z, w.w};
+}
+__device__ __forceinline__ uint32_t item_bytes(const GradItem& it) { return it.what & 0x3FFFFFFFu; }
+__device__ __forceinline__ uint32_t item_format(const GradItem& it) { return it.what >> 30; }
+
+template <bool NT>
+__device__ __forceinline__ void load_rows(Rows& q, const GradItem& it, const uint8_t* at, const int lane)
+{
+    const uint32_t bytes = item_bytes(it);
+    q.rest = 0;
+    if (bytes == kGradItemBytes) {
+        static_for<kRows>([&](auto r) { q.slot[int(r)] = load16_unaligned<NT>(at + 1024 * r + 16 * lane); });
+        return;
+    }
+    static_for<kRows>([&](auto r) {
+        q.slot[int(r)] = u32x4{0, 0, 0, 0};
+        if (1024 * r + 16u * lane + 16 <= bytes) q.slot[int(r)] = load16_unaligned<NT>(at + 1024 * r + 16 * lane);
+    });
+    const uint32_t whole = bytes & ~15u;
+    if (item_format(it) == kGradF32) {
+        const uint32_t o = whole + 4 * lane;
+        if (o < bytes) q.rest = *as_global(reinterpret_cast<const uint32_t*>(at + o));
+    } else {
+        const uint32_t o = whole + 2 * lane;
+        if (o < bytes) q.rest = *as_global(reinterpret_cast<const uint16_t*>(at + o));
+    }
+}
+
+template <uint32_t FORMAT>
+__device__ __forceinline__ void sum_item(const Rows& q, double& total, uint64_t& bad)
+{
+    double s[4] = {0, 0, 0, 0};
+    static_for<kRows>([&](auto r) { add_squares<FORMAT>(s, q.slot[int(r)]); });
+    add_squares<FORMAT>(s, u32x4{q.rest, 0, 0, 0});
+    const double sum = (s[0] + s[1]) + (s[2] + s[3]);
+    if (__any(!__builtin_isfinite(sum))) {
+        uint32_t n = count_nonfinite<FORMAT>(u32x4{q.rest, 0, 0, 0});
+        static_for<kRows>([&](auto r) { n += count_nonfinite<FORMAT>(q.slot[int(r)]); });
+        bad += n;
+    }
+    total += sum;
+}
+
+// What follows from the sum of the squares.  By one thread.
+__device__ __forceinline__ void write_stats(ff_grad_stats* out, double sumsq, uint64_t bad, double inv_scale,
+                                            double max_norm)
+{
+    const double norm = sqrt(sumsq) * inv_scale;
+    const double factor = norm > max_norm ? max_norm / norm : 1.0;
+    out->sumsq = sumsq;
+    out->n_nonfinite = bad;
+    out->norm = norm;
+    out->scale = bad ? 0.f : static_cast<float>(factor * inv_scale);
+    out->skip = bad ? 1u : 0u;
+}
+
+// Sums over a workgroup of THREADS, in thread 0.
+template <int THREADS>
+__device__ __forceinline__ void group_sum(double& sum, uint64_t& bad)
+{
+    constexpr int kWaves = THREADS / kWaveSize;
+    __shared__ double sums[kWaves];
+    __shared__ uint64_t bads[kWaves];
+    const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x / kWaveSize;
+    sum = wave_sum(sum);
+    if (__any(bad != 0)) {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) bad += __shfl_xor(static_cast<unsigned long long>(bad), d);
+    }
+    if (lane == 0) {
+        sums[wave] = sum;
+        bads[wave] = bad;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kWaves; w++) {
+            sum += sums[w];
+            bad += bads[w];
+        }
+    }
+}
+
+// Addresses of the tensors: the list's, in memory, or the call's, in the arguments.
+struct ListAddresses {
+    const uint64_t* p;
+    __device__ __forceinline__ uint64_t of(uint32_t tensor) const { return table_entry(p, tensor); }
+};
+struct CallAddresses {
+    uint32_t base;
+    GradPtrs grads;
+    __device__ __forceinline__ uint64_t of(uint32_t tensor) const { return grads.p[tensor - base]; }
+};
+
+template <class Addresses>
+__global__ __launch_bounds__(kThreads) void grad_norm_kernel(const GradItem* __restrict__ items, uint32_t n_items,
+                                                             GradPart* __restrict__ parts, Addresses addresses)
+{
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const uint32_t stride = gridDim.x * kGradWaves;
+    double sum = 0;
+    uint64_t bad = 0;
+    uint32_t i = blockIdx.x * kGradWaves + wave;
+    if (i < n_items) {
+        GradItem it = item_at(items, i);
+        Rows q;
+        load_rows<true>(q, it, reinterpret_cast<const uint8_t*>(addresses.of(it.tensor)) + it.begin, lane);
+        for (;;) {
+            i += stride;
+            const bool more = i < n_items;
+            GradItem next = it;
+            Rows ahead;
+            if (more) {
+                next = item_at(items, i);
+                load_rows<true>(ahead, next, reinterpret_cast<const uint8_t*>(addresses.of(next.tensor)) + next.begin, lane);
+            }
+            switch (item_format(it)) {
+            case kGradF32: sum_item<kGradF32>(q, sum, bad); break;
+            case kGradBf16: sum_item<kGradBf16>(q, sum, bad); break;
+            default: sum_item<kGradF16>(q, sum, bad);
+            }
+            if (!more) break;
+            it = next;
+            q = ahead;
+        }
+    }
+    group_sum<kThreads>(sum, bad);
+    if (threadIdx.x == 0) parts[blockIdx.x] = GradPart{sum, bad};
+}
+
+constexpr int kFinishThreads = 256;
+__global__ __launch_bounds__(kFinishThreads) void grad_finish_kernel(const GradPart* __restrict__ parts, uint32_t n,
+                                                                     double inv_scale, double max_norm,
+                                                                     ff_grad_stats* __restrict__ stats)
+{
+    double sum = 0;
+    uint64_t bad = 0;
+    for (uint32_t i = threadIdx.x; i < n; i += kFinishThreads) {
+        sum += parts[i].sumsq;
+        bad += parts[i].n_nonfinite;
+    }
+    group_sum<kFinishThreads>(sum, bad);
+    if (threadIdx.x == 0) write_stats(stats, sum, bad, inv_scale, max_norm);
+}
+
+__global__ void grad_join_kernel(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,
+                                 ff_grad_stats* stats)
+{
+    double sum = 0;
+    uint64_t bad = 0;
+    for (uint64_t i = 0; i < n; i++) {  // in rank order
+        sum += parts[i].sumsq;
+        bad += parts[i].n_nonfinite;
+    }
+    write_stats(stats, sum, bad, inv_scale, max_norm);
+}
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// The elements of a dword, multiplied in fp32 and rounded to nearest even.
+template <uint32_t FORMAT>
+__device__ __forceinline__ uint32_t scaled(uint32_t w, const float scale)
+{
+    float a, b;
+    elements<FORMAT>(w, a, b);
+    if constexpr (FORMAT == kGradF32) return __float_as_uint(a * scale);
+    if constexpr (FORMAT == kGradBf16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a * scale, b * scale}, bf16x2));
+    return __half_as_ushort(__float2half_rn(a * scale)) | uint32_t(__half_as_ushort(__float2half_rn(b * scale))) << 16;
+}
+
+template <uint32_t FORMAT>
+__device__ __forceinline__ void clip_item(const Rows& q, const uint32_t bytes, uint8_t* at, const float scale, const int lane)
+{
+    static_for<kRows>([&](auto r) {
+        u32x4 w = q.slot[int(r)];
+        static_for<4>([&](auto k) { w[int(k)] = scaled<FORMAT>(w[int(k)], scale); });
+        if (1024 * r + 16u * lane + 16 <= bytes) store16_unaligned<true>(at + 1024 * r + 16 * lane, w);
+    });
+    constexpr uint32_t kItem = FORMAT == kGradF32 ? 4 : 2;
+    const uint32_t o = (bytes & ~15u) + kItem * lane;
+    if (o < bytes) {
+        const uint32_t w = scaled<FORMAT>(q.rest, scale);
+        if constexpr (FORMAT == kGradF32)
+            *as_global(reinterpret_cast<uint32_t*>(at + o)) = w;
+        else
+            *as_global(reinterpret_cast<uint16_t*>(at + o)) = static_cast<uint16_t>(w);
+    }
+}
+
+template <class Addresses>
+__global__ __launch_bounds__(kThreads) void grad_clip_kernel(const GradItem* __restrict__ items, uint32_t n_items,
+                                                             const ff_grad_stats* __restrict__ stats, Addresses addresses)
+{
+    const float scale = stats->scale;
+    if (stats->skip || scale == 1.f) return;
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const uint32_t i = blockIdx.x * kGradWaves + wave;
+    if (i >= n_items) return;
+    const GradItem it = item_at(items, i);
+    uint8_t* const at = reinterpret_cast<uint8_t*>(addresses.of(it.tensor)) + it.begin;
+    const uint32_t bytes = item_bytes(it);
+    Rows q;
+    load_rows<true>(q, it, at, lane);
+    switch (item_format(it)) {
+    case kGradF32: clip_item<kGradF32>(q, bytes, at, scale, lane); break;
+    case kGradBf16: clip_item<kGradBf16>(q, bytes, at, scale, lane); break;
+    default: clip_item<kGradF16>(q, bytes, at, scale, lane);
+    }
+}
+
+CallAddresses call_addresses(const GradWork& work, const void* const* grads, uint64_t k)
+{
+    CallAddresses a;
+    a.base = static_cast<uint32_t>(k * kGradsPerLaunch);
+    for (uint32_t i = 0; i < kGradsPerLaunch; i++)
+        a.grads.p[i] = a.base + i < work.n ? reinterpret_cast<uint64_t>(grads[a.base + i]) : 0;
+    return a;
+}
+
+}  // namespace
+
+bool build_grad_items(const ff_segment* segs, uint64_t n, std::vector<GradItem>& items, std::vector<uint32_t>& begin)
+{
+    begin.push_back(0);
+    for (uint64_t k = 0; k < n; k++) {
+        if (k && k % kGradsPerLaunch == 0) begin.push_back(static_cast<uint32_t>(items.size()));
+        const uint32_t format = segs[k].dtype == FF_F32 ? kGradF32 : segs[k].dtype == FF_BF16 ? kGradBf16 : kGradF16;
+        const uint64_t pieces = (segs[k].nbytes + kGradItemBytes - 1) / kGradItemBytes;
+        if (items.size() + pieces > (1ull << 31)) return false;
+        for (uint64_t b = 0; b < segs[k].nbytes; b += kGradItemBytes) {
+            const uint64_t left = segs[k].nbytes - b;
+            items.push_back({b, static_cast<uint32_t>(k),
+                             static_cast<uint32_t>(left < kGradItemBytes ? left : kGradItemBytes) | format << 30});
+        }
+    }
+    begin.push_back(static_cast<uint32_t>(items.size()));
+    return true;
+}
+
+hipError_t launch_grad_norm(const GradWork& work, const void* const* grads, double inv_scale, double max_norm,
+                            void* workspace, ff_grad_stats* stats, hipStream_t stream)
+{
+    GradPart* const parts = static_cast<GradPart*>(workspace);
+    uint32_t n_parts = 0;
+    if (!grads) {
+        n_parts = grad_groups(work.launch.back());
+        hipLaunchKernelGGL(grad_norm_kernel<ListAddresses>, dim3(n_parts), dim3(kThreads), 0, stream, work.items,
+                           work.launch.back(), parts, ListAddresses{work.address});
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    } else {
+        for (size_t k = 0; k + 1 < work.launch.size(); k++) {
+            const uint32_t first = work.launch[k], n = work.launch[k + 1] - first, groups = grad_groups(n);
+            hipLaunchKernelGGL(grad_norm_kernel<CallAddresses>, dim3(groups), dim3(kThreads), 0, stream, work.items + first, n,
+                               parts + n_parts, call_addresses(work, grads, k));
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            n_parts += groups;
+        }
+    }
+    hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, parts, n_parts, inv_scale, max_norm, stats);
+    return hipGetLastError();
+}
+
+hipError_t launch_grad_join(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,
+                            ff_grad_stats* stats, hipStream_t stream)
+{
+    hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(1), 0, stream, parts, n, inv_scale, max_norm, stats);
+    return hipGetLastError();
+}
+
+hipError_t launch_grad_clip(const GradWork& work, const void* const* grads, const ff_grad_stats* stats, hipStream_t stream)
+{
+    auto groups = [](uint32_t n) { return dim3((n + kGradWaves - 1) / kGradWaves); };
+    if (!grads) {
+        if (!work.launch.back()) return hipSuccess;
+        hipLaunchKernelGGL(grad_clip_kernel<ListAddresses>, groups(work.launch.back()), dim3(kThreads), 0, stream, work.items,
+                           work.launch.back(), stats, ListAddresses{work.address});
+        return hipGetLastError();
+    }
+    for (size_t k = 0; k + 1 < work.launch.size(); k++) {
+        const uint32_t first = work.launch[k], n = work.launch[k + 1] - first;
+        if (!n) continue;
+        hipLaunchKernelGGL(grad_clip_kernel<CallAddresses>, groups(n), dim3(kThreads), 0, stream, work.items + first, n, stats,
+                           call_addresses(work, grads, k));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace ffsnap

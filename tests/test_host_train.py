@@ -1,0 +1,154 @@
+"""CPU-only checks of the calls between loss and step: what they refuse, and the sizes they report.  Every refusal
+comes before any work on the device, so none of them needs one."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2512_03644_amd import binding as ff
+
+HOST = ff.FF_PLAN_HOST_ONLY
+INF, NAN = float("inf"), float("nan")
+A16 = 1 << 20  # an address that is aligned to everything and never used
+
+
+def test_lists_count_elements_and_say_how_much_workspace_a_norm_takes():
+    ts = [torch.zeros(n, dtype=t) for n, t in ((5, torch.bfloat16), (0, torch.float32), (100000, torch.float16),
+                                                (3, torch.float32))]
+    lst = ff.ff_grad_list(ts, HOST)
+    assert lst.numel == 100008 and lst.workspace_bytes >= 16
+    empty = ff.ff_grad_list([], HOST)
+    assert empty.numel == 0 and empty.workspace_bytes >= 16
+    many = ff.ff_grad_list([torch.zeros(3)] * 5000, HOST)  # several launches where every call brings its addresses
+    assert many.numel == 15000 and many.workspace_bytes >= 16
+
+
+def test_lists_refuse_what_is_no_gradient():
+    L = ff.lib()
+    out = ctypes.c_void_p()
+
+    def status(field, value):
+        segs = ff.make_segments([torch.zeros(8, dtype=torch.float32)])
+        setattr(segs[0], field, value)
+        rc = L.ff_grad_list_create(segs, 1, HOST, ctypes.byref(out))
+        assert rc == ff.FF_OK or out.value is None
+        if rc == ff.FF_OK:
+            L.ff_grad_list_destroy(out)
+        return rc
+
+    assert status("dtype", 7) == ff.FF_ERR_INVALID and status("dtype", 0) == ff.FF_ERR_INVALID
+    assert status("kind", ff.FF_KIND_M) == ff.FF_ERR_INVALID and status("reserved", 1) == ff.FF_ERR_INVALID
+    assert status("nbytes", 30) == ff.FF_ERR_INVALID and status("ptr", A16 + 2) == ff.FF_ERR_INVALID
+    assert status("ptr", None) == ff.FF_OK  # addresses may come with every call
+    segs = ff.make_segments([torch.zeros(8)])
+    assert L.ff_grad_list_create(segs, 1, HOST, None) == ff.FF_ERR_NULL
+    assert L.ff_grad_list_create(None, 1, HOST, ctypes.byref(out)) == ff.FF_ERR_NULL
+    assert L.ff_grad_list_create(segs, 1, HOST | 2, ctypes.byref(out)) == ff.FF_ERR_INVALID
+    assert L.ff_grad_list_create(segs, 1 << 33, HOST, ctypes.byref(out)) == ff.FF_ERR_INVALID
+    L.ff_grad_list_destroy(None)
+
+
+def test_norm_and_clip_refuse_bad_arguments():
+    L = ff.lib()
+    lst = ff.ff_grad_list([torch.zeros(8), torch.zeros(0), torch.zeros(8, dtype=torch.bfloat16)], HOST)
+    ok = (ctypes.c_uint64 * 3)(A16, 0, A16)
+
+    def norm(handle=lst.handle, grads=ok, inv=1.0, most=1.0, ws=A16, stats=A16):
+        return L.ff_grad_norm(handle, grads, inv, most, ws, stats, None)
+
+    assert norm() == ff.FF_ERR_HOST_ONLY and norm(grads=None) == ff.FF_ERR_HOST_ONLY
+    assert norm(most=INF) == ff.FF_ERR_HOST_ONLY
+    assert norm(handle=None) == norm(ws=None) == norm(stats=None) == ff.FF_ERR_NULL
+    for inv in (0.0, -1.0, INF, NAN):
+        assert norm(inv=inv) == ff.FF_ERR_INVALID
+    for most in (0.0, -1.0, NAN):
+        assert norm(most=most) == ff.FF_ERR_INVALID
+    assert norm(ws=A16 + 8) == norm(stats=A16 + 4) == ff.FF_ERR_INVALID
+    assert norm(grads=(ctypes.c_uint64 * 3)(A16, 0, 0)) == ff.FF_ERR_NULL
+    assert norm(grads=(ctypes.c_uint64 * 3)(A16 + 2, 0, A16)) == ff.FF_ERR_INVALID   # fp32
+    assert norm(grads=(ctypes.c_uint64 * 3)(A16, 1, A16 + 2)) == ff.FF_ERR_HOST_ONLY  # bf16; an empty one's is ignored
+    assert norm(grads=(ctypes.c_uint64 * 3)(A16, 0, A16 + 1)) == ff.FF_ERR_INVALID
+    assert L.ff_grad_clip(lst.handle, ok, A16, None) == ff.FF_ERR_HOST_ONLY
+    assert L.ff_grad_clip(None, ok, A16, None) == L.ff_grad_clip(lst.handle, ok, None, None) == ff.FF_ERR_NULL
+    assert L.ff_grad_clip(lst.handle, ok, A16 + 4, None) == ff.FF_ERR_INVALID
+    segs = ff.make_segments([torch.zeros(8)])
+    segs[0].ptr = None
+    out = ctypes.c_void_p()
+    assert L.ff_grad_list_create(segs, 1, HOST, ctypes.byref(out)) == ff.FF_OK
+    assert norm(handle=out, grads=None) == L.ff_grad_clip(out, None, A16, None) == ff.FF_ERR_NULL
+    L.ff_grad_list_destroy(out)
+
+    def join(parts=A16, n=2, inv=1.0, most=1.0, stats=A16):
+        return L.ff_grad_norm_join(parts, n, inv, most, stats, None)
+
+    assert join(parts=None) == join(stats=None) == ff.FF_ERR_NULL
+    for bad in (dict(n=0), dict(inv=0.0), dict(inv=NAN), dict(most=0.0), dict(most=NAN), dict(parts=A16 + 4),
+                dict(stats=A16 + 4)):
+        assert join(**bad) == ff.FF_ERR_INVALID, bad
+
+
+def test_clipped_step_refuses_bad_arguments():
+    L = ff.lib()
+    t = [torch.zeros(64, dtype=torch.bfloat16)] + [torch.zeros(64) for _ in range(3)]
+    plan = ff.ff_snapshot_plan(t, 1024, HOST, [1, 2, 3, 4], [0] * 4)
+    hp = ff.ff_adam_hparams(3e-4, 0.9, 0.95, 1e-8, 0.1, 1)
+    g = (ctypes.c_uint64 * 1)(A16)
+
+    def step(handle=plan.handle, stats=A16):
+        return L.ff_adam_step_clipped(handle, g, ctypes.byref(hp), stats, None, A16, A16, None)
+
+    assert step() == ff.FF_ERR_HOST_ONLY
+    assert step(handle=None) == step(stats=None) == ff.FF_ERR_NULL
+    assert step(stats=A16 + 4) == ff.FF_ERR_INVALID
+
+
+def _batch(**change):
+    b = ff.ff_policy_batch(A16, 4, 100, 100, ff.FF_BF16, 0, A16, A16, A16, A16, A16, 0.2, 0.2, 0.1, 1.0)
+    for k, v in change.items():
+        setattr(b, k, v)
+    return b
+
+
+def test_policy_loss_refuses_bad_arguments():
+    L = ff.lib()
+
+    def loss(batch, logp=A16, token=A16, grad=None, stride=0, stats=A16, ws=A16):
+        return L.ff_policy_loss(ctypes.byref(batch), logp, token, grad, stride, stats, ws, None)
+
+    for name in ("logits", "targets", "old_logp", "advantages", "weights", "ref_logp"):
+        assert loss(_batch(**{name: None})) == ff.FF_ERR_NULL, name
+    for bad in (dict(logp=None), dict(token=None), dict(stats=None), dict(ws=None)):
+        assert loss(_batch(), **bad) == ff.FF_ERR_NULL, bad
+    assert L.ff_policy_loss(None, A16, A16, None, 0, A16, A16, None) == ff.FF_ERR_NULL
+    for bad in (dict(dtype=0), dict(dtype=9), dict(reserved=1), dict(vocab=0), dict(vocab=1 << 31),
+                dict(n_tokens=1 << 31), dict(row_stride=99), dict(logits=A16 + 1), dict(targets=A16 + 4),
+                dict(old_logp=A16 + 2), dict(ref_logp=A16 + 2), dict(advantages=A16 + 1), dict(weights=A16 + 2),
+                dict(clip_low=-0.1), dict(clip_low=1.5), dict(clip_low=NAN), dict(clip_high=-0.1),
+                dict(clip_high=INF), dict(clip_high=NAN), dict(beta=-1.0), dict(beta=NAN), dict(beta=INF),
+                dict(loss_scale=0.0), dict(loss_scale=INF), dict(loss_scale=NAN), dict(loss_scale=-1.0)):
+        assert loss(_batch(**bad)) == ff.FF_ERR_INVALID, bad
+    for bad in (dict(logp=A16 + 2), dict(token=A16 + 1), dict(stats=A16 + 4), dict(ws=A16 + 8),
+                dict(grad=A16 + 1, stride=100), dict(grad=A16 + 64, stride=99), dict(grad=A16, stride=101)):
+        assert loss(_batch(), **bad) == ff.FF_ERR_INVALID, bad
+
+
+def test_binding_refuses_shapes_and_types():
+    z, y = torch.zeros(4, 10, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
+    f = torch.zeros(4)
+    ok = dict(logits=z, targets=y, old_logp=f, advantages=f, weights=f)
+    b = ff.policy_batch(**ok)
+    assert (b.n_tokens, b.vocab, b.row_stride, b.dtype) == (4, 10, 10, ff.FF_BF16)
+    assert ff.policy_batch(**dict(ok, logits=torch.zeros(4, 16)[:, :10])).row_stride == 16
+    for name, v in (("logits", z.t()), ("logits", z[0]), ("targets", y.int()), ("targets", y[:3]), ("old_logp", f.double()),
+                    ("ref_logp", f[:2]), ("advantages", torch.zeros(8)[::2]), ("weights", torch.zeros(4, 1))):
+        with pytest.raises(ValueError):
+            ff.policy_batch(**dict(ok, **{name: v}))
+    with pytest.raises(KeyError):
+        ff.policy_batch(**dict(ok, logits=z.double()))
+    for bad in (dict(logp=f.double()), dict(token_loss=f[:3]), dict(dlogits=z.float()), dict(dlogits=z[:3]),
+                dict(dlogits=torch.zeros(10, 4, dtype=torch.bfloat16).t())):
+        args = dict(dict(logp=f, token_loss=f, dlogits=None), **bad)
+        with pytest.raises(ValueError):
+            ff.ff_policy_loss(b, args["logp"], args["token_loss"], f, f, args["dlogits"])
+    with pytest.raises(ValueError):
+        ff.ff_grad_list([torch.zeros(4, 4).t()], HOST)
