@@ -15,203 +15,283 @@ namespace ffsnap {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWaveSize;
-constexpr float kLog2E = 1.44269504088896340736f;
-
-__device__ __forceinline__ float f16_to_f32(uint32_t bits) { return __half2float(__ushort_as_half(static_cast<unsigned short>(bits))); }
-
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// 16 bytes of a row: kItem elements as floats, and back, rounded to nearest even.
-template <uint32_t DTYPE>
-struct Slot;
-template <>
-struct Slot<FF_F32> {
+// The sum of exp(z - base) over some logits, base the largest of them so far: -inf as long as all are, and the sum is 0;
+// or NaN, as ever after a NaN or +inf.  (With a base that is only moved where a logit is far above it, an exponent rounded to 24
+// bits takes 7e-8 off the log-probability of a likely token, against 1e-8.)
+constexpr float kLog2E = 0x1.715476p+0f, kLog2ELow = 0x1.4ae0bep-26f;  // log2(e) to 48 bits
+
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+// What rounding the constant to 24 bits takes off would add up over the vocabulary, always to the same side.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(fmaf(d, kLog2E, d * kLog2ELow)); }
+// What a sum against `from` is against `to`: with what the exponent loses in 24 bits, as this is not one error of many.
+__device__ __forceinline__ double moved(double sum, float from, float to)
+{
+    const float d = fmaxf(from - to, -1000.f), t = d * kLog2E, low = fmaf(d, kLog2E, -t) + d * kLog2ELow;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return from == -INFINITY ? sum : sum * (static_cast<double>(e) * (1.0 + 0.6931471805599453 * static_cast<double>(low)));
+}
+
+// 16 bytes of a row as floats.  gradient(), write(): what the softmax is multiplied by, -factor / total, is for 32-bit elements the
+// first of two factors; for 16-bit ones its logarithm joins the exponent, rounded to 24 bits and so to 2^-18 of the
+// gradient, and its sign goes on to the rounded elements two at a time.
+struct Slot32 {
     static constexpr int kItems = 4, kBytes = 4;
     static __device__ __forceinline__ void read(const u32x4 w, float (&z)[4])
     {
         static_for<4>([&](auto k) { z[int(k)] = __uint_as_float(w[int(k)]); });
     }
-    static __device__ __forceinline__ u32x4 write(const float (&z)[4])
+    static __device__ __forceinline__ float one(const uint8_t* p) { return *as_global(reinterpret_cast<const float*>(p)); }
+    static __device__ __forceinline__ void put(uint8_t* p, float v) { *as_global(reinterpret_cast<float*>(p)) = v; }
+    static __device__ __forceinline__ void set_factors(float* f, double factor, double total)
+    {
+        f[0] = static_cast<float>(-factor / total);
+        f[1] = 0.f;
+    }
+    static __device__ __forceinline__ float gradient(float d, float f0) { return f0 * exp_of(d); }
+    static __device__ __forceinline__ float signed_by(float g, float) { return g; }
+    static __device__ __forceinline__ u32x4 write(const float (&z)[4], float)
     {
         return u32x4{__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])};
     }
-    static __device__ __forceinline__ float one(const uint8_t* p) { return *as_global(reinterpret_cast<const float*>(p)); }
-    static __device__ __forceinline__ void put(uint8_t* p, float v) { *as_global(reinterpret_cast<float*>(p)) = v; }
-};
-template <>
-struct Slot<FF_BF16> {
-    static constexpr int kItems = 8, kBytes = 2;
-    static __device__ __forceinline__ void read(const u32x4 w, float (&z)[8])
+    static __device__ __forceinline__ u32x4 with(u32x4 w, uint32_t i, float v)
     {
-        static_for<4>([&](auto k) {
-            z[2 * k] = __uint_as_float(w[int(k)] << 16);
-            z[2 * k + 1] = __uint_as_float(w[int(k)] & 0xFFFF0000u);
-        });
+        static_for<4>([&](auto k) { w[int(k)] = i == k ? __float_as_uint(v) : w[int(k)]; });
+        return w;
+    }
+};
+template <bool BF16>
+struct Slot16 {
+    static constexpr int kItems = 8, kBytes = 2;
+    static __device__ __forceinline__ float low(uint32_t w)
+    {
+        return BF16 ? __uint_as_float(w << 16) : __half2float(__ushort_as_half(static_cast<unsigned short>(w & 0xFFFFu)));
+    }
+    static __device__ __forceinline__ float high(uint32_t w)
+    {
+        return BF16 ? __uint_as_float(w & 0xFFFF0000u) : __half2float(__ushort_as_half(static_cast<unsigned short>(w >> 16)));
     }
     static __device__ __forceinline__ uint32_t pair(float a, float b)
     {
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
-    }
-    static __device__ __forceinline__ u32x4 write(const float (&z)[8])
-    {
-        return u32x4{pair(z[0], z[1]), pair(z[2], z[3]), pair(z[4], z[5]), pair(z[6], z[7])};
-    }
-    static __device__ __forceinline__ float one(const uint8_t* p)
-    {
-        return __uint_as_float(uint32_t(*as_global(reinterpret_cast<const uint16_t*>(p))) << 16);
-    }
-    static __device__ __forceinline__ void put(uint8_t* p, float v)
-    {
-        *as_global(reinterpret_cast<uint16_t*>(p)) = static_cast<uint16_t>(pair(v, 0.f));
-    }
-};
-template <>
-struct Slot<FF_F16> {
-    static constexpr int kItems = 8, kBytes = 2;
-    static __device__ __forceinline__ void read(const u32x4 w, float (&z)[8])
-    {
-        static_for<4>([&](auto k) {
-            z[2 * k] = f16_to_f32(w[int(k)] & 0xFFFFu);
-            z[2 * k + 1] = f16_to_f32(w[int(k)] >> 16);
-        });
-    }
-    static __device__ __forceinline__ uint32_t pair(float a, float b)
-    {
+        if (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
         return __half_as_ushort(__float2half_rn(a)) | uint32_t(__half_as_ushort(__float2half_rn(b))) << 16;
     }
-    static __device__ __forceinline__ u32x4 write(const float (&z)[8])
+    static __device__ __forceinline__ void read(const u32x4 w, float (&z)[8])
     {
-        return u32x4{pair(z[0], z[1]), pair(z[2], z[3]), pair(z[4], z[5]), pair(z[6], z[7])};
+        static_for<4>([&](auto k) {
+            z[2 * k] = low(w[int(k)]);
+            z[2 * k + 1] = high(w[int(k)]);
+        });
     }
-    static __device__ __forceinline__ float one(const uint8_t* p)
-    {
-        return f16_to_f32(*as_global(reinterpret_cast<const uint16_t*>(p)));
-    }
+    static __device__ __forceinline__ float one(const uint8_t* p) { return low(*as_global(reinterpret_cast<const uint16_t*>(p))); }
     static __device__ __forceinline__ void put(uint8_t* p, float v)
     {
         *as_global(reinterpret_cast<uint16_t*>(p)) = static_cast<uint16_t>(pair(v, 0.f));
     }
+    static __device__ __forceinline__ void set_factors(float* f, double factor, double total)
+    {
+        f[0] = static_cast<float>(log2(fabs(factor)) - log2(total));
+        f[1] = __uint_as_float(factor > 0 ? 0x80008000u : 0u);
+    }
+    static __device__ __forceinline__ float gradient(float d, float f0) { return __builtin_amdgcn_exp2f(fmaf(d, kLog2E, f0)); }
+    static __device__ __forceinline__ float signed_by(float g, float f1)
+    {
+        return __uint_as_float(__float_as_uint(g) ^ (__float_as_uint(f1) & 0x80000000u));
+    }
+    static __device__ __forceinline__ u32x4 write(const float (&z)[8], float f1)
+    {
+        const uint32_t s = __float_as_uint(f1);
+        return u32x4{pair(z[0], z[1]) ^ s, pair(z[2], z[3]) ^ s, pair(z[4], z[5]) ^ s, pair(z[6], z[7]) ^ s};
+    }
+    static __device__ __forceinline__ u32x4 with(u32x4 w, uint32_t i, float v)
+    {
+        const uint32_t bits = pair(v, v), half = i % 2 ? 0xFFFF0000u : 0xFFFFu;
+        static_for<4>([&](auto k) { w[int(k)] = i / 2 == k ? (w[int(k)] & ~half) | (bits & half) : w[int(k)]; });
+        return w;
+    }
+};
+template <uint32_t DTYPE>
+struct SlotOf {
+    using Type = Slot16<DTYPE == FF_BF16>;
+};
+template <>
+struct SlotOf<FF_F32> {
+    using Type = Slot32;
 };
 
-// The largest of some logits, and the sum of exp(z - base(m)) over them.  Logits of -inf add nothing, and a row
-// of nothing else is left with m = -inf and s = 0; a NaN, which the maximum passes over, or +inf makes s NaN.
-struct Running {
-    float m, s;
-};
-__device__ __forceinline__ float base(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ float exp_from(float z, float b) { return __builtin_amdgcn_exp2f((z - b) * kLog2E); }
-__device__ __forceinline__ Running join(const Running x, const Running y)
-{
-    const float m = fmaxf(x.m, y.m), b = base(m);
-    return {m, x.s * exp_from(x.m, b) + y.s * exp_from(y.m, b)};
-}
 template <int N>
-__device__ __forceinline__ void add(Running& r, const float (&z)[N])
+__device__ __forceinline__ void add(float& base, double& sum, const float (&z)[N])
 {
-    float m = r.m;
-    static_for<N>([&](auto k) { m = fmaxf(m, z[int(k)]); });
-    const float b = base(m);
-    float s = r.s * exp_from(r.m, b);
-    static_for<N>([&](auto k) { s += exp_from(z[int(k)], b); });
-    r = {m, s};
+    float m = z[0];
+    static_for<N - 1>([&](auto k) { m = fmaxf(m, z[k + 1]); });
+    if (__any(m > base)) {
+        if (m > base) {
+            sum = moved(sum, base, m);
+            base = m;
+        }
+    }
+    const float b = base_of(base);
+    float s[N];
+    static_for<N>([&](auto k) { s[int(k)] = exp_of(z[int(k)] - b); });
+    for (int d = 1; d < N; d *= 2)
+        for (int k = 0; k + d < N; k += 2 * d) s[k] += s[k + d];
+    sum += static_cast<double>(s[0]);
 }
 
-// What hangs on the token's log-probability.  By one thread.
-__device__ void token(const ff_policy_batch& b, const uint64_t t, const float m, const double total, const float z_y,
-                      float* logp_out, float* loss_out, PolicyPart* part, float& share, float& target_grad)
+// What hangs on the token's log-probability.  By one wavefront; total: of exp(z - base).
+struct Token {
+    double old_logp, ref_logp, gain, weight;
+    float z;  // the target's logit
+};
+__device__ __forceinline__ void token(const ff_policy_batch& b, const Token& k, const double base, const double total, const int lane,
+                                      double& logp, double& loss, double& kl, bool& clipped, double& factor)
 {
-    const double logp = (static_cast<double>(z_y) - static_cast<double>(m)) - log(total);
-    const double w = b.weights[t], gain = b.advantages[t];
-    const double r = exp(logp - static_cast<double>(b.old_logp[t]));
+    logp = (static_cast<double>(k.z) - base) - log(total);
     const double lo = 1.0 - static_cast<double>(b.clip_low), hi = 1.0 + static_cast<double>(b.clip_high);
-    const double kept = r * gain, cut = (r < lo ? lo : r > hi ? hi : r) * gain;
-    const bool clipped = cut < kept;
-    double loss = clipped ? -cut : -kept, slope = clipped ? 0.0 : -kept, kl = 0.0;
+    const double r = exp(logp - k.old_logp);
+    const double kept = r * k.gain, cut = (r < lo ? lo : r > hi ? hi : r) * k.gain;
+    clipped = cut < kept;
+    loss = clipped ? -cut : -kept;
+    double slope = clipped ? 0.0 : -kept;
+    kl = 0.0;
     if (b.ref_logp) {
-        const double d = static_cast<double>(b.ref_logp[t]) - logp, e = expm1(d);
+        const double d = k.ref_logp - logp, e = expm1(d);
         kl = d == INFINITY ? d : e - d;
         if (b.beta > 0.f) {
             loss += static_cast<double>(b.beta) * kl;
             slope -= static_cast<double>(b.beta) * e;
         }
     }
-    logp_out[t] = static_cast<float>(logp);
-    loss_out[t] = static_cast<float>(loss);
-    part[t] = PolicyPart{w * loss, w * kl, kTokenCounts | (clipped ? kTokenClipped : 0u), 0u};
-    const double c = w * slope * static_cast<double>(b.loss_scale);
-    share = static_cast<float>(-c / total);
-    target_grad = static_cast<float>(c * -expm1(logp));
+    factor = k.weight * slope * static_cast<double>(b.loss_scale);
 }
 
-template <uint32_t DTYPE>
-__global__ __launch_bounds__(kThreads) void policy_kernel(const ff_policy_batch b, float* __restrict__ logp,
-                                                          float* __restrict__ token_loss, uint8_t* dlogits, uint64_t grad_stride,
-                                                          PolicyPart* __restrict__ parts)
+// One workgroup, one row.  A thread holds K slots of 16 bytes of it in registers (slot i * THREADS + thread); of longer rows what is
+// behind is read again for the gradient.
+template <uint32_t DTYPE, int THREADS, int K>
+__global__ __launch_bounds__(THREADS) void policy_kernel(const ff_policy_batch b, float* __restrict__ logp_out,
+                                                         float* __restrict__ loss_out, uint8_t* dlogits, uint64_t grad_stride,
+                                                         PolicyPart* __restrict__ parts)
 {
-    using S = Slot<DTYPE>;
-    constexpr int N = S::kItems;
-    __shared__ Running joined[kWaves];
-    __shared__ float factors[2];
+    using S = typename SlotOf<DTYPE>::Type;
+    constexpr int N = S::kItems, kWaves = THREADS / kWaveSize;
+    __shared__ float bases[kWaves];
+    __shared__ double sums[kWaves];
+    __shared__ float factors[3];
     const uint64_t t = blockIdx.x;
-    const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x / kWaveSize;
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     const uint32_t vocab = static_cast<uint32_t>(b.vocab), slots = vocab / N;
     const uint8_t* const row = static_cast<const uint8_t*>(b.logits) + t * b.row_stride * S::kBytes;
     uint8_t* const out = dlogits + t * grad_stride * S::kBytes;
     const int64_t y = b.targets[t];
-    const bool wanted = b.weights[t] != 0.f, inside = y >= 0 && y < static_cast<int64_t>(vocab);
+    const float w = b.weights[t];
+    const bool wanted = w != 0.f, inside = y >= 0 && y < static_cast<int64_t>(vocab);
     const uint32_t rest = slots * N + threadIdx.x;  // elements behind the last whole slot, one to a thread
-    Running r = {-INFINITY, 0.f};
+    const uint32_t wave_first = wave * kWaveSize;   // a wavefront's first slot of a round
+    bool empty = true;
+    double total = 0;
+    float base = 0;
+    u32x4 held[K];
+    Token k;
     if (wanted && inside) {
-        for (uint32_t k = threadIdx.x; k < slots; k += kThreads) {
+        const uint32_t last = slots ? slots - 1 : 0;
+        static_for<K>([&](auto i) {
+            const uint32_t slot = i * THREADS + threadIdx.x;
+            if (i * THREADS + wave_first < slots) held[int(i)] = load16_unaligned<true>(row + 16ull * (slot < slots ? slot : last));
+        });
+        k.z = S::one(row + y * S::kBytes);
+        k.old_logp = b.old_logp[t];
+        k.ref_logp = b.ref_logp ? b.ref_logp[t] : 0.f;
+        k.gain = b.advantages[t];
+        k.weight = w;
+        double sum = 0;
+        float own = -INFINITY;  // the thread's base
+        static_for<K>([&](auto i) {
+            if (i * THREADS + wave_first < slots) {
+                float z[N];
+                S::read(held[int(i)], z);
+                if (i * THREADS + wave_first + kWaveSize > slots) {  // the row's last wavefront
+                    const bool mine = i * THREADS + threadIdx.x < slots;
+                    static_for<N>([&](auto j) { z[int(j)] = mine ? z[int(j)] : -INFINITY; });
+                }
+                add(own, sum, z);
+            }
+        });
+        for (uint32_t first = K * THREADS + wave_first; first < slots; first += THREADS) {
+            const uint32_t slot = first + lane;
             float z[N];
-            S::read(load16_unaligned<false>(row + 16ull * k), z);
-            add(r, z);
+            S::read(load16_unaligned<false>(row + 16ull * (slot < slots ? slot : last)), z);
+            static_for<N>([&](auto j) { z[int(j)] = slot < slots ? z[int(j)] : -INFINITY; });
+            add(own, sum, z);
         }
-        if (rest < vocab) {
-            const float z[1] = {S::one(row + uint64_t(rest) * S::kBytes)};
-            add(r, z);
+        if (wave == 0) {
+            float z[1] = {rest < vocab ? S::one(row + uint64_t(rest) * S::kBytes) : -INFINITY};
+            add(own, sum, z);
         }
+        base = own;
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) r = join(r, Running{__shfl_xor(r.m, d), __shfl_xor(r.s, d)});
-        if (lane == 0) joined[wave] = r;
+        for (int d = 32; d >= 1; d >>= 1) base = fmaxf(base, __shfl_xor(base, d));
+        sum = moved(sum, own, base);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) {
+            bases[wave] = base;
+            sums[wave] = sum;
+        }
         __syncthreads();
-        r = joined[0];
-        for (int w = 1; w < kWaves; w++) r = join(r, joined[w]);
+        base = bases[0];
+        for (int i = 1; i < kWaves; i++) base = fmaxf(base, bases[i]);
+        for (int i = 0; i < kWaves; i++) total += moved(sums[i], bases[i], base);
+        empty = base == -INFINITY && total == 0;
+        base = base_of(base);
     }
-    if (!wanted || !inside || (r.m == -INFINITY && r.s == 0.f)) {
+    if (empty) {
         if (threadIdx.x == 0) {
-            logp[t] = token_loss[t] = 0.f;
+            logp_out[t] = loss_out[t] = 0.f;
             parts[t] = PolicyPart{0, 0, wanted ? kTokenInvalid : 0u, 0u};
         }
         if (dlogits) {
-            for (uint32_t k = threadIdx.x; k < slots; k += kThreads) store16_unaligned<false>(out + 16ull * k, u32x4{0, 0, 0, 0});
+            for (uint32_t i = threadIdx.x; i < slots; i += THREADS) store16_unaligned<true>(out + 16ull * i, u32x4{0, 0, 0, 0});
             if (rest < vocab) S::put(out + uint64_t(rest) * S::kBytes, 0.f);
         }
         return;
     }
-    if (threadIdx.x == 0) {
-        float share, target_grad;
-        token(b, t, r.m, r.s, S::one(row + y * S::kBytes), logp, token_loss, parts, share, target_grad);
-        factors[0] = share;
-        factors[1] = target_grad;
+    if (wave == 0) {
+        double logp, loss, kl, factor;
+        bool clipped;
+        token(b, k, base, total, lane, logp, loss, kl, clipped, factor);
+        if (lane == 0) {
+            logp_out[t] = static_cast<float>(logp);
+            loss_out[t] = static_cast<float>(loss);
+            parts[t] = PolicyPart{k.weight * loss, k.weight * kl, kTokenCounts | (clipped ? kTokenClipped : 0u), 0u};
+            S::set_factors(factors, factor, total);
+            factors[2] = static_cast<float>(factor * -expm1(logp));
+        }
     }
     if (!dlogits) return;
     __syncthreads();
-    const float share = factors[0], target_grad = factors[1], from = base(r.m);
-    for (uint32_t k = threadIdx.x; k < slots; k += kThreads) {
+    const float f0 = factors[0], f1 = factors[1], target_grad = factors[2];
+    const uint32_t y32 = static_cast<uint32_t>(y);
+    auto gradient = [&](const u32x4 in, const uint32_t slot) {
         float z[N];
-        S::read(load16_unaligned<false>(row + 16ull * k), z);
-        static_for<N>([&](auto i) {
-            z[int(i)] = share * exp_from(z[int(i)], from);
-            if (N * k + i == static_cast<uint32_t>(y)) z[int(i)] = target_grad;
-        });
-        store16_unaligned<false>(out + 16ull * k, S::write(z));
-    }
+        S::read(in, z);
+        static_for<N>([&](auto j) { z[int(j)] = S::gradient(z[int(j)] - base, f0); });
+        u32x4 g = S::write(z, f1);
+        if (slot == y32 / N) g = S::with(g, y32 % N, target_grad);
+        return g;
+    };
+    static_for<K>([&](auto i) {
+        const uint32_t slot = i * THREADS + threadIdx.x;
+        if (i * THREADS + wave_first < slots && slot < slots)
+            store16_unaligned<true>(out + 16ull * slot, gradient(held[int(i)], slot));
+    });
+    for (uint32_t slot = K * THREADS + threadIdx.x; slot < slots; slot += THREADS)
+        store16_unaligned<true>(out + 16ull * slot, gradient(load16_unaligned<false>(row + 16ull * slot), slot));
     if (rest < vocab) {
         const float z = S::one(row + uint64_t(rest) * S::kBytes);
-        S::put(out + uint64_t(rest) * S::kBytes, rest == static_cast<uint32_t>(y) ? target_grad : share * exp_from(z, from));
+        S::put(out + uint64_t(rest) * S::kBytes, rest == y32 ? target_grad : S::signed_by(S::gradient(z - base, f0), f1));
     }
 }
 
@@ -247,6 +327,21 @@ __global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const Pol
     *stats = ff_policy_stats{static_cast<float>(sums[0]), static_cast<float>(sums[1]), counts[0], counts[1], counts[2]};
 }
 
+using Kernel = void (*)(const ff_policy_batch, float*, float*, uint8_t*, uint64_t, PolicyPart*);
+struct Choice {
+    Kernel kernel;
+    int threads;
+};
+// By the slots of a row: whole rows in registers up to 16384.
+template <uint32_t DTYPE>
+Choice choose(uint64_t slots)
+{
+    if (slots <= 1024) return {policy_kernel<DTYPE, 256, 4>, 256};
+    if (slots <= 4096) return {policy_kernel<DTYPE, 512, 8>, 512};
+    if (slots <= 8192) return {policy_kernel<DTYPE, 1024, 8>, 1024};
+    return {policy_kernel<DTYPE, 1024, 16>, 1024};
+}
+
 }  // namespace
 
 uint64_t policy_workspace(uint64_t n_tokens, uint64_t)
@@ -259,8 +354,8 @@ hipError_t launch_policy(const ff_policy_batch& b, float* logp, float* token_los
 {
     PolicyPart* const parts = static_cast<PolicyPart*>(workspace);
     if (b.n_tokens) {
-        const auto kernel = b.dtype == FF_F32 ? policy_kernel<FF_F32> : b.dtype == FF_BF16 ? policy_kernel<FF_BF16> : policy_kernel<FF_F16>;
-        hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(b.n_tokens)), dim3(kThreads), 0, stream, b, logp, token_loss,
+        const Choice c = b.dtype == FF_F32 ? choose<FF_F32>(b.vocab / 4) : b.dtype == FF_BF16 ? choose<FF_BF16>(b.vocab / 8) : choose<FF_F16>(b.vocab / 8);
+        hipLaunchKernelGGL(c.kernel, dim3(static_cast<uint32_t>(b.n_tokens)), dim3(c.threads), 0, stream, b, logp, token_loss,
                            static_cast<uint8_t*>(dlogits), grad_stride, parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
