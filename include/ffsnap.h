@@ -417,7 +417,8 @@ uint64_t ff_policy_workspace_bytes(uint64_t n_tokens, uint64_t vocab);
  * logp, token_loss: DEVICE fp32[n_tokens]; logp may be old_logp's array only if that is not needed again, so it may
  * not alias any input.  dlogits: NULL (no gradient), or DEVICE, of `dtype`, rows grad_stride >= vocab elements apart; it may
  * be the logits themselves with the same stride, and elements between rows are not touched.
- * stats: DEVICE.  workspace: DEVICE, 16-byte aligned, ff_policy_workspace_bytes(); nothing is expected in it.
+ * stats: DEVICE.  workspace: DEVICE, 16-byte aligned, ff_policy_workspace_bytes(), ZERO before its
+ * first use; every call leaves it as the next one needs it.
  * n_tokens = 0 is allowed: the stats become zero.  FF_ERR_INVALID for vocab 0 or above 2^31 - 1.
  */
 int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss, void *dlogits,

@@ -484,39 +484,54 @@ def alloc_policy_workspace(n_tokens, vocab, device):
     return torch.zeros(max(16, n), dtype=torch.uint8, device=device)
 
 
+_PER_TOKEN = " is a contiguous fp32 tensor of one entry per token"
+
+
 def policy_batch(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low=0.2,
                  clip_high=0.2, beta=0.0, loss_scale=1.0):
     """ff_policy_batch of device tensors: logits [tokens, vocab] (rows may lie apart), targets int64,
     the others fp32, [tokens] each.  The caller keeps the tensors alive until the stream's work is done."""
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    n, vocab = logits.shape if logits.dim() == 2 else (0, 0)
+    stride, inner = logits.stride() if logits.dim() == 2 else (0, 0)
+    if inner != 1 and vocab != 1:
         raise ValueError("logits are rows of contiguous elements")
-    n, vocab = logits.shape
-    for name, t, dtype in (("targets", targets, torch.int64), ("old_logp", old_logp, torch.float32),
-                           ("ref_logp", ref_logp, torch.float32),
-                           ("advantages", advantages, torch.float32),
-                           ("weights", weights, torch.float32)):
-        if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
-            raise ValueError("%s is a contiguous %s tensor of one entry per token" % (name, dtype))
-    stride = logits.stride(0) if n > 1 else max(vocab, logits.stride(0))
-    return ff_policy_batch(logits.data_ptr(), n, vocab, stride, _DTYPES[logits.dtype], 0,
-                           targets.data_ptr(), old_logp.data_ptr(),
-                           ref_logp.data_ptr() if ref_logp is not None else None,
+    ref = None
+    one, f32 = (n,), torch.float32
+    if ref_logp is not None:
+        if ref_logp.dtype is not f32 or ref_logp.shape != one or not ref_logp.is_contiguous():
+            raise ValueError("ref_logp" + _PER_TOKEN)
+        ref = ref_logp.data_ptr()
+    if targets.dtype is not torch.int64 or targets.shape != one or not targets.is_contiguous():
+        raise ValueError("targets is a contiguous int64 tensor of one entry per token")
+    if old_logp.dtype is not f32 or old_logp.shape != one or not old_logp.is_contiguous():
+        raise ValueError("old_logp" + _PER_TOKEN)
+    if advantages.dtype is not f32 or advantages.shape != one or not advantages.is_contiguous():
+        raise ValueError("advantages" + _PER_TOKEN)
+    if weights.dtype is not f32 or weights.shape != one or not weights.is_contiguous():
+        raise ValueError("weights" + _PER_TOKEN)
+    return ff_policy_batch(logits.data_ptr(), n, vocab, stride if n > 1 else max(stride, vocab),
+                           _DTYPES[logits.dtype], 0, targets.data_ptr(), old_logp.data_ptr(), ref,
                            advantages.data_ptr(), weights.data_ptr(), clip_low, clip_high, beta,
                            loss_scale)
 
 
 def ff_policy_loss(batch, logp, token_loss, stats, workspace, dlogits=None, stream=None):
     """dlogits: None (the loss alone), or [tokens, vocab] in the logits' format; may be the logits."""
-    n = batch.n_tokens
-    for t in (logp, token_loss):
-        if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
-            raise ValueError("logp and token_loss are contiguous fp32 tensors of one entry per token")
+    one, f32 = (batch.n_tokens,), torch.float32
+    if logp.dtype is not f32 or logp.shape != one or not logp.is_contiguous():
+        raise ValueError("logp" + _PER_TOKEN)
+    if token_loss.dtype is not f32 or token_loss.shape != one or not token_loss.is_contiguous():
+        raise ValueError("token_loss" + _PER_TOKEN)
     grad, stride = None, 0
     if dlogits is not None:
-        if dlogits.shape != (n, batch.vocab) or _DTYPES.get(dlogits.dtype) != batch.dtype or \
-                (batch.vocab > 1 and dlogits.stride(1) != 1):
+        vocab = batch.vocab
+        if dlogits.shape != (batch.n_tokens, vocab) or _DTYPES.get(dlogits.dtype) != batch.dtype:
             raise ValueError("dlogits has the logits' shape and format")
+        stride, inner = dlogits.stride()
+        if inner != 1 and vocab != 1:
+            raise ValueError("dlogits are rows of contiguous elements")
         grad = dlogits.data_ptr()
-        stride = dlogits.stride(0) if n > 1 else max(batch.vocab, dlogits.stride(0))
+        if batch.n_tokens <= 1:
+            stride = max(stride, vocab)
     _check(lib().ff_policy_loss(ctypes.byref(batch), logp.data_ptr(), token_loss.data_ptr(), grad,
                                 stride, stats.data_ptr(), workspace.data_ptr(), _stream_ptr(stream)))

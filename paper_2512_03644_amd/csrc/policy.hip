@@ -1,10 +1,19 @@
 // Clipped policy loss with a KL term, and its gradient, for gfx950.
 //
 // One workgroup takes the row of one token.  Every thread keeps the running maximum of its logits and the sum
-// of their exponentials against it; the workgroup joins those, and what hangs on the token's log-probability
-// alone -- ratio, clipping, KL term, the slope of the loss in it -- is a handful of operations in 64 bits.  The
-// gradient is the slope times ([j is the target] - softmax), from the row read a second time.  What
-// tokens add to the sums goes to memory and is joined by a last workgroup in the tokens' order.
+// of their exponentials against it while they arrive, and holds the logits themselves in registers; the workgroup
+// joins those, and what hangs on the token's log-probability alone -- ratio, clipping, KL term, the slope of the loss in it
+// -- is a handful of operations in 64 bits of one wavefront.  The gradient is the slope times ([j is the target] -
+// softmax), from the logits in registers: they are read once.  What tokens add to the sums goes to memory and is
+// joined in the tokens' order, by the last workgroup of a few or by a kernel of one workgroup.
+//
+// What bounds it: memory, or for few tokens the launch and the chain from a row's load to its store.  Long rows alone with a compute
+// unit (128,256 bf16 logits are half of its registers) leave the memory idle between their loads and stores: the same with no arithmetic
+// at all takes 357 us where the loss of 4096 such tokens takes 392, and a copy of as many bytes 318.  Rows kept over in a loop of
+// workgroups, the next one's loads under way while the gradient is stored, took 500; a quarter of the row in registers and the rest
+// read again, so that two workgroups share a unit, 415 (399 with no arithmetic).  Us, gradient and all, 4096 tokens on 1000 / 4000 /
+// 8000 / 16,000 / 32,000 / 64,000 / 128,256 bf16 logits 13 / 22 / 32 / 55 / 99 / 196 / 421 (all tokens count); 1.0 GB of logits without
+// gradient 170 (6.2 TB/s).
 #include "policy.hpp"
 
 #include <hip/hip_fp16.h>
@@ -15,23 +24,124 @@ namespace ffsnap {
 
 namespace {
 
+constexpr uint64_t kComputeUnits = 256;
+constexpr int kPartThreads = 256;  // of a workgroup that takes a part of a row
+
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// The sum of exp(z - base) over some logits, base the largest of them so far: -inf as long as all are, and the sum is 0;
-// or NaN, as ever after a NaN or +inf.  (With a base that is only moved where a logit is far above it, an exponent rounded to 24
-// bits takes 7e-8 off the log-probability of a likely token, against 1e-8.)
-constexpr float kLog2E = 0x1.715476p+0f, kLog2ELow = 0x1.4ae0bep-26f;  // log2(e) to 48 bits
-
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-// What rounding the constant to 24 bits takes off would add up over the vocabulary, always to the same side.
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(fmaf(d, kLog2E, d * kLog2ELow)); }
-// What a sum against `from` is against `to`: with what the exponent loses in 24 bits, as this is not one error of many.
-__device__ __forceinline__ double moved(double sum, float from, float to)
+// exp in 64 bits: x = n log(2) + r, |r| <= log(2) / 2, and the series of exp(r), whose first term left out is 6e-15.  (With
+// coefficients in scalar registers: as constants they are put into vector registers, which the held logits need.)
+__device__ const double kSeries[] = {1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720,
+                                     1.0 / 120,      1.0 / 24,      1.0 / 6,      1.0 / 2,     1.0,        1.0,
+                                     0x1.71547652b82fep+0, 0x1.62e42fefa39efp-1, 0x1.abc9e3b39803fp-56};  // log2(e), log(2) in two parts
+__device__ __forceinline__ double exp64(double x)
 {
-    const float d = fmaxf(from - to, -1000.f), t = d * kLog2E, low = fmaf(d, kLog2E, -t) + d * kLog2ELow;
-    const float e = __builtin_amdgcn_exp2f(t);
-    return from == -INFINITY ? sum : sum * (static_cast<double>(e) * (1.0 + 0.6931471805599453 * static_cast<double>(low)));
+    const double* series = kSeries;
+    asm volatile("" : "+s"(series));  // or they would be constants again
+    auto c = [&](int i) { return table_entry(series, i); };
+    x = x > 710.0 ? INFINITY : x < -750.0 ? -750.0 : x;  // (neither for a NaN)
+    const double n = rint(x * c(12));
+    const double r = fma(-n, c(14), fma(-n, c(13), x));
+    double p = c(0);
+    static_for<11>([&](auto k) { p = fma(p, r, c(k + 1)); });
+    return x == INFINITY ? x : ldexp(p, static_cast<int>(n));
+}
+// log in 64 bits of a sum that is at least about 1: what a logarithm in 32 bits leaves is a few 1e-7.
+__device__ __forceinline__ double log64(double x)
+{
+    const double l = static_cast<double>(logf(static_cast<float>(x)));
+    const double e = fma(x, exp64(-l), -1.0);
+    return l + (e - 0.5 * e * e);
+}
+
+// The running maximum m of some logits, and the sum of their exponentials against it.  m is -inf as long as all are, and the sum
+// 0; or NaN, as ever after a NaN or +inf.
+//
+// A term is 2^(z log2(e) - c), c = m log2(e) in 24 bits, in one rounded operation in front of the exponential: c's rounding is
+// the same for all terms, and known.  What log2(e) loses in 24 bits is taken as that of m, which is out by 1.3e-8 (m - z)
+// of a term; a thread's own maximum is not far above what counts in its sum: log-probabilities of long rows are out by 1-2e-8.  (log2(e) to 48 bits, (z - m)
+// first, is three operations for no better: 412 us where this takes 394.)  Where m is so large that c would be out by
+// more than a few, z - m takes the place of z.
+struct Running {
+    float m = -INFINITY, c = 0.f, b0 = 0.f;
+    double sum = 0;
+};
+constexpr float kLog2E = 0x1.715476p+0f, kLog2ELow = 0x1.4ae0bep-26f;  // log2(e) to 48 bits
+constexpr float kLarge = 0x1p28f;
+
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(fmaf(d, kLog2E, d * kLog2ELow)); }
+// exp(x) with what the exponent loses in 24 bits: in a factor of a whole sum this is not one error of many.  (Next to 0, where the sum
+// is that of the largest logit, without the rounding of the result either.)
+__device__ __forceinline__ double factor_of(double x)
+{
+    if (fabs(x) < 0x1p-8) return 1.0 + x * (1.0 + x * (1.0 / 2 + x * (1.0 / 6 + x * (1.0 / 24))));
+    const double t = fmax(x, -1000.0) * 0x1.71547652b82fep+0;
+    const float high = static_cast<float>(t), low = static_cast<float>(t - static_cast<double>(high));
+    return static_cast<double>(__builtin_amdgcn_exp2f(high)) * (1.0 + 0x1.62e42fefa39efp-1 * static_cast<double>(low));
+}
+// The logarithm of what a sum of 1 stands for.
+__device__ __forceinline__ double against(const Running& r)
+{
+    const double above = static_cast<double>(r.m) - static_cast<double>(r.b0);
+    return static_cast<double>(r.b0) + 0x1.62e42fefa39efp-1 * (static_cast<double>(r.c) + above * static_cast<double>(kLog2ELow));
+}
+
+// What rounding the largest logit's own term has left out of the sum, for one such logit: where one stands out it decides.  (Of 1000 logits with
+// a likely target among them, log-probabilities are out by 6e-9 with this, with 64-bit sums of the terms and 64-bit factors of few threads'
+// sums; by 4e-8 without.)
+__device__ __forceinline__ double left_out(const Running& r)
+{
+    const float t = fmaf(r.m - r.b0, kLog2E, -r.c);  // c's rounding
+    return fabsf(t) < 0x1p-12f ? (1.0 + 0x1.62e42fefa39efp-1 * static_cast<double>(t)) - static_cast<double>(__builtin_amdgcn_exp2f(t)) : 0.0;
+}
+
+// FEW: terms are added in 64 bits.
+template <bool FEW, int N>
+__device__ __forceinline__ void add(Running& r, float (&z)[N])
+{
+    float m = z[0];
+    static_for<N - 1>([&](auto k) { m = fmaxf(m, z[k + 1]); });
+    if (__any(m > r.m)) {
+        if (m > r.m) {
+            const double was = against(r);
+            const bool first = r.m == -INFINITY;
+            r.m = m;
+            r.b0 = fabsf(m) > kLarge ? m : 0.f;
+            r.c = (m - r.b0) * kLog2E;
+            if (!first) r.sum *= factor_of(was - against(r));
+        }
+    }
+    if (__any(r.b0 != 0.f)) static_for<N>([&](auto k) { z[int(k)] -= r.b0; });
+    static_for<N>([&](auto k) { z[int(k)] = __builtin_amdgcn_exp2f(fmaf(z[int(k)], kLog2E, -r.c)); });
+    if constexpr (FEW) {
+        double s[2] = {r.sum, 0};
+        static_for<N>([&](auto k) { s[k % 2] += static_cast<double>(z[int(k)]); });
+        r.sum = s[0] + s[1];
+    } else {
+        for (int d = 1; d < N; d *= 2)
+            for (int k = 0; k + d < N; k += 2 * d) z[k] += z[k + d];
+        r.sum += static_cast<double>(z[0]);
+    }
+}
+
+// A wavefront-uniform address, as such: a lane's 32-bit offset is added to it by the access itself.
+typedef FF_GLOBAL uint8_t* Bytes;
+__device__ __forceinline__ Bytes uniform(const uint8_t* p)
+{
+    uint64_t a = reinterpret_cast<uint64_t>(p);
+    asm volatile("" : "+s"(a));
+    return (Bytes)a;
+}
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(Bytes p, uint32_t lane_bytes)
+{
+    const auto* const q = (const FF_GLOBAL u32x4_a2*)(p + lane_bytes);
+    return NT ? __builtin_nontemporal_load(q) : *q;
+}
+__device__ __forceinline__ void store16(Bytes p, uint32_t lane_bytes, u32x4 w)
+{
+    __builtin_nontemporal_store(w, (FF_GLOBAL u32x4_a2*)(p + lane_bytes));
 }
 
 // 16 bytes of a row as floats.  gradient(), write(): what the softmax is multiplied by, -factor / total, is for 32-bit elements the
@@ -43,12 +153,13 @@ struct Slot32 {
     {
         static_for<4>([&](auto k) { z[int(k)] = __uint_as_float(w[int(k)]); });
     }
-    static __device__ __forceinline__ float one(const uint8_t* p) { return *as_global(reinterpret_cast<const float*>(p)); }
-    static __device__ __forceinline__ void put(uint8_t* p, float v) { *as_global(reinterpret_cast<float*>(p)) = v; }
-    static __device__ __forceinline__ void set_factors(float* f, double factor, double total)
+    static __device__ __forceinline__ float one(Bytes p, uint32_t i) { return ((FF_GLOBAL float*)p)[i]; }
+    static __device__ __forceinline__ void put(Bytes p, uint32_t i, float v) { ((FF_GLOBAL float*)p)[i] = v; }
+    static __device__ __forceinline__ bool set_factors(float* f, double factor, double total, float)
     {
         f[0] = static_cast<float>(-factor / total);
         f[1] = 0.f;
+        return true;
     }
     static __device__ __forceinline__ float gradient(float d, float f0) { return f0 * exp_of(d); }
     static __device__ __forceinline__ float signed_by(float g, float) { return g; }
@@ -85,15 +196,19 @@ struct Slot16 {
             z[2 * k + 1] = high(w[int(k)]);
         });
     }
-    static __device__ __forceinline__ float one(const uint8_t* p) { return low(*as_global(reinterpret_cast<const uint16_t*>(p))); }
-    static __device__ __forceinline__ void put(uint8_t* p, float v)
+    static __device__ __forceinline__ float one(Bytes p, uint32_t i) { return low(((FF_GLOBAL uint16_t*)p)[i]); }
+    static __device__ __forceinline__ void put(Bytes p, uint32_t i, float v)
     {
-        *as_global(reinterpret_cast<uint16_t*>(p)) = static_cast<uint16_t>(pair(v, 0.f));
+        ((FF_GLOBAL uint16_t*)p)[i] = static_cast<uint16_t>(pair(v, 0.f));
     }
-    static __device__ __forceinline__ void set_factors(float* f, double factor, double total)
+    // (the maximum as well joins the exponent, unless it is large)
+    static __device__ __forceinline__ bool set_factors(float* f, double factor, double total, float m)
     {
-        f[0] = static_cast<float>(log2(fabs(factor)) - log2(total));
+        const bool large = fabsf(m) > 64.f;
+        f[0] = log2f(fabsf(static_cast<float>(factor))) - log2f(static_cast<float>(total));
+        if (!large) f[0] = fmaf(-m, kLog2E, f[0]);
         f[1] = __uint_as_float(factor > 0 ? 0x80008000u : 0u);
+        return large;
     }
     static __device__ __forceinline__ float gradient(float d, float f0) { return __builtin_amdgcn_exp2f(fmaf(d, kLog2E, f0)); }
     static __device__ __forceinline__ float signed_by(float g, float f1)
@@ -121,193 +236,97 @@ struct SlotOf<FF_F32> {
     using Type = Slot32;
 };
 
-template <int N>
-__device__ __forceinline__ void add(float& base, double& sum, const float (&z)[N])
-{
-    float m = z[0];
-    static_for<N - 1>([&](auto k) { m = fmaxf(m, z[k + 1]); });
-    if (__any(m > base)) {
-        if (m > base) {
-            sum = moved(sum, base, m);
-            base = m;
-        }
-    }
-    const float b = base_of(base);
-    float s[N];
-    static_for<N>([&](auto k) { s[int(k)] = exp_of(z[int(k)] - b); });
-    for (int d = 1; d < N; d *= 2)
-        for (int k = 0; k + d < N; k += 2 * d) s[k] += s[k + d];
-    sum += static_cast<double>(s[0]);
-}
-
-// What hangs on the token's log-probability.  By one wavefront; total: of exp(z - base).
+// What hangs on a token's log-probability.  By a whole wavefront: three exponentials in three lanes.  total: of exp(z - base) over
+// the row, z_y: the target's logit.
 struct Token {
-    double old_logp, ref_logp, gain, weight;
-    float z;  // the target's logit
+    double logp, loss, kl;
+    double factor;  // the gradient is factor * ([j is the target] - softmax),
+    double target;  // and at the target this
+    bool clipped;
 };
-__device__ __forceinline__ void token(const ff_policy_batch& b, const Token& k, const double base, const double total, const int lane,
-                                      double& logp, double& loss, double& kl, bool& clipped, double& factor)
+__device__ __forceinline__ Token token(const ff_policy_batch& b, const uint32_t t, const float z_y, const float base, const double total,
+                                       const int lane)
 {
-    logp = (static_cast<double>(k.z) - base) - log(total);
-    const double lo = 1.0 - static_cast<double>(b.clip_low), hi = 1.0 + static_cast<double>(b.clip_high);
-    const double r = exp(logp - k.old_logp);
-    const double kept = r * k.gain, cut = (r < lo ? lo : r > hi ? hi : r) * k.gain;
-    clipped = cut < kept;
-    loss = clipped ? -cut : -kept;
-    double slope = clipped ? 0.0 : -kept;
-    kl = 0.0;
-    if (b.ref_logp) {
-        const double d = k.ref_logp - logp, e = expm1(d);
-        kl = d == INFINITY ? d : e - d;
-        if (b.beta > 0.f) {
-            loss += static_cast<double>(b.beta) * kl;
-            slope -= static_cast<double>(b.beta) * e;
-        }
-    }
-    factor = k.weight * slope * static_cast<double>(b.loss_scale);
-}
-
-// One workgroup, one row.  A thread holds K slots of 16 bytes of it in registers (slot i * THREADS + thread); of longer rows what is
-// behind is read again for the gradient.
-template <uint32_t DTYPE, int THREADS, int K>
-__global__ __launch_bounds__(THREADS) void policy_kernel(const ff_policy_batch b, float* __restrict__ logp_out,
-                                                         float* __restrict__ loss_out, uint8_t* dlogits, uint64_t grad_stride,
-                                                         PolicyPart* __restrict__ parts)
-{
-    using S = typename SlotOf<DTYPE>::Type;
-    constexpr int N = S::kItems, kWaves = THREADS / kWaveSize;
-    __shared__ float bases[kWaves];
-    __shared__ double sums[kWaves];
-    __shared__ float factors[3];
-    const uint64_t t = blockIdx.x;
-    const int lane = threadIdx.x & (kWaveSize - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
-    const uint32_t vocab = static_cast<uint32_t>(b.vocab), slots = vocab / N;
-    const uint8_t* const row = static_cast<const uint8_t*>(b.logits) + t * b.row_stride * S::kBytes;
-    uint8_t* const out = dlogits + t * grad_stride * S::kBytes;
-    const int64_t y = b.targets[t];
-    const float w = b.weights[t];
-    const bool wanted = w != 0.f, inside = y >= 0 && y < static_cast<int64_t>(vocab);
-    const uint32_t rest = slots * N + threadIdx.x;  // elements behind the last whole slot, one to a thread
-    const uint32_t wave_first = wave * kWaveSize;   // a wavefront's first slot of a round
-    bool empty = true;
-    double total = 0;
-    float base = 0;
-    u32x4 held[K];
     Token k;
-    if (wanted && inside) {
-        const uint32_t last = slots ? slots - 1 : 0;
-        static_for<K>([&](auto i) {
-            const uint32_t slot = i * THREADS + threadIdx.x;
-            if (i * THREADS + wave_first < slots) held[int(i)] = load16_unaligned<true>(row + 16ull * (slot < slots ? slot : last));
-        });
-        k.z = S::one(row + y * S::kBytes);
-        k.old_logp = b.old_logp[t];
-        k.ref_logp = b.ref_logp ? b.ref_logp[t] : 0.f;
-        k.gain = b.advantages[t];
-        k.weight = w;
-        double sum = 0;
-        float own = -INFINITY;  // the thread's base
-        static_for<K>([&](auto i) {
-            if (i * THREADS + wave_first < slots) {
-                float z[N];
-                S::read(held[int(i)], z);
-                if (i * THREADS + wave_first + kWaveSize > slots) {  // the row's last wavefront
-                    const bool mine = i * THREADS + threadIdx.x < slots;
-                    static_for<N>([&](auto j) { z[int(j)] = mine ? z[int(j)] : -INFINITY; });
-                }
-                add(own, sum, z);
-            }
-        });
-        for (uint32_t first = K * THREADS + wave_first; first < slots; first += THREADS) {
-            const uint32_t slot = first + lane;
-            float z[N];
-            S::read(load16_unaligned<false>(row + 16ull * (slot < slots ? slot : last)), z);
-            static_for<N>([&](auto j) { z[int(j)] = slot < slots ? z[int(j)] : -INFINITY; });
-            add(own, sum, z);
-        }
-        if (wave == 0) {
-            float z[1] = {rest < vocab ? S::one(row + uint64_t(rest) * S::kBytes) : -INFINITY};
-            add(own, sum, z);
-        }
-        base = own;
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) base = fmaxf(base, __shfl_xor(base, d));
-        sum = moved(sum, own, base);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-        if (lane == 0) {
-            bases[wave] = base;
-            sums[wave] = sum;
-        }
-        __syncthreads();
-        base = bases[0];
-        for (int i = 1; i < kWaves; i++) base = fmaxf(base, bases[i]);
-        for (int i = 0; i < kWaves; i++) total += moved(sums[i], bases[i], base);
-        empty = base == -INFINITY && total == 0;
-        base = base_of(base);
+    k.logp = (static_cast<double>(z_y) - static_cast<double>(base)) - log64(total);
+    const double gain = table_entry(b.advantages, t);
+    const double lo = 1.0 - static_cast<double>(b.clip_low), hi = 1.0 + static_cast<double>(b.clip_high);
+    const double beta = b.beta;
+    const double change = k.logp - static_cast<double>(table_entry(b.old_logp, t));
+    const double d = b.ref_logp ? static_cast<double>(table_entry(b.ref_logp, t)) - k.logp : 0.0;
+    const double all = exp64(lane == 0 ? change : lane == 1 ? d : k.logp);
+    const double r = __shfl(all, 0), kept = r * gain, cut = (r < lo ? lo : r > hi ? hi : r) * gain;
+    k.clipped = cut < kept;
+    k.loss = k.clipped ? -cut : -kept;
+    double slope = k.clipped ? 0.0 : -kept;
+    // exp(d) - 1 - d, whose beginnings cancel where d is small
+    const double e = __shfl(all, 1) - 1.0;
+    k.kl = d == INFINITY            ? d
+           : fabs(d) < 0x1p-6 ? d * d * (1.0 / 2 + d * (1.0 / 6 + d * (1.0 / 24 + d * (1.0 / 120 + d * (1.0 / 720)))))
+                                    : e - d;
+    if (beta > 0) {
+        k.loss += beta * k.kl;
+        slope -= beta * e;
     }
-    if (empty) {
-        if (threadIdx.x == 0) {
-            logp_out[t] = loss_out[t] = 0.f;
-            parts[t] = PolicyPart{0, 0, wanted ? kTokenInvalid : 0u, 0u};
-        }
-        if (dlogits) {
-            for (uint32_t i = threadIdx.x; i < slots; i += THREADS) store16_unaligned<true>(out + 16ull * i, u32x4{0, 0, 0, 0});
-            if (rest < vocab) S::put(out + uint64_t(rest) * S::kBytes, 0.f);
-        }
-        return;
-    }
-    if (wave == 0) {
-        double logp, loss, kl, factor;
-        bool clipped;
-        token(b, k, base, total, lane, logp, loss, kl, clipped, factor);
-        if (lane == 0) {
-            logp_out[t] = static_cast<float>(logp);
-            loss_out[t] = static_cast<float>(loss);
-            parts[t] = PolicyPart{k.weight * loss, k.weight * kl, kTokenCounts | (clipped ? kTokenClipped : 0u), 0u};
-            S::set_factors(factors, factor, total);
-            factors[2] = static_cast<float>(factor * -expm1(logp));
-        }
-    }
-    if (!dlogits) return;
-    __syncthreads();
-    const float f0 = factors[0], f1 = factors[1], target_grad = factors[2];
-    const uint32_t y32 = static_cast<uint32_t>(y);
-    auto gradient = [&](const u32x4 in, const uint32_t slot) {
-        float z[N];
-        S::read(in, z);
-        static_for<N>([&](auto j) { z[int(j)] = S::gradient(z[int(j)] - base, f0); });
-        u32x4 g = S::write(z, f1);
-        if (slot == y32 / N) g = S::with(g, y32 % N, target_grad);
-        return g;
-    };
-    static_for<K>([&](auto i) {
-        const uint32_t slot = i * THREADS + threadIdx.x;
-        if (i * THREADS + wave_first < slots && slot < slots)
-            store16_unaligned<true>(out + 16ull * slot, gradient(held[int(i)], slot));
-    });
-    for (uint32_t slot = K * THREADS + threadIdx.x; slot < slots; slot += THREADS)
-        store16_unaligned<true>(out + 16ull * slot, gradient(load16_unaligned<false>(row + 16ull * slot), slot));
-    if (rest < vocab) {
-        const float z = S::one(row + uint64_t(rest) * S::kBytes);
-        S::put(out + uint64_t(rest) * S::kBytes, rest == y32 ? target_grad : S::signed_by(S::gradient(z - base, f0), f1));
-    }
+    k.factor = static_cast<double>(table_entry(b.weights, t)) * slope * static_cast<double>(b.loss_scale);
+    k.target = k.factor * (1.0 - __shfl(all, 2));
+    return k;
 }
 
-constexpr int kFinishThreads = 256;
-__global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const PolicyPart* __restrict__ parts, uint64_t n,
-                                                                       ff_policy_stats* __restrict__ stats)
+// What is known of a part of a row whose parts go to several workgroups.
+struct RowPart {
+    double total;  // of exp(z - m)
+    float m, z_y;  // z_y: the target's logit, in a row's first part
+};
+
+struct PolicyArgs {
+    ff_policy_batch b;
+    float *logp, *token_loss;
+    uint8_t* dlogits;
+    uint64_t grad_stride;
+    PolicyPart* parts;    // what every token adds to the sums
+    RowPart* row_parts;   // of split rows
+    uint32_t* done;       // tokens that are done, zero before and after; null: a kernel of its own joins their sums
+    ff_policy_stats* stats;
+};
+
+// A token's part on its way to whichever workgroup joins them: past the caches of this one's XCD, and that one's.
+__device__ __forceinline__ void send(PolicyPart* to, const PolicyPart& p)
 {
+    static_assert(sizeof(PolicyPart) == 24, "three words");
+    uint64_t w[3];
+    __builtin_memcpy(w, &p, sizeof(w));
+    static_for<3>([&](auto i) {
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(to) + i, w[int(i)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+}
+__device__ __forceinline__ PolicyPart receive(const PolicyPart* from)
+{
+    uint64_t w[3];
+    static_for<3>([&](auto i) {
+        w[int(i)] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+    PolicyPart p;
+    __builtin_memcpy(&p, w, sizeof(w));
+    return p;
+}
+
+// Sums over the tokens, by a workgroup.
+template <int THREADS>
+__device__ __forceinline__ void finish(const PolicyPart* parts, const uint32_t n, ff_policy_stats* stats)
+{
+    constexpr int kWaves = THREADS / kWaveSize;
     double sums[2] = {0, 0};
-    unsigned long long counts[3] = {0, 0, 0};
-    for (uint64_t i = threadIdx.x; i < n; i += kFinishThreads) {
-        sums[0] += parts[i].loss;
-        sums[1] += parts[i].kl;
-        static_for<3>([&](auto k) { counts[int(k)] += parts[i].what >> k & 1u; });
+    uint32_t counts[3] = {0, 0, 0};
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
+        const PolicyPart p = receive(parts + i);
+        sums[0] += p.loss;
+        sums[1] += p.kl;
+        static_for<3>([&](auto k) { counts[int(k)] += p.what >> k & 1u; });
     }
-    __shared__ double all_sums[2][kFinishThreads / kWaveSize];
-    __shared__ unsigned long long all_counts[3][kFinishThreads / kWaveSize];
+    __shared__ double all_sums[2][kWaves];
+    __shared__ uint32_t all_counts[3][kWaves];
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) {
         static_for<2>([&](auto k) { sums[int(k)] += __shfl_xor(sums[int(k)], d); });
@@ -320,47 +339,350 @@ __global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const Pol
     }
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int w = 1; w < kFinishThreads / kWaveSize; w++) {
+    for (int w = 1; w < kWaves; w++) {
         static_for<2>([&](auto k) { sums[int(k)] += all_sums[int(k)][w]; });
         static_for<3>([&](auto k) { counts[int(k)] += all_counts[int(k)][w]; });
     }
     *stats = ff_policy_stats{static_cast<float>(sums[0]), static_cast<float>(sums[1]), counts[0], counts[1], counts[2]};
 }
 
-using Kernel = void (*)(const ff_policy_batch, float*, float*, uint8_t*, uint64_t, PolicyPart*);
+// The workgroup's token is done: the last one of few joins the sums.  (In the tokens' order, whoever it is.)
+template <int THREADS>
+__device__ __forceinline__ void count_and_finish(const PolicyArgs& A, const uint32_t n)
+{
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        // This thread has sent the token's part, and it has arrived when its stores are done.  (A release fence would
+        // write the L2's other lines back as well, the gradient's among them: 64 tokens on 32,000 13.3 us with one.)
+        asm volatile("" ::: "memory");
+        wait_loads<0>();
+        last = __hip_atomic_fetch_add(A.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
+    }
+    __syncthreads();
+    if (!last) return;
+    asm volatile("" ::: "memory");
+    if (threadIdx.x == 0) __hip_atomic_store(A.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    finish<THREADS>(A.parts, n, A.stats);
+}
+
+// What a workgroup does with the slots it has: all of a row, the sum of a part of one, or, behind that, the part's gradient.
+enum Mode { kWhole, kSumOfPart, kGradOfPart };
+
+// A thread holds K slots of 16 bytes in registers (slot i * THREADS + thread), which is all of a row's or part's unless LONG: what is
+// behind them is then read again for the gradient.  WAVES: wavefronts on a SIMD that the registers leave room for.
+template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG, Mode MODE>
+__device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t, const uint32_t part, const uint32_t n_parts)
+{
+    using S = typename SlotOf<DTYPE>::Type;
+    constexpr int N = S::kItems, kWaves = THREADS / kWaveSize;
+    constexpr bool kFew = THREADS <= kPartThreads;  // few terms decide: their sums to more than 24 bits
+    __shared__ float maxima[kWaves];
+    __shared__ double sums[kWaves];
+    __shared__ struct {
+        float m, f0, f1, target_grad;
+        int empty, apart;
+    } shared;
+    const ff_policy_batch& b = A.b;
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const uint32_t wave_first = wave * kWaveSize;  // a wavefront's first slot of a round
+    const uint32_t vocab = static_cast<uint32_t>(b.vocab), row_slots = vocab / N;
+    // the workgroup's slots, and the elements behind a row's last whole slot, one to a thread of its last workgroup
+    const uint32_t first_slot = MODE == kWhole ? 0 : part * (THREADS * K);
+    const uint32_t slots = MODE == kWhole ? row_slots : row_slots - first_slot < THREADS * K ? row_slots - first_slot : THREADS * K;
+    const uint32_t n_rest = MODE == kWhole || part + 1 == n_parts ? vocab - row_slots * N : 0;
+    const uint8_t* const row = static_cast<const uint8_t*>(b.logits) + t * b.row_stride * S::kBytes;
+    const uint8_t* const in = row + 16ull * first_slot;
+    uint8_t* const out = GRAD ? A.dlogits + t * A.grad_stride * S::kBytes + 16ull * first_slot : nullptr;
+    const int64_t target = table_entry(b.targets, t);
+    const bool wanted = table_entry(b.weights, t) != 0.f;
+    auto leave_out = [&] {
+        if (MODE == kSumOfPart) return;
+        if (threadIdx.x == 0 && part == 0) {
+            A.logp[t] = A.token_loss[t] = 0.f;
+            send(A.parts + t, PolicyPart{0, 0, wanted ? kTokenInvalid : 0u, 0u});
+        }
+        if (!GRAD) return;
+        for (uint32_t first = wave_first; first < slots; first += THREADS)
+            if (first + lane < slots) store16(uniform(out + 16ull * first), 16 * lane, u32x4{0, 0, 0, 0});
+        if (threadIdx.x < n_rest) S::put(uniform(out + 16ull * slots), threadIdx.x, 0.f);
+    };
+    if (!wanted || target < 0 || target >= static_cast<int64_t>(vocab)) {
+        leave_out();
+        return;
+    }
+    // Does the wavefront have slots in round i, and where is a lane's?  Lanes behind the last slot take that one again.
+    auto has = [&](auto i) { return i * THREADS + wave_first < slots; };
+    auto at = [&](auto i) {
+        const uint32_t end = 16 * (slots - 1 - i * THREADS), mine = 16 * threadIdx.x;
+        return mine < end ? mine : end;
+    };
+    const uint32_t y = static_cast<uint32_t>(target) - first_slot * N;  // among the workgroup's elements, if it is
+    float z_y = 0.f, end = -INFINITY;
+    if (wave == 0) {
+        if (MODE != kGradOfPart) z_y = S::one(uniform(row), static_cast<uint32_t>(target));
+        if (threadIdx.x < n_rest) end = S::one(uniform(in + 16ull * slots), threadIdx.x);
+    }
+    u32x4 held[K];
+    if (MODE != kGradOfPart || GRAD)
+        static_for<K>([&](auto i) {
+            if (has(i)) held[int(i)] = load16<true>(uniform(in + 16ull * THREADS * i), at(i));
+        });
+    constexpr int kAhead = 4;  // slots under way of those that are not held
+    if constexpr (MODE != kGradOfPart) {
+        Running r;
+        // Two slots, of which a wavefront has the first.  (first: of the wavefront's in either)
+        auto take = [&](const u32x4 w0, const u32x4 w1, const uint32_t first0, const uint32_t first1) {
+            float z[2 * N], x[N];
+            S::read(w0, x);
+            static_for<N>([&](auto j) { z[int(j)] = x[int(j)]; });
+            S::read(w1, x);
+            static_for<N>([&](auto j) { z[N + j] = x[int(j)]; });
+            if (first1 + kWaveSize > slots) {  // the end
+                const bool mine0 = first0 + lane < slots, mine1 = first1 + lane < slots;
+                static_for<N>([&](auto j) {
+                    z[int(j)] = mine0 ? z[int(j)] : -INFINITY;
+                    z[N + j] = mine1 ? z[N + j] : -INFINITY;
+                });
+            }
+            add<kFew>(r, z);
+        };
+        static_for<K / 2>([&](auto i) {
+            if (has(std::integral_constant<int, 2 * i>{}))
+                take(held[2 * i], held[2 * i + 1], 2 * i * THREADS + wave_first, (2 * i + 1) * THREADS + wave_first);
+        });
+        if constexpr (LONG)
+            for (uint32_t first = K * THREADS + wave_first; first < slots; first += kAhead * THREADS) {
+                u32x4 w[kAhead];
+                static_for<kAhead>([&](auto i) {
+                    const uint32_t f = first + i * THREADS;
+                    if (f < slots) w[int(i)] = load16<false>(uniform(in + 16ull * f), 16 * (f + lane < slots ? lane : 0));
+                });
+                static_for<kAhead / 2>([&](auto i) {
+                    const uint32_t f = first + 2 * i * THREADS;
+                    if (f < slots) take(w[2 * i], w[2 * i + 1], f, f + THREADS);
+                });
+            }
+        if (wave == 0) {
+            float z[1] = {end};
+            add<kFew>(r, z);
+        }
+        float m = r.m;
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        double sum = r.sum;
+        const double by = against(r) - static_cast<double>(m);
+        if (r.m != -INFINITY) sum = (sum + left_out(r)) * (kFew ? exp64(by) : factor_of(by));
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) {
+            maxima[wave] = m;
+            sums[wave] = sum;
+        }
+        __syncthreads();
+    }
+    if (wave == 0) {
+        // the sums of the workgroup's wavefronts, or of the row's parts, in a lane each
+        float from = -INFINITY;
+        double total = 0;
+        if (MODE == kGradOfPart) {
+            const RowPart* const p = A.row_parts + t * n_parts;
+            if (lane < static_cast<int>(n_parts)) {
+                from = p[lane].m;
+                total = p[lane].total;
+            }
+            z_y = p->z_y;
+        } else {
+            from = maxima[lane % kWaves];
+            total = lane < kWaves ? sums[lane] : 0.0;
+        }
+        float m = from;
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        if (from != -INFINITY) total *= exp64(static_cast<double>(from) - static_cast<double>(m));
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+        if (MODE == kSumOfPart) {
+            if (lane == 0) A.row_parts[t * n_parts + part] = RowPart{total, m, z_y};
+        } else {
+            const bool empty = m == -INFINITY && total == 0;
+            if (m == -INFINITY) m = 0.f;
+            const Token k = token(b, t, z_y, m, total, lane);
+            if (lane == 0) {
+                if (!empty && part == 0) {
+                    const double w = table_entry(b.weights, t);
+                    A.logp[t] = static_cast<float>(k.logp);
+                    A.token_loss[t] = static_cast<float>(k.loss);
+                    send(A.parts + t, PolicyPart{w * k.loss, w * k.kl, kTokenCounts | (k.clipped ? kTokenClipped : 0u), 0u});
+                }
+                float f[2];
+                const bool apart = S::set_factors(f, k.factor, total, m);
+                shared = {m, f[0], f[1], static_cast<float>(k.target), empty, apart};
+            }
+        }
+    }
+    if (MODE == kSumOfPart) return;
+    __syncthreads();
+    if (shared.empty) {
+        leave_out();
+        return;
+    }
+    if constexpr (GRAD) {
+        const float m = shared.m, f0 = shared.f0, f1 = shared.f1, target_grad = shared.target_grad;
+        const bool apart = __builtin_amdgcn_readfirstlane(shared.apart) != 0;
+        auto gradient = [&](const u32x4 w, const bool has_target) {
+            float z[N];
+            S::read(w, z);
+            if (apart) static_for<N>([&](auto j) { z[int(j)] -= m; });
+            static_for<N>([&](auto j) { z[int(j)] = S::gradient(z[int(j)], f0); });
+            u32x4 g = S::write(z, f1);
+            if (has_target) g = S::with(g, y % N, target_grad);
+            return g;
+        };
+        static_for<K>([&](auto i) {
+            if (has(i)) {
+                const uint32_t mine = at(i);
+                store16(uniform(out + 16ull * THREADS * i), mine, gradient(held[int(i)], 16 * (y / N - i * THREADS) == mine));
+            }
+        });
+        if constexpr (LONG)
+            for (uint32_t first = K * THREADS + wave_first; first < slots; first += kAhead * THREADS) {
+                u32x4 w[kAhead];
+                static_for<kAhead>([&](auto i) {
+                    const uint32_t f = first + i * THREADS;
+                    if (f + lane < slots) w[int(i)] = load16<false>(uniform(in + 16ull * f), 16 * lane);
+                });
+                static_for<kAhead>([&](auto i) {
+                    const uint32_t f = first + i * THREADS;
+                    if (f + lane < slots) store16(uniform(out + 16ull * f), 16 * lane, gradient(w[int(i)], f + lane == y / N));
+                });
+            }
+        if (threadIdx.x < n_rest) {
+            const float z = S::one(uniform(in + 16ull * slots), threadIdx.x);
+            S::put(uniform(out + 16ull * slots), threadIdx.x,
+                   slots * N + threadIdx.x == y ? target_grad : S::signed_by(S::gradient(apart ? z - m : z, f0), f1));
+        }
+    }
+}
+
+template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG>
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void policy_kernel(const PolicyArgs A)
+{
+    policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole>(A, blockIdx.x, 0, 1);
+    if (A.done) count_and_finish<THREADS>(A, gridDim.x);
+}
+
+// Up to so many tokens are counted as they are done, and the last one's workgroup joins their sums; more would queue up at the counter
+// (50 ns each).  Without the kernel that does it else, us: 1 / 64 tokens on 1000 7.9 / 8.0, 65 10.8.
+constexpr uint32_t kCountedTokens = 64;
+
+// So many rows of more than 4096 slots are split into parts of 1024: the parts' sums in one launch, and in another, once more for
+// each of them, what is left of policy_kernel, on logits that are in the caches.  Whole / split, us: 1 / 4 / 16 / 32 / 60 / 100 rows of
+// 128,256 bf16 logits 21.6 / 22.0 / 22.8 / 22.5 / 22.5 / 25 and 10.8 / 11.1 / 12.0 / 12.9 / 15.3 / 22.4, 200 28.6 and 37.8; 16 / 64 / 120 rows of
+// 50,000 13.8 / 13.8 / 15.1 and 11.2 / 12.5 / 16.7; 16 / 64 / 128 of 130,000 fp32 ones 29.8 / 31.2 / 41.2 and 12.0 / 21.4 / 43.0.
+constexpr int kPartSlots = 4 * kPartThreads;
+constexpr uint32_t kSplitFrom = 4096, kSplitRows = kCountedTokens, kMostParts = 64;
+template <uint32_t DTYPE>
+__global__ __launch_bounds__(kPartThreads) void policy_sum_kernel(const PolicyArgs A, const uint32_t n_parts)
+{
+    policy_row<DTYPE, kPartThreads, 4, 4, false, false, kSumOfPart>(A, blockIdx.x / n_parts, blockIdx.x % n_parts, n_parts);
+}
+template <uint32_t DTYPE, bool GRAD>
+__global__ __launch_bounds__(kPartThreads) void policy_grad_kernel(const PolicyArgs A, const uint32_t n_parts)
+{
+    const uint32_t per = GRAD ? n_parts : 1, part = blockIdx.x % per;
+    policy_row<DTYPE, kPartThreads, 4, 4, GRAD, false, kGradOfPart>(A, blockIdx.x / per, part, n_parts);
+    if (part == 0) count_and_finish<kPartThreads>(A, gridDim.x / per);
+}
+
+constexpr int kFinishThreads = 1024;
+__global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const PolicyPart* __restrict__ parts, uint32_t n,
+                                                                       ff_policy_stats* __restrict__ stats)
+{
+    finish<kFinishThreads>(parts, n, stats);
+}
+
 struct Choice {
-    Kernel kernel;
+    void (*kernel)(const PolicyArgs);
     int threads;
 };
-// By the slots of a row: whole rows in registers up to 16384.
+// By the slots of a row: as many threads as hold it with four slots each, which leave room for 2048 on a compute unit; with sixteen from
+// where two rows no longer fit.  (Us, 4096 rows of 2000 slots by 256 / 512 / 1024 threads 63 / 56 / 60, of 4000 128 / 113 / 99; of 8000
+// by 512 threads with 16, by 1024 with 8, with 4 of 8 slots held 195 / 222 / 217; 1024 fp32 rows of 32,500 by 1024 threads with
+// 16 / 8 / 4 held 247 / 281 / 278.)  Few rows take 1024 threads where many would take 512.  Without a gradient nothing is held, and four
+// slots are on their way; the threads that share a row are the same, and so are the order of the sums and the loss.
 template <uint32_t DTYPE>
-Choice choose(uint64_t slots)
+Choice choose(uint64_t slots, uint64_t rows, bool grad)
 {
-    if (slots <= 1024) return {policy_kernel<DTYPE, 256, 4>, 256};
-    if (slots <= 4096) return {policy_kernel<DTYPE, 512, 8>, 512};
-    if (slots <= 8192) return {policy_kernel<DTYPE, 1024, 8>, 1024};
-    return {policy_kernel<DTYPE, 1024, 16>, 1024};
+    const bool many = rows > kComputeUnits;
+    if (slots <= 256) return {grad ? policy_kernel<DTYPE, 64, 4, 8, true, false> : policy_kernel<DTYPE, 64, 4, 8, false, false>, 64};
+    if (slots <= 1024) return {grad ? policy_kernel<DTYPE, 256, 4, 8, true, false> : policy_kernel<DTYPE, 256, 4, 8, false, false>, 256};
+    if (slots <= 2048 && many) return {grad ? policy_kernel<DTYPE, 512, 4, 8, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
+    if (slots <= 4096) return {grad ? policy_kernel<DTYPE, 1024, 4, 8, true, false> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
+    if (slots <= 8192 && many) return {grad ? policy_kernel<DTYPE, 512, 16, 4, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
+    return {grad ? policy_kernel<DTYPE, 1024, 16, 4, true, true> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
 }
+
+template <uint32_t DTYPE>
+hipError_t launch(const PolicyArgs& A, hipStream_t stream)
+{
+    const uint32_t rows = static_cast<uint32_t>(A.b.n_tokens);
+    const uint64_t slots = A.b.vocab / SlotOf<DTYPE>::Type::kItems;
+    const uint64_t n_parts = (slots + kPartSlots - 1) / kPartSlots;
+    const bool grad = A.dlogits != nullptr;
+    if (slots > kSplitFrom && n_parts <= kMostParts && rows <= kSplitRows) {
+        const uint32_t parts = static_cast<uint32_t>(n_parts);
+        hipLaunchKernelGGL(policy_sum_kernel<DTYPE>, dim3(rows * parts), dim3(kPartThreads), 0, stream, A, parts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (grad)
+            hipLaunchKernelGGL((policy_grad_kernel<DTYPE, true>), dim3(rows * parts), dim3(kPartThreads), 0, stream, A, parts);
+        else
+            hipLaunchKernelGGL((policy_grad_kernel<DTYPE, false>), dim3(rows), dim3(kPartThreads), 0, stream, A, parts);
+        return hipGetLastError();
+    }
+    const Choice c = choose<DTYPE>(slots, rows, grad);
+    hipLaunchKernelGGL(c.kernel, dim3(rows), dim3(c.threads), 0, stream, A);
+    return hipGetLastError();
+}
+
+// The workspace: how many tokens are done, on a line of its own; what they add to the sums; the parts of split rows.
+constexpr uint64_t kDoneBytes = 64;
+uint64_t parts_bytes(uint64_t n_tokens) { return (n_tokens * sizeof(PolicyPart) + 15) / 16 * 16; }
 
 }  // namespace
 
-uint64_t policy_workspace(uint64_t n_tokens, uint64_t)
+uint64_t policy_workspace(uint64_t n_tokens, uint64_t vocab)
 {
-    return n_tokens * sizeof(PolicyPart);
+    uint64_t row_parts = 0;
+    if (n_tokens <= kSplitRows) {
+        const uint64_t most = vocab / (4 * kPartSlots) + 1;  // of 32-bit logits
+        row_parts = n_tokens * (most < kMostParts ? most : kMostParts);
+    }
+    return kDoneBytes + parts_bytes(n_tokens) + row_parts * sizeof(RowPart);
 }
 
 hipError_t launch_policy(const ff_policy_batch& b, float* logp, float* token_loss, void* dlogits, uint64_t grad_stride,
                          ff_policy_stats* stats, void* workspace, hipStream_t stream)
 {
-    PolicyPart* const parts = static_cast<PolicyPart*>(workspace);
+    uint8_t* const w = static_cast<uint8_t*>(workspace);
+    const bool counted = b.n_tokens && b.n_tokens <= kCountedTokens;
+    const PolicyArgs A = {b,
+                          logp,
+                          token_loss,
+                          static_cast<uint8_t*>(dlogits),
+                          grad_stride,
+                          reinterpret_cast<PolicyPart*>(w + kDoneBytes),
+                          reinterpret_cast<RowPart*>(w + kDoneBytes + parts_bytes(b.n_tokens)),
+                          counted ? reinterpret_cast<uint32_t*>(w) : nullptr,
+                          stats};
     if (b.n_tokens) {
-        const Choice c = b.dtype == FF_F32 ? choose<FF_F32>(b.vocab / 4) : b.dtype == FF_BF16 ? choose<FF_BF16>(b.vocab / 8) : choose<FF_F16>(b.vocab / 8);
-        hipLaunchKernelGGL(c.kernel, dim3(static_cast<uint32_t>(b.n_tokens)), dim3(c.threads), 0, stream, b, logp, token_loss,
-                           static_cast<uint8_t*>(dlogits), grad_stride, parts);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        const hipError_t e = b.dtype == FF_F32    ? launch<FF_F32>(A, stream)
+                             : b.dtype == FF_BF16 ? launch<FF_BF16>(A, stream)
+                                                  : launch<FF_F16>(A, stream);
+        if (e != hipSuccess || counted) return e;
     }
-    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, parts, b.n_tokens, stats);
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, A.parts, static_cast<uint32_t>(b.n_tokens), stats);
     return hipGetLastError();
 }
 

@@ -414,6 +414,45 @@ def test_policy_gradient_in_place_of_the_logits(n, v, pad, dtype):
     assert (got["beside"] == 9).all()
 
 
+# one workgroup to a row, or several; tokens counted one by one, or joined by a kernel of their own; rows that registers hold whole, or
+# in part, or that have more parts than are joined
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("n,slots", [(64, 4097), (65, 4097), (64, 256), (65, 257), (300, 1025), (257, 4097), (2, 8193), (70, 16385),
+                                     (1, 65535), (1, 65537)])
+@pytest.mark.parametrize("in_place", [False, True], ids=["apart", "inplace"])
+def test_policy_on_both_sides_of_every_rule(n, slots, dtype, in_place):
+    items = 4 if dtype == F32 else 8
+    v = slots * items + 3
+    rows, y, old, ref, adv, w = _policy_inputs(n, v, dtype, slots, 1)
+    y[0] = v - 1
+    y[-1] = (slots - 1) * items
+    w[n // 2] = 0 if n > 2 else w[n // 2]
+    got = _run_policy(rows, v, y, old, adv, w, ref, 0.1, in_place=in_place)
+    _check_policy(got, rows, v, y, old, adv, w, ref, 0.1)
+    assert (got["beside"] == 9).all() or not in_place
+
+
+def test_policy_workspace_serves_call_after_call():
+    """Counted tokens leave the count as they found it: calls of several sizes on one workspace, back to back."""
+    v = 2000
+    ws = ff.alloc_policy_workspace(64, 40000, DEV)
+    calls = []
+    for k, (n, vocab) in enumerate(((64, v), (1, 40000), (7, v), (64, 36000), (3, 40000), (64, v))):
+        rows, y, old, ref, adv, w = _policy_inputs(n, vocab, BF16, 100 + k)
+        t = [x.to(DEV) for x in (rows, y, old, adv, w, ref)]
+        stats, logp, token = ff.PolicyStats(DEV), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        calls.append((ff.policy_batch(*t, beta=0.1), logp, token, stats, t, trainref.policy(rows, y, old, adv, w, ref, 0.2, 0.2, 0.1)))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for batch, logp, token, stats, _, _ in calls:
+            ff.ff_policy_loss(batch, logp, token, stats, ws)
+    torch.cuda.synchronize()
+    for _, _, _, stats, _, want in calls:
+        assert int(stats.n_tokens) == want["n_tokens"] and float(stats.loss) == pytest.approx(want["loss"], rel=1e-4)
+        assert float(stats.kl) == pytest.approx(want["kl"], rel=1e-4)
+    assert int(ws[:64].max()) == 0
+
+
 def test_policy_rows_that_leave_nothing_targets_outside_and_masked_rows():
     n, v = 24, 3001
     rows, y, old, ref, adv, w = _policy_inputs(n, v, BF16, 77)
