@@ -780,6 +780,9 @@ __device__ __forceinline__ void step_body(const WorkWave* __restrict__ waves, co
         return;
     }
     fetch_tables(tabs, lds, wave, lane);
+    // (by scalar loads, under way with the entry's)
+    const bool keep = CLIP && table_entry(&C.stats->skip, 0) != 0;
+    if (CLIP) C.inv_scale = table_entry(&C.stats->scale, 0);
     const WorkWave e = waves[group * kWavesPerBlock + wave];
     const uint32_t run_entry = group * kWavesPerBlock + ((e.info >> 4) & 7u);
     if (e.tile == kNoTile) {
@@ -789,9 +792,6 @@ __device__ __forceinline__ void step_body(const WorkWave* __restrict__ waves, co
     // the tile descriptor is uniform and read-only: the loads below go through scalar registers
     // (a private copy indexed by the stream number would live in scratch memory instead)
     const WorkTile& t = tiles[e.tile];
-    // (by scalar loads, as the descriptor below)
-    const bool keep = CLIP && table_entry(&C.stats->skip, 0) != 0;
-    if (CLIP) C.inv_scale = table_entry(&C.stats->scale, 0);
     const int sub = e.info & 15u;
     const uint32_t* const lane_tab = tabs + kFusedWeightWords;
     if (t.kind == kWorkRaw) {
@@ -869,6 +869,9 @@ __device__ __forceinline__ void warm_step_body(const uint32_t block, const WorkW
         return;
     }
     fetch_tables(tabs, lds, wave, lane);
+    // (by scalar loads, under way with the entry's)
+    const bool keep = CLIP && table_entry(&C.stats->skip, 0) != 0;
+    if (CLIP) C.inv_scale = table_entry(&C.stats->scale, 0);
     WorkWave e = waves[group * kWavesPerBlock + wave];
     const uint32_t run_entry = group * kWavesPerBlock + ((e.info >> 4) & 7u);
     if (e.tile == kNoTile) {
@@ -885,9 +888,6 @@ __device__ __forceinline__ void warm_step_body(const uint32_t block, const WorkW
         asm("" : "+s"(e.info) : "s"(all), "s"(grad_at));
         __builtin_amdgcn_sched_barrier(0);
     }
-    // (by scalar loads, as the descriptor below)
-    const bool keep = CLIP && table_entry(&C.stats->skip, 0) != 0;
-    if (CLIP) C.inv_scale = table_entry(&C.stats->scale, 0);
     const int sub = e.info & 15u;
     const uint32_t* const lane_tab = tabs + kFusedWeightWords;
     if (t.kind == kWorkRaw) {

@@ -1,17 +1,20 @@
 // Gradient norm and clipping for gfx950.
 //
-// The norm is one pass over all gradients, which bounds it.  A wavefront takes items of 8 KiB of one tensor
-// (grads.hpp), lane l of a row of 1 KiB taking 16 bytes, and asks for the next item's rows before it sums up
-// those that have come.  Every element is squared and summed in 64 bits: squares of 16- and 32-bit
-// floats are exact there and cannot overflow, and so no finite gradient needs a second look.  An item's sum
-// that is not finite tells that the item holds an infinity or NaN; only then are those counted.  Sums go from lanes to
-// the wavefront to the workgroup to memory in an order that depends on the list alone, and a last workgroup
-// joins them: no atomics, the same bits every time.
+// The norm is one pass over all gradients, which bounds it: 6.8 TB/s on 1.7 and 3.2 GB (249 and 472 us; the pass of a restore that only
+// reads reaches 7.0 on 12 GB).  A wavefront takes items of 8 KiB of one tensor (grads.hpp), lane l of a row of 1 KiB taking 16 bytes.
+// Every element is squared and summed in 64 bits: squares of 16- and 32-bit floats are exact there and cannot overflow, so
+// no finite gradient needs a second look.  An item's sum that is not finite tells that the item holds an infinity or NaN; only then are
+// those counted.  Sums go from lanes to the wavefront to the workgroup to memory in an order that depends on the list alone,
+// and the last workgroup to be done joins them: the same bits every time.  Short lists are bound by the launch and that chain (64
+// tensors, 4 MB: 5.3 us; 8.4 where a second kernel joined the parts).
+//
+// Clipping reads and writes every gradient once.
 #include "grads.hpp"
 
 #include <hip/hip_fp16.h>
 
 #include "fold.h"
+#include "xcd_order.h"
 
 namespace ffsnap {
 
@@ -57,6 +60,7 @@ __device__ __forceinline__ void add_squares(double (&sum)[4], const u32x4 w)
     });
 }
 
+// Of the whole wavefront.  (By scalar additions: this is hardly ever looked at, and should not cost the sums their registers.)
 template <uint32_t FORMAT>
 __device__ __forceinline__ uint32_t count_nonfinite(const u32x4 w)
 {
@@ -64,7 +68,8 @@ __device__ __forceinline__ uint32_t count_nonfinite(const u32x4 w)
     static_for<4>([&](auto k) {
         float a, b;
         elements<FORMAT>(w[int(k)], a, b);
-        n += (__builtin_isfinite(a) ? 0u : 1u) + (__builtin_isfinite(b) ? 0u : 1u);
+        n += __popcll(__ballot(!__builtin_isfinite(a)));
+        if constexpr (FORMAT != kGradF32) n += __popcll(__ballot(!__builtin_isfinite(b)));
     });
     return n;
 }
@@ -111,7 +116,10 @@ template <uint32_t FORMAT>
 __device__ __forceinline__ void sum_item(const Rows& q, double& total, uint64_t& bad)
 {
     double s[4] = {0, 0, 0, 0};
-    static_for<kRows>([&](auto r) { add_squares<FORMAT>(s, q.slot[int(r)]); });
+    static_for<kRows>([&](auto r) {
+        add_squares<FORMAT>(s, q.slot[int(r)]);
+        __builtin_amdgcn_sched_barrier(0);  // (a row at a time, not 64 elements in 64 bits before the first is added)
+    });
     add_squares<FORMAT>(s, u32x4{q.rest, 0, 0, 0});
     const double sum = (s[0] + s[1]) + (s[2] + s[3]);
     if (__any(!__builtin_isfinite(sum))) {
@@ -135,7 +143,7 @@ __device__ __forceinline__ void write_stats(ff_grad_stats* out, double sumsq, ui
     out->skip = bad ? 1u : 0u;
 }
 
-// Sums over a workgroup of THREADS, in thread 0.
+// Sums over a workgroup of THREADS, in thread 0.  bad: of a whole wavefront.
 template <int THREADS>
 __device__ __forceinline__ void group_sum(double& sum, uint64_t& bad)
 {
@@ -144,10 +152,6 @@ __device__ __forceinline__ void group_sum(double& sum, uint64_t& bad)
     __shared__ uint64_t bads[kWaves];
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x / kWaveSize;
     sum = wave_sum(sum);
-    if (__any(bad != 0)) {
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) bad += __shfl_xor(static_cast<unsigned long long>(bad), d);
-    }
     if (lane == 0) {
         sums[wave] = sum;
         bads[wave] = bad;
@@ -159,6 +163,69 @@ __device__ __forceinline__ void group_sum(double& sum, uint64_t& bad)
             bad += bads[w];
         }
     }
+}
+
+// How the parts of all workgroups are joined in the same launch: the last workgroup of every sixty-fourth of them counts there, and the
+// last of those joins the parts, in their order whoever it is.  (On one counter workgroups that end together would queue up, 50 ns each.)
+// Counters, on lines of their own, are zero before and after.
+struct Joining {
+    uint64_t* counts;  // kLeaves, and the root
+    GradPart* parts;
+    uint32_t first, n;  // of this launch's workgroups among all, and all
+    double inv_scale, max_norm;
+    ff_grad_stats* stats;
+};
+constexpr uint32_t kLeaves = 32, kLineWords = 8;
+constexpr uint64_t kCountBytes = (kLeaves + 1) * kLineWords * 8;
+
+__device__ __forceinline__ bool is_last(uint64_t* count, uint64_t n)
+{
+    if (__hip_atomic_fetch_add(count, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 != n) return false;
+    __hip_atomic_store(count, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
+// By the whole workgroup, whose sums thread 0 has.
+__device__ __forceinline__ void join_parts(const Joining& J, double sum, uint64_t bad)
+{
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        const uint32_t at = J.first + blockIdx.x;
+        // past the caches of this workgroup's XCD, and of the one that joins
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(&J.parts[at].sumsq), __builtin_bit_cast(uint64_t, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&J.parts[at].n_nonfinite, bad, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("" ::: "memory");
+        wait_loads<0>();  // (and stores: they have arrived)
+        const uint32_t leaf = at % kLeaves, leaves = J.n < kLeaves ? J.n : kLeaves;
+        last = is_last(J.counts + leaf * kLineWords, (J.n - leaf + kLeaves - 1) / kLeaves) &&
+               is_last(J.counts + kLeaves * kLineWords, leaves);
+    }
+    __syncthreads();
+    if (!last) return;
+    asm volatile("" ::: "memory");
+    sum = 0;
+    bad = 0;
+    constexpr int kAtOnce = 8;  // on their way
+    for (uint32_t i0 = threadIdx.x; i0 < J.n; i0 += kAtOnce * kThreads) {
+        uint64_t part[kAtOnce][2];
+        static_for<kAtOnce>([&](auto k) {
+            const uint32_t i = i0 + k * kThreads;
+            const auto* const p = reinterpret_cast<const uint64_t*>(J.parts + (i < J.n ? i : i0));
+            static_for<2>([&](auto w) { part[int(k)][int(w)] = __hip_atomic_load(p + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
+        });
+        static_for<kAtOnce>([&](auto k) {
+            if (i0 + k * kThreads < J.n) {
+                sum += __builtin_bit_cast(double, part[int(k)][0]);
+                bad += part[int(k)][1];
+            }
+        });
+    }
+    if (__any(bad != 0)) {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) bad += __shfl_xor(static_cast<unsigned long long>(bad), d);
+    }
+    group_sum<kThreads>(sum, bad);
+    if (threadIdx.x == 0) write_stats(J.stats, sum, bad, J.inv_scale, J.max_norm);
 }
 
 // Addresses of the tensors: the list's, in memory, or the call's, in the arguments.
@@ -174,54 +241,25 @@ struct CallAddresses {
 
 template <class Addresses>
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const GradItem* __restrict__ items, uint32_t n_items,
-                                                             GradPart* __restrict__ parts, Addresses addresses)
+                                                             const Joining J, Addresses addresses)
 {
     const int lane = threadIdx.x & (kWaveSize - 1);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     const uint32_t stride = gridDim.x * kGradWaves;
     double sum = 0;
     uint64_t bad = 0;
-    uint32_t i = blockIdx.x * kGradWaves + wave;
-    if (i < n_items) {
-        GradItem it = item_at(items, i);
+    for (uint32_t i = blockIdx.x * kGradWaves + wave; i < n_items; i += stride) {
+        const GradItem it = item_at(items, i);
         Rows q;
         load_rows<true>(q, it, reinterpret_cast<const uint8_t*>(addresses.of(it.tensor)) + it.begin, lane);
-        for (;;) {
-            i += stride;
-            const bool more = i < n_items;
-            GradItem next = it;
-            Rows ahead;
-            if (more) {
-                next = item_at(items, i);
-                load_rows<true>(ahead, next, reinterpret_cast<const uint8_t*>(addresses.of(next.tensor)) + next.begin, lane);
-            }
-            switch (item_format(it)) {
-            case kGradF32: sum_item<kGradF32>(q, sum, bad); break;
-            case kGradBf16: sum_item<kGradBf16>(q, sum, bad); break;
-            default: sum_item<kGradF16>(q, sum, bad);
-            }
-            if (!more) break;
-            it = next;
-            q = ahead;
+        switch (item_format(it)) {
+        case kGradF32: sum_item<kGradF32>(q, sum, bad); break;
+        case kGradBf16: sum_item<kGradBf16>(q, sum, bad); break;
+        default: sum_item<kGradF16>(q, sum, bad);
         }
     }
     group_sum<kThreads>(sum, bad);
-    if (threadIdx.x == 0) parts[blockIdx.x] = GradPart{sum, bad};
-}
-
-constexpr int kFinishThreads = 256;
-__global__ __launch_bounds__(kFinishThreads) void grad_finish_kernel(const GradPart* __restrict__ parts, uint32_t n,
-                                                                     double inv_scale, double max_norm,
-                                                                     ff_grad_stats* __restrict__ stats)
-{
-    double sum = 0;
-    uint64_t bad = 0;
-    for (uint32_t i = threadIdx.x; i < n; i += kFinishThreads) {
-        sum += parts[i].sumsq;
-        bad += parts[i].n_nonfinite;
-    }
-    group_sum<kFinishThreads>(sum, bad);
-    if (threadIdx.x == 0) write_stats(stats, sum, bad, inv_scale, max_norm);
+    join_parts(J, sum, bad);
 }
 
 __global__ void grad_join_kernel(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,
@@ -270,6 +308,10 @@ __device__ __forceinline__ void clip_item(const Rows& q, const uint32_t bytes, u
     }
 }
 
+// Workgroups to a run of an XCD (xcd_order.h), us, 1.7 GB of bf16 in place, in launch order / 2 / 4 / 8 / 16 / 32 / 64 / 2048 615 / 600 / 559 /
+// 561 / 560 / 588 / 575 / 586 (a copy of as many bytes: 529); plain loads or stores instead of non-temporal ones, in launch order, 670 and
+// 636; two or four items to a wavefront, one after the other, 591 and 589.
+constexpr uint32_t kClipXcdGroup = 8;
 template <class Addresses>
 __global__ __launch_bounds__(kThreads) void grad_clip_kernel(const GradItem* __restrict__ items, uint32_t n_items,
                                                              const ff_grad_stats* __restrict__ stats, Addresses addresses)
@@ -278,7 +320,7 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(const GradItem* __r
     if (stats->skip || scale == 1.f) return;
     const int lane = threadIdx.x & (kWaveSize - 1);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
-    const uint32_t i = blockIdx.x * kGradWaves + wave;
+    const uint32_t i = xcd_order(blockIdx.x, gridDim.x, kClipXcdGroup) * kGradWaves + wave;
     if (i >= n_items) return;
     const GradItem it = item_at(items, i);
     uint8_t* const at = reinterpret_cast<uint8_t*>(addresses.of(it.tensor)) + it.begin;
@@ -324,26 +366,28 @@ bool build_grad_items(const ff_segment* segs, uint64_t n, std::vector<GradItem>&
 hipError_t launch_grad_norm(const GradWork& work, const void* const* grads, double inv_scale, double max_norm,
                             void* workspace, ff_grad_stats* stats, hipStream_t stream)
 {
-    GradPart* const parts = static_cast<GradPart*>(workspace);
-    uint32_t n_parts = 0;
+    uint8_t* const w = static_cast<uint8_t*>(workspace);
+    Joining J = {reinterpret_cast<uint64_t*>(w), reinterpret_cast<GradPart*>(w + kCountBytes), 0, work.n_parts(!grads), inv_scale, max_norm, stats};
     if (!grads) {
-        n_parts = grad_groups(work.launch.back());
-        hipLaunchKernelGGL(grad_norm_kernel<ListAddresses>, dim3(n_parts), dim3(kThreads), 0, stream, work.items,
-                           work.launch.back(), parts, ListAddresses{work.address});
+        hipLaunchKernelGGL(grad_norm_kernel<ListAddresses>, dim3(J.n), dim3(kThreads), 0, stream, work.items, work.launch.back(), J,
+                           ListAddresses{work.address});
+        return hipGetLastError();
+    }
+    for (size_t k = 0; k + 1 < work.launch.size(); k++) {
+        const uint32_t first = work.launch[k], n = work.launch[k + 1] - first, groups = grad_groups(n);
+        hipLaunchKernelGGL(grad_norm_kernel<CallAddresses>, dim3(groups), dim3(kThreads), 0, stream, work.items + first, n, J,
+                           call_addresses(work, grads, k));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-    } else {
-        for (size_t k = 0; k + 1 < work.launch.size(); k++) {
-            const uint32_t first = work.launch[k], n = work.launch[k + 1] - first, groups = grad_groups(n);
-            hipLaunchKernelGGL(grad_norm_kernel<CallAddresses>, dim3(groups), dim3(kThreads), 0, stream, work.items + first, n,
-                               parts + n_parts, call_addresses(work, grads, k));
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            n_parts += groups;
-        }
+        J.first += groups;
     }
-    hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, parts, n_parts, inv_scale, max_norm, stats);
-    return hipGetLastError();
+    return hipSuccess;
+}
+
+uint64_t grad_workspace(const GradWork& work)
+{
+    const uint64_t own = work.n_parts(true), given = work.n_parts(false);
+    return kCountBytes + (own > given ? own : given) * sizeof(GradPart);
 }
 
 hipError_t launch_grad_join(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,

@@ -25,7 +25,7 @@ bool build_grad_items(const ff_segment* segs, uint64_t n, std::vector<GradItem>&
 
 constexpr uint32_t kGradWaves = 4;  // of a workgroup
 // Workgroups over n items: no more than the chip holds at once, each goes on to further items.
-constexpr uint32_t kGradGroups = 2048;
+constexpr uint32_t kGradGroups = 512;
 inline uint32_t grad_groups(uint32_t n_items)
 {
     const uint32_t g = (n_items + kGradWaves - 1) / kGradWaves;
@@ -51,6 +51,9 @@ struct GradWork {
         return sum;
     }
 };
+
+// What launch_grad_norm is given, zero before the first call.
+uint64_t grad_workspace(const GradWork& work);
 
 // grads: HOST array of addresses, or null for the list's own.
 hipError_t launch_grad_norm(const GradWork& work, const void* const* grads, double inv_scale, double max_norm,

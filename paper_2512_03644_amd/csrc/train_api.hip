@@ -125,12 +125,7 @@ void ff_grad_list_destroy(ff_grad_list* list)
 
 uint64_t ff_grad_list_numel(const ff_grad_list* list) { return list ? list->numel : 0; }
 
-uint64_t ff_grad_list_workspace_bytes(const ff_grad_list* list)
-{
-    if (!list) return 0;
-    const uint32_t own = list->work.n_parts(true), given = list->work.n_parts(false);
-    return (own > given ? own : given) * sizeof(GradPart);
-}
+uint64_t ff_grad_list_workspace_bytes(const ff_grad_list* list) { return list ? grad_workspace(list->work) : 0; }
 
 int ff_grad_norm(const ff_grad_list* list, const void* const* grads, double inv_loss_scale, double max_norm,
                  void* workspace, ff_grad_stats* stats, void* hip_stream)
