@@ -333,7 +333,7 @@ typedef struct {
  * sums are held in 64 bits: no finite element overflows or underflows; the order of the sums depends on the
  * list alone, so the same values give the same bits.  grads: HOST array of n DEVICE pointers in the list's order, each
  * aligned to its element (entries of empty tensors are ignored), or NULL for the list's own addresses.
- * inv_loss_scale: finite and > 0 (1 without a loss scale); max_norm: > 0, INFINITY for no clipping.
+ * inv_loss_scale: finite and > 0 in fp32 as well (1 without a loss scale); max_norm: > 0, INFINITY for no clipping.
  * stats: DEVICE, 8-byte aligned.  workspace: DEVICE, 16-byte aligned, ff_grad_list_workspace_bytes() bytes,
  * ZERO before its first use; every call leaves it as the next one needs it.
  */

@@ -400,6 +400,7 @@ class GradList:
     def __init__(self, handle, keepalive):
         self.handle = handle
         self._keepalive = keepalive
+        self.num_tensors = len(keepalive)
 
     def destroy(self):
         if self.handle:
@@ -427,10 +428,12 @@ def alloc_grad_workspace(grad_list, device):
     return torch.zeros(max(16, grad_list.workspace_bytes), dtype=torch.uint8, device=device)
 
 
-def _list_pointers(grads):
+def _list_pointers(grad_list, grads):
     """(array to keep alive across the call, its address): none for the list's own addresses."""
     if grads is None:
         return None, None
+    if len(grads) != grad_list.num_tensors:
+        raise ValueError("the list is of %d tensors" % grad_list.num_tensors)
     ptrs = _grad_pointers(grads)
     return ptrs, ptrs.buffer_info()[0]
 
@@ -438,7 +441,7 @@ def _list_pointers(grads):
 def ff_grad_norm(grad_list, stats, workspace, max_norm=float("inf"), inv_loss_scale=1.0, grads=None,
                  stream=None):
     """grads: other tensors than the list's own, of the same sizes and formats."""
-    keep, ptrs = _list_pointers(grads)
+    keep, ptrs = _list_pointers(grad_list, grads)
     _check(lib().ff_grad_norm(grad_list.handle, ptrs, inv_loss_scale, max_norm, workspace.data_ptr(),
                               stats.data_ptr(), _stream_ptr(stream)))
 
@@ -450,13 +453,15 @@ def ff_grad_norm_join(parts, stats, max_norm=float("inf"), inv_loss_scale=1.0, s
 
 
 def ff_grad_clip(grad_list, stats, grads=None, stream=None):
-    keep, ptrs = _list_pointers(grads)
+    keep, ptrs = _list_pointers(grad_list, grads)
     _check(lib().ff_grad_clip(grad_list.handle, ptrs, stats.data_ptr(), _stream_ptr(stream)))
 
 
 def ff_adam_step_clipped(plan, grads, hparams, stats, chunks, crcs, prev_chunks=None, stream=None):
     """The step on gradients clipped (and unscaled) by stats.scale; in place, or from the previous
     snapshot.  grads in the plan's 16-bit format."""
+    if len(grads) != plan.num_params:
+        raise ValueError("the plan has %d parameter groups" % plan.num_params)
     ptrs = _grad_pointers(grads)
     hp = ff_adam_hparams(hparams["lr"], hparams["beta1"], hparams["beta2"], hparams["eps"],
                          hparams["weight_decay"], hparams["step"])

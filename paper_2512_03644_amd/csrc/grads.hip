@@ -262,16 +262,22 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const GradItem* __r
     join_parts(J, sum, bad);
 }
 
-__global__ void grad_join_kernel(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,
-                                 ff_grad_stats* stats)
+// One wavefront: it loads the parts side by side, and adds them one after the other.
+__global__ __launch_bounds__(kWaveSize) void grad_join_kernel(const ff_grad_stats* parts, uint64_t n, double inv_scale,
+                                                              double max_norm, ff_grad_stats* stats)
 {
     double sum = 0;
     uint64_t bad = 0;
-    for (uint64_t i = 0; i < n; i++) {  // in rank order
-        sum += parts[i].sumsq;
-        bad += parts[i].n_nonfinite;
+    for (uint64_t i0 = 0; i0 < n; i0 += kWaveSize) {
+        const uint64_t i = i0 + threadIdx.x;
+        const double s = i < n ? parts[i].sumsq : 0.0;
+        const unsigned long long b = i < n ? parts[i].n_nonfinite : 0;
+        for (int k = 0; k < kWaveSize; k++) {
+            sum += __shfl(s, k);
+            bad += __shfl(b, k);
+        }
     }
-    write_stats(stats, sum, bad, inv_scale, max_norm);
+    if (threadIdx.x == 0) write_stats(stats, sum, bad, inv_scale, max_norm);
 }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -393,7 +399,7 @@ uint64_t grad_workspace(const GradWork& work)
 hipError_t launch_grad_join(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,
                             ff_grad_stats* stats, hipStream_t stream)
 {
-    hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(1), 0, stream, parts, n, inv_scale, max_norm, stats);
+    hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(kWaveSize), 0, stream, parts, n, inv_scale, max_norm, stats);
     return hipGetLastError();
 }
 

@@ -414,8 +414,8 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
     // Does the wavefront have slots in round i, and where is a lane's?  Lanes behind the last slot take that one again.
     auto has = [&](auto i) { return i * THREADS + wave_first < slots; };
     auto at = [&](auto i) {
-        const uint32_t end = 16 * (slots - 1 - i * THREADS), mine = 16 * threadIdx.x;
-        return mine < end ? mine : end;
+        const uint32_t last = slots - 1 - i * THREADS;
+        return threadIdx.x < last ? threadIdx.x : last;
     };
     const uint32_t y = static_cast<uint32_t>(target) - first_slot * N;  // among the workgroup's elements, if it is
     float z_y = 0.f, end = -INFINITY;
@@ -426,7 +426,7 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
     u32x4 held[K];
     if (MODE != kGradOfPart || GRAD)
         static_for<K>([&](auto i) {
-            if (has(i)) held[int(i)] = load16<true>(uniform(in + 16ull * THREADS * i), at(i));
+            if (has(i)) held[int(i)] = load16<true>(uniform(in + 16ull * THREADS * i), 16 * at(i));
         });
     constexpr int kAhead = 4;  // slots under way of those that are not held
     if constexpr (MODE != kGradOfPart) {
@@ -542,7 +542,7 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
         static_for<K>([&](auto i) {
             if (has(i)) {
                 const uint32_t mine = at(i);
-                store16(uniform(out + 16ull * THREADS * i), mine, gradient(held[int(i)], 16 * (y / N - i * THREADS) == mine));
+                store16(uniform(out + 16ull * THREADS * i), 16 * mine, gradient(held[int(i)], y / N - i * THREADS == mine));
             }
         });
         if constexpr (LONG)

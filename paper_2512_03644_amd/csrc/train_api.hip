@@ -48,7 +48,8 @@ int check_grads(const ff_grad_list* list, const void* const* grads)
 }
 
 bool positive(double v) { return v > 0.0; }  // not a NaN
-bool scale_ok(double v) { return positive(v) && std::isfinite(v); }
+// A loss scale, or its reciprocal, that is one in 32 bits as well.
+bool scale_ok(double v) { return positive(static_cast<float>(v)) && std::isfinite(static_cast<float>(v)); }
 
 int upload(ff_grad_list* list, const std::vector<GradItem>& items, const std::vector<uint64_t>& address)
 {

@@ -607,3 +607,88 @@ def _unclipped(batch, dz):
     ff.ff_policy_loss(batch, logp, token, ff.PolicyStats(DEV), ff.alloc_policy_workspace(n, v, DEV), out)
     torch.cuda.synchronize()
     return out
+
+
+def test_offsets_beyond_32_bits():
+    """A gradient of more than 4 GiB, and rows of logits that lie 4 GiB apart."""
+    n = (1 << 30) + 4099  # fp32
+    t = torch.zeros(n, device=DEV)
+    places = [0, 1, (1 << 29) + 5, (1 << 30) - 1, 1 << 30, (1 << 30) + 7, n - 1]
+    for k, i in enumerate(places):
+        t[i] = k + 1.0
+    lst, stats, _ = _norm([t, torch.ones(3, device=DEV)], 2.0)
+    want = math.sqrt(sum((k + 1) ** 2 for k in range(len(places))) + 3)
+    assert float(stats.norm) == pytest.approx(want, rel=1e-12)
+    ff.ff_grad_clip(lst, stats)
+    for k, i in enumerate(places):
+        assert float(t[i]) == float(np.float32(k + 1) * np.float32(float(stats.scale)))
+    assert int((t != 0).sum()) == len(places)
+    del t, lst
+    v, stride = 3001, 1 << 31  # bf16 rows
+    rows, y, old, ref, adv, w = _policy_inputs(3, v, BF16, 90)
+    far = torch.empty(2 * stride + v, dtype=BF16, device=DEV)
+    z = far.as_strided((3, v), (stride, 1))
+    z.copy_(rows.to(DEV))
+    dev = [x.to(DEV) for x in (y, old, adv, w, ref)]
+    logp, token, stats = torch.empty(3, device=DEV), torch.empty(3, device=DEV), ff.PolicyStats(DEV)
+    ff.ff_policy_loss(ff.policy_batch(z, *dev, 0.2, 0.3, 0.1), logp, token, stats, ff.alloc_policy_workspace(3, v, DEV), z)
+    near = _run_policy(rows, v, y, old, adv, w, ref, 0.1)
+    assert torch.equal(z.cpu(), near["dlogits"]) and torch.equal(logp.cpu(), near["logp"])
+
+
+def test_join_of_many_workers_is_in_rank_order():
+    n = 200
+    g = torch.Generator().manual_seed(2)
+    values = torch.randn(n, generator=g).double().exp()
+    parts, total = ff.GradStats(DEV, n), ff.GradStats(DEV)
+    parts.words[:, 0] = values.to(DEV)
+    ff.ff_grad_norm_join(parts, total)
+    want = 0.0
+    for x in values.tolist():
+        want += x
+    assert float(total.sumsq) == want and float(total.norm) == math.sqrt(want) and float(total.scale) == 1.0
+
+
+@pytest.mark.parametrize("skip", [False, True], ids=["update", "skip"])
+@pytest.mark.parametrize("chained", [False, True], ids=["inplace", "chained"])
+def test_clipped_step_copies_tensors_that_are_not_trained(chained, skip, oracle):
+    shard = _shard([5000, 257], BF16, 1.0)
+    g = torch.Generator().manual_seed(4)
+    raw = [torch.randn(n, generator=g).to(DEV) for n in (1, 3001, 20000)]
+    segs = [raw[0]] + shard.segments[:4] + [raw[1]] + shard.segments[4:] + [raw[2]]
+    four = [ff.FF_KIND_W16, ff.FF_KIND_MASTER, ff.FF_KIND_M, ff.FF_KIND_V]
+    kinds = [ff.FF_KIND_RAW] + four + [ff.FF_KIND_RAW] + four + [ff.FF_KIND_RAW]
+    plan = ff.ff_snapshot_plan(segs, 1 << 14, 0, kinds, [0] + [0] * 4 + [0] + [1] * 4 + [0])
+    chunks, crcs, _, _ = ff.alloc_outputs(plan, DEV)
+    prev = None
+    if chained:
+        prev, prev_crcs, _, _ = ff.alloc_outputs(plan, DEV)
+        ff.ff_pack(plan, prev, prev_crcs)
+    grads = [q.grad for q in shard.params]
+    if skip:
+        grads[0][77] = NAN
+    lst, stats, _ = _norm(grads, 1e-3)
+    old = [[t.clone() for t in (q.w16, q.master, q.m, q.v)] for q in shard.params]
+    ff.ff_adam_step_clipped(plan, grads, HP, stats, chunks, crcs, prev)
+    torch.cuda.synchronize()
+    new = [trainref.step(*o, gr, HP, float(stats.scale), skip) for o, gr in zip(old, grads)]
+    flat = [[n[0].view(torch.int16).numpy(), *n[1:]] for n in new]
+    r = [t.cpu().numpy() for t in raw]
+    buf, want = oracle.pack([r[0], *flat[0], r[1], *flat[1], r[2]], 1 << 14, threads=2)
+    assert np.array_equal(chunks.cpu().numpy(), buf)
+    assert np.array_equal(crcs.cpu().numpy().view(np.uint32), want)
+
+
+@pytest.mark.parametrize("half", [BF16, F16], ids=["bf16", "fp16"])
+def test_example_learns_and_its_snapshot_is_taken_over(half):
+    """The example's program: its loss falls, its gradients are clipped, and the newcomer has the trained weights."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "policy_training.py")
+    spec = importlib.util.spec_from_file_location("policy_training", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses, norms, trained, taken_over = example.train(20, half, report=lambda s: None)
+    assert losses[-1] < losses[0] - 0.02 and all(math.isfinite(x) for x in losses + norms)
+    assert norms[0] > example.MAX_NORM
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(trained, taken_over))

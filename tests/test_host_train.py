@@ -59,7 +59,7 @@ def test_norm_and_clip_refuse_bad_arguments():
     assert norm() == ff.FF_ERR_HOST_ONLY and norm(grads=None) == ff.FF_ERR_HOST_ONLY
     assert norm(most=INF) == ff.FF_ERR_HOST_ONLY
     assert norm(handle=None) == norm(ws=None) == norm(stats=None) == ff.FF_ERR_NULL
-    for inv in (0.0, -1.0, INF, NAN):
+    for inv in (0.0, -1.0, INF, NAN, 1e300, 1e-300):
         assert norm(inv=inv) == ff.FF_ERR_INVALID
     for most in (0.0, -1.0, NAN):
         assert norm(most=most) == ff.FF_ERR_INVALID
@@ -152,3 +152,17 @@ def test_binding_refuses_shapes_and_types():
             ff.ff_policy_loss(b, args["logp"], args["token_loss"], f, f, args["dlogits"])
     with pytest.raises(ValueError):
         ff.ff_grad_list([torch.zeros(4, 4).t()], HOST)
+
+
+def test_binding_counts_gradients():
+    lst = ff.ff_grad_list([torch.zeros(8), torch.zeros(3)], HOST)
+    stats = ff.GradStats("cpu")
+    with pytest.raises(ValueError):
+        ff.ff_grad_norm(lst, stats, stats, grads=[torch.zeros(8)])
+    with pytest.raises(ValueError):
+        ff.ff_grad_clip(lst, stats, grads=[torch.zeros(8)] * 3)
+    t = [torch.zeros(64, dtype=torch.bfloat16)] + [torch.zeros(64) for _ in range(3)]
+    plan = ff.ff_snapshot_plan(t, 1024, HOST, [1, 2, 3, 4], [0] * 4)
+    hp = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.0, step=1)
+    with pytest.raises(ValueError):
+        ff.ff_adam_step_clipped(plan, [], hp, stats, t[1], t[1])
