@@ -414,8 +414,7 @@ uint64_t ff_policy_workspace_bytes(uint64_t n_tokens, uint64_t vocab);
  * fp64; the gradient is rounded once.  Logits of -inf are probabilities of 0.  A row with a NaN or +inf gives NaN in its outputs and
  * its whole gradient row (which ff_grad_norm finds downstream).  A token that is left out (weight 0 or invalid) has logp and token
  * loss 0 and a gradient row of zeros.
- * logp, token_loss: DEVICE fp32[n_tokens]; logp may be old_logp's array only if that is not needed again, so it may
- * not alias any input.  dlogits: NULL (no gradient), or DEVICE, of `dtype`, rows grad_stride >= vocab elements apart; it may
+ * logp, token_loss: DEVICE fp32[n_tokens], apart from each other and from every input.  dlogits: NULL (no gradient), or DEVICE, of `dtype`, rows grad_stride >= vocab elements apart; it may
  * be the logits themselves with the same stride, and elements between rows are not touched.
  * stats: DEVICE.  workspace: DEVICE, 16-byte aligned, ff_policy_workspace_bytes(), ZERO before its
  * first use; every call leaves it as the next one needs it.
