@@ -1,6 +1,7 @@
 """CPU-only checks of the calls between loss and step: what they refuse, and the sizes they report.  Every refusal
 comes before any work on the device, so none of them needs one."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -166,3 +167,34 @@ def test_binding_counts_gradients():
     hp = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.0, step=1)
     with pytest.raises(ValueError):
         ff.ff_adam_step_clipped(plan, [], hp, stats, t[1], t[1])
+
+
+def test_binding_refuses_workspaces_that_are_too_small():
+    lst = ff.ff_grad_list([torch.zeros(8), torch.zeros(3)], HOST)
+    stats = ff.GradStats("cpu")
+    with pytest.raises(ValueError):
+        ff.ff_grad_norm(lst, stats, ff.alloc_grad_workspace(lst, "cpu")[:-1])
+    with pytest.raises(ff.FFError):  # (a list without a device)
+        ff.ff_grad_norm(lst, stats, ff.alloc_grad_workspace(lst, "cpu"), stream=types.SimpleNamespace(cuda_stream=0))
+    for n, v in ((1, 8), (64, 300000), (65, 1000), (5000, 10)):
+        rows = torch.zeros(n, v, dtype=torch.bfloat16)
+        f = torch.zeros(n)
+        b = ff.policy_batch(rows, torch.zeros(n, dtype=torch.int64), f, f, f)
+        with pytest.raises(ValueError):
+            ff.ff_policy_loss(b, f, f, ff.PolicyStats("cpu"), ff.alloc_policy_workspace(n, v, "cpu")[:-1])
+
+
+def test_segments_are_filled_as_they_were():
+    """Field by field, whatever the list: empty tensors have no address, kinds and groups as given."""
+    ts = [torch.zeros(n, dtype=t) for n, t in ((5, torch.bfloat16), (0, torch.float32), (7, torch.float16), (3, torch.float32))]
+    for kinds, ids in ((None, None), ([1, 0, 0, 2], [0, 0, 0xFFFFFFFF, 3])):
+        segs = ff.make_segments(ts, kinds, ids)
+        assert len(segs) == 4
+        for k, (s, t) in enumerate(zip(segs, ts)):
+            assert (s.ptr, s.nbytes) == (t.data_ptr() if t.numel() else None, t.numel() * t.element_size())
+            assert s.dtype == {torch.bfloat16: ff.FF_BF16, torch.float16: ff.FF_F16, torch.float32: ff.FF_F32}[t.dtype]
+            assert (s.kind, s.param_id, s.reserved) == (kinds[k] if kinds else 0, ids[k] if ids else 0, 0)
+    none = ff.make_segments([])
+    assert len(none) == 1 and (none[0].ptr, none[0].nbytes, none[0].dtype) == (None, 0, 0)
+    with pytest.raises(ValueError, match="segment 1 "):
+        ff.make_segments([ts[0], torch.zeros(4, 4).t()])
