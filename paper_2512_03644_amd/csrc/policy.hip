@@ -5,7 +5,7 @@
 // joins those, and what hangs on the token's log-probability alone -- ratio, clipping, KL term, the slope of the loss in it
 // -- is a handful of operations in 64 bits of one wavefront.  The gradient is the slope times ([j is the target] -
 // softmax), from the logits in registers: they are read once.  What tokens add to the sums goes to memory and is
-// joined in the tokens' order, by the last workgroup of a few or by a kernel of one workgroup.
+// joined, always in the same order, by the last workgroups to be done (count_and_finish).
 //
 // What bounds it: memory, or for few tokens the launch and the chain from a row's load to its store.  Long rows alone with a compute
 // unit (128,256 bf16 logits are half of its registers) leave the memory idle between their loads and stores: the same with no arithmetic
@@ -244,16 +244,29 @@ struct Token {
     double target;  // and at the target this
     bool clipped;
 };
-__device__ __forceinline__ Token token(const ff_policy_batch& b, const uint32_t t, const float z_y, const float base, const double total,
+struct Given {  // of a token, by scalar loads with the row's first
+    float weight, gain, old_logp, ref_logp;
+};
+__device__ __forceinline__ Given given(const ff_policy_batch& b, const uint32_t t)
+{
+    const float* const ref = b.ref_logp ? b.ref_logp : b.old_logp;  // (a load either way)
+    Given g = {table_entry(b.weights, t), table_entry(b.advantages, t), table_entry(b.old_logp, t), table_entry(ref, t)};
+    const double* series = kSeries;
+    asm volatile("" : "+s"(series));
+    const double first = table_entry(series, 0), last = table_entry(series, 14);  // exp64's lines, for later
+    asm volatile("" : "+s"(g.weight), "+s"(g.gain), "+s"(g.old_logp), "+s"(g.ref_logp) : "s"(first), "s"(last));
+    return g;
+}
+__device__ __forceinline__ Token token(const ff_policy_batch& b, const Given& given, const float z_y, const float base, const double total,
                                        const int lane)
 {
     Token k;
     k.logp = (static_cast<double>(z_y) - static_cast<double>(base)) - log64(total);
-    const double gain = table_entry(b.advantages, t);
+    const double gain = given.gain;
     const double lo = 1.0 - static_cast<double>(b.clip_low), hi = 1.0 + static_cast<double>(b.clip_high);
     const double beta = b.beta;
-    const double change = k.logp - static_cast<double>(table_entry(b.old_logp, t));
-    const double d = b.ref_logp ? static_cast<double>(table_entry(b.ref_logp, t)) - k.logp : 0.0;
+    const double change = k.logp - static_cast<double>(given.old_logp);
+    const double d = b.ref_logp ? static_cast<double>(given.ref_logp) - k.logp : 0.0;
     const double all = exp64(lane == 0 ? change : lane == 1 ? d : k.logp);
     const double r = __shfl(all, 0), kept = r * gain, cut = (r < lo ? lo : r > hi ? hi : r) * gain;
     k.clipped = cut < kept;
@@ -268,7 +281,7 @@ __device__ __forceinline__ Token token(const ff_policy_batch& b, const uint32_t 
         k.loss += beta * k.kl;
         slope -= beta * e;
     }
-    k.factor = static_cast<double>(table_entry(b.weights, t)) * slope * static_cast<double>(b.loss_scale);
+    k.factor = static_cast<double>(given.weight) * slope * static_cast<double>(b.loss_scale);
     k.target = k.factor * (1.0 - __shfl(all, 2));
     return k;
 }
@@ -286,7 +299,7 @@ struct PolicyArgs {
     uint64_t grad_stride;
     PolicyPart* parts;    // what every token adds to the sums
     RowPart* row_parts;   // of split rows
-    uint32_t* done;       // tokens that are done, zero before and after; null: a kernel of its own joins their sums
+    struct Counters* counters;
     ff_policy_stats* stats;
 };
 
@@ -311,58 +324,118 @@ __device__ __forceinline__ PolicyPart receive(const PolicyPart* from)
     return p;
 }
 
-// Sums over the tokens, by a workgroup.
-template <int THREADS>
-__device__ __forceinline__ void finish(const PolicyPart* parts, const uint32_t n, ff_policy_stats* stats)
-{
-    constexpr int kWaves = THREADS / kWaveSize;
-    double sums[2] = {0, 0};
-    uint32_t counts[3] = {0, 0, 0};
-#pragma unroll 4
-    for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
-        const PolicyPart p = receive(parts + i);
-        sums[0] += p.loss;
-        sums[1] += p.kl;
+// Sums over tokens.
+struct Sums {
+    double loss, kl;
+    uint32_t counts[3];
+    __device__ __forceinline__ void add(const PolicyPart& p)
+    {
+        loss += p.loss;
+        kl += p.kl;
         static_for<3>([&](auto k) { counts[int(k)] += p.what >> k & 1u; });
     }
-    __shared__ double all_sums[2][kWaves];
-    __shared__ uint32_t all_counts[3][kWaves];
+    __device__ __forceinline__ void add(const Sums& s)
+    {
+        loss += s.loss;
+        kl += s.kl;
+        static_for<3>([&](auto k) { counts[int(k)] += s.counts[int(k)]; });
+    }
+    // of a wavefront's lanes, in all of them
+    __device__ __forceinline__ void join()
+    {
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        static_for<2>([&](auto k) { sums[int(k)] += __shfl_xor(sums[int(k)], d); });
-        static_for<3>([&](auto k) { counts[int(k)] += __shfl_xor(counts[int(k)], d); });
+        for (int d = 32; d >= 1; d >>= 1) {
+            loss += __shfl_xor(loss, d);
+            kl += __shfl_xor(kl, d);
+            static_for<3>([&](auto k) { counts[int(k)] += __shfl_xor(counts[int(k)], d); });
+        }
     }
-    const int wave = threadIdx.x / kWaveSize;
-    if (threadIdx.x % kWaveSize == 0) {
-        static_for<2>([&](auto k) { all_sums[int(k)][wave] = sums[int(k)]; });
-        static_for<3>([&](auto k) { all_counts[int(k)][wave] = counts[int(k)]; });
+    __device__ __forceinline__ ff_policy_stats stats() const
+    {
+        return {static_cast<float>(loss), static_cast<float>(kl), counts[0], counts[1], counts[2]};
     }
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < kWaves; w++) {
-        static_for<2>([&](auto k) { sums[int(k)] += all_sums[int(k)][w]; });
-        static_for<3>([&](auto k) { counts[int(k)] += all_counts[int(k)][w]; });
-    }
-    *stats = ff_policy_stats{static_cast<float>(sums[0]), static_cast<float>(sums[1]), counts[0], counts[1], counts[2]};
+};
+
+// Tokens in groups: token t is in group t % kGroups, whose last token adds the group's up, and the last group of all
+// adds those; one counter for all of more than kCountedTokens would queue up, 50 ns each.  Whoever is last,
+// the sums are in the same order.  (A kernel of one workgroup behind the others instead: 4096 tokens on 1000 / 8000 / 32,000 15.6 / 33.9 / 89.6 us
+// where this takes 12.5 / 31.3 / 86.9, 777 on 50,021 without gradient 36.0 and 34.2.)
+constexpr uint32_t kCountedTokens = 64, kGroups = 64;
+struct Counters {
+    struct {
+        uint32_t done, unused[15];
+    } all, group[kGroups];  // zero before and after
+    struct {
+        uint64_t loss, kl, counts[3], unused[3];
+    } sums[kGroups];
+};
+
+__device__ __forceinline__ bool is_last(uint32_t* count, const uint32_t n)
+{
+    // What this thread has sent has arrived when its stores are done.  (A release fence would
+    // write the L2's other lines back as well, the gradient's among them: 64 tokens on 32,000 13.3 us with one.)
+    asm volatile("" ::: "memory");
+    wait_loads<0>();
+    if (__hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 != n) return false;
+    __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::: "memory");
+    return true;
 }
 
-// The workgroup's token is done: the last one of few joins the sums.  (In the tokens' order, whoever it is.)
-template <int THREADS>
-__device__ __forceinline__ void count_and_finish(const PolicyArgs& A, const uint32_t n)
+// Token t is done, and its part on its way.  By the wavefront that has sent it.
+__device__ __forceinline__ void count_and_finish(const PolicyArgs& A, const uint32_t t, const int lane)
 {
-    __shared__ int last;
-    if (threadIdx.x == 0) {
-        // This thread has sent the token's part, and it has arrived when its stores are done.  (A release fence would
-        // write the L2's other lines back as well, the gradient's among them: 64 tokens on 32,000 13.3 us with one.)
-        asm volatile("" ::: "memory");
-        wait_loads<0>();
-        last = __hip_atomic_fetch_add(A.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
+    const uint32_t n = static_cast<uint32_t>(A.b.n_tokens);
+    if (n == 1) return;  // (deliver)
+    const bool few = n <= kCountedTokens;
+    const uint32_t group = few ? 0 : t % kGroups, step = few ? 1 : kGroups;
+    int last = 0;
+    if (lane == 0) last = is_last(few ? &A.counters->all.done : &A.counters->group[group].done, (n - group + step - 1) / step);
+    if (!__shfl(last, 0)) return;
+    Sums s = {};
+    constexpr int kAtOnce = 4;  // on their way
+    for (uint64_t i0 = group + uint64_t(lane) * step; i0 < n; i0 += kAtOnce * kWaveSize * step) {
+        PolicyPart p[kAtOnce];
+        static_for<kAtOnce>([&](auto k) {
+            const uint64_t i = i0 + k * kWaveSize * step;
+            p[int(k)] = receive(A.parts + (i < n ? i : i0));
+        });
+        static_for<kAtOnce>([&](auto k) {
+            if (i0 + k * kWaveSize * step < n) s.add(p[int(k)]);
+        });
     }
-    __syncthreads();
-    if (!last) return;
-    asm volatile("" ::: "memory");
-    if (threadIdx.x == 0) __hip_atomic_store(A.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    finish<THREADS>(A.parts, n, A.stats);
+    s.join();
+    if (!few) {
+        last = 0;
+        auto& mine = A.counters->sums[group];
+        auto put = [&](uint64_t* to, uint64_t v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        if (lane == 0) {
+            put(&mine.loss, __builtin_bit_cast(uint64_t, s.loss));
+            put(&mine.kl, __builtin_bit_cast(uint64_t, s.kl));
+            static_for<3>([&](auto k) { put(&mine.counts[int(k)], s.counts[int(k)]); });
+            last = is_last(&A.counters->all.done, kGroups);
+        }
+        if (!__shfl(last, 0)) return;
+        auto get = [&](const uint64_t* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        const auto& other = A.counters->sums[lane];
+        s.loss = __builtin_bit_cast(double, get(&other.loss));
+        s.kl = __builtin_bit_cast(double, get(&other.kl));
+        static_for<3>([&](auto k) { s.counts[int(k)] = static_cast<uint32_t>(get(&other.counts[int(k)])); });
+        s.join();
+    }
+    if (lane == 0) *A.stats = s.stats();
+}
+
+// What a token adds, from the thread that knows it: to those that join the tokens, or at once, if it is the only one.
+__device__ __forceinline__ void deliver(const PolicyArgs& A, const uint32_t t, const PolicyPart& p)
+{
+    if (A.b.n_tokens != 1) {
+        send(A.parts + t, p);
+        return;
+    }
+    Sums s = {};
+    s.add(p);
+    *A.stats = s.stats();
 }
 
 // What a workgroup does with the slots it has: all of a row, the sum of a part of one, or, behind that, the part's gradient.
@@ -395,12 +468,13 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
     const uint8_t* const in = row + 16ull * first_slot;
     uint8_t* const out = GRAD ? A.dlogits + t * A.grad_stride * S::kBytes + 16ull * first_slot : nullptr;
     const int64_t target = table_entry(b.targets, t);
-    const bool wanted = table_entry(b.weights, t) != 0.f;
+    const Given have = given(b, t);
+    const bool wanted = have.weight != 0.f;
     auto leave_out = [&] {
         if (MODE == kSumOfPart) return;
         if (threadIdx.x == 0 && part == 0) {
             A.logp[t] = A.token_loss[t] = 0.f;
-            send(A.parts + t, PolicyPart{0, 0, wanted ? kTokenInvalid : 0u, 0u});
+            deliver(A, t, PolicyPart{0, 0, wanted ? kTokenInvalid : 0u, 0u});
         }
         if (!GRAD) return;
         for (uint32_t first = wave_first; first < slots; first += THREADS)
@@ -507,13 +581,13 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
         } else {
             const bool empty = m == -INFINITY && total == 0;
             if (m == -INFINITY) m = 0.f;
-            const Token k = token(b, t, z_y, m, total, lane);
+            const Token k = token(b, have, z_y, m, total, lane);
             if (lane == 0) {
                 if (!empty && part == 0) {
-                    const double w = table_entry(b.weights, t);
+                    const double w = have.weight;
                     A.logp[t] = static_cast<float>(k.logp);
                     A.token_loss[t] = static_cast<float>(k.loss);
-                    send(A.parts + t, PolicyPart{w * k.loss, w * k.kl, kTokenCounts | (k.clipped ? kTokenClipped : 0u), 0u});
+                    deliver(A, t, PolicyPart{w * k.loss, w * k.kl, kTokenCounts | (k.clipped ? kTokenClipped : 0u), 0u});
                 }
                 float f[2];
                 const bool apart = S::set_factors(f, k.factor, total, m);
@@ -569,19 +643,16 @@ template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void policy_kernel(const PolicyArgs A)
 {
     policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole>(A, blockIdx.x, 0, 1);
-    if (A.done) count_and_finish<THREADS>(A, gridDim.x);
+    if (threadIdx.x < kWaveSize) count_and_finish(A, blockIdx.x, threadIdx.x);
 }
-
-// Up to so many tokens are counted as they are done, and the last one's workgroup joins their sums; more would queue up at the counter
-// (50 ns each).  Without the kernel that does it else, us: 1 / 64 tokens on 1000 7.9 / 8.0, 65 10.8.
-constexpr uint32_t kCountedTokens = 64;
 
 // So many rows of more than 4096 slots are split into parts of 1024: the parts' sums in one launch, and in another, once more for
 // each of them, what is left of policy_kernel, on logits that are in the caches.  Whole / split, us: 1 / 4 / 16 / 32 / 60 / 100 rows of
 // 128,256 bf16 logits 21.6 / 22.0 / 22.8 / 22.5 / 22.5 / 25 and 10.8 / 11.1 / 12.0 / 12.9 / 15.3 / 22.4, 200 28.6 and 37.8; 16 / 64 / 120 rows of
-// 50,000 13.8 / 13.8 / 15.1 and 11.2 / 12.5 / 16.7; 16 / 64 / 128 of 130,000 fp32 ones 29.8 / 31.2 / 41.2 and 12.0 / 21.4 / 43.0.
+// 50,000 13.8 / 13.8 / 15.1 and 11.2 / 12.5 / 16.7; 16 / 64 / 128 of 130,000 fp32 ones 29.8 / 31.2 / 41.2 and 12.0 / 21.4 / 43.0.  Without a gradient 100 / 300 / 777 / 2000 rows of 50,021 fp32 ones
+// 12.9 / 20.4 / 34.2 / 70.6 and 13.9 / 19.9 / 33.4 / 75, of 128,256 21.0 / 43.5 / 82 / 176 and 18.1 / 32.7 / 74 / 176, bf16 777 / 2000 47 / 90 and 48 / 111.
 constexpr int kPartSlots = 4 * kPartThreads;
-constexpr uint32_t kSplitFrom = 4096, kSplitRows = kCountedTokens, kMostParts = 64;
+constexpr uint32_t kSplitFrom = 4096, kSplitRows = 64, kMostParts = 64;
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kPartThreads) void policy_sum_kernel(const PolicyArgs A, const uint32_t n_parts)
 {
@@ -592,15 +663,10 @@ __global__ __launch_bounds__(kPartThreads) void policy_grad_kernel(const PolicyA
 {
     const uint32_t per = GRAD ? n_parts : 1, part = blockIdx.x % per;
     policy_row<DTYPE, kPartThreads, 4, 4, GRAD, false, kGradOfPart>(A, blockIdx.x / per, part, n_parts);
-    if (part == 0) count_and_finish<kPartThreads>(A, gridDim.x / per);
+    if (part == 0 && threadIdx.x < kWaveSize) count_and_finish(A, blockIdx.x / per, threadIdx.x);
 }
 
-constexpr int kFinishThreads = 1024;
-__global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const PolicyPart* __restrict__ parts, uint32_t n,
-                                                                       ff_policy_stats* __restrict__ stats)
-{
-    finish<kFinishThreads>(parts, n, stats);
-}
+__global__ void policy_of_nothing_kernel(ff_policy_stats* stats) { *stats = {}; }
 
 struct Choice {
     void (*kernel)(const PolicyArgs);
@@ -620,7 +686,7 @@ Choice choose(uint64_t slots, uint64_t rows, bool grad)
     if (slots <= 2048 && many) return {grad ? policy_kernel<DTYPE, 512, 4, 8, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
     if (slots <= 4096) return {grad ? policy_kernel<DTYPE, 1024, 4, 8, true, false> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
     if (slots <= 8192 && many) return {grad ? policy_kernel<DTYPE, 512, 16, 4, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
-    return {grad ? policy_kernel<DTYPE, 1024, 16, 4, true, true> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
+        return {grad ? policy_kernel<DTYPE, 1024, 16, 4, true, true> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
 }
 
 template <uint32_t DTYPE>
@@ -646,8 +712,7 @@ hipError_t launch(const PolicyArgs& A, hipStream_t stream)
     return hipGetLastError();
 }
 
-// The workspace: how many tokens are done, on a line of its own; what they add to the sums; the parts of split rows.
-constexpr uint64_t kDoneBytes = 64;
+// The workspace: the counters; what tokens add to the sums; the parts of split rows.
 uint64_t parts_bytes(uint64_t n_tokens) { return (n_tokens * sizeof(PolicyPart) + 15) / 16 * 16; }
 
 }  // namespace
@@ -659,30 +724,25 @@ uint64_t policy_workspace(uint64_t n_tokens, uint64_t vocab)
         const uint64_t most = vocab / (4 * kPartSlots) + 1;  // of 32-bit logits
         row_parts = n_tokens * (most < kMostParts ? most : kMostParts);
     }
-    return kDoneBytes + parts_bytes(n_tokens) + row_parts * sizeof(RowPart);
+    return sizeof(Counters) + parts_bytes(n_tokens) + row_parts * sizeof(RowPart);
 }
 
 hipError_t launch_policy(const ff_policy_batch& b, float* logp, float* token_loss, void* dlogits, uint64_t grad_stride,
                          ff_policy_stats* stats, void* workspace, hipStream_t stream)
 {
     uint8_t* const w = static_cast<uint8_t*>(workspace);
-    const bool counted = b.n_tokens && b.n_tokens <= kCountedTokens;
     const PolicyArgs A = {b,
                           logp,
                           token_loss,
                           static_cast<uint8_t*>(dlogits),
                           grad_stride,
-                          reinterpret_cast<PolicyPart*>(w + kDoneBytes),
-                          reinterpret_cast<RowPart*>(w + kDoneBytes + parts_bytes(b.n_tokens)),
-                          counted ? reinterpret_cast<uint32_t*>(w) : nullptr,
+                          reinterpret_cast<PolicyPart*>(w + sizeof(Counters)),
+                          reinterpret_cast<RowPart*>(w + sizeof(Counters) + parts_bytes(b.n_tokens)),
+                          reinterpret_cast<Counters*>(w),
                           stats};
-    if (b.n_tokens) {
-        const hipError_t e = b.dtype == FF_F32    ? launch<FF_F32>(A, stream)
-                             : b.dtype == FF_BF16 ? launch<FF_BF16>(A, stream)
-                                                  : launch<FF_F16>(A, stream);
-        if (e != hipSuccess || counted) return e;
-    }
-    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, A.parts, static_cast<uint32_t>(b.n_tokens), stats);
+    if (b.n_tokens)
+        return b.dtype == FF_F32 ? launch<FF_F32>(A, stream) : b.dtype == FF_BF16 ? launch<FF_BF16>(A, stream) : launch<FF_F16>(A, stream);
+    hipLaunchKernelGGL(policy_of_nothing_kernel, dim3(1), dim3(1), 0, stream, stats);
     return hipGetLastError();
 }
 

@@ -483,6 +483,35 @@ def test_policy_rows_that_leave_nothing_targets_outside_and_masked_rows():
     assert torch.isfinite(got["dlogits"]).all()
 
 
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 127, 129, 4095, 4096, 20000])
+def test_policy_tokens_are_joined_whatever_their_number(n):
+    """Counted in one group or in 64 of unequal sizes; the same bits every time, on a workspace that other sizes use in between."""
+    v = 40
+    ws = ff.alloc_policy_workspace(20000, v, DEV)
+    rows, y, old, ref, adv, w = _policy_inputs(n, v, F32, n)
+    w[::3] = 0
+    y[1] = v  # outside
+    want = trainref.policy(rows, y, old, adv, w, ref, 0.2, 0.2, 0.1)
+    other, t = ([x.to(DEV) for x in given] for given in (
+        [x for x in _policy_inputs(70, v, F32, 1)], (rows, y, old, ref, adv, w)))
+    calls = []
+    for z, yy, o, r, a, ww in (t, other):
+        logp, token = (torch.empty(z.shape[0], device=DEV) for _ in range(2))
+        calls.append((ff.policy_batch(z, yy, o, a, ww, r, 0.2, 0.2, 0.1), logp, token, ff.PolicyStats(DEV)))
+    seen = set()
+    for _ in range(4):
+        for batch, logp, token, stats in calls:
+            ff.ff_policy_loss(batch, logp, token, stats, ws)
+        seen.add(tuple(calls[0][3].words.tolist()))
+    assert len(seen) == 1
+    stats = calls[0][3]
+    assert [int(stats.n_tokens), int(stats.n_clipped), int(stats.n_invalid)] == [want[k] for k in ("n_tokens", "n_clipped", "n_invalid")]
+    # the sums add the tokens' own losses in 64 bits: what is out is the tokens' rounding to 32, and that of the result
+    token, ww = calls[0][2].double().cpu(), w.double()
+    size = float((ww * token.abs()).sum())
+    assert abs(float(stats.loss) - float((ww * token).sum())) <= U32 * (1.01 * size + abs(float(stats.loss)))
+
+
 @pytest.mark.parametrize("bad", [NAN, INF])
 @pytest.mark.parametrize("n,v", [(6, 3001), (2, 64000)])
 def test_policy_rows_with_a_nan_or_infinity_say_so(bad, n, v):
