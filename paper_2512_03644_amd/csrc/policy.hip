@@ -7,13 +7,12 @@
 // softmax), from the logits in registers: they are read once.  What tokens add to the sums goes to memory and is
 // joined, always in the same order, by the last workgroups to be done (count_and_finish).
 //
-// What bounds it: memory, or for few tokens the launch and the chain from a row's load to its store.  Long rows alone with a compute
-// unit (128,256 bf16 logits are half of its registers) leave the memory idle between their loads and stores: the same with no arithmetic
-// at all takes 357 us where the loss of 4096 such tokens takes 392, and a copy of as many bytes 318.  Rows kept over in a loop of
-// workgroups, the next one's loads under way while the gradient is stored, took 500; a quarter of the row in registers and the rest
-// read again, so that two workgroups share a unit, 415 (399 with no arithmetic).  Us, gradient and all, 4096 tokens on 1000 / 4000 /
-// 8000 / 16,000 / 32,000 / 64,000 / 128,256 bf16 logits 13 / 22 / 32 / 55 / 99 / 196 / 421 (all tokens count); 1.0 GB of logits without
-// gradient 170 (6.2 TB/s).
+// What bounds it: memory, or for few tokens the launch and the chain from a row's load to its store.  A workgroup's loads do not overlap its
+// stores, so what counts is how many rows a compute unit has at once (choose): with one row of 128,256 bf16 logits to a unit 4096 of them took
+// 427 us, with two, parts of which are in LDS, 393; a copy of their bytes takes 330.  The arithmetic of a row, two exponentials and some ten
+// other operations a logit, would fill half of that time by itself.  Rows kept over in a loop of workgroups, the next one's loads
+// under way while the gradient is stored, took 500.  Us, gradient and all, 4096 tokens on 1000 / 4000 / 8000 / 16,000 / 32,000 / 64,000 /
+// 128,256 bf16 logits 12.5 / 22 / 32 / 54 / 97 / 193 / 391 (all tokens count); 1.05 GB of logits without gradient 170 (6.2 TB/s).
 #include "policy.hpp"
 
 #include <hip/hip_fp16.h>
@@ -441,9 +440,9 @@ __device__ __forceinline__ void deliver(const PolicyArgs& A, const uint32_t t, c
 // What a workgroup does with the slots it has: all of a row, the sum of a part of one, or, behind that, the part's gradient.
 enum Mode { kWhole, kSumOfPart, kGradOfPart };
 
-// A thread holds K slots of 16 bytes in registers (slot i * THREADS + thread), which is all of a row's or part's unless LONG: what is
+// A thread holds L slots of 16 bytes in LDS and K in registers (slot i * THREADS + thread), which is all of a row's or part's unless LONG: what is
 // behind them is then read again for the gradient.  WAVES: wavefronts on a SIMD that the registers leave room for.
-template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG, Mode MODE>
+template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG, Mode MODE, int L = 0>
 __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t, const uint32_t part, const uint32_t n_parts)
 {
     using S = typename SlotOf<DTYPE>::Type;
@@ -497,12 +496,16 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
         if (MODE != kGradOfPart) z_y = S::one(uniform(row), static_cast<uint32_t>(target));
         if (threadIdx.x < n_rest) end = S::one(uniform(in + 16ull * slots), threadIdx.x);
     }
-    u32x4 held[K];
-    if (MODE != kGradOfPart || GRAD)
-        static_for<K>([&](auto i) {
-            if (has(i)) held[int(i)] = load16<true>(uniform(in + 16ull * THREADS * i), 16 * at(i));
-        });
-    constexpr int kAhead = 4;  // slots under way of those that are not held
+    u32x4 held[K], early[L ? L : 1];
+    __shared__ u32x4 in_lds[L ? L * THREADS : 1];
+    auto fetch = [&](u32x4& to, auto round) {
+        if (has(round)) to = load16<true>(uniform(in + 16ull * THREADS * round), 16 * at(round));
+    };
+    if (MODE != kGradOfPart || GRAD) {
+        static_for<L>([&](auto i) { fetch(early[int(i)], i); });
+        static_for<K - L>([&](auto i) { fetch(held[L + i], std::integral_constant<int, 2 * L + i>{}); });
+    }
+    constexpr int kAhead = L ? 2 : 4;  // slots under way of those that are not held
     if constexpr (MODE != kGradOfPart) {
         Running r;
         // Two slots, of which a wavefront has the first.  (first: of the wavefront's in either)
@@ -521,12 +524,23 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
             }
             add<kFew>(r, z);
         };
-        static_for<K / 2>([&](auto i) {
+        static_for<L / 2>([&](auto i) {
             if (has(std::integral_constant<int, 2 * i>{}))
-                take(held[2 * i], held[2 * i + 1], 2 * i * THREADS + wave_first, (2 * i + 1) * THREADS + wave_first);
+                take(early[2 * i], early[2 * i + 1], 2 * i * THREADS + wave_first, (2 * i + 1) * THREADS + wave_first);
+            in_lds[2 * i * THREADS + threadIdx.x] = early[2 * i];
+            in_lds[(2 * i + 1) * THREADS + threadIdx.x] = early[2 * i + 1];
+            fetch(held[2 * i], std::integral_constant<int, L + 2 * i>{});
+            fetch(held[2 * i + 1], std::integral_constant<int, L + 2 * i + 1>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        static_for<K / 2>([&](auto i) {
+            constexpr int h = (2 * i + L) % K;  // those that were asked for first
+            if (has(std::integral_constant<int, L + h>{}))
+                take(held[h], held[h + 1], (L + h) * THREADS + wave_first, (L + h + 1) * THREADS + wave_first);
+            if constexpr (L) __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (LONG)
-            for (uint32_t first = K * THREADS + wave_first; first < slots; first += kAhead * THREADS) {
+            for (uint32_t first = (L + K) * THREADS + wave_first; first < slots; first += kAhead * THREADS) {
                 u32x4 w[kAhead];
                 static_for<kAhead>([&](auto i) {
                     const uint32_t f = first + i * THREADS;
@@ -613,14 +627,19 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
             if (has_target) g = S::with(g, y % N, target_grad);
             return g;
         };
+        auto put_round = [&](const u32x4 w, auto i) {
+            const uint32_t mine = at(i);
+            store16(uniform(out + 16ull * THREADS * i), 16 * mine, gradient(w, y / N - i * THREADS == mine));
+        };
+        static_for<L>([&](auto i) {
+            if (has(i)) put_round(in_lds[i * THREADS + threadIdx.x], i);
+        });
         static_for<K>([&](auto i) {
-            if (has(i)) {
-                const uint32_t mine = at(i);
-                store16(uniform(out + 16ull * THREADS * i), 16 * mine, gradient(held[int(i)], y / N - i * THREADS == mine));
-            }
+            constexpr std::integral_constant<int, L + i> round;
+            if (has(round)) put_round(held[int(i)], round);
         });
         if constexpr (LONG)
-            for (uint32_t first = K * THREADS + wave_first; first < slots; first += kAhead * THREADS) {
+            for (uint32_t first = (L + K) * THREADS + wave_first; first < slots; first += kAhead * THREADS) {
                 u32x4 w[kAhead];
                 static_for<kAhead>([&](auto i) {
                     const uint32_t f = first + i * THREADS;
@@ -639,10 +658,10 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
     }
 }
 
-template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG>
+template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG, int L = 0>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void policy_kernel(const PolicyArgs A)
 {
-    policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole>(A, blockIdx.x, 0, 1);
+    policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole, L>(A, blockIdx.x, 0, 1);
     if (threadIdx.x < kWaveSize) count_and_finish(A, blockIdx.x, threadIdx.x);
 }
 
@@ -672,11 +691,26 @@ struct Choice {
     void (*kernel)(const PolicyArgs);
     int threads;
 };
-// By the slots of a row: as many threads as hold it with four slots each, which leave room for 2048 on a compute unit; with sixteen from
-// where two rows no longer fit.  (Us, 4096 rows of 2000 slots by 256 / 512 / 1024 threads 63 / 56 / 60, of 4000 128 / 113 / 99; of 8000
-// by 512 threads with 16, by 1024 with 8, with 4 of 8 slots held 195 / 222 / 217; 1024 fp32 rows of 32,500 by 1024 threads with
-// 16 / 8 / 4 held 247 / 281 / 278.)  Few rows take 1024 threads where many would take 512.  Without a gradient nothing is held, and four
-// slots are on their way; the threads that share a row are the same, and so are the order of the sums and the loss.
+// By the slots of a row and the number of rows, so that as many rows as possible are on a compute unit at once, and are held there whole.
+// Threads hold four slots each in registers where that leaves room for 2048 on a compute unit, sixteen where two rows of 1024 threads no
+// longer fit.  LDS holds more of them:
+// - Rows of 2049-4096 slots: four on a unit, half of each in LDS (512 threads), or two, in registers (1024).  Many short rounds beat few
+//   long ones where the rows then end in one round, or are far from 4096 slots.  us, four / two, 600 / 1000 / 1500 / 2000 / 3000 bf16 rows of
+//   20,000 16.3 / 20.4 / 29.6 / 37.0 / 51.0 and 18.1 / 23.6 / 31.3 / 38.8 / 53.2, of 24,000 16.8 / 21.5 / 32.0 / 40.5 / 56.9 and 19.8 / 26.3 /
+//   35.2 / 43.3 / 60.0, of 28,000 20.0 / 25.0 / 38.1 / 48.8 / 69.9 and 21.4 / 29.0 / 38.8 / 48.7 / 68.0, of 32,000 21.3 / 26.0 / 42.1 / 52.2 /
+//   75.2 and 22.1 / 30.6 / 42.0 / 53.0 / 74.6; 4096 of 32,000 99.7 and 97.4, a quarter of them masked 93.0 and 87.3.
+// - Rows of 8193-20,480: two on a unit, one's loads under the other's stores, 20 slots of a thread in registers and 8 in LDS (14,336 in all;
+//   what is behind them is read again), or one, 16 of its 1024 threads each.  us, two / one, 4096 rows of 80,000 / 100,000 / 128,256 bf16 logits
+//   244 / 322 / 393 and 281 / 352 / 427, 300 / 500 / 1000 of 128,256 41.7 / 47.7 / 97.0 and 47.8 / 57.7 / 113, 2000 of 147,000 / 164,000 /
+//   180,000 256 / 280 / 315 and 271 / 280 / 313, of 50,000 / 65,000 fp32 ones 159 / 216 and 167 / 227, 1024 of 130,000 301 and 245.
+//   (18 slots in registers 399 where 20 take 393, with no LDS 436; 22 need scratch memory; what is read again four rounds at a time instead of
+//   two, or in front of what is held, 395 and 396.)
+// Three rows of 4097-8192 slots on a unit, 10 slots of a thread in registers and 6 in LDS (some scratch memory): 600 / 777 / 2000 / 4096 rows of
+// 50,000 30.7 / 40.7 / 82.7 / 162 where two take 34.8 / 42.2 / 86 / 164, of 64,000 34.8 / 49.0 / 103 / 198 and 39.9 / 49.0 / 100 / 193; 1000 fp32
+// rows of 32,000 58 and 50: not kept.
+// Other splits, us: 4096 rows of 2000 slots by 256 / 512 / 1024 threads 63 / 56 / 60; of 8000 by 512 threads with 16, by 1024 with 8, with 4 of 8
+// slots held 195 / 222 / 217; 1024 fp32 rows of 32,500 by 1024 threads with 16 / 8 / 4 held 247 / 281 / 278.  Few rows take 1024 threads where
+// many would take 512.  Without a gradient nothing is held, and four slots are on their way.
 template <uint32_t DTYPE>
 Choice choose(uint64_t slots, uint64_t rows, bool grad)
 {
@@ -684,9 +718,12 @@ Choice choose(uint64_t slots, uint64_t rows, bool grad)
     if (slots <= 256) return {grad ? policy_kernel<DTYPE, 64, 4, 8, true, false> : policy_kernel<DTYPE, 64, 4, 8, false, false>, 64};
     if (slots <= 1024) return {grad ? policy_kernel<DTYPE, 256, 4, 8, true, false> : policy_kernel<DTYPE, 256, 4, 8, false, false>, 256};
     if (slots <= 2048 && many) return {grad ? policy_kernel<DTYPE, 512, 4, 8, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
+    if (slots <= 4096 && grad && rows > 2 * kComputeUnits && (rows <= 4 * kComputeUnits || slots <= 3072))
+        return {policy_kernel<DTYPE, 512, 4, 8, true, false, 4>, 512};
     if (slots <= 4096) return {grad ? policy_kernel<DTYPE, 1024, 4, 8, true, false> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
     if (slots <= 8192 && many) return {grad ? policy_kernel<DTYPE, 512, 16, 4, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
-        return {grad ? policy_kernel<DTYPE, 1024, 16, 4, true, true> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
+        if (slots <= 20480 && many && grad) return {policy_kernel<DTYPE, 512, 20, 4, true, true, 8>, 512};
+    return {grad ? policy_kernel<DTYPE, 1024, 16, 4, true, true> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
 }
 
 template <uint32_t DTYPE>

@@ -432,6 +432,30 @@ def test_policy_on_both_sides_of_every_rule(n, slots, dtype, in_place):
     assert (got["beside"] == 9).all() or not in_place
 
 
+@pytest.mark.parametrize("n,slots,dtype,in_place", [
+    (257, 8193, BF16, True), (257, 14336, F32, False), (257, 14337, BF16, False), (300, 16033, F16, True), (258, 20480, F32, True),
+    (257, 20481, F32, False), (513, 2049, F32, True), (513, 4096, F16, True), (1025, 3072, BF16, False), (1025, 3073, BF16, True),
+    (512, 2050, F16, False)], ids=lambda x: str(x).replace("torch.", ""))
+def test_policy_of_many_long_rows(n, slots, dtype, in_place):
+    """Rows in registers and LDS, whole and with an end that is read again, and those too long for it."""
+    items = 4 if dtype == F32 else 8
+    v = slots * items + 1
+    rows, y, old, ref, adv, w = _policy_inputs(n, v, dtype, slots, 1)
+    for k, at in enumerate((0, 511, 512, 8 * 512 - 1, 8 * 512, slots - 1)):  # targets at the borders of what is held where
+        y[k] = min(slots - 1, at) * items + k % items
+    y[6] = v - 1
+    w[7] = 0
+    rows[8, :v] = -INF
+    rows[9, 5:v - 5] = -INF
+    y[9] = 2
+    moved = [0, 1, 2, 3, 4, 5, 6, 9]
+    logp = rows[moved, :v].double().log_softmax(1).gather(1, y[moved, None])[:, 0]
+    old[moved], ref[moved] = (logp - 0.1).float(), (logp + 0.2).float()
+    got = _run_policy(rows, v, y, old, adv, w, ref, 0.1, in_place=in_place)
+    _check_policy(got, rows, v, y, old, adv, w, ref, 0.1)
+    assert (got["beside"] == 9).all() or not in_place
+
+
 def test_policy_workspace_serves_call_after_call():
     """Counted tokens leave the count as they found it: calls of several sizes on one workspace, back to back."""
     v = 2000
