@@ -377,7 +377,6 @@ __device__ __forceinline__ bool is_last(uint32_t* count, const uint32_t n)
     wait_loads<0>();
     if (__hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 != n) return false;
     __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("" ::: "memory");
     return true;
 }
 
@@ -391,6 +390,7 @@ __device__ __forceinline__ void count_and_finish(const PolicyArgs& A, const uint
     int last = 0;
     if (lane == 0) last = is_last(few ? &A.counters->all.done : &A.counters->group[group].done, (n - group + step - 1) / step);
     if (!__shfl(last, 0)) return;
+    asm volatile("" ::: "memory");
     Sums s = {};
     constexpr int kAtOnce = 4;  // on their way
     for (uint64_t i0 = group + uint64_t(lane) * step; i0 < n; i0 += kAtOnce * kWaveSize * step) {
@@ -415,6 +415,7 @@ __device__ __forceinline__ void count_and_finish(const PolicyArgs& A, const uint
             last = is_last(&A.counters->all.done, kGroups);
         }
         if (!__shfl(last, 0)) return;
+        asm volatile("" ::: "memory");
         auto get = [&](const uint64_t* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
         const auto& other = A.counters->sums[lane];
         s.loss = __builtin_bit_cast(double, get(&other.loss));
