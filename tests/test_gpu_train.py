@@ -653,6 +653,43 @@ def test_calls_on_another_stream_and_in_a_graph(oracle):
         assert all(torch.equal(a, b) for a, b in zip(first, bits())), k
 
 
+@pytest.mark.parametrize("n,v", [(130, 1000), (300, 70001), (600, 20000)])
+def test_policy_of_many_tokens_in_a_graph(n, v):
+    """Tokens counted in groups, rows partly in LDS: replayed with eager calls on the same workspace between the replays."""
+    rows, y, old, ref, adv, w = (t.to(DEV) for t in _policy_inputs(n, v, BF16, n))
+    batch = ff.policy_batch(rows, y, old, adv, w, ref, beta=0.1)
+    logp, token, dz = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty_like(rows)
+    stats, ws = ff.PolicyStats(DEV), ff.alloc_policy_workspace(n, v, DEV)
+    outputs = [logp, token, dz, stats.words]
+
+    def call(stream=None):
+        ff.ff_policy_loss(batch, logp, token, stats, ws, dz, stream)
+
+    def bits():
+        torch.cuda.synchronize()
+        got = [t.clone().view(torch.uint8) for t in outputs]
+        for t in outputs:
+            t.view(torch.uint8).fill_(0x33)
+        return got
+
+    call()
+    first = bits()
+    assert int(first[3].view(torch.int64)[1]) == n
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        graph.capture_begin()
+        call(s)
+        graph.capture_end()
+    torch.cuda.synchronize()
+    for k in range(3):
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(first, bits())), k
+        call()
+        assert all(torch.equal(a, b) for a, b in zip(first, bits())), k
+
+
 def _unclipped(batch, dz):
     out = torch.empty_like(dz)
     n, v = dz.shape
