@@ -12,12 +12,13 @@
 // 427 us, with two, parts of which are in LDS, 393; a copy of their bytes takes 330.  The arithmetic of a row, two exponentials and some ten
 // other operations a logit, would fill half of that time by itself.  Rows kept over in a loop of workgroups, the next one's loads
 // under way while the gradient is stored, took 500.  Us, gradient and all, 4096 tokens on 1000 / 4000 / 8000 / 16,000 / 32,000 / 64,000 /
-// 128,256 bf16 logits 12.5 / 22 / 32 / 54 / 97 / 193 / 391 (all tokens count); 1.05 GB of logits without gradient 170 (6.2 TB/s).
+// 128,256 bf16 logits 12.3 / 22 / 31 / 53 / 94 / 192 / 391 (all tokens count); 1.05 GB of logits without gradient 170 (6.2 TB/s).
 #include "policy.hpp"
 
 #include <hip/hip_fp16.h>
 
 #include "fold.h"
+#include "xcd_order.h"
 
 namespace ffsnap {
 
@@ -659,11 +660,18 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
     }
 }
 
+// Rows that follow each other go to one XCD, four at a time (xcd_order.h), unless they are among the longest.  us, 4096 rows of 4000 / 8000 /
+// 16,000 / 32,000 / 64,000 / 128,256 bf16 logits in launch order 22.4 / 31.3 / 54.4 / 97.0 / 194 / 382, by two 22.5 / 31.4 / 52.9 / 94.8 / 191 / 385, by
+// eight 22.4 / 31.1 / 52.8 / 94.8 / 192 / 386, by 64 - / 31.6 / 53.5 / 95.0 / 195 / 388 (the last with a tenth masked).  Plain loads and stores instead of
+// non-temporal ones: stores 3-6 % slower; loads 2-3 % slower from 128 MB of logits on, and below 80 MB 10 % faster if the same logits are read
+// again and again, but 4-10 us slower where they are not in the caches.
+constexpr uint32_t kXcdRows = 4;
 template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG, int L = 0>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void policy_kernel(const PolicyArgs A)
 {
-    policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole, L>(A, blockIdx.x, 0, 1);
-    if (threadIdx.x < kWaveSize) count_and_finish(A, blockIdx.x, threadIdx.x);
+    const uint32_t t = xcd_order(blockIdx.x, gridDim.x, THREADS * (K + L) <= 8192 ? kXcdRows : 0);
+    policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole, L>(A, t, 0, 1);
+    if (threadIdx.x < kWaveSize) count_and_finish(A, t, threadIdx.x);
 }
 
 // So many rows of more than 4096 slots are split into parts of 1024: the parts' sums in one launch, and in another, once more for
@@ -723,7 +731,7 @@ Choice choose(uint64_t slots, uint64_t rows, bool grad)
         return {policy_kernel<DTYPE, 512, 4, 8, true, false, 4>, 512};
     if (slots <= 4096) return {grad ? policy_kernel<DTYPE, 1024, 4, 8, true, false> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
     if (slots <= 8192 && many) return {grad ? policy_kernel<DTYPE, 512, 16, 4, true, false> : policy_kernel<DTYPE, 512, 4, 8, false, true>, 512};
-        if (slots <= 20480 && many && grad) return {policy_kernel<DTYPE, 512, 20, 4, true, true, 8>, 512};
+    if (slots <= 20480 && many && grad) return {policy_kernel<DTYPE, 512, 20, 4, true, true, 8>, 512};
     return {grad ? policy_kernel<DTYPE, 1024, 16, 4, true, true> : policy_kernel<DTYPE, 1024, 4, 8, false, true>, 1024};
 }
 
