@@ -401,6 +401,8 @@ typedef struct {
     uint64_t n_invalid;  /* weight not 0 and yet left out: target outside the vocabulary, or every logit -inf */
 } ff_policy_stats;
 
+/* What ff_policy_loss is given.  Never falls with either argument: the workspace of the largest batch and
+ * vocabulary serves every smaller call. */
 uint64_t ff_policy_workspace_bytes(uint64_t n_tokens, uint64_t vocab);
 
 /*

@@ -763,14 +763,12 @@ uint64_t parts_bytes(uint64_t n_tokens) { return (n_tokens * sizeof(PolicyPart) 
 
 }  // namespace
 
+// (With room for the parts of split rows however many tokens there are: a workspace serves smaller calls as well.)
 uint64_t policy_workspace(uint64_t n_tokens, uint64_t vocab)
 {
-    uint64_t row_parts = 0;
-    if (n_tokens <= kSplitRows) {
-        const uint64_t most = vocab / (4 * kPartSlots) + 1;  // of 32-bit logits
-        row_parts = n_tokens * (most < kMostParts ? most : kMostParts);
-    }
-    return sizeof(Counters) + parts_bytes(n_tokens) + row_parts * sizeof(RowPart);
+    const uint64_t rows = n_tokens < kSplitRows ? n_tokens : kSplitRows;
+    const uint64_t most = vocab / (4 * kPartSlots) + 1;  // of 32-bit logits
+    return sizeof(Counters) + parts_bytes(n_tokens) + rows * (most < kMostParts ? most : kMostParts) * sizeof(RowPart);
 }
 
 hipError_t launch_policy(const ff_policy_batch& b, float* logp, float* token_loss, void* dlogits, uint64_t grad_stride,

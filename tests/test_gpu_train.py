@@ -782,3 +782,24 @@ def test_example_learns_and_its_snapshot_is_taken_over(half):
     assert losses[-1] < losses[0] - 0.02 and all(math.isfinite(x) for x in losses + norms)
     assert norms[0] > example.MAX_NORM
     assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(trained, taken_over))
+
+
+@pytest.mark.parametrize("most", [65, 200, 512])
+def test_policy_workspace_of_a_large_batch_serves_the_last_small_one(most):
+    """A program's workspace is that of its largest batch; an epoch ends with fewer tokens, whose rows are split."""
+    v = 40003
+    size = ff.alloc_policy_workspace(most, v, "cpu").nbytes
+    arena = torch.zeros(size + (1 << 16), dtype=torch.uint8, device=DEV)
+    arena[size:] = 0xA7
+    ws = arena[:size]
+    for n in (60, most, 64, 3):
+        rows, y, old, ref, adv, w = _policy_inputs(n, v, BF16, n)
+        t = [x.to(DEV) for x in (rows, y, old, adv, w, ref)]
+        logp, token, dz = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty_like(t[0])
+        stats = ff.PolicyStats(DEV)
+        ff.ff_policy_loss(ff.policy_batch(*t, 0.2, 0.3, 0.1), logp, token, stats, ws, dz)
+        torch.cuda.synchronize()
+        got = dict(logp=logp.cpu(), token_loss=token.cpu(), loss=float(stats.loss), kl=float(stats.kl), n_tokens=int(stats.n_tokens),
+                   n_clipped=int(stats.n_clipped), n_invalid=int(stats.n_invalid), dlogits=dz.cpu())
+        _check_policy(got, rows, v, y, old, adv, w, ref, 0.1)
+        assert bool((arena[size:] == 0xA7).all())

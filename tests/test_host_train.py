@@ -198,3 +198,14 @@ def test_segments_are_filled_as_they_were():
     assert len(none) == 1 and (none[0].ptr, none[0].nbytes, none[0].dtype) == (None, 0, 0)
     with pytest.raises(ValueError, match="segment 1 "):
         ff.make_segments([ts[0], torch.zeros(4, 4).t()])
+
+
+def test_a_policy_workspace_serves_every_smaller_call():
+    """Sizes never fall with the tokens or the vocabulary: rows are split, and their parts stored, where there are few."""
+    tokens = [0, 1, 2, 16, 63, 64, 65, 66, 100, 512, 4096, 1 << 20, (1 << 31) - 1]
+    vocabs = [1, 8, 4096, 16384, 16385, 32000, 32769, 128256, 262144, 1 << 20, (1 << 31) - 1]
+    sizes = [[ff.lib().ff_policy_workspace_bytes(n, v) for v in vocabs] for n in tokens]
+    for row, more in zip(sizes, sizes[1:]):
+        assert all(a <= b for a, b in zip(row, more))
+    for row in sizes:
+        assert row == sorted(row)
