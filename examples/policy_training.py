@@ -73,8 +73,8 @@ def train(steps=30, half=torch.bfloat16, seed=0, report=print):
     # the policy that made the tokens, which is the reference as well
     _, logits = forward()
     old_logp = torch.empty(TOKENS, device=DEV)
-    zeros = torch.zeros(TOKENS, device=DEV)
-    scored = ff.policy_batch(logits, targets, zeros, zeros, torch.ones(TOKENS, device=DEV))
+    zeros, ones = torch.zeros(TOKENS, device=DEV), torch.ones(TOKENS, device=DEV)
+    scored = ff.policy_batch(logits, targets, zeros, zeros, ones)
     ff.ff_policy_loss(scored, old_logp, token_loss, loss_stats, loss_space)
 
     losses, norms = [], []

@@ -64,6 +64,8 @@ class ff_adam_hparams(ctypes.Structure):
 
 
 class ff_policy_batch(ctypes.Structure):
+    tensors = ()  # those that it points at (policy_batch), kept alive
+
     _fields_ = [("logits", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
                 ("vocab", ctypes.c_uint64), ("row_stride", ctypes.c_uint64),
                 ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
@@ -504,7 +506,8 @@ _PER_TOKEN = " is a contiguous fp32 tensor of one entry per token"
 def policy_batch(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low=0.2,
                  clip_high=0.2, beta=0.0, loss_scale=1.0):
     """ff_policy_batch of device tensors: logits [tokens, vocab] (rows may lie apart), targets int64,
-    the others fp32, [tokens] each.  The caller keeps the tensors alive until the stream's work is done."""
+    the others fp32, [tokens] each.  It keeps the tensors alive, and is itself kept until the calls on it are enqueued (on another
+    stream than the tensors' own: until they are done)."""
     n, vocab = logits.shape if logits.dim() == 2 else (0, 0)
     stride, inner = logits.stride() if logits.dim() == 2 else (0, 0)
     if inner != 1 and vocab != 1:
@@ -523,10 +526,12 @@ def policy_batch(logits, targets, old_logp, advantages, weights, ref_logp=None, 
         raise ValueError("advantages" + _PER_TOKEN)
     if weights.dtype is not f32 or weights.shape != one or not weights.is_contiguous():
         raise ValueError("weights" + _PER_TOKEN)
-    return ff_policy_batch.from_buffer_copy(_BATCH.pack(
+    batch = ff_policy_batch.from_buffer_copy(_BATCH.pack(
         logits.data_ptr(), n, vocab, stride if n > 1 else max(stride, vocab), _DTYPES[logits.dtype], 0,
         targets.data_ptr(), old_logp.data_ptr(), ref, advantages.data_ptr(), weights.data_ptr(), clip_low,
         clip_high, beta, loss_scale))
+    batch.tensors = (logits, targets, old_logp, advantages, weights, ref_logp)
+    return batch
 
 
 def ff_policy_loss(batch, logp, token_loss, stats, workspace, dlogits=None, stream=None):

@@ -2,6 +2,7 @@
 comes before any work on the device, so none of them needs one."""
 import ctypes
 import types
+import weakref
 
 import pytest
 import torch
@@ -209,3 +210,17 @@ def test_a_policy_workspace_serves_every_smaller_call():
         assert all(a <= b for a, b in zip(row, more))
     for row in sizes:
         assert row == sorted(row)
+
+
+def test_a_policy_batch_keeps_its_tensors_alive():
+    """Its addresses are read when the call comes: tensors that only the batch was given are not back with the allocator by then."""
+    def make():
+        z, y = torch.zeros(4, 10, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
+        per_token = [torch.zeros(4) for _ in range(4)]
+        return ff.policy_batch(z, y, *per_token), [weakref.ref(t) for t in (z, y, *per_token)]
+
+    batch, kept = make()
+    assert all(r() is not None for r in kept)
+    assert {batch.logits, batch.targets, batch.old_logp, batch.advantages, batch.weights, batch.ref_logp} == {r().data_ptr() for r in kept}
+    del batch
+    assert all(r() is None for r in kept)
