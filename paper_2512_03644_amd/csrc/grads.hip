@@ -406,19 +406,21 @@ hipError_t launch_grad_join(const ff_grad_stats* parts, uint64_t n, double inv_s
 
 hipError_t launch_grad_clip(const GradWork& work, const void* const* grads, const ff_grad_stats* stats, hipStream_t stream)
 {
-    auto groups = [](uint32_t n) { return dim3((n + kGradWaves - 1) / kGradWaves); };
-    if (!grads) {
-        if (!work.launch.back()) return hipSuccess;
-        hipLaunchKernelGGL(grad_clip_kernel<ListAddresses>, groups(work.launch.back()), dim3(kThreads), 0, stream, work.items,
-                           work.launch.back(), stats, ListAddresses{work.address});
-        return hipGetLastError();
-    }
+    auto clip = [&](uint32_t begin, const uint32_t end, const auto& addresses) {
+        constexpr uint32_t kMost = most_groups(kThreads) * kGradWaves;
+        while (begin < end) {
+            const uint32_t n = end - begin < kMost ? end - begin : kMost;
+            hipLaunchKernelGGL(grad_clip_kernel<std::decay_t<decltype(addresses)>>, dim3((n + kGradWaves - 1) / kGradWaves), dim3(kThreads), 0,
+                               stream, work.items + begin, n, stats, addresses);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            begin += n;
+        }
+        return hipSuccess;
+    };
+    if (!grads) return clip(0, work.launch.back(), ListAddresses{work.address});
     for (size_t k = 0; k + 1 < work.launch.size(); k++) {
-        const uint32_t first = work.launch[k], n = work.launch[k + 1] - first;
-        if (!n) continue;
-        hipLaunchKernelGGL(grad_clip_kernel<CallAddresses>, groups(n), dim3(kThreads), 0, stream, work.items + first, n, stats,
-                           call_addresses(work, grads, k));
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = clip(work.launch[k], work.launch[k + 1], call_addresses(work, grads, k));
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

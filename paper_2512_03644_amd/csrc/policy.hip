@@ -667,9 +667,9 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& A, const uint32_t t
 // again and again, but 4-10 us slower where they are not in the caches.
 constexpr uint32_t kXcdRows = 4;
 template <uint32_t DTYPE, int THREADS, int K, int WAVES, bool GRAD, bool LONG, int L = 0>
-__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void policy_kernel(const PolicyArgs A)
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void policy_kernel(const PolicyArgs A, const uint32_t first)
 {
-    const uint32_t t = xcd_order(blockIdx.x, gridDim.x, THREADS * (K + L) <= 8192 ? kXcdRows : 0);
+    const uint32_t t = first + xcd_order(blockIdx.x, gridDim.x, THREADS * (K + L) <= 8192 ? kXcdRows : 0);
     policy_row<DTYPE, THREADS, K, WAVES, GRAD, LONG, kWhole, L>(A, t, 0, 1);
     if (threadIdx.x < kWaveSize) count_and_finish(A, t, threadIdx.x);
 }
@@ -697,7 +697,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_grad_kernel(const PolicyA
 __global__ void policy_of_nothing_kernel(ff_policy_stats* stats) { *stats = {}; }
 
 struct Choice {
-    void (*kernel)(const PolicyArgs);
+    void (*kernel)(const PolicyArgs, uint32_t first);
     int threads;
 };
 // By the slots of a row and the number of rows, so that as many rows as possible are on a compute unit at once, and are held there whole.
@@ -754,8 +754,15 @@ hipError_t launch(const PolicyArgs& A, hipStream_t stream)
         return hipGetLastError();
     }
     const Choice c = choose<DTYPE>(slots, rows, grad);
-    hipLaunchKernelGGL(c.kernel, dim3(rows), dim3(c.threads), 0, stream, A);
-    return hipGetLastError();
+    // in one launch, up to 4 million rows and more; tokens are counted over all
+    const uint32_t most = most_groups(c.threads);
+    for (uint64_t first = 0; first < rows; first += most) {
+        const uint32_t left = rows - static_cast<uint32_t>(first);
+        hipLaunchKernelGGL(c.kernel, dim3(left < most ? left : most), dim3(c.threads), 0, stream, A, static_cast<uint32_t>(first));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // The workspace: the counters; what tokens add to the sums; the parts of split rows.

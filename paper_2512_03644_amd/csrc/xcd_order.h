@@ -33,4 +33,7 @@ FF_XCD_HD inline uint32_t xcd_order(uint32_t b, uint32_t n, uint32_t g)
     return b - in + ((in & (kXcds - 1)) << l) + (in >> kXcdsLog2);
 }
 
+// Workgroups that one launch can have: its work items are counted in 32 bits.
+constexpr uint32_t most_groups(uint32_t threads) { return 0xFFFFFFFFu / threads; }
+
 }  // namespace ffsnap

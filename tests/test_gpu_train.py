@@ -803,3 +803,37 @@ def test_policy_workspace_of_a_large_batch_serves_the_last_small_one(most):
                    n_clipped=int(stats.n_clipped), n_invalid=int(stats.n_invalid), dlogits=dz.cpu())
         _check_policy(got, rows, v, y, old, adv, w, ref, 0.1)
         assert bool((arena[size:] == 0xA7).all())
+
+
+def test_policy_of_more_tokens_than_one_launch_has_work_items_for():
+    """A wavefront to a row: 67,108,863 rows fill the 32 bits that a launch's work items are counted in."""
+    n, v = (1 << 26) + 6, 8
+    g = torch.Generator(device=DEV).manual_seed(6)
+    z = torch.empty(n, v, dtype=BF16, device=DEV).normal_(0, 2.0, generator=g)
+    y = torch.randint(0, v, (n,), generator=g, device=DEV)
+    old, adv = torch.full((n,), -2.0, device=DEV), torch.empty(n, device=DEV).normal_(generator=g)
+    w = torch.full((n,), 1.0 / n, device=DEV)
+    w[5::9] = 0
+    logp, token, dz = torch.full((n,), 7.0, device=DEV), torch.full((n,), 7.0, device=DEV), torch.full_like(z, 7.0)
+    stats, ws = ff.PolicyStats(DEV), ff.alloc_policy_workspace(n, v, DEV)
+    for _ in range(2):  # counters are left as they were
+        ff.ff_policy_loss(ff.policy_batch(z, y, old, adv, w, None, 0.2, 0.3), logp, token, stats, ws, dz, None)
+    torch.cuda.synchronize()
+    assert int(stats.n_tokens) == int((w != 0).sum()) and int(stats.n_invalid) == 0
+    loss = size = 0.0
+    for a in range(0, n, 1 << 24):
+        part = slice(a, a + (1 << 24))
+        want = torch.log_softmax(z[part].double(), 1).gather(1, y[part, None])[:, 0] * (w[part] != 0)
+        # eight terms, 2 U32 of each and 3 of its distance, at most 20 here; the result's rounding
+        assert bool(((logp[part].double() - want).abs() <= 128 * U32 + U32 * want.abs()).all())
+        counted = (w[part].double() * token[part].double())
+        loss, size = loss + float(counted.sum()), size + float(counted.abs().sum())
+    assert abs(float(stats.loss) - loss) <= U32 * (1.01 * size + abs(loss))
+    border = (1 << 26) - 1
+    for a in (0, border - 20, n - 20):
+        part = slice(a, min(n, a + 40))
+        small = [t[part].cpu() for t in (z, y, old, adv, w)]
+        want = trainref.policy(*small, None, 0.2, 0.3)
+        assert torch.equal(want["used"], small[4] != 0)
+        assert torch.allclose(token[part].cpu().double(), want["token_loss"], rtol=200 * U32, atol=0)
+        assert torch.allclose(dz[part].cpu().double(), want["dlogits"], rtol=2.0 ** -7, atol=2.0 ** -126)
