@@ -354,12 +354,16 @@ CallAddresses call_addresses(const GradWork& work, const void* const* grads, uin
 
 bool build_grad_items(const ff_segment* segs, uint64_t n, std::vector<GradItem>& items, std::vector<uint32_t>& begin)
 {
+    uint64_t count = 0;  // before any of them is stored
+    for (uint64_t k = 0; k < n; k++) {
+        count += segs[k].nbytes / kGradItemBytes + (segs[k].nbytes % kGradItemBytes != 0);
+        if (count > (1ull << 31)) return false;
+    }
+    items.reserve(count);
     begin.push_back(0);
     for (uint64_t k = 0; k < n; k++) {
         if (k && k % kGradsPerLaunch == 0) begin.push_back(static_cast<uint32_t>(items.size()));
         const uint32_t format = segs[k].dtype == FF_F32 ? kGradF32 : segs[k].dtype == FF_BF16 ? kGradBf16 : kGradF16;
-        const uint64_t pieces = (segs[k].nbytes + kGradItemBytes - 1) / kGradItemBytes;
-        if (items.size() + pieces > (1ull << 31)) return false;
         for (uint64_t b = 0; b < segs[k].nbytes; b += kGradItemBytes) {
             const uint64_t left = segs[k].nbytes - b;
             items.push_back({b, static_cast<uint32_t>(k),

@@ -224,3 +224,16 @@ def test_a_policy_batch_keeps_its_tensors_alive():
     assert {batch.logits, batch.targets, batch.old_logp, batch.advantages, batch.weights, batch.ref_logp} == {r().data_ptr() for r in kept}
     del batch
     assert all(r() is None for r in kept)
+
+
+def test_lists_refuse_tensors_of_impossible_sizes():
+    """Sizes that pass 64 bits when they are rounded up to items, and together."""
+    L = ff.lib()
+    out = ctypes.c_void_p()
+    for dtype, sizes in ((ff.FF_F32, [2 ** 64 - 4]), (ff.FF_BF16, [2 ** 64 - 2]), (ff.FF_F32, [2 ** 64 - 8192]), (ff.FF_F32, [8, 2 ** 63]),
+                         (ff.FF_F16, [2 ** 45]), (ff.FF_BF16, [2 ** 43, 2 ** 43 + 2])):
+        segs = ff.make_segments([torch.zeros(2)] * len(sizes))
+        for s, size in zip(segs, sizes):
+            s.dtype, s.nbytes, s.ptr = dtype, size, A16
+        assert L.ff_grad_list_create(segs, len(sizes), HOST, ctypes.byref(out)) == ff.FF_ERR_INVALID, sizes
+        assert out.value is None
