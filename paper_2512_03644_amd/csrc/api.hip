@@ -71,6 +71,7 @@ thread_local char g_hip_error[256] = "";
 int ffsnap::hip_fail(hipError_t e)
 {
     std::snprintf(g_hip_error, sizeof(g_hip_error), "%s", hipGetErrorString(e));
+    (void)hipGetLastError();
     return FF_ERR_HIP;
 }
 
@@ -202,8 +203,7 @@ int upload_tables(ff_plan* p)
     FF_HIP_TRY(hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, p->device));
     p->compute_units = units > 0 ? static_cast<uint64_t>(units) : 0;
     hipError_t e = hipMalloc(&p->dev_block, total);
-    if (e == hipErrorOutOfMemory) return FF_ERR_NOMEM;
-    FF_HIP_TRY(e);
+    if (e != hipSuccess) return alloc_fail(e);
     FF_HIP_TRY(hipMemcpy(p->dev_block, host.data(), total, hipMemcpyHostToDevice));
 
     unsigned char* d = static_cast<unsigned char*>(p->dev_block);
@@ -833,8 +833,7 @@ int ff_crc32c(const void* dev_buf, uint64_t nbytes, uint32_t* dev_out, void* hip
     const uint64_t scratch_bytes = kTabWords * 4 + (static_cast<uint64_t>(t.n_tiles) + 1) * 4;
     void* scratch = nullptr;
     hipError_t e = hipMalloc(&scratch, scratch_bytes);
-    if (e == hipErrorOutOfMemory) return FF_ERR_NOMEM;
-    FF_HIP_TRY(e);
+    if (e != hipSuccess) return alloc_fail(e);
     uint32_t tab[kTabWords];
     build_tab_u(tab);
     int rc = FF_OK;

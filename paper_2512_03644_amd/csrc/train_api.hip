@@ -60,8 +60,7 @@ int upload(ff_grad_list* list, const std::vector<GradItem>& items, const std::ve
     if (item_bytes) std::memcpy(host.data(), items.data(), item_bytes);
     if (address_bytes) std::memcpy(host.data() + item_bytes, address.data(), address_bytes);
     const hipError_t e = hipMalloc(&list->dev_block, host.size());
-    if (e == hipErrorOutOfMemory) return FF_ERR_NOMEM;
-    FF_HIP_TRY(e);
+    if (e != hipSuccess) return alloc_fail(e);
     FF_HIP_TRY(hipMemcpy(list->dev_block, host.data(), host.size(), hipMemcpyHostToDevice));
     unsigned char* const d = static_cast<unsigned char*>(list->dev_block);
     list->work.items = reinterpret_cast<const GradItem*>(d);

@@ -37,15 +37,24 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, si
     g_log.push_back(l);
     return hipSuccess;
 }
-hipError_t hipGetLastError() { return hipSuccess; }
-hipError_t hipMalloc(void**, size_t) { return hipErrorOutOfMemory; }
+static hipError_t g_error = hipSuccess, g_malloc = hipErrorOutOfMemory;
+hipError_t hipGetLastError() { const hipError_t e = g_error; g_error = hipSuccess; return e; }
+hipError_t hipMalloc(void**, size_t) { return g_error = g_malloc; }
 hipError_t hipFree(void*) { return hipSuccess; }
 hipError_t hipMemcpy(void*, const void*, size_t, hipMemcpyKind) { return hipSuccess; }
 hipError_t hipGetDevice(int* d) { *d = 0; return hipSuccess; }
-const char* hipGetErrorString(hipError_t) { return ""; }
+hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t, int) { *v = 256; return hipSuccess; }
+const char* hipGetErrorString(hipError_t) { return "stand-in"; }
+// (of calls that are not made here)
+hipError_t hipMemcpyAsync(void*, const void*, size_t, hipMemcpyKind, hipStream_t) { return hipSuccess; }
+hipError_t hipGetSymbolAddress(void**, const void*) { return hipErrorNotFound; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* st) { *st = hipStreamCaptureStatusNone; return hipSuccess; }
+hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipStreamWaitEvent(hipStream_t, hipEvent_t, unsigned) { return hipSuccess; }
+hipError_t hipEventCreateWithFlags(hipEvent_t* e, unsigned) { *e = nullptr; return hipSuccess; }
+hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return hipSuccess; }
+hipError_t hipEventDestroy(hipEvent_t) { return hipSuccess; }
 }
-
-int ffsnap::hip_fail(hipError_t) { return FF_ERR_HIP; }
 
 #define CHECK(c) do { if (!(c)) { std::printf("line %d: %s\n", __LINE__, #c); return 1; } } while (0)
 
@@ -102,6 +111,18 @@ int main()
             next += l.args[1];
         }
         CHECK(next == n);
+    }
+    // What a call has reported is not the next one's error.
+    const ff_segment seg = {address(1 << 20), 64, FF_F32, FF_KIND_RAW, 0, 0};
+    for (hipError_t e : {hipErrorOutOfMemory, hipErrorInvalidValue}) {
+        g_malloc = e;
+        ff_grad_list* list;
+        CHECK(ff_grad_list_create(&seg, 1, 0, &list) == (e == hipErrorOutOfMemory ? FF_ERR_NOMEM : FF_ERR_HIP) && !list);
+        ff_grad_stats* const stats = reinterpret_cast<ff_grad_stats*>(1 << 20);
+        CHECK(ff_grad_norm_join(stats, 1, 1.0, 1.0, stats, nullptr) == FF_OK);
+        ff_plan* plan;
+        CHECK(ff_snapshot_plan(&seg, 1, 1024, 0, &plan) == (e == hipErrorOutOfMemory ? FF_ERR_NOMEM : FF_ERR_HIP) && !plan);
+        CHECK(ff_grad_norm_join(stats, 1, 1.0, 1.0, stats, nullptr) == FF_OK);
     }
     std::printf("ok\n");
     return 0;

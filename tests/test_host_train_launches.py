@@ -18,7 +18,8 @@ def test_launches_fit_the_device_and_cover_everything(tmp_path):
                         "--offload-host-only", "-c", "-o", obj, src], check=True, capture_output=True, text=True)
         return obj
 
-    srcs = [os.path.join(CSRC, s) for s in ("grads.hip", "policy.hip", "train_api.hip")]
+    srcs = [os.path.join(CSRC, s) for s in ("api.hip", "kernels.hip", "blocks.hip", "fused.hip", "grads.hip", "policy.hip",
+                                              "train_api.hip", "layout.cpp")]
     srcs.append(os.path.join(ROOT, "tests", "native", "train_launches_check.cpp"))
     with ThreadPoolExecutor(len(srcs)) as ex:
         objs = list(ex.map(compile_host, srcs))
