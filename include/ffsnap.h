@@ -331,7 +331,7 @@ typedef struct {
 /*
  * Global L2 norm over all tensors of the list, and what follows from it for clipping.  Squares and
  * sums are held in 64 bits: no finite element overflows or underflows; the order of the sums depends on the
- * list alone, so the same values give the same bits.  grads: HOST array of n DEVICE pointers in the list's order, each
+ * list alone, so the same values give the same bits, wherever they lie.  grads: HOST array of n DEVICE pointers in the list's order, each
  * aligned to its element (entries of empty tensors are ignored), or NULL for the list's own addresses.
  * inv_loss_scale: finite and > 0 in fp32 as well (1 without a loss scale); max_norm: > 0, INFINITY for no clipping.
  * stats: DEVICE, 8-byte aligned.  workspace: DEVICE, 16-byte aligned, ff_grad_list_workspace_bytes() bytes,

@@ -166,13 +166,13 @@ __device__ __forceinline__ void group_sum(double& sum, uint64_t& bad)
     }
 }
 
-// How the parts of all workgroups are joined in the same launch: the last workgroup of every sixty-fourth of them counts there, and the
-// last of those joins the parts, in their order whoever it is.  (On one counter workgroups that end together would queue up, 50 ns each.)
+// How the parts of all workgroups are joined in the same launch: workgroups count at one of 32 places, the last one at each
+// of them at the root, and the last of those joins the parts, in their order whoever it is.  (On one counter workgroups that end together would queue up, 50 ns each.)
 // Counters, on lines of their own, are zero before and after.
 struct Joining {
     uint64_t* counts;  // kLeaves, and the root
     GradPart* parts;
-    uint32_t first, n;  // of this launch's workgroups among all, and all
+    uint32_t n;  // workgroups
     double inv_scale, max_norm;
     ff_grad_stats* stats;
 };
@@ -191,7 +191,7 @@ __device__ __forceinline__ void join_parts(const Joining& J, double sum, uint64_
 {
     __shared__ int last;
     if (threadIdx.x == 0) {
-        const uint32_t at = J.first + blockIdx.x;
+        const uint32_t at = blockIdx.x;
         // past the caches of this workgroup's XCD, and of the one that joins
         __hip_atomic_store(reinterpret_cast<uint64_t*>(&J.parts[at].sumsq), __builtin_bit_cast(uint64_t, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __hip_atomic_store(&J.parts[at].n_nonfinite, bad, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -261,6 +261,14 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const GradItem* __r
     }
     group_sum<kThreads>(sum, bad);
     join_parts(J, sum, bad);
+}
+
+// The addresses of a call into its workspace, for lists of more tensors than a launch's arguments hold: the norm is one launch, over the same
+// parts in the same order, wherever addresses come from.
+__global__ __launch_bounds__(kThreads) void grad_addresses_kernel(const CallAddresses addresses, const uint32_t n, uint64_t* table)
+{
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
+    if (i < n) table[addresses.base + i] = addresses.grads.p[i];
 }
 
 // One wavefront: it loads the parts side by side, and adds them one after the other.
@@ -374,31 +382,35 @@ bool build_grad_items(const ff_segment* segs, uint64_t n, std::vector<GradItem>&
     return true;
 }
 
+// The workspace: counters, parts, and the addresses of a call on a long list.
 hipError_t launch_grad_norm(const GradWork& work, const void* const* grads, double inv_scale, double max_norm,
                             void* workspace, ff_grad_stats* stats, hipStream_t stream)
 {
     uint8_t* const w = static_cast<uint8_t*>(workspace);
-    Joining J = {reinterpret_cast<uint64_t*>(w), reinterpret_cast<GradPart*>(w + kCountBytes), 0, work.n_parts(!grads), inv_scale, max_norm, stats};
-    if (!grads) {
-        hipLaunchKernelGGL(grad_norm_kernel<ListAddresses>, dim3(J.n), dim3(kThreads), 0, stream, work.items, work.launch.back(), J,
-                           ListAddresses{work.address});
+    const uint32_t n_items = work.launch.back(), groups = grad_groups(n_items);
+    const Joining J = {reinterpret_cast<uint64_t*>(w), reinterpret_cast<GradPart*>(w + kCountBytes), groups, inv_scale, max_norm, stats};
+    auto norm = [&](const auto& addresses) {
+        hipLaunchKernelGGL(grad_norm_kernel<std::decay_t<decltype(addresses)>>, dim3(groups), dim3(kThreads), 0, stream, work.items, n_items, J,
+                           addresses);
         return hipGetLastError();
-    }
-    for (size_t k = 0; k + 1 < work.launch.size(); k++) {
-        const uint32_t first = work.launch[k], n = work.launch[k + 1] - first, groups = grad_groups(n);
-        hipLaunchKernelGGL(grad_norm_kernel<CallAddresses>, dim3(groups), dim3(kThreads), 0, stream, work.items + first, n, J,
-                           call_addresses(work, grads, k));
+    };
+    if (!grads) return norm(ListAddresses{work.address});
+    if (work.n <= kGradsPerLaunch) return norm(call_addresses(work, grads, 0));
+    uint64_t* const table = reinterpret_cast<uint64_t*>(w + kCountBytes + groups * sizeof(GradPart));
+    for (uint64_t k = 0; k * kGradsPerLaunch < work.n; k++) {
+        const uint64_t left = work.n - k * kGradsPerLaunch;
+        const uint32_t n = static_cast<uint32_t>(left < kGradsPerLaunch ? left : kGradsPerLaunch);
+        hipLaunchKernelGGL(grad_addresses_kernel, dim3((n + kThreads - 1) / kThreads), dim3(kThreads), 0, stream,
+                           call_addresses(work, grads, k), n, table);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        J.first += groups;
     }
-    return hipSuccess;
+    return norm(ListAddresses{table});
 }
 
 uint64_t grad_workspace(const GradWork& work)
 {
-    const uint64_t own = work.n_parts(true), given = work.n_parts(false);
-    return kCountBytes + (own > given ? own : given) * sizeof(GradPart);
+    return kCountBytes + grad_groups(work.launch.back()) * sizeof(GradPart) + (work.n > kGradsPerLaunch ? work.n * sizeof(uint64_t) : 0);
 }
 
 hipError_t launch_grad_join(const ff_grad_stats* parts, uint64_t n, double inv_scale, double max_norm,

@@ -43,13 +43,6 @@ struct GradWork {
     const uint64_t* address = nullptr;  // DEVICE: of every tensor; null where every call brings its own
     std::vector<uint32_t> launch;       // build_grad_items
     uint64_t n = 0;                     // tensors
-    uint32_t n_parts(bool own_addresses) const
-    {
-        if (own_addresses) return grad_groups(launch.back());
-        uint32_t sum = 0;
-        for (size_t k = 0; k + 1 < launch.size(); k++) sum += grad_groups(launch[k + 1] - launch[k]);
-        return sum;
-    }
 };
 
 // What launch_grad_norm is given, zero before the first call.

@@ -112,6 +112,25 @@ int main()
         }
         CHECK(next == n);
     }
+    // A norm is one launch over all items, whose parts are joined in their order; the workspace holds the addresses of a long list's call.
+    for (uint64_t n : {1ull, 2048ull, 2049ull, 5000ull}) {
+        const std::vector<const void*> grads(n, address(1 << 20));
+        work.n = n;
+        work.launch = {0};
+        for (uint64_t k = 2048; k < n; k += 2048) work.launch.push_back(static_cast<uint32_t>(3 * k));
+        work.launch.push_back(static_cast<uint32_t>(3 * n));
+        uint32_t groups[2];
+        for (int given : {0, 1}) {
+            g_log.clear();
+            CHECK(launch_grad_norm(work, given ? grads.data() : nullptr, 1.0, 1.0, address(1 << 20), nullptr, nullptr) == hipSuccess);
+            CHECK(g_log.back().kernel.find("grad_norm_kernel") != std::string::npos);
+            for (size_t k = 0; k + 1 < g_log.size(); k++) CHECK(g_log[k].kernel.find("grad_norm_kernel") == std::string::npos);
+            groups[given] = g_log.back().groups;
+        }
+        CHECK(groups[0] == groups[1]);
+        CHECK(grad_workspace(work) >= groups[0] * sizeof(GradPart) + (n > 2048 ? 8 * n : 0));
+    }
+
     // What a call has reported is not the next one's error.
     const ff_segment seg = {address(1 << 20), 64, FF_F32, FF_KIND_RAW, 0, 0};
     for (hipError_t e : {hipErrorOutOfMemory, hipErrorInvalidValue}) {

@@ -837,3 +837,23 @@ def test_policy_of_more_tokens_than_one_launch_has_work_items_for():
         assert torch.equal(want["used"], small[4] != 0)
         assert torch.allclose(token[part].cpu().double(), want["token_loss"], rtol=200 * U32, atol=0)
         assert torch.allclose(dz[part].cpu().double(), want["dlogits"], rtol=2.0 ** -7, atol=2.0 ** -126)
+
+
+@pytest.mark.parametrize("n", [2048, 2049, 4500, 10000])
+def test_norm_has_the_same_bits_wherever_its_addresses_come_from(n):
+    """Lists whose addresses fit a launch's arguments, and longer ones."""
+    rng = np.random.default_rng(n)
+    ts, _ = _tensors([(int(k), (BF16, F16, F32)[i % 3]) for i, k in enumerate(rng.integers(0, 3000, size=n))], n, 1.0, 1)
+    lst, stats, ws = _norm(ts, 10.0)
+    _check_norm(stats, ts, 10.0, 1.0)
+    first = stats.words.clone()
+    others = [t.clone() for t in ts]
+    for grads in (others, ts, None, others):
+        stats.words.fill_(-1.0)
+        ff.ff_grad_norm(lst, stats, ws, 10.0, grads=grads)
+        torch.cuda.synchronize()
+        assert torch.equal(stats.words.view(torch.int64), first.view(torch.int64))
+    others[n // 2] = torch.full_like(others[n // 2], 3.0)
+    ff.ff_grad_norm(lst, stats, ws, 10.0, grads=others)
+    torch.cuda.synchronize()
+    _check_norm(stats, others, 10.0, 1.0)
