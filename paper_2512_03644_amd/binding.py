@@ -8,6 +8,7 @@ import array
 import ctypes
 import os
 import struct
+from operator import index
 
 import torch
 
@@ -209,10 +210,10 @@ def make_segments(tensors, kinds=None, param_ids=None):
         words[1::4] = array.array("Q", sizes)
         dtypes = [_DTYPES[t.dtype] for t in tensors]
         if kinds is not None:
-            dtypes = [d | (kinds[i] & 0xFFFFFFFF) << 32 for i, d in enumerate(dtypes)]
+            dtypes = [d | (index(kinds[i]) & 0xFFFFFFFF) << 32 for i, d in enumerate(dtypes)]
         words[2::4] = array.array("Q", dtypes)
         if param_ids is not None:
-            words[3::4] = array.array("Q", [param_ids[i] & 0xFFFFFFFF for i in range(n)])
+            words[3::4] = array.array("Q", [index(param_ids[i]) & 0xFFFFFFFF for i in range(n)])
     return (ff_segment * max(n, 1)).from_buffer(words)
 
 

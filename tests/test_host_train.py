@@ -4,6 +4,7 @@ import ctypes
 import types
 import weakref
 
+import numpy as np
 import pytest
 import torch
 
@@ -237,3 +238,16 @@ def test_lists_refuse_tensors_of_impossible_sizes():
             s.dtype, s.nbytes, s.ptr = dtype, size, A16
         assert L.ff_grad_list_create(segs, len(sizes), HOST, ctypes.byref(out)) == ff.FF_ERR_INVALID, sizes
         assert out.value is None
+
+
+@pytest.mark.parametrize("kind", [int, np.uint8, np.int8, np.int32, np.uint32, np.int64, np.uint64, torch.tensor], ids=lambda k: k.__name__)
+def test_segments_take_kinds_and_groups_of_any_integer_type(kind):
+    """As they come out of an array: whatever has an index."""
+    ts = [torch.zeros(4), torch.zeros(3, dtype=torch.bfloat16), torch.zeros(2)]
+    kinds, ids = [1, 2, 4], [7, 0, 100]
+    segs = ff.make_segments(ts, [kind(k) for k in kinds], [kind(k) for k in ids])
+    assert [(s.dtype, s.kind, s.param_id, s.reserved) for s in segs] == [
+        (ff.FF_F32, 1, 7, 0), (ff.FF_BF16, 2, 0, 0), (ff.FF_F32, 4, 100, 0)]
+    if kind is not int:
+        with pytest.raises(TypeError):
+            ff.make_segments(ts, [1.0, 2.0, 3.0])
