@@ -155,9 +155,22 @@ struct Slot32 {
     }
     static __device__ __forceinline__ float one(Bytes p, uint32_t i) { return ((FF_GLOBAL float*)p)[i]; }
     static __device__ __forceinline__ void put(Bytes p, uint32_t i, float v) { ((FF_GLOBAL float*)p)[i] = v; }
-    static __device__ __forceinline__ bool set_factors(float* f, double factor, double total, float)
+    // A large factor's products with probabilities below 2^-126, or above 2^128 the factor itself, would be lost in 32 bits: there a lower
+    // maximum takes its exponent, and what rounding makes of that is in the factor.
+    static __device__ __forceinline__ bool set_factors(float* f, double factor, double total, float& m)
     {
-        f[0] = static_cast<float>(-factor / total);
+        double both = -factor / total;
+        if (fabs(both) > 0x1p64 && fabs(both) != INFINITY) {
+            int e;
+            const double part = 2.0 * frexp(fabs(both), &e);  // 1 to 2
+            const double wanted = static_cast<double>(m) - (log64(part) + 0x1.62e42fefa39efp-1 * (e - 1));
+            float lower = static_cast<float>(wanted);
+            if (static_cast<double>(lower) > wanted) lower = nextafterf(lower, -INFINITY);
+            both *= exp64(static_cast<double>(lower) - static_cast<double>(m));
+            both = copysign(fmax(fabs(both), 0x1p-126), both);  // (about 1, unless the maximum is beyond 2^20)
+            m = lower;
+        }
+        f[0] = static_cast<float>(both);
         f[1] = 0.f;
         return true;
     }
@@ -202,10 +215,13 @@ struct Slot16 {
         ((FF_GLOBAL uint16_t*)p)[i] = static_cast<uint16_t>(pair(v, 0.f));
     }
     // (the maximum as well joins the exponent, unless it is large)
-    static __device__ __forceinline__ bool set_factors(float* f, double factor, double total, float m)
+    static __device__ __forceinline__ bool set_factors(float* f, double factor, double total, float& m)
     {
         const bool large = fabsf(m) > 64.f;
-        f[0] = log2f(fabsf(static_cast<float>(factor))) - log2f(static_cast<float>(total));
+        int e = 0;
+        const bool over = fabs(factor) > 0x1.fffffep+127 && fabs(factor) != INFINITY;  // (its products with small probabilities are not)
+        const double part = over ? frexp(factor, &e) : factor;
+        f[0] = log2f(fabsf(static_cast<float>(part))) + static_cast<float>(e) - log2f(static_cast<float>(total));
         if (!large) f[0] = fmaf(-m, kLog2E, f[0]);
         f[1] = __uint_as_float(factor > 0 ? 0x80008000u : 0u);
         return large;

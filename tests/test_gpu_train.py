@@ -857,3 +857,34 @@ def test_norm_has_the_same_bits_wherever_its_addresses_come_from(n):
     ff.ff_grad_norm(lst, stats, ws, 10.0, grads=others)
     torch.cuda.synchronize()
     _check_norm(stats, others, 10.0, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("n,v", [(5, 1003), (5, 40003), (300, 16011)])
+@pytest.mark.parametrize("far", [60.0, 100.0, 200.0, 400.0])
+def test_policy_slopes_beyond_32_bits(n, v, dtype, far):
+    """A token that the policy had all but ruled out, or the reference had not: the slope passes the largest float, its products with small
+    probabilities do not, and what is ruled out stays without a gradient."""
+    rows, y, old, ref, adv, w = _policy_inputs(n, v, dtype, 17)
+    y[:2] = 3
+    rows[:2, v // 2:] = -INF
+    rows[:2, 5:v // 3] = torch.linspace(-300.0, 0.0, v // 3 - 5).to(dtype)
+    logp = rows.double().log_softmax(1).gather(1, y[:, None])[:, 0]
+    old[0], ref[0] = float(logp[0] - far), float(logp[0])  # a ratio of exp(far), and a loss
+    old[1], ref[1] = float(logp[1]), float(logp[1] + far)  # the KL term's slope
+    adv[:2] = -1.0
+    got = _run_policy(rows, v, y, old, adv, w, ref, 0.1)
+    want = trainref.policy(rows, y, old, adv, w, ref, 0.2, 0.3, 0.1)
+    g, x = got["dlogits"].double(), want["dlogits"]
+    assert not torch.isnan(g).any() and bool((g[:2, v // 2:] == 0).all())
+    # the slope follows the log-probability (v / 256 + 66 U32, and 4 U32 of what is added to it); the exponents of factor and distance
+    # (up to 600 and 300) in 24 bits, a few roundings each; then the result's own
+    fi = torch.finfo(dtype)
+    floor = fi.smallest_normal * fi.eps / 2 if dtype == F16 else 2.0 ** -126
+    err = x.abs() * (fi.eps / 2 + (v / 256 + 66 + 4 * far + 4 * 900) * U32) * 1.02 + floor
+    most = float(fi.max)
+    over = x.abs() > most * 1.01
+    assert bool((torch.isinf(g[over]) & (torch.sign(g[over]) == torch.sign(x[over]))).all())
+    close = (x.abs() < most * 0.99)
+    assert bool(((g - x).abs() <= err)[close].all())
+    assert far == 400 or int((close[:2] & (x[:2] != 0)).sum()) > 0
