@@ -78,7 +78,7 @@ def train(steps=30, half=torch.bfloat16, seed=0, report=print):
     ff.ff_policy_loss(scored, old_logp, token_loss, loss_stats, loss_space)
 
     losses, norms = [], []
-    for step in range(1, steps + 1):
+    for step in range(1, steps + 1):  # (iterations: one whose update is left out counts in the bias correction)
         hidden, logits = forward()
         batch = ff.policy_batch(logits, targets, old_logp, advantages, weights, old_logp, CLIP, CLIP, BETA, loss_scale)
         ff.ff_policy_loss(batch, logp, token_loss, loss_stats, loss_space, dlogits=logits)

@@ -362,7 +362,9 @@ int ff_grad_clip(const ff_grad_list *list, const void *const *grads, const ff_gr
  * ff_adam_step_snapshot_f16, with g = float(grad) * stats->scale (one rounded fp32 multiplication, the
  * loss scale included); prev_chunks: NULL, or the previous snapshot as for ff_adam_step_chained.  If stats->skip is
  * set the update is left out: master, m and v keep their bits, the 16-bit weights are rounded from
- * the master (a NaN to the format's canonical one), and the snapshot holds that state.  stats: DEVICE, read when the
+ * the master (a NaN to the format's canonical one), and the snapshot holds that state.  hp->step is the caller's: a step that
+ * was left out counts in the next one's bias correction if the caller counts it, and does not if the caller, who has
+ * looked at stats->skip, hands the same step in again.  stats: DEVICE, read when the
  * stream gets there.  Gradients, hp, chunks, crcs and errors as for those steps.
  */
 int ff_adam_step_clipped(const ff_plan *plan, const void *const *grads, const ff_adam_hparams *hp,
@@ -419,8 +421,9 @@ uint64_t ff_policy_workspace_bytes(uint64_t n_tokens, uint64_t vocab);
  * logp, token_loss: DEVICE fp32[n_tokens], apart from each other and from every input.  dlogits: NULL (no gradient), or DEVICE, of `dtype`, rows grad_stride >= vocab elements apart; it may
  * be the logits themselves with the same stride, and elements between rows are not touched.
  * stats: DEVICE.  workspace: DEVICE, 16-byte aligned, ff_policy_workspace_bytes(), ZERO before its
- * first use; every call leaves it as the next one needs it.
- * n_tokens = 0 is allowed: the stats become zero.  FF_ERR_INVALID for vocab 0 or above 2^31 - 1.
+ * first use; every call leaves it as the next one needs it.  Calls that are in flight at once need outputs, stats and workspaces of
+ * their own.
+ * n_tokens = 0 is allowed: the stats become zero.  FF_ERR_INVALID for vocab 0, and for vocab or n_tokens above 2^31 - 1.
  */
 int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss, void *dlogits,
                    uint64_t grad_stride, ff_policy_stats *stats, void *workspace, void *hip_stream);

@@ -1,6 +1,6 @@
 // Gradient norm and clipping for gfx950.
 //
-// The norm is one pass over all gradients, which bounds it: 6.8 TB/s on 1.7 and 3.2 GB (249 and 472 us; the pass of a restore that only
+// The norm is one pass over all gradients, which bounds it: 6.8 and 7.0 TB/s on 1.7 and 3.2 GB (247 and 461 us; the pass of a restore that only
 // reads reaches 7.0 on 12 GB).  A wavefront takes items of 8 KiB of one tensor (grads.hpp), lane l of a row of 1 KiB taking 16 bytes.
 // Every element is squared and summed in 64 bits: squares of 16- and 32-bit floats are exact there and cannot overflow, so
 // no finite gradient needs a second look.  An item's sum that is not finite tells that the item holds an infinity or NaN; only then are

@@ -8,11 +8,12 @@
 // joined, always in the same order, by the last workgroups to be done (count_and_finish).
 //
 // What bounds it: memory, or for few tokens the launch and the chain from a row's load to its store.  A workgroup's loads do not overlap its
-// stores, so what counts is how many rows a compute unit has at once (choose): with one row of 128,256 bf16 logits to a unit 4096 of them took
-// 427 us, with two, parts of which are in LDS, 393; a copy of their bytes takes 330.  The arithmetic of a row, two exponentials and some ten
-// other operations a logit, would fill half of that time by itself.  Rows kept over in a loop of workgroups, the next one's loads
-// under way while the gradient is stored, took 500.  Us, gradient and all, 4096 tokens on 1000 / 4000 / 8000 / 16,000 / 32,000 / 64,000 /
-// 128,256 bf16 logits 12.3 / 22 / 31 / 53 / 94 / 192 / 391 (all tokens count); 1.05 GB of logits without gradient 170 (6.2 TB/s).
+// stores, so what counts is how many rows a compute unit has at once (choose).  The arithmetic of a row, two exponentials and some ten
+// other operations a logit, would fill half of the longest rows' time by itself.  Rows kept over in a loop of workgroups, the next one's loads
+// under way while the gradient is stored, took a third more.  Us, gradient and all, 4096 tokens on 1000 / 4000 / 8000 / 16,000 / 32,000 /
+// 64,000 / 128,256 bf16 logits 13.5 / 23.7 / 31.9 / 54.1 / 94.7 / 191 / 371 (all tokens count; a copy of the last one's bytes takes 330), fp16
+// 13.2 / 22.9 / 31.7 / 54.7 / 95.0 / 192 / 372, fp32 13.2 / 28.3 / 49.7 / 89.6 / 186 / 370 / 829; 1.05 GB of bf16 logits without gradient 170 (6.2 TB/s).
+// Machines differ by 5 %: of figures elsewhere in this file, those that stand beside each other are of one.
 #include "policy.hpp"
 
 #include <hip/hip_fp16.h>
@@ -61,7 +62,7 @@ __device__ __forceinline__ double log64(double x)
 // A term is 2^(z log2(e) - c), c = m log2(e) in 24 bits, in one rounded operation in front of the exponential: c's rounding is
 // the same for all terms, and known.  What log2(e) loses in 24 bits is taken as that of m, which is out by 1.3e-8 (m - z)
 // of a term; a thread's own maximum is not far above what counts in its sum: log-probabilities of long rows are out by 1-2e-8.  (log2(e) to 48 bits, (z - m)
-// first, is three operations for no better: 412 us where this takes 394.)  Where m is so large that c would be out by
+// first, is three operations for no better: 5 % slower on long rows.)  Where m is so large that c would be out by
 // more than a few, z - m takes the place of z.
 struct Running {
     float m = -INFINITY, c = 0.f, b0 = 0.f;
@@ -736,6 +737,9 @@ struct Choice {
 // Other splits, us: 4096 rows of 2000 slots by 256 / 512 / 1024 threads 63 / 56 / 60; of 8000 by 512 threads with 16, by 1024 with 8, with 4 of 8
 // slots held 195 / 222 / 217; 1024 fp32 rows of 32,500 by 1024 threads with 16 / 8 / 4 held 247 / 281 / 278.  Few rows take 1024 threads where
 // many would take 512.  Without a gradient nothing is held, and four slots are on their way.
+// As a row is one workgroup's, 65 / 100 / 150 / 200 / 300 rows fill part of the chip, or two rows some units: of 32,000 bf16 logits 11.5 / 11.9 / 12.0 /
+// 12.5 / 15.5 us, of 50,021 16.6 / 16.9 / 17.2 / 17.2 / 24.7, of 128,256 22.5 / 23.1 / 23.5 / 26.8 / 40.6 (fp16 within 3 %; fp32 31 / 35 / 39 / 47 / 82,
+// half of a row read twice); without a gradient, of 128,256, 16.8 / 16.8 / 17.2 / 18.0 / 26.9.
 template <uint32_t DTYPE>
 Choice choose(uint64_t slots, uint64_t rows, bool grad)
 {
