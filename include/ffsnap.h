@@ -428,6 +428,99 @@ uint64_t ff_policy_workspace_bytes(uint64_t n_tokens, uint64_t vocab);
 int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss, void *dlogits,
                    uint64_t grad_stride, ff_policy_stats *stats, void *workspace, void *hip_stream);
 
+/* ---- the two ends of a model: embedding, layer norm, head with cross entropy -------------------- */
+
+/*
+ * Embedding: out[t] = scale * table[ids[t]], one fp32 product rounded to the format.  table: DEVICE, vocab rows of `width` elements of
+ * dtype (FF_BF16, FF_F16 or FF_F32), table_stride >= width elements apart; ids: DEVICE int64; out: DEVICE, n_tokens rows,
+ * out_stride >= width apart.  All aligned to their elements.  An id outside [0, vocab), padding, gives a row of zeros.  n_tokens 0:
+ * nothing.  Limits: vocab, n_tokens < 2^31, width <= FF_EMBED_MAX_WIDTH.
+ */
+#define FF_EMBED_MAX_WIDTH (1u << 24)
+int ff_embed(const void *table, uint64_t vocab, uint64_t width, uint64_t table_stride, uint32_t dtype,
+             const int64_t *ids, uint64_t n_tokens, float scale, void *out, uint64_t out_stride,
+             void *hip_stream);
+
+/*
+ * Its gradient: dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] == v), in fp32 and in the tokens' order, whatever else
+ * runs, rounded once.  Every row is written, those without tokens with zeros.  With FF_GRAD_ADD the sum is added to
+ * what is there (a table that is the head's too has the head's gradient there), and rows without tokens are neither read nor
+ * written.  Ids outside the vocabulary count nowhere.  workspace: DEVICE, 16-byte aligned, ff_embed_workspace_bytes(), which never
+ * falls with any argument; its content does not matter.
+ */
+#define FF_GRAD_ADD 1u
+uint64_t ff_embed_workspace_bytes(uint64_t n_tokens, uint64_t vocab, uint64_t width);
+int ff_embed_grad(const void *dout, uint64_t dout_stride, uint32_t dtype, const int64_t *ids,
+                  uint64_t n_tokens, uint64_t vocab, uint64_t width, float scale, void *dtable,
+                  uint64_t dtable_stride, uint32_t flags, void *workspace, void *hip_stream);
+
+/*
+ * Layer norm of n_rows rows of `width` elements: y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(variance + eps), the variance
+ * that of the row itself; all in fp32, y rounded once.  x, weight, bias (or NULL), y: DEVICE, of one dtype (FF_BF16, FF_F16 or FF_F32),
+ * aligned to it; y may be x.  mean, rstd: DEVICE, n_rows each, what the gradient is given; or NULL.  n_rows < 2^31.
+ */
+#define FF_NORM_MAX_WIDTH 16384u
+int ff_layer_norm(const void *x, uint64_t n_rows, uint64_t width, uint64_t x_stride, uint32_t dtype,
+                  const void *weight, const void *bias, float eps, void *y, uint64_t y_stride,
+                  float *mean, float *rstd, void *hip_stream);
+
+/*
+ * Its gradients from dy, that of y: dx (may be dy, or x), and, unless NULL, dweight and dbias, sums over all rows in an
+ * order that n_rows and width give; in fp32, each rounded once to dtype.  mean, rstd: the forward pass's.  workspace: DEVICE, 16-byte
+ * aligned, ff_layer_norm_workspace_bytes() bytes (0 for a width that is refused), which never falls with n_rows; its content does not
+ * matter.  It may be NULL if neither dweight nor dbias is wanted.
+ */
+uint64_t ff_layer_norm_workspace_bytes(uint64_t n_rows, uint64_t width);
+int ff_layer_norm_grad(const void *x, uint64_t n_rows, uint64_t width, uint64_t x_stride,
+                       uint32_t dtype, const void *weight, const float *mean, const float *rstd,
+                       const void *dy, uint64_t dy_stride, void *dx, uint64_t dx_stride,
+                       void *dweight, void *dbias, void *workspace, void *hip_stream);
+
+/*
+ * Head: the cross entropy of targets over a vocabulary, from the hidden states, without logits in memory.  hidden: n_tokens rows of `width`
+ * elements of dtype (FF_BF16 or FF_F16), hidden_stride >= width elements apart; weight: vocab such rows.  All arrays DEVICE and
+ * aligned to their elements; rows of `weight` that are 16-byte aligned, of a width that is a multiple of 8, are read where they lie,
+ * others are copied piece by piece first.  targets int64; weights fp32: what a token counts in the loss, its share of the mean included; 0
+ * leaves it out (prompts, padding): its row is not read.
+ */
+typedef struct {
+    const void *hidden, *weight;
+    uint64_t n_tokens, vocab, width, hidden_stride, weight_stride;
+    uint32_t dtype;
+    uint32_t reserved; /* must be 0 */
+    const int64_t *targets;
+    const float *weights;
+    float loss_scale;  /* finite, > 0: the gradients are those of loss * loss_scale */
+    uint32_t reserved2; /* ignored */
+} ff_head_batch;
+
+/* DEVICE, 8-byte aligned */
+typedef struct {
+    float loss;         /* sum of -weight * log-probability                            */
+    uint32_t reserved;  /* 0                                                           */
+    uint64_t n_tokens;  /* that count                                                  */
+    uint64_t n_invalid; /* weight not 0 and yet left out: target outside the vocabulary */
+} ff_head_stats;
+
+/* What ff_head_loss is given; gradient: whether either is wanted.  0 for a batch that is refused.  About 0.5 GB at the most and what the tokens
+ * need: 8 bytes for every token and 256 entries of the vocabulary, 2 to 6 for every element of the hidden states. */
+#define FF_HEAD_MAX_TOKENS (1u << 22)
+#define FF_HEAD_MAX_WIDTH 65536u
+uint64_t ff_head_workspace_bytes(const ff_head_batch *b, uint32_t gradient);
+
+/*
+ * logits z = hidden . weight^T, log-probability logp[t] = z[t][target] - log(sum of exp(z[t])), 0 for a token that is left out.
+ * Logits are sums of exact products in fp32; logp is rounded once from what is known of it.
+ * dhidden, dweight: DEVICE, either may be NULL; rows of `width` elements of dtype, their strides apart: with g[t][v] = weights[t] * loss_scale *
+ * (softmax(z[t])[v] - [v is the target]), rounded to dtype relative to the largest weight, dhidden = g . weight (rows of zeros for
+ * tokens that are left out) and dweight = g^T . hidden, summed in fp32 in an order that the sizes give and rounded once.
+ * dhidden may be hidden (of the same stride).  Without either, scoring: one product in place of four.
+ * workspace: DEVICE, 256-byte aligned, ff_head_workspace_bytes() bytes; its content does not matter.
+ */
+int ff_head_loss(const ff_head_batch *b, float *logp, void *dhidden, uint64_t dhidden_stride,
+                 void *dweight, uint64_t dweight_stride, ff_head_stats *stats, void *workspace,
+                 void *hip_stream);
+
 /* Test helper: CRC32C of nbytes at dev_buf (DEVICE, 16-byte aligned) into *dev_out (DEVICE),
  * computed by the same tile and combine kernels as ff_pack.  Allocates and frees a small
  * scratch array, so it synchronises the stream before returning. */

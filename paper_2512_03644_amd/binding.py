@@ -49,7 +49,12 @@ EXPORTS = ["ff_snapshot_plan", "ff_plan_destroy", "ff_plan_payload_bytes", "ff_p
            "ff_copy_ceiling", "ff_mix_ceiling", "ff_strerror",
            "ff_grad_list_create", "ff_grad_list_destroy", "ff_grad_list_numel",
            "ff_grad_list_workspace_bytes", "ff_grad_norm", "ff_grad_norm_join", "ff_grad_clip",
-           "ff_adam_step_clipped", "ff_policy_workspace_bytes", "ff_policy_loss"]
+           "ff_adam_step_clipped", "ff_policy_workspace_bytes", "ff_policy_loss",
+           "ff_embed", "ff_embed_workspace_bytes", "ff_embed_grad", "ff_layer_norm",
+           "ff_layer_norm_workspace_bytes", "ff_layer_norm_grad", "ff_head_workspace_bytes", "ff_head_loss"]
+
+FF_GRAD_ADD = 1
+FF_EMBED_MAX_WIDTH, FF_NORM_MAX_WIDTH, FF_HEAD_MAX_WIDTH, FF_HEAD_MAX_TOKENS = 1 << 24, 16384, 65536, 1 << 22
 
 
 class ff_segment(ctypes.Structure):
@@ -75,6 +80,16 @@ class ff_policy_batch(ctypes.Structure):
                 ("weights", ctypes.c_void_p), ("clip_low", ctypes.c_float),
                 ("clip_high", ctypes.c_float), ("beta", ctypes.c_float),
                 ("loss_scale", ctypes.c_float)]
+
+
+class ff_head_batch(ctypes.Structure):
+    tensors = ()  # those that it points at (head_batch), kept alive
+
+    _fields_ = [("hidden", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
+                ("vocab", ctypes.c_uint64), ("width", ctypes.c_uint64), ("hidden_stride", ctypes.c_uint64),
+                ("weight_stride", ctypes.c_uint64), ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
+                ("targets", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("loss_scale", ctypes.c_float),
+                ("reserved2", ctypes.c_uint32)]
 
 
 class ff_razor_config(ctypes.Structure):
@@ -161,6 +176,21 @@ def lib():
         L.ff_policy_workspace_bytes.restype, L.ff_policy_workspace_bytes.argtypes = u64, [u64, u64]
         L.ff_policy_loss.restype = i32
         L.ff_policy_loss.argtypes = [ctypes.POINTER(ff_policy_batch), vp, vp, vp, u64, vp, vp, vp]
+        f32 = ctypes.c_float
+        L.ff_embed.restype = i32
+        L.ff_embed.argtypes = [vp, u64, u64, u64, u32, vp, u64, f32, vp, u64, vp]
+        L.ff_embed_workspace_bytes.restype, L.ff_embed_workspace_bytes.argtypes = u64, [u64, u64, u64]
+        L.ff_embed_grad.restype = i32
+        L.ff_embed_grad.argtypes = [vp, u64, u32, vp, u64, u64, u64, f32, vp, u64, u32, vp, vp]
+        L.ff_layer_norm.restype = i32
+        L.ff_layer_norm.argtypes = [vp, u64, u64, u64, u32, vp, vp, f32, vp, u64, vp, vp, vp]
+        L.ff_layer_norm_workspace_bytes.restype, L.ff_layer_norm_workspace_bytes.argtypes = u64, [u64, u64]
+        L.ff_layer_norm_grad.restype = i32
+        L.ff_layer_norm_grad.argtypes = [vp, u64, u64, u64, u32, vp, vp, vp, vp, u64, vp, u64, vp, vp, vp, vp]
+        L.ff_head_workspace_bytes.restype = u64
+        L.ff_head_workspace_bytes.argtypes = [ctypes.POINTER(ff_head_batch), u32]
+        L.ff_head_loss.restype = i32
+        L.ff_head_loss.argtypes = [ctypes.POINTER(ff_head_batch), vp, vp, u64, vp, u64, vp, vp, vp]
         L.ff_strerror.restype, L.ff_strerror.argtypes = ctypes.c_char_p, [i32]
         _lib = L
     return _lib
@@ -557,3 +587,137 @@ def ff_policy_loss(batch, logp, token_loss, stats, workspace, dlogits=None, stre
         raise ValueError("the workspace is smaller than ff_policy_workspace_bytes()")
     _check(lib().ff_policy_loss(ctypes.byref(batch), logp.data_ptr(), token_loss.data_ptr(), grad,
                                 stride, stats.data_ptr(), workspace.data_ptr(), _stream_ptr(stream)))
+
+
+# ---- the two ends of a model ----------------------------------------------------------------------
+
+def _rows(t, name, shape, dtype):
+    """Elements between a matrix's rows; the rows themselves are contiguous."""
+    if t.dim() != 2 or t.dtype is not dtype or tuple(t.shape) != shape:
+        raise ValueError("%s is a tensor %s of %s" % (name, shape, dtype))
+    stride, inner = t.stride()
+    if inner != 1 and shape[1] != 1:
+        raise ValueError("%s are rows of contiguous elements" % name)
+    return stride if shape[0] > 1 else max(stride, shape[1])
+
+
+def _vector(t, name, n, dtype):
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError("%s is a contiguous tensor of %d entries of %s" % (name, n, dtype))
+    return t.data_ptr()
+
+
+def _optional(t, name, n, dtype):
+    return None if t is None else _vector(t, name, n, dtype)
+
+
+def _matrix(t, name):
+    if t.dim() != 2:
+        raise ValueError("%s is a matrix" % name)
+    return t.shape
+
+
+def ff_embed(table, ids, out, scale=1.0, stream=None):
+    """out[t] = scale * table[ids[t]]; table [vocab, width] of bf16, fp16 or fp32, ids int64 [tokens], out [tokens, width] in
+    the table's format.  Rows may lie apart.  An id outside the table (padding) gives a row of zeros."""
+    vocab, width = _matrix(table, "table")
+    n, dtype = ids.numel(), table.dtype
+    _check(lib().ff_embed(table.data_ptr(), vocab, width, _rows(table, "table", (vocab, width), dtype), _DTYPES[dtype],
+                          _vector(ids, "ids", n, torch.int64), n, scale, out.data_ptr(), _rows(out, "out", (n, width), dtype),
+                          _stream_ptr(stream)))
+
+
+def alloc_embed_workspace(n_tokens, vocab, width, device):
+    return torch.empty(int(lib().ff_embed_workspace_bytes(n_tokens, vocab, width)), dtype=torch.uint8, device=device)
+
+
+def ff_embed_grad(dout, ids, dtable, workspace, scale=1.0, add=False, stream=None):
+    """dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] == v); add: added to what is there, rows that no
+    token asks for left alone."""
+    vocab, width = _matrix(dtable, "dtable")
+    n, dtype = ids.numel(), dtable.dtype
+    if workspace.nbytes < lib().ff_embed_workspace_bytes(n, vocab, width):
+        raise ValueError("the workspace is smaller than ff_embed_workspace_bytes()")
+    _check(lib().ff_embed_grad(dout.data_ptr(), _rows(dout, "dout", (n, width), dtype), _DTYPES[dtype],
+                               _vector(ids, "ids", n, torch.int64), n, vocab, width, scale, dtable.data_ptr(),
+                               _rows(dtable, "dtable", (vocab, width), dtype), FF_GRAD_ADD if add else 0, workspace.data_ptr(),
+                               _stream_ptr(stream)))
+
+
+def ff_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, stream=None):
+    """y = (x - mean) * rstd * weight + bias over the rows of x [rows, width]; bias may be None; y may be x.  mean, rstd: fp32
+    [rows], for the gradient, or None."""
+    n, width = _matrix(x, "x")
+    dtype, f32 = x.dtype, torch.float32
+    _check(lib().ff_layer_norm(x.data_ptr(), n, width, _rows(x, "x", (n, width), dtype), _DTYPES[dtype],
+                               _vector(weight, "weight", width, dtype), _optional(bias, "bias", width, dtype), eps, y.data_ptr(),
+                               _rows(y, "y", (n, width), dtype), _optional(mean, "mean", n, f32), _optional(rstd, "rstd", n, f32),
+                               _stream_ptr(stream)))
+
+
+def alloc_norm_workspace(n_rows, width, device):
+    return torch.empty(int(lib().ff_layer_norm_workspace_bytes(n_rows, width)), dtype=torch.uint8, device=device)
+
+
+def ff_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight=None, dbias=None, workspace=None, stream=None):
+    """Gradients of ff_layer_norm from dy; dx may be dy or x; dweight and dbias [width], or None."""
+    n, width = _matrix(x, "x")
+    dtype, f32 = x.dtype, torch.float32
+    if dweight is not None or dbias is not None:
+        if workspace is None or workspace.nbytes < lib().ff_layer_norm_workspace_bytes(n, width):
+            raise ValueError("the workspace is smaller than ff_layer_norm_workspace_bytes()")
+    _check(lib().ff_layer_norm_grad(
+        x.data_ptr(), n, width, _rows(x, "x", (n, width), dtype), _DTYPES[dtype], _vector(weight, "weight", width, dtype),
+        _vector(mean, "mean", n, f32), _vector(rstd, "rstd", n, f32), dy.data_ptr(), _rows(dy, "dy", (n, width), dtype),
+        dx.data_ptr(), _rows(dx, "dx", (n, width), dtype), _optional(dweight, "dweight", width, dtype),
+        _optional(dbias, "dbias", width, dtype), None if workspace is None else workspace.data_ptr(), _stream_ptr(stream)))
+
+
+class HeadStats:
+    """Device memory for an ff_head_stats, and views of its fields (see GradStats)."""
+
+    def __init__(self, device):
+        self.words = torch.zeros(3, dtype=torch.int64, device=device)
+        self.loss = self.words.view(torch.float32)[0]
+        self.n_tokens, self.n_invalid = self.words[1], self.words[2]
+
+    def data_ptr(self):
+        return self.words.data_ptr()
+
+
+_HEAD = struct.Struct("7Q2I2QfI")
+
+
+def head_batch(hidden, weight, targets, weights, loss_scale=1.0):
+    """ff_head_batch of device tensors: hidden [tokens, width], weight [vocab, width] (bf16 or fp16, rows may lie apart), targets
+    int64 and weights fp32 [tokens].  It keeps the tensors alive (see policy_batch)."""
+    n, width = _matrix(hidden, "hidden")
+    vocab, dtype = _matrix(weight, "weight")[0], hidden.dtype
+    batch = ff_head_batch.from_buffer_copy(_HEAD.pack(
+        hidden.data_ptr(), weight.data_ptr(), n, vocab, width, _rows(hidden, "hidden", (n, width), dtype),
+        _rows(weight, "weight", (vocab, width), dtype), _DTYPES[dtype], 0, _vector(targets, "targets", n, torch.int64),
+        _vector(weights, "weights", n, torch.float32), loss_scale, 0))
+    batch.tensors = (hidden, weight, targets, weights)
+    return batch
+
+
+def alloc_head_workspace(batch, device, grad=True):
+    """For this batch, with or without gradients."""
+    return torch.empty(max(16, int(lib().ff_head_workspace_bytes(ctypes.byref(batch), 1 if grad else 0))), dtype=torch.uint8,
+                       device=device)
+
+
+def ff_head_loss(batch, logp, stats, workspace, dhidden=None, dweight=None, stream=None):
+    """Cross entropy of the batch's targets: log-probabilities into logp [tokens], the loss into stats (HeadStats); dhidden
+    [tokens, width] (may be the hidden states), dweight [vocab, width], or None."""
+    n, width, vocab, dtype = batch.n_tokens, batch.width, batch.vocab, batch.tensors[0].dtype
+    grad = dhidden is not None or dweight is not None
+    dh = dw = (None, 0)
+    if dhidden is not None:
+        dh = dhidden.data_ptr(), _rows(dhidden, "dhidden", (n, width), dtype)
+    if dweight is not None:
+        dw = dweight.data_ptr(), _rows(dweight, "dweight", (vocab, width), dtype)
+    if workspace.nbytes < lib().ff_head_workspace_bytes(ctypes.byref(batch), 1 if grad else 0):
+        raise ValueError("the workspace is smaller than ff_head_workspace_bytes()")
+    _check(lib().ff_head_loss(ctypes.byref(batch), _vector(logp, "logp", n, torch.float32), *dh, *dw, stats.data_ptr(),
+                              workspace.data_ptr(), _stream_ptr(stream)))

@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libffsnap.so")
 SOURCES = ["api.hip", "kernels.hip", "blocks.hip", "fused.hip", "grads.hip", "policy.hip",
-           "train_api.hip", "layout.cpp"]
+           "train_api.hip", "embed.hip", "norm.hip", "head.hip", "model_api.hip", "layout.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Wno-align-mismatch",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

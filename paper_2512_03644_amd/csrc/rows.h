@@ -1,0 +1,89 @@
+// Rows of 16- and 32-bit floats, eight elements to a lane: at any element's address, and with any number of elements.
+#pragma once
+#include "fold.h"
+#include "../../include/ffsnap.h"
+
+namespace ffsnap {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8v __attribute__((ext_vector_type(8)));
+
+constexpr int kLaneItems = 8;
+
+template <uint32_t DTYPE>
+struct Items {
+    static constexpr uint32_t kBytes = DTYPE == FF_F32 ? 4 : 2;
+
+    static __device__ __forceinline__ float one(const uint8_t* p)
+    {
+        if constexpr (DTYPE == FF_F32) return *(const FF_GLOBAL float*)p;
+        else if constexpr (DTYPE == FF_BF16) return __builtin_bit_cast(float, static_cast<uint32_t>(*(const FF_GLOBAL uint16_t*)p) << 16);
+        else return static_cast<float>(*(const FF_GLOBAL _Float16*)p);
+    }
+    static __device__ __forceinline__ void put(uint8_t* p, float v)
+    {
+        if constexpr (DTYPE == FF_F32) *(FF_GLOBAL float*)p = v;
+        else if constexpr (DTYPE == FF_BF16) *(FF_GLOBAL __bf16*)p = static_cast<__bf16>(v);
+        else *(FF_GLOBAL _Float16*)p = static_cast<_Float16>(v);
+    }
+    // What eight elements lie in memory as: values are held like this until they are used.
+    struct Held {
+        u32x4 w[kBytes / 2];
+    };
+    static __device__ __forceinline__ Held load8(const uint8_t* p)
+    {
+        Held h;
+        for (uint32_t i = 0; i < kBytes / 2; i++) h.w[i] = ((const FF_GLOBAL u32x4_a2*)p)[i];
+        return h;
+    }
+    static __device__ __forceinline__ f32x8 wide(const Held& h)
+    {
+        f32x8 v;
+        if constexpr (DTYPE == FF_F32) {
+            v = __builtin_bit_cast(f32x8, h);
+        } else if constexpr (DTYPE == FF_BF16) {
+            for (int i = 0; i < 8; i++) {
+                const uint32_t both = h.w[0][i / 2];
+                v[i] = __builtin_bit_cast(float, i % 2 ? both & 0xFFFF0000u : both << 16);
+            }
+        } else {
+            v = __builtin_convertvector(__builtin_bit_cast(f16x8v, h.w[0]), f32x8);
+        }
+        return v;
+    }
+    static __device__ __forceinline__ Held narrow(f32x8 v)
+    {
+        Held h;
+        if constexpr (DTYPE == FF_F32) {
+            h = __builtin_bit_cast(Held, v);
+        } else if constexpr (DTYPE == FF_BF16) {
+            h.w[0] = __builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8v));
+        } else {
+            h.w[0] = __builtin_bit_cast(u32x4, __builtin_convertvector(v, f16x8v));
+        }
+        return h;
+    }
+    // Elements [at, at + 8) of a row of `width`, at < width; those behind it are zeros.
+    static __device__ __forceinline__ Held load(const uint8_t* row, uint32_t at, uint32_t width)
+    {
+        const uint8_t* const p = row + static_cast<uint64_t>(at) * kBytes;
+        if (at + kLaneItems <= width) return load8(p);
+        f32x8 v;
+        for (uint32_t i = 0; i < kLaneItems; i++) v[i] = at + i < width ? one(p + i * kBytes) : 0.f;
+        return narrow(v);
+    }
+    static __device__ __forceinline__ void store(uint8_t* row, uint32_t at, uint32_t width, const Held& h)
+    {
+        uint8_t* const p = row + static_cast<uint64_t>(at) * kBytes;
+        if (at + kLaneItems <= width) {
+            for (uint32_t i = 0; i < kBytes / 2; i++) ((FF_GLOBAL u32x4_a2*)p)[i] = h.w[i];
+            return;
+        }
+        const f32x8 v = wide(h);
+        for (uint32_t i = 0; i < kLaneItems; i++)
+            if (at + i < width) put(p + i * kBytes, v[i]);
+    }
+};
+
+}  // namespace ffsnap

@@ -1,0 +1,228 @@
+"""CPU-only checks of the operators at a model's two ends: what they refuse, the sizes they report, and the plain forms that
+the GPU tests hold them to, against differences and closed forms."""
+import ctypes
+import math
+import types
+import weakref
+
+import pytest
+import torch
+
+import modelref
+from paper_2512_03644_amd import binding as ff
+
+INF, NAN = float("inf"), float("nan")
+A16 = 1 << 20  # an address that is aligned to everything and never used
+BIG = 1 << 31
+NOWHERE = types.SimpleNamespace(cuda_stream=0)  # calls that get so far fail without a device
+
+
+def test_embedding_refuses_bad_arguments():
+    L = ff.lib()
+
+    def look(table=A16, vocab=10, width=8, stride=8, dtype=ff.FF_BF16, ids=A16, n=4, scale=1.0, out=A16, out_stride=8):
+        return L.ff_embed(table, vocab, width, stride, dtype, ids, n, scale, out, out_stride, None)
+
+    def grad(dout=A16, stride=8, dtype=ff.FF_BF16, ids=A16, n=4, vocab=10, width=8, scale=1.0, dtable=A16, out_stride=8, flags=0, ws=A16):
+        return L.ff_embed_grad(dout, stride, dtype, ids, n, vocab, width, scale, dtable, out_stride, flags, ws, None)
+
+    for f, names in ((look, ("table", "ids", "out")), (grad, ("dout", "ids", "dtable", "ws"))):
+        for name in names:
+            assert f(**{name: None}) == ff.FF_ERR_NULL, name
+        for bad in (dict(dtype=0), dict(dtype=4), dict(vocab=0), dict(vocab=BIG), dict(width=0), dict(width=ff.FF_EMBED_MAX_WIDTH + 1, stride=1 << 30, out_stride=1 << 30),
+                    dict(n=BIG), dict(stride=7), dict(out_stride=7), dict(stride=(1 << 40) + 1), dict(out_stride=1 << 60), dict(scale=INF), dict(scale=NAN),
+                    {names[0]: A16 + 1}, {names[1]: A16 + 4}, {names[2]: A16 + 1}, {names[0]: A16 + 2, "dtype": ff.FF_F32}, {names[2]: A16 + 2, "dtype": ff.FF_F32}):
+            assert f(**bad) == ff.FF_ERR_INVALID, bad
+    assert grad(flags=2) == grad(ws=A16 + 8) == ff.FF_ERR_INVALID
+    assert look(table=None, ids=None, out=None, n=0) == ff.FF_OK  # nothing to do
+    assert grad(dout=None, ids=None, dtable=None, n=0, flags=ff.FF_GRAD_ADD) == ff.FF_OK
+    assert grad(dout=None, ids=None, dtable=None, n=0) == ff.FF_ERR_NULL  # rows of zeros are wanted
+
+
+def test_layer_norm_refuses_bad_arguments():
+    L = ff.lib()
+
+    def norm(x=A16, n=4, width=8, stride=8, dtype=ff.FF_BF16, weight=A16, bias=A16, eps=1e-5, out=2 * A16, out_stride=8, mean=A16, rstd=A16):
+        return L.ff_layer_norm(x, n, width, stride, dtype, weight, bias, eps, out, out_stride, mean, rstd, None)
+
+    def grad(x=A16, n=4, width=8, stride=8, dtype=ff.FF_BF16, weight=A16, mean=A16, rstd=A16, dy=3 * A16, dy_stride=8, out=2 * A16, out_stride=8, dw=A16, db=A16,
+             ws=A16):
+        return L.ff_layer_norm_grad(x, n, width, stride, dtype, weight, mean, rstd, dy, dy_stride, out, out_stride, dw, db, ws, None)
+
+    for name in ("x", "weight", "out"):
+        assert norm(**{name: None}) == grad(**{name: None}) == ff.FF_ERR_NULL, name
+    for name in ("mean", "rstd", "dy", "ws"):
+        assert grad(**{name: None}) == ff.FF_ERR_NULL, name
+    wide = ff.FF_NORM_MAX_WIDTH + 1
+    for bad in (dict(dtype=0), dict(dtype=9), dict(width=0), dict(width=wide, stride=wide, out_stride=wide), dict(n=BIG), dict(stride=7), dict(out_stride=7),
+                dict(stride=1 << 60), dict(x=A16 + 1), dict(weight=A16 + 1), dict(out=A16 + 1), dict(mean=A16 + 2), dict(rstd=A16 + 1),
+                dict(x=A16 + 2, dtype=ff.FF_F32)):
+        assert norm(**bad) == ff.FF_ERR_INVALID, bad
+        if "width" not in bad or bad["width"]:
+            assert grad(**dict(bad, **({"dy_stride": wide} if bad.get("width") else {}))) == ff.FF_ERR_INVALID, bad
+    for bad in (dict(eps=-1e-5), dict(eps=NAN), dict(eps=INF), dict(bias=A16 + 1), dict(out=A16, out_stride=16)):
+        assert norm(**bad) == ff.FF_ERR_INVALID, bad
+    for bad in (dict(dy_stride=7), dict(dy=A16 + 1), dict(dw=A16 + 1), dict(db=A16 + 1), dict(ws=A16 + 8), dict(out=3 * A16, out_stride=16),
+                dict(out=A16, out_stride=16)):
+        assert grad(**bad) == ff.FF_ERR_INVALID, bad
+    assert norm(x=None, out=None, n=0, mean=None, rstd=None) == ff.FF_OK
+
+
+def _batch(**change):
+    b = ff.ff_head_batch(A16, A16, 4, 100, 64, 64, 64, ff.FF_BF16, 0, A16, A16, 1.0, 0)
+    for k, v in change.items():
+        setattr(b, k, v)
+    return b
+
+
+def test_head_refuses_bad_arguments():
+    L = ff.lib()
+
+    def loss(batch, logp=A16, dh=None, dh_stride=0, dw=None, dw_stride=0, stats=A16, ws=A16):
+        return L.ff_head_loss(ctypes.byref(batch), logp, dh, dh_stride, dw, dw_stride, stats, ws, None)
+
+    for name in ("hidden", "weight", "targets", "weights"):
+        assert loss(_batch(**{name: None})) == ff.FF_ERR_NULL, name
+    for bad in (dict(logp=None), dict(stats=None), dict(ws=None)):
+        assert loss(_batch(), **bad) == ff.FF_ERR_NULL, bad
+    assert L.ff_head_loss(None, A16, None, 0, None, 0, A16, A16, None) == ff.FF_ERR_NULL
+    for bad in (dict(dtype=0), dict(dtype=ff.FF_F32), dict(reserved=1), dict(vocab=0), dict(vocab=BIG), dict(n_tokens=ff.FF_HEAD_MAX_TOKENS + 1), dict(width=0),
+                dict(width=65), dict(hidden_stride=63), dict(weight_stride=63), dict(weight_stride=1 << 60),
+                dict(width=ff.FF_HEAD_MAX_WIDTH + 1, hidden_stride=1 << 20, weight_stride=1 << 20), dict(hidden=A16 + 1), dict(weight=A16 + 1), dict(targets=A16 + 4),
+                dict(weights=A16 + 2), dict(loss_scale=0.0), dict(loss_scale=-1.0), dict(loss_scale=INF), dict(loss_scale=NAN)):
+        assert loss(_batch(**bad)) == ff.FF_ERR_INVALID, bad
+    for bad in (dict(logp=A16 + 2), dict(stats=A16 + 4), dict(ws=A16 + 16), dict(dh=A16 + 1, dh_stride=64), dict(dh=2 * A16, dh_stride=63),
+                dict(dh=A16, dh_stride=72), dict(dw=A16 + 1, dw_stride=64), dict(dw=A16, dw_stride=63)):
+        assert loss(_batch(), **bad) == ff.FF_ERR_INVALID, bad
+    assert L.ff_head_workspace_bytes(None, 1) == 0 and L.ff_head_workspace_bytes(ctypes.byref(_batch(dtype=ff.FF_F32)), 1) == 0
+
+
+def test_workspaces_never_fall_with_any_size():
+    L = ff.lib()
+    tokens = [0, 1, 63, 64, 65, 128, 255, 256, 257, 1000, 1024, 2047, 2049, 4096, 100000, 1 << 20, 1 << 22]
+    vocabs = [1, 255, 256, 257, 4099, 32000, 128256, 1 << 20]
+    widths = [1, 8, 63, 64, 65, 256, 1000, 4096, 8192]
+    for f in (lambda n, v, w: L.ff_embed_workspace_bytes(n, v, w), lambda n, v, w: L.ff_layer_norm_workspace_bytes(n, w) if v == 1 else 0):
+        for v in vocabs:
+            for w in widths:
+                sizes = [f(n, v, w) for n in tokens]
+                assert sizes == sorted(sizes)
+        for n in tokens:
+            for w in widths:
+                sizes = [f(n, v, w) for v in vocabs[1:]]
+                assert sizes == sorted(sizes)
+    assert L.ff_layer_norm_workspace_bytes(4, ff.FF_NORM_MAX_WIDTH + 1) == L.ff_layer_norm_workspace_bytes(4, 0) == 0
+    for aligned in (True, False):
+        for grad in (0, 1):
+            def size(n, v, w):
+                b = _batch(n_tokens=n, vocab=v, width=w, hidden_stride=w, weight_stride=(w + 7) // 8 * 8 if aligned else w + 1)
+                return L.ff_head_workspace_bytes(ctypes.byref(b), grad)
+            for v in vocabs:
+                for w in widths:
+                    sizes = [size(n, v, w) for n in tokens]
+                    assert sizes == sorted(sizes) and sizes[0] > 0, (v, w, grad)
+            for n in tokens:
+                for w in widths:
+                    sizes = [size(n, v, w) for v in vocabs]
+                    assert sizes == sorted(sizes), (n, w, grad)
+                for v in vocabs:
+                    sizes = [size(n, v, w) for w in ([8, 64, 256, 1000, 4096, 8192] if aligned else widths)]
+                    assert sizes == sorted(sizes), (n, v, grad)
+
+
+def test_binding_refuses_shapes_types_and_small_workspaces():
+    bf, f, ids = torch.bfloat16, torch.zeros(4), torch.zeros(4, dtype=torch.int64)
+    table, out = torch.zeros(10, 8, dtype=bf), torch.zeros(4, 8, dtype=bf)
+    for args in ((table, ids.int(), out), (table, ids[::2], out), (table, ids, out.float()), (table, ids, out[:3]), (table.t(), ids, out), (table, ids, out[:, :7]),
+                 (table[0], ids, out)):
+        with pytest.raises(ValueError):
+            ff.ff_embed(*args, stream=NOWHERE)
+    ws = ff.alloc_embed_workspace(4, 10, 8, "cpu")
+    for args in ((out, ids, table, ws[:-1]), (out.float(), ids, table, ws), (out, ids[:3], table, ws), (out, ids, table.t(), ws)):
+        with pytest.raises(ValueError):
+            ff.ff_embed_grad(*args, stream=NOWHERE)
+    w8 = torch.zeros(8, dtype=bf)
+    for change in (dict(weight=w8.float()), dict(weight=w8[:7]), dict(bias=w8[:7]), dict(y=out.float()), dict(y=out[:3]), dict(mean=f.double()), dict(rstd=f[:3]), dict(x=out[0])):
+        with pytest.raises(ValueError):
+            ff.ff_layer_norm(**dict(dict(x=out, weight=w8, bias=w8, y=out), **change), stream=NOWHERE)
+    ws = ff.alloc_norm_workspace(4, 8, "cpu")
+    ok = dict(x=out, weight=w8, mean=f, rstd=f, dy=out, dx=out, dweight=w8, dbias=w8, workspace=ws)
+    for change in (dict(workspace=ws[:-1]), dict(workspace=None), dict(dweight=w8.float()), dict(dbias=w8[:3]), dict(dy=out[:2]), dict(dx=out.float()), dict(mean=f[:3])):
+        with pytest.raises(ValueError):
+            ff.ff_layer_norm_grad(**dict(ok, **change), stream=NOWHERE)
+    b = ff.head_batch(out, table, ids, f, 2.0)
+    assert (b.n_tokens, b.vocab, b.width, b.hidden_stride, b.weight_stride, b.dtype, b.loss_scale) == (4, 10, 8, 8, 8, ff.FF_BF16, 2.0)
+    for args in ((out.t(), table, ids, f), (out, table.float(), ids, f), (out, table[:, :7], ids, f), (out, table, ids.int(), f), (out, table, ids, f[:3]), (out, table, ids, f.double())):
+        with pytest.raises(ValueError):
+            ff.head_batch(*args)
+    stats, ws = ff.HeadStats("cpu"), ff.alloc_head_workspace(b, "cpu")
+    for change in (dict(workspace=ws[:-1]), dict(logp=f[:3]), dict(dhidden=out.float()), dict(dhidden=out[:3]), dict(dweight=out), dict(dweight=table.t())):
+        with pytest.raises(ValueError):
+            ff.ff_head_loss(**dict(dict(batch=b, logp=f, stats=stats, workspace=ws, dhidden=out, dweight=table), **change), stream=NOWHERE)
+
+
+def test_a_head_batch_keeps_its_tensors_alive():
+    def make():
+        ts = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(10, 8, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64), torch.zeros(4)
+        return ff.head_batch(*ts), [weakref.ref(t) for t in ts]
+
+    batch, kept = make()
+    assert {batch.hidden, batch.weight, batch.targets, batch.weights} == {r().data_ptr() for r in kept}
+    del batch
+    assert all(r() is None for r in kept)
+
+
+# ---- the plain forms ------------------------------------------------------------------------------
+
+def _difference(f, x, at, h=1e-6):
+    """df/dx[at] in 64 bits."""
+    a, b = x.clone(), x.clone()
+    a[at] += h
+    b[at] -= h
+    return (f(a) - f(b)) / (2 * h)
+
+
+def test_plain_head_is_its_differences():
+    g = torch.Generator().manual_seed(0)
+    h, w = torch.randn(5, 6, generator=g, dtype=torch.float64), torch.randn(9, 6, generator=g, dtype=torch.float64)
+    y, weights = torch.tensor([0, 8, 3, -1, 9]), torch.tensor([0.5, 0.25, 0.0, 1.0, 1.0])
+    modelref.HALF[torch.float64] = modelref.SMALL[torch.float64] = 0.0
+    try:
+        out = modelref.head(h, w, y, weights, 3.0)
+        loss = lambda h, w: float(modelref.head(h, w, y, weights)["loss"])  # noqa: E731
+        assert (out["n_tokens"], out["n_invalid"]) == (2, 2)
+        for at in ((0, 0), (1, 5), (2, 1), (3, 3)):
+            assert float(out["dhidden"][at]) == pytest.approx(3.0 * _difference(lambda x: loss(x, w), h, at), abs=1e-7)
+        for at in ((0, 0), (8, 5), (4, 1)):
+            assert float(out["dweight"][at]) == pytest.approx(3.0 * _difference(lambda x: loss(h, x), w, at), abs=1e-7)
+    finally:
+        del modelref.HALF[torch.float64], modelref.SMALL[torch.float64]
+    z = h @ w.t()
+    assert float(out["logp"][1]) == pytest.approx(float(z[1, 8] - z[1].exp().sum().log()))
+
+
+def test_plain_norm_is_its_differences():
+    g = torch.Generator().manual_seed(1)
+    n, width = 3, 7
+    x, w, b, dy = (torch.randn(s, generator=g, dtype=torch.float64) for s in ((n, width), (width,), (width,), (n, width)))
+    modelref.HALF[torch.float64] = modelref.SMALL[torch.float64] = 0.0
+    try:
+        f = lambda x, w, b: float((modelref.norm(x, w, b, 1e-5)["y"] * dy).sum())  # noqa: E731
+        out = modelref.norm(x, w, b, 1e-5)
+        grad = modelref.norm_grad(x, w, out["mean"], out["rstd"], dy)
+        for at in ((0, 0), (1, 6), (2, 3)):
+            assert float(grad["dx"][at]) == pytest.approx(_difference(lambda v: f(v, w, b), x, at), abs=1e-6)
+        for k in range(width):
+            assert float(grad["dweight"][k]) == pytest.approx(_difference(lambda v: f(x, v, b), w, k), abs=1e-6)
+            assert float(grad["dbias"][k]) == pytest.approx(_difference(lambda v: f(x, w, v), b, k), abs=1e-6)
+    finally:
+        del modelref.HALF[torch.float64], modelref.SMALL[torch.float64]
+
+
+def test_plain_embedding():
+    table = torch.arange(12.0).view(4, 3)
+    ids = torch.tensor([3, -1, 0, 3, 4])
+    assert modelref.embed(table, ids, 2.0).tolist() == [[18.0, 20.0, 22.0], [0.0] * 3, [0.0, 2.0, 4.0], [18.0, 20.0, 22.0], [0.0] * 3]
+    total, tol = modelref.embed_grad(torch.ones(5, 3), ids, 4, 2.0, table)
+    assert total.tolist() == [[2.0, 3.0, 4.0], [3.0, 4.0, 5.0], [6.0, 7.0, 8.0], [13.0, 14.0, 15.0]]
+    assert float(tol.max()) < 1e-5 and math.isfinite(float(tol.min()))
