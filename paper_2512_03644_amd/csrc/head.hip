@@ -40,7 +40,6 @@ struct State {
     uint32_t used, invalid;  // tokens that count; tokens with a weight but no target
     float scale;             // of the gradients: what G has been divided by
     uint32_t unused;
-    uint8_t zeros[64];
 };
 
 struct HeadArgs {
@@ -69,7 +68,7 @@ struct HeadArgs {
 
 __device__ __forceinline__ OperandTile hidden_tile(const HeadArgs& A, uint32_t m0, uint32_t used)
 {
-    return {A.hidden + static_cast<uint64_t>(m0) * A.stride, A.stride, used - m0, A.stride / 2, A.state->zeros};
+    return {A.hidden + static_cast<uint64_t>(m0) * A.stride, A.stride, used - m0, A.stride / 2};
 }
 // Rows [v0, ...) of W; `first` is the piece's.
 __device__ __forceinline__ const uint8_t* weight_row(const HeadArgs& A, uint32_t first, uint32_t v0, uint64_t* stride)
@@ -128,7 +127,6 @@ __global__ __launch_bounds__(kSelectThreads) void head_select_kernel(const HeadA
         A.state->invalid = invalid;
         A.state->scale = most;
     }
-    if (threadIdx.x < 64) A.state->zeros[threadIdx.x] = 0;
 }
 
 // `width` elements of a row to a packed one; elements behind them are zeros.
@@ -182,7 +180,7 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
                                                                                                              const uint32_t n)
 {
     using S = Share<BM>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kLdsBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kProductLds<BM, kAlongK, kAlongK>];
     const uint32_t used = A.state->used;
     uint32_t m0, n0;
     tile_at(xcd_order(blockIdx.x, gridDim.x, kXcdTiles), A.tokens_up / BM, (n + kTile - 1) / kTile, &m0, &n0);
@@ -193,7 +191,6 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     OperandTile b;
     b.base = weight_row(A, first, v0, &b.stride);
     b.valid = n - n0;
-    b.zeros = A.state->zeros;
     b.k_valid = A.weight ? A.stride / 2 : static_cast<uint32_t>(A.b.width);
     const uint32_t steps = A.stride / (2 * kStepK);
     f32x4 z[S::kM][S::kN];
@@ -325,7 +322,7 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
                                                                                                               const uint32_t n)
 {
     using S = Share<BM>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kLdsBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kProductLds<BM, kAlongK, kAcrossK>];
     const uint32_t used = A.state->used, width_up = A.stride / 2;
     const uint32_t tiles_m = A.tokens_up / BM, tiles_n = (width_up + kTile - 1) / kTile;
     const uint32_t tile = xcd_order(blockIdx.x, gridDim.x, kXcdTiles), slice = tile / (tiles_m * tiles_n);
@@ -337,12 +334,11 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     const uint32_t steps = (n + kStepK - 1) / kStepK, each = (steps + A.slices - 1) / A.slices;
     const uint32_t from = slice * each, to = from + each < steps ? from + each : steps;
     if (first && from >= to) return;
-    const OperandTile a = {A.grad + static_cast<uint64_t>(m0) * A.piece * 2, static_cast<uint64_t>(A.piece) * 2, A.tokens_up - m0, A.piece, nullptr};
+    const OperandTile a = {A.grad + static_cast<uint64_t>(m0) * A.piece * 2, static_cast<uint64_t>(A.piece) * 2, A.tokens_up - m0, A.piece};
     OperandTile b;
     b.base = weight_row(A, first, first, &b.stride) + n0 * 2;
     b.valid = (A.weight ? width_up : static_cast<uint32_t>(A.b.width)) - n0;
     b.k_valid = n;
-    b.zeros = nullptr;
     f32x4 sum[S::kM][S::kN];
     product<BF16, BM, kAlongK, kAcrossK>(a, b, from, to, n % kStepK ? steps - 1 : ~0u, (FF_LDS uint8_t*)lds, sum);
     const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
@@ -396,15 +392,15 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
                                                                                                               const uint32_t n)
 {
     using S = Share<256>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kLdsBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kProductLds<256, kAcrossK, kAcrossK>];
     const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width);
     uint32_t m0, n0;
     tile_at(xcd_order(blockIdx.x, gridDim.x, kXcdTiles), (n + kTile - 1) / kTile, (A.stride / 2 + kTile - 1) / kTile, &m0, &n0);
     m0 *= kTile;
     n0 *= kTile;
     const uint32_t steps = (used + kStepK - 1) / kStepK;
-    const OperandTile a = {A.grad + m0 * 2, static_cast<uint64_t>(A.piece) * 2, A.piece - m0, A.tokens_up, nullptr};
-    const OperandTile b = {A.hidden + n0 * 2, A.stride, A.stride / 2 - n0, A.tokens_up, nullptr};
+    const OperandTile a = {A.grad + m0 * 2, static_cast<uint64_t>(A.piece) * 2, A.piece - m0, A.tokens_up};
+    const OperandTile b = {A.hidden + n0 * 2, A.stride, A.stride / 2 - n0, A.tokens_up};
     f32x4 sum[S::kM][S::kN];
     product<BF16, 256, kAcrossK, kAcrossK>(a, b, 0, steps, ~0u, (FF_LDS uint8_t*)lds, sum);
     const float scale = A.state->scale;

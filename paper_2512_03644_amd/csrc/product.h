@@ -30,20 +30,19 @@ constexpr int kProductThreads = 512, kProductWaves = 8, kStepK = 64;
 
 // Where an operand's tile lies.
 struct OperandTile {
-    const uint8_t* base;   // of the tile's first row (kAlongK) or column (kAcrossK), at k = 0 of the product
-    uint64_t stride;       // bytes between rows; times 256 below 2^32
-    uint32_t valid;        // kAlongK: rows that are there; kAcrossK: columns, a multiple of 8.  Others repeat the last.
-    uint32_t k_valid;      // kAlongK: a multiple of 8, `zeros` stand for what is behind; kAcrossK: rows behind repeat the last
-    const uint8_t* zeros;  // 16 bytes
+    const uint8_t* base;  // of the tile's first row (kAlongK) or column (kAcrossK), at k = 0 of the product
+    uint64_t stride;      // bytes between rows; times 256 below 2^32
+    uint32_t valid;       // kAlongK: rows that are there; kAcrossK: columns, a multiple of 8.  Others repeat the last.
+    uint32_t k_valid;     // kAlongK: a multiple of 8, zeros stand for what is behind; kAcrossK: rows behind repeat the last
 };
-
-// What spreads the rows of a kAcrossK tile over the banks: rows that one transposing read takes differ in it.
-__device__ __forceinline__ uint32_t row_spread(uint32_t k) { return (k & 3) | (k >> 1 & 12); }
 
 template <Layout LAYOUT, int SIZE>
 struct Operand {
     static constexpr int kLoads = SIZE / 64;            // of a wavefront a step, 1 KiB each
-    static constexpr uint32_t kBytes = SIZE * kStepK * 2;
+    // What a load brings lies together; between those of a kAcrossK tile, two rows each, 64 bytes are left free, and in odd rows the two
+    // halves of every 64 bytes are exchanged: the four rows that a transposing read of 16 lanes takes are in different banks.
+    static constexpr uint32_t kChunk = LAYOUT == kAlongK ? 1024 : 1024 + 64;
+    static constexpr uint32_t kBytes = kProductWaves * kLoads * kChunk;
     static constexpr uint32_t kRowBytes = LAYOUT == kAlongK ? kStepK * 2 : SIZE * 2;
     static_assert(LAYOUT == kAlongK || SIZE == 256, "a row is 32 pieces of 16 bytes");
 
@@ -58,7 +57,7 @@ struct Operand {
     }
     static __device__ __forceinline__ uint32_t piece_of(int i, int wave, int lane)
     {
-        return LAYOUT == kAlongK ? (lane & 7) ^ (lane >> 3) : (lane & 31) ^ row_spread(row_of(i, wave, lane)) << 1;
+        return LAYOUT == kAlongK ? (lane & 7) ^ (lane >> 3) : (lane & 31) ^ (lane >> 5) << 1;
     }
     __device__ __forceinline__ void init(const OperandTile& t, int wave, int lane)
     {
@@ -71,27 +70,36 @@ struct Operand {
             at[i] = row * static_cast<uint32_t>(t.stride) + piece * 16;
         }
     }
-    static __device__ __forceinline__ void load(const uint8_t* p, FF_LDS uint8_t* to)
-    {
-        __builtin_amdgcn_global_load_lds((const FF_GLOBAL void*)p, (FF_LDS void*)to, 16, 0, 0);
-    }
-    // Step k of the product, into a buffer.
+    // Step k of the product, into a buffer: 16 bytes a lane, to consecutive places.  (By hand: behind the builtin for this the compiler waits
+    // for all of them in front of any read of LDS, as it cannot tell the two buffers apart.  There is no result in registers; `meet` waits.)
     __device__ __forceinline__ void fetch(uint32_t k, FF_LDS uint8_t* buffer, int wave) const
     {
         const uint8_t* const p = base + k * step;
-        for (int i = 0; i < kLoads; i++) load(p + at[i], buffer + (wave * kLoads + i) * 1024);
+        for (int i = 0; i < kLoads; i++)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :
+                         : "s"(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(buffer + (wave * kLoads + i) * kChunk))), "v"(at[i]), "s"(p)
+                         : "m0");
     }
-    // The same for a step of which only a part is there.
-    __device__ __forceinline__ void fetch_end(const OperandTile& t, uint32_t k, FF_LDS uint8_t* buffer, int wave, int lane) const
+    // In front of the fetch of a last step of which only a part is there.
+    __device__ __forceinline__ void cut(const OperandTile& t, uint32_t k, int wave, int lane)
     {
-        const uint8_t* const p = base + k * step;
         const uint32_t left = t.k_valid - k * kStepK;
+        if (left >= kStepK) return;
         for (int i = 0; i < kLoads; i++) {
-            const uint8_t* q = p + at[i];
-            const uint32_t row = row_of(i, wave, lane);
-            if (LAYOUT == kAlongK && piece_of(i, wave, lane) * 8 >= left) q = t.zeros;
-            if (LAYOUT == kAcrossK && row >= left) q -= (row - (left - 1)) * t.stride;
-            load(q, buffer + (wave * kLoads + i) * 1024);
+            const uint32_t row = row_of(i, wave, lane), piece = piece_of(i, wave, lane);
+            if (LAYOUT == kAlongK && piece * 8 >= left) at[i] -= (piece - (left / 8 - 1)) * 16;
+            if (LAYOUT == kAcrossK && row >= left) at[i] -= (row - (left - 1)) * static_cast<uint32_t>(step / kStepK);
+        }
+    }
+    // And when it has arrived: zeros for what is not there.
+    static __device__ __forceinline__ void clear(const OperandTile& t, uint32_t k, FF_LDS uint8_t* buffer)
+    {
+        const uint32_t left = t.k_valid - k * kStepK;
+        if (LAYOUT != kAlongK || left >= kStepK) return;
+        for (uint32_t i = threadIdx.x; i < SIZE * 8; i += kProductThreads) {
+            const uint32_t row = i / 8, piece = i % 8;
+            if (piece * 8 >= left) *(FF_LDS u32x4*)(buffer + row * kRowBytes + (piece ^ (row & 7)) * 16) = u32x4{0, 0, 0, 0};
         }
     }
     // Fragment of 16 rows (columns) from `first` on for the step's 32 k from 32 * half on: lane l has row l % 16, k 8 (l / 16) + 0..7.
@@ -101,11 +109,11 @@ struct Operand {
             const uint32_t piece = (half * 4 + lane / 16) ^ (lane & 7);
             return *(const FF_LDS s16x8*)(buffer + (lane % 16) * kRowBytes + piece * 16 + first * kRowBytes);
         } else {
-            const uint32_t row = 8 * (lane / 16) + (lane % 16) / 4;  // and row + 4
-            const uint32_t unit = (first / 16) ^ row_spread(row);
-            const FF_LDS uint8_t* const p = buffer + (half * 32 + row) * kRowBytes + unit * 32 + (lane % 4) * 8;
+            const uint32_t row = 8 * (lane / 16) + (lane % 16) / 4, odd = row & 1;  // and row + 4
+            const uint32_t at = row / 2 * kChunk + odd * kRowBytes + (lane % 4) * 8 + (first / 16 % 2 ? 1 - odd : odd) * 32;
+            const FF_LDS uint8_t* const p = buffer + at + half * 16 * kChunk + first / 32 * 64;
             const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FF_LDS s16x4*)p);
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FF_LDS s16x4*)(p + 4 * kRowBytes));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FF_LDS s16x4*)(p + 2 * kChunk));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
@@ -133,12 +141,14 @@ template <int BM>
 struct Share {
     static constexpr int kAcross = BM == 256 ? 4 : 8;  // wavefronts along n
     static constexpr int kM = BM == 256 ? 8 : 4, kN = BM == 256 ? 4 : 2;  // fragments of a wavefront
-    static constexpr uint32_t kLdsBytes = 2 * (BM + 256) * kStepK * 2;
 };
+
+template <int BM, Layout A_LAYOUT, Layout B_LAYOUT>
+constexpr uint32_t kProductLds = 2 * (Operand<A_LAYOUT, BM>::kBytes + Operand<B_LAYOUT, 256>::kBytes);
 
 // The sums of a wavefront's part over steps [k_from, k_to): fragment (i, j), lane l, element e is row 16 i + l % 16,
 // column 16 j + 4 (l / 16) + e of the part (operands in exchanged places: a lane's elements follow each other along n).
-// The last step of the whole product is `end` if a part of it is missing.  lds: Share<BM>::kLdsBytes.
+// The last step of the whole product is `end` if a part of it is missing.  lds: kProductLds<...>.
 template <bool BF16, int BM, Layout A_LAYOUT, Layout B_LAYOUT>
 __device__ __forceinline__ void product(const OperandTile& a_tile, const OperandTile& b_tile, uint32_t k_from, uint32_t k_to, uint32_t end,
                                         FF_LDS uint8_t* lds, f32x4 (&sum)[Share<BM>::kM][Share<BM>::kN])
@@ -158,12 +168,11 @@ __device__ __forceinline__ void product(const OperandTile& a_tile, const Operand
     FF_LDS uint8_t* const buffers[2] = {lds, lds + A::kBytes + B::kBytes};
     auto fetch = [&](uint32_t k, FF_LDS uint8_t* buffer) {
         if (k == end) {
-            a.fetch_end(a_tile, k, buffer, wave, lane);
-            b.fetch_end(b_tile, k, buffer + A::kBytes, wave, lane);
-        } else {
-            a.fetch(k, buffer, wave);
-            b.fetch(k, buffer + A::kBytes, wave);
+            a.cut(a_tile, k, wave, lane);
+            b.cut(b_tile, k, wave, lane);
         }
+        a.fetch(k, buffer, wave);
+        b.fetch(k, buffer + A::kBytes, wave);
     };
     struct Half {
         s16x8 a[S::kM], b[S::kN];
@@ -179,14 +188,18 @@ __device__ __forceinline__ void product(const OperandTile& a_tile, const Operand
     // all of this wavefront's loads are here, and all it has read from LDS
     auto meet = [&] {
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
+    };
+    auto clear = [&](uint32_t k, FF_LDS uint8_t* buffer) {
+        if (k != end) return;
+        A::clear(a_tile, k, buffer);
+        B::clear(b_tile, k, buffer + A::kBytes);
+        meet();
     };
     fetch(k_from, buffers[0]);
     meet();
+    clear(k_from, buffers[0]);
     if (k_from + 1 < k_to) fetch(k_from + 1, buffers[1]);
     read(first, buffers[0], 0);
     for (uint32_t k = k_from; k < k_to; k += 2) {
@@ -198,12 +211,15 @@ __device__ __forceinline__ void product(const OperandTile& a_tile, const Operand
                 read(second, mine, 1);
                 multiply_all(first);
                 meet();
+                if (now + 1 < k_to) clear(now + 1, next);
                 if (now + 2 < k_to) fetch(now + 2, mine);
                 if (now + 1 < k_to) read(first, next, 0);
                 multiply_all(second);
             }
         });
     }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");  // LDS is free
 }
 
 // Tiles in an order in which those that run at one time share operands: bands of 8 tiles along m, within them along n; the
