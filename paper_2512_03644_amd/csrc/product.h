@@ -70,16 +70,14 @@ struct Operand {
             at[i] = row * static_cast<uint32_t>(t.stride) + piece * 16;
         }
     }
-    // Step k of the product, into a buffer: 16 bytes a lane, to consecutive places.  (By hand: behind the builtin for this the compiler waits
+    // Load i of step k of the product, into a buffer: 16 bytes a lane, to consecutive places.  (By hand: behind the builtin for this the compiler waits
     // for all of them in front of any read of LDS, as it cannot tell the two buffers apart.  There is no result in registers; `meet` waits.)
-    __device__ __forceinline__ void fetch(uint32_t k, FF_LDS uint8_t* buffer, int wave) const
+    __device__ __forceinline__ void fetch(int i, uint32_t k, FF_LDS uint8_t* buffer, int wave) const
     {
-        const uint8_t* const p = base + k * step;
-        for (int i = 0; i < kLoads; i++)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                         :
-                         : "s"(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(buffer + (wave * kLoads + i) * kChunk))), "v"(at[i]), "s"(p)
-                         : "m0");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :
+                     : "s"(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(buffer + (wave * kLoads + i) * kChunk))), "v"(at[i]), "s"(base + k * step)
+                     : "m0");
     }
     // In front of the fetch of a last step of which only a part is there.
     __device__ __forceinline__ void cut(const OperandTile& t, uint32_t k, int wave, int lane)
@@ -165,25 +163,38 @@ __device__ __forceinline__ void product(const OperandTile& a_tile, const Operand
     a.init(a_tile, wave, lane);
     b.init(b_tile, wave, lane);
     const int m0 = (wave / S::kAcross) * (16 * S::kM), n0 = (wave % S::kAcross) * (16 * S::kN);
-    FF_LDS uint8_t* const buffers[2] = {lds, lds + A::kBytes + B::kBytes};
-    auto fetch = [&](uint32_t k, FF_LDS uint8_t* buffer) {
-        if (k == end) {
-            a.cut(a_tile, k, wave, lane);
-            b.cut(b_tile, k, wave, lane);
-        }
-        a.fetch(k, buffer, wave);
-        b.fetch(k, buffer + A::kBytes, wave);
+    constexpr uint32_t kBuffer = A::kBytes + B::kBytes;
+    auto cut = [&](uint32_t k) {
+        if (k != end) return;
+        a.cut(a_tile, k, wave, lane);
+        b.cut(b_tile, k, wave, lane);
+    };
+    // load i of a step, of A's and B's
+    auto fetch = [&](int i, uint32_t k, FF_LDS uint8_t* buffer) {
+        if (i < A::kLoads) a.fetch(i, k, buffer, wave);
+        else if (i < A::kLoads + B::kLoads) b.fetch(i - A::kLoads, k, buffer + A::kBytes, wave);
+    };
+    auto fetch_all = [&](uint32_t k, FF_LDS uint8_t* buffer) {
+        cut(k);
+        static_for<A::kLoads + B::kLoads>([&](auto i) { fetch(i, k, buffer); });
     };
     struct Half {
         s16x8 a[S::kM], b[S::kN];
     } first, second;
-    auto read = [&](Half& h, const FF_LDS uint8_t* buffer, int half) {
-        for (int j = 0; j < S::kN; j++) h.b[j] = B::fragment(buffer + A::kBytes, n0 + 16 * j, half, lane);
-        for (int i = 0; i < S::kM; i++) h.a[i] = A::fragment(buffer, m0 + 16 * i, half, lane);
+    // fragment i of a half, in the order in which they are used
+    auto read = [&](auto i, Half& h, const FF_LDS uint8_t* buffer, int half) {
+        if constexpr (i < S::kN) h.b[int(i)] = B::fragment(buffer + A::kBytes, n0 + 16 * i, half, lane);
+        else if constexpr (i < S::kN + S::kM) h.a[i - S::kN] = A::fragment(buffer, m0 + 16 * (i - S::kN), half, lane);
     };
-    auto multiply_all = [&](const Half& h) {
-        for (int i = 0; i < S::kM; i++)
-            for (int j = 0; j < S::kN; j++) sum[i][j] = multiply<BF16>(h.b[j], h.a[i], sum[i][j]);
+    // The products of a half, and between them the reads of the next one and the loads of a step.
+    constexpr int kGroups = S::kM, kReads = (S::kN + S::kM + kGroups - 3) / (kGroups - 2), kFetches = (A::kLoads + B::kLoads + kGroups - 1) / kGroups;
+    auto multiply_all = [&](const Half& h, Half& to, const FF_LDS uint8_t* from, int half, uint32_t k, FF_LDS uint8_t* into, auto fetches) {
+        static_for<kGroups>([&](auto g) {
+            static_for<S::kN>([&](auto j) { sum[int(g)][int(j)] = multiply<BF16>(h.b[int(j)], h.a[int(g)], sum[int(g)][int(j)]); });
+            static_for<kReads>([&](auto i) { read(std::integral_constant<int, g * kReads + i>{}, to, from, half); });
+            if constexpr (fetches) static_for<kFetches>([&](auto i) { fetch(g * kFetches + i, k, into); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
     // all of this wavefront's loads are here, and all it has read from LDS
     auto meet = [&] {
@@ -197,27 +208,25 @@ __device__ __forceinline__ void product(const OperandTile& a_tile, const Operand
         B::clear(b_tile, k, buffer + A::kBytes);
         meet();
     };
-    fetch(k_from, buffers[0]);
+    uint32_t mine = 0;  // the buffer of the step
+    fetch_all(k_from, lds);
     meet();
-    clear(k_from, buffers[0]);
-    if (k_from + 1 < k_to) fetch(k_from + 1, buffers[1]);
-    read(first, buffers[0], 0);
-    for (uint32_t k = k_from; k < k_to; k += 2) {
-        static_for<2>([&](auto which) {
-            const uint32_t now = k + which;
-            if (now < k_to) {
-                FF_LDS uint8_t* const mine = buffers[int(which)];
-                FF_LDS uint8_t* const next = buffers[1 - int(which)];
-                read(second, mine, 1);
-                multiply_all(first);
-                meet();
-                if (now + 1 < k_to) clear(now + 1, next);
-                if (now + 2 < k_to) fetch(now + 2, mine);
-                if (now + 1 < k_to) read(first, next, 0);
-                multiply_all(second);
-            }
-        });
-    }
+    clear(k_from, lds);
+    if (k_from + 1 < k_to) fetch_all(k_from + 1, lds + kBuffer);
+    static_for<S::kN + S::kM>([&](auto i) { read(i, first, lds, 0); });
+    // (behind the last step there is nothing to read, and what is read is not used)
+    auto step = [&](uint32_t now, auto fetches) {
+        FF_LDS uint8_t *const here = lds + mine, *const next = lds + (kBuffer - mine);
+        multiply_all(first, second, here, 1, 0, here, std::false_type{});
+        meet();
+        if (now + 1 == end) clear(end, next);
+        if (fetches && now + 2 == end) cut(end);
+        multiply_all(second, first, next, 0, now + 2, here, fetches);
+        mine = kBuffer - mine;
+    };
+    uint32_t k = k_from;
+    for (; k + 2 < k_to; k++) step(k, std::true_type{});
+    for (; k < k_to; k++) step(k, std::false_type{});
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");  // LDS is free
 }
