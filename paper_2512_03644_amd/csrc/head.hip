@@ -38,8 +38,9 @@ struct Row {
 // Known on the device alone.
 struct State {
     uint32_t used, invalid;  // tokens that count; tokens with a weight but no target
+    float largest;           // weight of those that count
     float scale;             // of the gradients: what G has been divided by
-    uint32_t unused;
+    uint32_t done;           // rows whose loss is known, of few
 };
 
 struct HeadArgs {
@@ -51,6 +52,8 @@ struct HeadArgs {
     // the workspace
     State* state;
     uint32_t* index;    // of the tokens that count, in their order
+    float* weights;     // theirs
+    int32_t* targets;
     Row* rows;
     double* losses;     // of each of them, times its weight
     float* picked;      // logit of the target
@@ -58,12 +61,14 @@ struct HeadArgs {
     uint8_t* hidden;    // packed rows of those tokens: `stride` bytes, zeros behind the width and behind the last up to 64 rows
     uint8_t* weight;    // packed rows of a piece, if W's own do not lie as the loads want them; or null
     uint8_t* grad;      // G of a piece: [tokens up to a tile][piece]
+    float* logits;      // [token][piece]: of the last piece, if they are kept
     float* dh;          // [slice][token][width up to 64]: dH so far
     uint32_t tokens_up; // tokens, up to a whole tile
     uint32_t tiles;     // of the vocabulary
     uint32_t stride;    // bytes of a packed row
     uint32_t piece;     // vocabulary entries of a piece, a multiple of 256
     uint32_t slices;    // of dH's sum over a piece
+    float grad_scale;   // loss scale, and what G is too large by
 };
 
 __device__ __forceinline__ OperandTile hidden_tile(const HeadArgs& A, uint32_t m0, uint32_t used)
@@ -83,16 +88,16 @@ __device__ __forceinline__ const uint8_t* weight_row(const HeadArgs& A, uint32_t
 
 // ---- which tokens count ---------------------------------------------------------------------------
 
-// In their order; the largest weight.  One workgroup: a few thousand tokens are a few rounds.
-constexpr int kSelectThreads = 1024;
-__global__ __launch_bounds__(kSelectThreads) void head_select_kernel(const HeadArgs A)
+// In their order, by a whole workgroup: index[k] of the k-th; the workgroup that writes leaves what is known of them in the workspace.
+template <int THREADS>
+__device__ __forceinline__ uint32_t select(const HeadArgs& A, uint32_t* index, bool writes)
 {
-    __shared__ uint32_t count[kSelectThreads / kWaveSize];
-    __shared__ float largest[kSelectThreads / kWaveSize];
+    __shared__ uint32_t count[THREADS / kWaveSize];
+    __shared__ float largest[THREADS / kWaveSize];
     const uint32_t n = static_cast<uint32_t>(A.b.n_tokens), wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
     uint32_t used = 0, invalid = 0;
     float most = 0.f;
-    for (uint64_t first = 0; first < n; first += kSelectThreads) {
+    for (uint64_t first = 0; first < n; first += THREADS) {
         const uint64_t t = first + threadIdx.x;
         const float w = t < n ? A.b.weights[t] : 0.f;
         const int64_t y = t < n ? A.b.targets[t] : -1;
@@ -100,34 +105,37 @@ __global__ __launch_bounds__(kSelectThreads) void head_select_kernel(const HeadA
         const uint64_t who = __ballot(mine);
         if (lane == 0) count[wave] = __popcll(who);
         __syncthreads();
-        uint32_t before = used, all = 0;
-        for (uint32_t k = 0; k < kSelectThreads / kWaveSize; k++) {
-            if (k < wave) before += count[k];
+        uint32_t at = used + __popcll(who & ((1ull << lane) - 1)), all = 0;
+        for (uint32_t k = 0; k < THREADS / kWaveSize; k++) {
+            if (k < wave) at += count[k];
             all += count[k];
         }
-        __syncthreads();
-        if (mine) {
-            const uint32_t at = before + __popcll(who & ((1ull << lane) - 1));
+        if (mine) index[at] = static_cast<uint32_t>(t);
+        if (mine && writes) {
             A.index[at] = static_cast<uint32_t>(t);
-            A.rows[at].factor = w;
-            A.rows[at].y = static_cast<int32_t>(y);
+            A.weights[at] = w;
+            A.targets[at] = static_cast<int32_t>(y);
             if (__builtin_isfinite(w)) most = fmaxf(most, fabsf(w));
-        } else if (t < n) {
-            A.logp[t] = 0.f;
         }
+        if (!mine && writes && t < n) A.logp[t] = 0.f;
         used += all;
         invalid += __syncthreads_count(wanted && !inside);
     }
-    for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
-    if (lane == 0) largest[wave] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (uint32_t k = 0; k < kSelectThreads / kWaveSize; k++) most = fmaxf(most, largest[k]);
-        A.state->used = used;
-        A.state->invalid = invalid;
-        A.state->scale = most;
+    if (writes) {
+        for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
+        if (lane == 0) largest[wave] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (uint32_t k = 0; k < THREADS / kWaveSize; k++) most = fmaxf(most, largest[k]);
+            *A.state = {used, invalid, most, most * A.grad_scale, 0};
+        }
     }
+    return used;
 }
+
+// One workgroup: a few thousand tokens are a few rounds.
+constexpr int kSelectThreads = 1024;
+__global__ __launch_bounds__(kSelectThreads) void head_select_kernel(const HeadArgs A) { select<kSelectThreads>(A, A.index, true); }
 
 // `width` elements of a row to a packed one; elements behind them are zeros.
 __device__ __forceinline__ void copy_row(uint8_t* to, uint32_t bytes, const uint8_t* from, uint32_t width)
@@ -146,11 +154,11 @@ __device__ __forceinline__ void copy_row(uint8_t* to, uint32_t bytes, const uint
 }
 
 // Hidden states of the tokens that count, one behind the other, and zeros up to 64 rows; gradients of the other tokens.
-__global__ __launch_bounds__(256) void head_gather_kernel(const HeadArgs A)
+__device__ __forceinline__ void gather(const HeadArgs& A, const uint32_t used, const uint32_t* index)
 {
-    const uint32_t used = A.state->used, until = (used + 63) / 64 * 64, n = static_cast<uint32_t>(A.b.n_tokens);
+    const uint32_t until = (used + 63) / 64 * 64, n = static_cast<uint32_t>(A.b.n_tokens);
     for (uint32_t r = blockIdx.x; r < until; r += gridDim.x) {
-        const uint64_t t = r < used ? A.index[r] : 0;
+        const uint64_t t = r < used ? index[r] : 0;
         copy_row(A.hidden + static_cast<uint64_t>(r) * A.stride, A.stride,
                  static_cast<const uint8_t*>(A.b.hidden) + t * A.b.hidden_stride * 2, r < used ? static_cast<uint32_t>(A.b.width) : 0);
     }
@@ -163,6 +171,17 @@ __global__ __launch_bounds__(256) void head_gather_kernel(const HeadArgs A)
         for (uint32_t i = threadIdx.x; i < A.b.width; i += blockDim.x) as_global(to)[i] = 0;
     }
 }
+__global__ __launch_bounds__(256) void head_gather_kernel(const HeadArgs A) { gather(A, A.state->used, A.index); }
+
+// Both, where every workgroup can look at all tokens by itself.
+constexpr uint32_t kSelectFew = 1024;
+__global__ __launch_bounds__(256) void head_few_kernel(const HeadArgs A)
+{
+    __shared__ uint32_t index[kSelectFew];
+    const uint32_t used = select<256>(A, index, blockIdx.x == 0);
+    __syncthreads();
+    gather(A, used, index);
+}
 
 // Rows [first, first + n) of W, packed.
 __global__ __launch_bounds__(256) void head_pack_kernel(const HeadArgs A, const uint32_t first, const uint32_t n)
@@ -172,10 +191,18 @@ __global__ __launch_bounds__(256) void head_pack_kernel(const HeadArgs A, const 
                  static_cast<const uint8_t*>(A.b.weight) + (static_cast<uint64_t>(first) + r) * A.b.weight_stride * 2, static_cast<uint32_t>(A.b.width));
 }
 
+// An element of G.
+__device__ __forceinline__ float gradient(float z, uint32_t v, uint32_t vocab, const Row& r)
+{
+    const float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2E, -r.lse2)) * r.factor;
+    return v >= vocab ? 0.f : static_cast<int32_t>(v) == r.y ? r.target : p;
+}
+
 // ---- logits ---------------------------------------------------------------------------------------
 
-// The tiles of vocabulary entries [first, first + n).  Without GRAD the tile's part of the sums, with GRAD its G.
-template <bool BF16, int BM, bool GRAD>
+// The tiles of vocabulary entries [first, first + n): their parts of the sums, with kKeep the logits as well; or G.
+enum Mode { kSums, kKeep, kGrad };
+template <bool BF16, int BM, Mode MODE>
 __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu(2))) void head_logits_kernel(const HeadArgs A, const uint32_t first,
                                                                                                              const uint32_t n)
 {
@@ -198,7 +225,7 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
     const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;                    // + 16 i
     const uint32_t v = v0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);              // + 16 j + e
-    if constexpr (GRAD) {
+    if constexpr (MODE == kGrad) {
         const uint32_t at = v - first;
         for (int i = 0; i < S::kM; i++) {
             const uint32_t t = m + 16 * i;
@@ -209,10 +236,8 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
             for (int j = 0; j < S::kN; j++) {
                 f32x4 g;
                 for (int e = 0; e < 4; e++) {
-                    const uint32_t vocab_entry = v + 16 * j + e;
-                    float p = __builtin_amdgcn_exp2f(fmaf(z[i][j][e], kLog2E, -r.lse2)) * r.factor;
-                    p = static_cast<int32_t>(vocab_entry) == r.y ? r.target : p;
-                    g[e] = there && vocab_entry < vocab ? p : 0.f;
+                    const float x = gradient(z[i][j][e], v + 16 * j + e, vocab, r);
+                    g[e] = there ? x : 0.f;
                 }
                 *(FF_GLOBAL u32x2*)(out + 32 * j) = to_half<BF16>(g);
             }
@@ -221,9 +246,14 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
         __shared__ float2 part[S::kAcross][BM];
         for (int i = 0; i < S::kM; i++) {
             const uint32_t t = m + 16 * i;
-            const int32_t y = t < used ? A.rows[t].y : -1;
+            const int32_t y = t < used ? A.targets[t] : -1;
             float top = -INFINITY, total = 0.f, target = 0.f;
             bool mine = false;
+            if constexpr (MODE == kKeep) {
+                float* const out = A.logits + static_cast<uint64_t>(t) * A.piece + (v - first);
+                for (int j = 0; j < S::kN; j++)
+                    if (t < used) *(FF_GLOBAL f32x4*)(out + 16 * j) = z[i][j];
+            }
             for (int j = 0; j < S::kN; j++)
                 for (int e = 0; e < 4; e++) {
                     const uint32_t vocab_entry = v + 16 * j + e;
@@ -257,16 +287,23 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     }
 }
 
-// ---- log-probabilities ----------------------------------------------------------------------------
+// ---- log-probabilities, G of kept logits ------------------------------------------------------------
 
-// A wavefront joins the tiles' parts of a token, in 64 bits from the exponentials on.
-template <bool BF16>
-__global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs A)
+// The loss, from every row's in an order that their number gives, by a wavefront.
+__device__ __forceinline__ void put_stats(const HeadArgs& A, double loss, const uint32_t used)
 {
-    const uint32_t used = A.state->used, lane = threadIdx.x % kWaveSize;
-    const float largest = A.state->scale;
-    const uint32_t r = blockIdx.x * (256 / kWaveSize) + threadIdx.x / kWaveSize;
-    if (r >= used) return;
+    A.stats->loss = static_cast<float>(loss);
+    A.stats->reserved = 0;
+    A.stats->n_tokens = used;
+    A.stats->n_invalid = A.state->invalid;
+}
+
+// A wavefront joins the tiles' parts of row r, in 64 bits from the exponentials on.  The one that writes leaves the results; of few rows
+// (kFewTokens) the last one to do so adds their losses up.
+template <bool BF16>
+__device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const uint32_t used, const bool writes)
+{
+    const uint32_t lane = threadIdx.x % kWaveSize;
     const float2* const parts = A.parts + static_cast<uint64_t>(r) * A.tiles;
     float top = -INFINITY;
     for (uint32_t k = lane; k < A.tiles; k += kWaveSize) top = fmaxf(top, parts[k].x);
@@ -278,22 +315,67 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs A)
         total += static_cast<double>(p.y) * exp(static_cast<double>(p.x) - static_cast<double>(against));
     }
     for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
-    if (lane == 0) {
-        const double rest = log(total);
-        const double logp = (static_cast<double>(A.picked[r]) - static_cast<double>(against)) - rest;
-        const uint32_t t = A.index[r];
-        const float w = A.rows[r].factor;
-        A.logp[t] = static_cast<float>(logp);
-        A.losses[r] = -static_cast<double>(w) * logp;
-        const float f = w / largest * (BF16 ? 1.f : 0x1p14f);
-        A.rows[r].lse2 = static_cast<float>((static_cast<double>(against) + rest) * 1.4426950408889634);
-        A.rows[r].factor = f;
-        A.rows[r].target = f * static_cast<float>(expm1(logp));
+    const double rest = log(total), logp = (static_cast<double>(A.picked[r]) - static_cast<double>(against)) - rest;
+    const float w = A.weights[r], f = w / A.state->largest * (BF16 ? 1.f : 0x1p14f);
+    const Row row = {static_cast<float>((static_cast<double>(against) + rest) * 1.4426950408889634), f, f * static_cast<float>(expm1(logp)), A.targets[r]};
+    if (writes && lane == 0) {
+        A.logp[A.index[r]] = static_cast<float>(logp);
+        A.rows[r] = row;
+        __hip_atomic_store(A.losses + r, -static_cast<double>(w) * logp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (writes && A.b.n_tokens <= kFewTokens) {
+        bool last = false;
+        if (lane == 0) {
+            // (the loss has arrived when the store is done; a release would write the caches back)
+            asm volatile("" ::: "memory");
+            wait_loads<0>();
+            last = __hip_atomic_fetch_add(&A.state->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == used;
+        }
+        if (__any(last)) {
+            double s = lane < used ? __hip_atomic_load(A.losses + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+            for (int d = 32; d; d /= 2) s += __shfl_xor(s, d);
+            if (lane == 0) put_stats(A, s, used);
+        }
+    }
+    return row;
+}
+
+// A wavefront to a row.
+template <bool BF16>
+__global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs A)
+{
+    const uint32_t used = A.state->used, r = blockIdx.x * (256 / kWaveSize) + threadIdx.x / kWaveSize;
+    if (r < used) finish<BF16>(A, r, used, true);
+    if (used == 0 && r == 0 && threadIdx.x == 0) put_stats(A, 0.0, 0);
+}
+
+// The same, and G of vocabulary entries [first, first + n), whose logits were kept; rows of zeros up to 64.
+template <bool BF16>
+__global__ __launch_bounds__(256) void head_kept_kernel(const HeadArgs A, const uint32_t first, const uint32_t n, const uint32_t wide)
+{
+    const uint32_t used = A.state->used, vocab = static_cast<uint32_t>(A.b.vocab), until = (used + 63) / 64 * 64;
+    const uint32_t t = blockIdx.x / wide, part = blockIdx.x - t * wide;  // of `wide` parts of a row
+    if (used == 0 && blockIdx.x == 0 && threadIdx.x == 0) put_stats(A, 0.0, 0);
+    if (t >= until) return;
+    Row r = {};
+    if (t < used) r = finish<BF16>(A, t, used, part == 0 && threadIdx.x < kWaveSize);
+    const uint32_t end = (n + kTile - 1) / kTile * kTile;
+    for (uint32_t at = (part * 256 + threadIdx.x) * 8; at < end; at += wide * 2048) {
+        u32x4 out = {0, 0, 0, 0};
+        if (t < used) {
+            const FF_GLOBAL f32x4* const z = (const FF_GLOBAL f32x4*)(A.logits + static_cast<uint64_t>(t) * A.piece + at);
+            f32x4 g[2] = {z[0], z[1]};
+            for (int k = 0; k < 2; k++)
+                for (int e = 0; e < 4; e++) g[k][e] = gradient(g[k][e], first + at + 4 * k + e, vocab, r);
+            const u32x2 a = to_half<BF16>(g[0]), b = to_half<BF16>(g[1]);
+            out = u32x4{a.x, a.y, b.x, b.y};
+        }
+        *(FF_GLOBAL u32x4*)(A.grad + (static_cast<uint64_t>(t) * A.piece + at) * 2) = out;
     }
 }
 
-// The loss, in an order that the number of tokens gives.
-__global__ __launch_bounds__(kSelectThreads) void head_sum_kernel(const HeadArgs A, const float grad_scale)
+// The loss of many rows.
+__global__ __launch_bounds__(kSelectThreads) void head_sum_kernel(const HeadArgs A)
 {
     __shared__ double sum[kSelectThreads];
     const uint32_t used = A.state->used;
@@ -305,56 +387,10 @@ __global__ __launch_bounds__(kSelectThreads) void head_sum_kernel(const HeadArgs
         if (static_cast<int>(threadIdx.x) < d) sum[threadIdx.x] += sum[threadIdx.x + d];
         __syncthreads();
     }
-    if (threadIdx.x == 0) {
-        A.stats->loss = static_cast<float>(sum[0]);
-        A.stats->reserved = 0;
-        A.stats->n_tokens = used;
-        A.stats->n_invalid = A.state->invalid;
-        A.state->scale *= grad_scale;
-    }
+    if (threadIdx.x == 0) put_stats(A, sum[0], used);
 }
 
 // ---- gradients ------------------------------------------------------------------------------------
-
-// dH (+)= G W over a slice of the piece [first, first + n).
-template <bool BF16, int BM>
-__global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu(2))) void head_dhidden_kernel(const HeadArgs A, const uint32_t first,
-                                                                                                              const uint32_t n)
-{
-    using S = Share<BM>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kProductLds<BM, kAlongK, kAcrossK>];
-    const uint32_t used = A.state->used, width_up = A.stride / 2;
-    const uint32_t tiles_m = A.tokens_up / BM, tiles_n = (width_up + kTile - 1) / kTile;
-    const uint32_t tile = xcd_order(blockIdx.x, gridDim.x, kXcdTiles), slice = tile / (tiles_m * tiles_n);
-    uint32_t m0, n0;
-    tile_at(tile - slice * (tiles_m * tiles_n), tiles_m, tiles_n, &m0, &n0);
-    m0 *= BM;
-    n0 *= kTile;
-    if (m0 >= used) return;
-    const uint32_t steps = (n + kStepK - 1) / kStepK, each = (steps + A.slices - 1) / A.slices;
-    const uint32_t from = slice * each, to = from + each < steps ? from + each : steps;
-    if (first && from >= to) return;
-    const OperandTile a = {A.grad + static_cast<uint64_t>(m0) * A.piece * 2, static_cast<uint64_t>(A.piece) * 2, A.tokens_up - m0, A.piece};
-    OperandTile b;
-    b.base = weight_row(A, first, first, &b.stride) + n0 * 2;
-    b.valid = (A.weight ? width_up : static_cast<uint32_t>(A.b.width)) - n0;
-    b.k_valid = n;
-    f32x4 sum[S::kM][S::kN];
-    product<BF16, BM, kAlongK, kAcrossK>(a, b, from, to, n % kStepK ? steps - 1 : ~0u, (FF_LDS uint8_t*)lds, sum);
-    const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
-    const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;
-    const uint32_t d = n0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);
-    for (int i = 0; i < S::kM; i++) {
-        const uint32_t t = m + 16 * i;
-        if (t >= used) continue;
-        float* const out = A.dh + (static_cast<uint64_t>(slice) * A.tokens_up + t) * width_up + d;
-        for (int j = 0; j < S::kN; j++) {
-            if (d + 16 * j >= width_up) continue;
-            FF_GLOBAL f32x4* const p = (FF_GLOBAL f32x4*)(out + 16 * j);
-            *p = first ? *p + sum[i][j] : sum[i][j];
-        }
-    }
-}
 
 // Elements [at, at + 4) of a row of `width`, rounded.
 template <bool BF16>
@@ -367,6 +403,53 @@ __device__ __forceinline__ void put4(uint8_t* row, uint32_t at, uint32_t width, 
     } else {
         for (uint32_t e = 0; at + e < width; e++) as_global(reinterpret_cast<uint16_t*>(p))[e] = static_cast<uint16_t>((e & 2 ? h.y : h.x) >> (e & 1) * 16);
     }
+}
+
+// dH (+)= G W over a slice of the piece [first, first + n); where that is all of it, in its place.
+enum Sum { kOnly, kFirst, kNext };
+template <bool BF16, int BM>
+__device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first, const uint32_t n, const Sum which, const uint32_t block,
+                                        const uint32_t blocks, FF_LDS uint8_t* lds)
+{
+    using S = Share<BM>;
+    const uint32_t used = A.state->used, width_up = A.stride / 2;
+    const uint32_t tiles_m = A.tokens_up / BM, tiles_n = (width_up + kTile - 1) / kTile;
+    const uint32_t tile = xcd_order(block, blocks, kXcdTiles), slice = tile / (tiles_m * tiles_n);
+    uint32_t m0, n0;
+    tile_at(tile - slice * (tiles_m * tiles_n), tiles_m, tiles_n, &m0, &n0);
+    m0 *= BM;
+    n0 *= kTile;
+    if (m0 >= used) return;
+    const uint32_t steps = (n + kStepK - 1) / kStepK, each = (steps + A.slices - 1) / A.slices;
+    const uint32_t from = slice * each, to = from + each < steps ? from + each : steps;
+    if (which == kNext && from >= to) return;
+    const OperandTile a = {A.grad + static_cast<uint64_t>(m0) * A.piece * 2, static_cast<uint64_t>(A.piece) * 2, A.tokens_up - m0, A.piece};
+    OperandTile b;
+    b.base = weight_row(A, first, first, &b.stride) + n0 * 2;
+    b.valid = (A.weight ? width_up : static_cast<uint32_t>(A.b.width)) - n0;
+    b.k_valid = n;
+    f32x4 sum[S::kM][S::kN];
+    product<BF16, BM, kAlongK, kAcrossK>(a, b, from, to, n % kStepK ? steps - 1 : ~0u, lds, sum);
+    const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
+    const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;
+    const uint32_t d = n0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);
+    const float scale = A.state->scale;
+    static_for<S::kM>([&](auto i) {
+        const uint32_t t = m + 16 * i;
+        if (t >= used) return;
+        if (which == kOnly) {
+            uint8_t* const out = A.dhidden + A.index[t] * A.dhidden_stride * 2;
+            static_for<S::kN>([&](auto j) {
+                if (d + 16 * j < A.b.width) put4<BF16>(out, d + 16 * j, static_cast<uint32_t>(A.b.width), sum[int(i)][int(j)] * scale);
+            });
+        } else {
+            float* const out = A.dh + (static_cast<uint64_t>(slice) * A.tokens_up + t) * width_up + d;
+            static_for<S::kN>([&](auto j) {
+                FF_GLOBAL f32x4* const p = (FF_GLOBAL f32x4*)(out + 16 * j);
+                if (d + 16 * j < width_up) *p = which == kNext ? *p + sum[int(i)][int(j)] : sum[int(i)][int(j)];
+            });
+        }
+    });
 }
 
 // dH of all pieces and slices, in its place.
@@ -388,21 +471,20 @@ __global__ __launch_bounds__(256) void head_put_kernel(const HeadArgs A)
 
 // dW = G^T H of the piece [first, first + n).
 template <bool BF16>
-__global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu(2))) void head_dweight_kernel(const HeadArgs A, const uint32_t first,
-                                                                                                              const uint32_t n)
+__device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first, const uint32_t n, const uint32_t block, const uint32_t blocks,
+                                        FF_LDS uint8_t* lds)
 {
     using S = Share<256>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kProductLds<256, kAcrossK, kAcrossK>];
     const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width);
     uint32_t m0, n0;
-    tile_at(xcd_order(blockIdx.x, gridDim.x, kXcdTiles), (n + kTile - 1) / kTile, (A.stride / 2 + kTile - 1) / kTile, &m0, &n0);
+    tile_at(xcd_order(block, blocks, kXcdTiles), (n + kTile - 1) / kTile, (A.stride / 2 + kTile - 1) / kTile, &m0, &n0);
     m0 *= kTile;
     n0 *= kTile;
     const uint32_t steps = (used + kStepK - 1) / kStepK;
     const OperandTile a = {A.grad + m0 * 2, static_cast<uint64_t>(A.piece) * 2, A.piece - m0, A.tokens_up};
     const OperandTile b = {A.hidden + n0 * 2, A.stride, A.stride / 2 - n0, A.tokens_up};
     f32x4 sum[S::kM][S::kN];
-    product<BF16, 256, kAcrossK, kAcrossK>(a, b, 0, steps, ~0u, (FF_LDS uint8_t*)lds, sum);
+    product<BF16, 256, kAcrossK, kAcrossK>(a, b, 0, steps, ~0u, lds, sum);
     const float scale = A.state->scale;
     const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
     const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;
@@ -415,20 +497,37 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     }
 }
 
+// Both: the first `dh_blocks` workgroups make dH, whose sums are longer, the others dW.
+template <bool BF16, int BM>
+__global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu(2))) void head_grads_kernel(const HeadArgs A, const uint32_t first,
+                                                                                                            const uint32_t n, const Sum which,
+                                                                                                            const uint32_t dh_blocks)
+{
+    constexpr uint32_t kOne = kProductLds<BM, kAlongK, kAcrossK>, kOther = kProductLds<256, kAcrossK, kAcrossK>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kOne > kOther ? kOne : kOther];
+    if (blockIdx.x < dh_blocks) dhidden<BF16, BM>(A, first, n, which, blockIdx.x, dh_blocks, (FF_LDS uint8_t*)lds);
+    else dweight<BF16>(A, first, n, blockIdx.x - dh_blocks, gridDim.x - dh_blocks, (FF_LDS uint8_t*)lds);
+}
+
 __global__ void head_of_nothing_kernel(ff_head_stats* stats) { *stats = {}; }
 
 // ---- the workspace ----------------------------------------------------------------------------------
 
-constexpr uint64_t kPieceElements = 1ull << 27;  // of G, and of a piece's packed rows
+constexpr uint64_t kPieceElements = 1ull << 28;  // of G, and of a piece's packed rows
 constexpr uint32_t kSliceTokens = 2048;          // tokens times slices, up to so many
+constexpr uint32_t kKeptBlocks = 2048;           // workgroups that make G of kept logits, about
 
 bool weight_as_it_is(const ff_head_batch& b)
 {
     return reinterpret_cast<uint64_t>(b.weight) % 16 == 0 && b.weight_stride % 8 == 0 && b.width % 8 == 0 && b.weight_stride <= (1u << 22);
 }
 
+// Is it better to keep the logits of a piece than to make them again?  (Of the last piece, which is all there is for the smaller calls.)
+bool keeps(const ff_head_batch& b) { return b.width >= 1024 || b.n_tokens * 4 <= b.width; }
+uint32_t up64(uint64_t n) { return static_cast<uint32_t>(up(std::max<uint64_t>(n, 1), 64)); }
+
 struct Places {
-    uint64_t state, index, rows, losses, picked, parts, hidden, weight, grad, dh, bytes;
+    uint64_t state, index, weights, targets, rows, losses, picked, parts, hidden, weight, grad, logits, dh, bytes;
 };
 
 Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
@@ -453,6 +552,8 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     };
     p.state = take(sizeof(State));
     p.index = take(n * 4);
+    p.weights = take(n * 4);
+    p.targets = take(n * 4);
     p.rows = take(n * sizeof(Row));
     p.losses = take(n * 8);
     p.picked = take(n * 4);
@@ -464,6 +565,7 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     p.weight = take(packed ? piece_of(width_up) : 0);
     if (grad) {
         p.grad = take(piece_of(A->tokens_up));
+        p.logits = take(2 * piece_of(A->tokens_up));
         p.dh = take(static_cast<uint64_t>(std::max(A->tokens_up, kSliceTokens)) * width_up * 4);
     }
     p.bytes = at;
@@ -475,33 +577,47 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
 {
     const uint32_t n = static_cast<uint32_t>(A.b.n_tokens), vocab = static_cast<uint32_t>(A.b.vocab), tiles_m = A.tokens_up / BM;
     const uint32_t tiles_d = (A.stride / 2 + kTile - 1) / kTile;
-    hipLaunchKernelGGL(head_select_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
-    hipLaunchKernelGGL(head_gather_kernel, dim3(std::min(A.tokens_up, 4096u)), dim3(256), 0, stream, A);
-    auto pieces = [&](auto&& fn) {
-        for (uint64_t first = 0; first < vocab; first += A.piece) {
-            const uint32_t m = static_cast<uint32_t>(std::min<uint64_t>(A.piece, vocab - first));
-            fn(static_cast<uint32_t>(first), m, (m + kTile - 1) / kTile);
-        }
+    if (n <= kSelectFew) {
+        hipLaunchKernelGGL(head_few_kernel, dim3(up64(n)), dim3(256), 0, stream, A);
+    } else {
+        hipLaunchKernelGGL(head_select_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
+        hipLaunchKernelGGL(head_gather_kernel, dim3(std::min(A.tokens_up, 4096u)), dim3(256), 0, stream, A);
+    }
+    const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.piece - 1) / A.piece);
+    const bool grad = A.dhidden || A.dweight, keep = grad && keeps(A.b);
+    uint32_t first = 0, m = 0, tiles = 0, packed = ~0u;
+    // makes piece i the one that the following launches are for
+    auto take = [&](uint32_t i) {
+        first = i * A.piece;
+        m = std::min(A.piece, vocab - first);
+        tiles = (m + kTile - 1) / kTile;
+        if (A.weight && packed != i) hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, 8192u)), dim3(256), 0, stream, A, first, m);
+        packed = i;
     };
-    auto pack = [&](uint32_t first, uint32_t m) {
-        if (A.weight) hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, 8192u)), dim3(256), 0, stream, A, first, m);
-    };
-    pieces([&](uint32_t first, uint32_t m, uint32_t tiles) {
-        pack(first, m);
-        hipLaunchKernelGGL((head_logits_kernel<BF16, BM, false>), dim3(tiles * tiles_m), dim3(kProductThreads), 0, stream, A, first, m);
-    });
-    hipLaunchKernelGGL(head_finish_kernel<BF16>, dim3(n / 4 + 1), dim3(256), 0, stream, A);
-    hipLaunchKernelGGL(head_sum_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A, A.b.loss_scale * (BF16 ? 1.f : 0x1p-14f));
-    if (!A.dhidden && !A.dweight) return hipGetLastError();
-    const bool one = A.piece >= vocab;
-    pieces([&](uint32_t first, uint32_t m, uint32_t tiles) {
-        if (!one) pack(first, m);
-        hipLaunchKernelGGL((head_logits_kernel<BF16, BM, true>), dim3(tiles * tiles_m), dim3(kProductThreads), 0, stream, A, first, m);
-        if (A.dhidden)
-            hipLaunchKernelGGL((head_dhidden_kernel<BF16, BM>), dim3(tiles_m * tiles_d * A.slices), dim3(kProductThreads), 0, stream, A, first, m);
-        if (A.dweight) hipLaunchKernelGGL(head_dweight_kernel<BF16>, dim3(tiles * tiles_d), dim3(kProductThreads), 0, stream, A, first, m);
-    });
-    if (A.dhidden) hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(std::min(n + 1, 4096u)), dim3(256), 0, stream, A);
+    const dim3 threads(kProductThreads);
+    for (uint32_t i = 0; i < n_pieces; i++) {
+        take(i);
+        const dim3 grid(tiles * tiles_m);
+        if (keep && i == n_pieces - 1) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kKeep>), grid, threads, 0, stream, A, first, m);
+        else hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kSums>), grid, threads, 0, stream, A, first, m);
+    }
+    if (keep) {
+        const uint32_t rows = up64(n), wide = std::min((tiles * kTile + 2047) / 2048, (kKeptBlocks + rows - 1) / rows);
+        hipLaunchKernelGGL(head_kept_kernel<BF16>, dim3(rows * wide), dim3(256), 0, stream, A, first, m, wide);
+    } else {
+        hipLaunchKernelGGL(head_finish_kernel<BF16>, dim3(n / 4 + 1), dim3(256), 0, stream, A);
+    }
+    if (n > kFewTokens) hipLaunchKernelGGL(head_sum_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
+    if (!grad) return hipGetLastError();
+    const Sum start = n_pieces == 1 && A.slices == 1 ? kOnly : kFirst;
+    for (uint32_t i = n_pieces; i-- > 0;) {  // from the last one, whose logits and packed rows are at hand
+        take(i);
+        const bool last = i == n_pieces - 1;
+        if (!keep || !last) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kGrad>), dim3(tiles * tiles_m), threads, 0, stream, A, first, m);
+        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight ? tiles * tiles_d : 0;
+        hipLaunchKernelGGL((head_grads_kernel<BF16, BM>), dim3(dh_blocks + dw_blocks), threads, 0, stream, A, first, m, last ? start : kNext, dh_blocks);
+    }
+    if (A.dhidden && start != kOnly) hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(std::min(n + 1, 4096u)), dim3(256), 0, stream, A);
     return hipGetLastError();
 }
 
@@ -532,6 +648,8 @@ hipError_t launch_head(const ff_head_batch& b, float* logp, void* dhidden, uint6
     A.stats = stats;
     A.state = reinterpret_cast<State*>(w + p.state);
     A.index = reinterpret_cast<uint32_t*>(w + p.index);
+    A.weights = reinterpret_cast<float*>(w + p.weights);
+    A.targets = reinterpret_cast<int32_t*>(w + p.targets);
     A.rows = reinterpret_cast<Row*>(w + p.rows);
     A.losses = reinterpret_cast<double*>(w + p.losses);
     A.picked = reinterpret_cast<float*>(w + p.picked);
@@ -539,7 +657,9 @@ hipError_t launch_head(const ff_head_batch& b, float* logp, void* dhidden, uint6
     A.hidden = w + p.hidden;
     A.weight = weight_as_it_is(b) ? nullptr : w + p.weight;
     A.grad = w + p.grad;
+    A.logits = reinterpret_cast<float*>(w + p.logits);
     A.dh = reinterpret_cast<float*>(w + p.dh);
+    A.grad_scale = b.loss_scale * (b.dtype == FF_BF16 ? 1.f : 0x1p-14f);
     if (b.dtype == FF_BF16) return b.n_tokens <= kFewTokens ? launch<true, 64>(A, stream) : launch<true, 256>(A, stream);
     return b.n_tokens <= kFewTokens ? launch<false, 64>(A, stream) : launch<false, 256>(A, stream);
 }
