@@ -434,8 +434,9 @@ int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss,
  * Embedding: out[t] = scale * table[ids[t]], one fp32 product rounded to the format.  table: DEVICE, vocab rows of `width` elements of
  * dtype (FF_BF16, FF_F16 or FF_F32), table_stride >= width elements apart; ids: DEVICE int64; out: DEVICE, n_tokens rows,
  * out_stride >= width apart.  All aligned to their elements.  An id outside [0, vocab), padding, gives a row of zeros.  n_tokens 0:
- * nothing.  Limits: vocab, n_tokens < 2^31, width <= FF_EMBED_MAX_WIDTH.
+ * nothing.  Limits: n_tokens < 2^31, vocab <= FF_EMBED_MAX_VOCAB, width <= FF_EMBED_MAX_WIDTH.
  */
+#define FF_EMBED_MAX_VOCAB (1u << 28)
 #define FF_EMBED_MAX_WIDTH (1u << 24)
 int ff_embed(const void *table, uint64_t vocab, uint64_t width, uint64_t table_stride, uint32_t dtype,
              const int64_t *ids, uint64_t n_tokens, float scale, void *out, uint64_t out_stride,

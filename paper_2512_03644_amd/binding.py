@@ -54,7 +54,8 @@ EXPORTS = ["ff_snapshot_plan", "ff_plan_destroy", "ff_plan_payload_bytes", "ff_p
            "ff_layer_norm_workspace_bytes", "ff_layer_norm_grad", "ff_head_workspace_bytes", "ff_head_loss"]
 
 FF_GRAD_ADD = 1
-FF_EMBED_MAX_WIDTH, FF_NORM_MAX_WIDTH, FF_HEAD_MAX_WIDTH, FF_HEAD_MAX_TOKENS = 1 << 24, 16384, 65536, 1 << 22
+FF_EMBED_MAX_VOCAB, FF_EMBED_MAX_WIDTH, FF_NORM_MAX_WIDTH = 1 << 28, 1 << 24, 16384
+FF_HEAD_MAX_TOKENS, FF_HEAD_MAX_WIDTH = 1 << 22, 65536
 
 
 class ff_segment(ctypes.Structure):

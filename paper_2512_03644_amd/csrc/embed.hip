@@ -5,9 +5,9 @@
 // Gradient: dtable[v] (+)= scale * (sum of dout[t] over the tokens t with id v).  Tokens are sorted by id, and among equal ids
 // by their position, so that a row's sum has one order.  The table's ids are dealt out to workgroups in ranges; each reads all ids,
 // keeps its own in order, and knows from how many it has seen below its range where its part of the sorted list begins: one launch, with
-// no workgroup waiting for another.  Then a wavefront makes 512 elements of a row of the table: the sum of its tokens' rows.  Rows of more than
-// kPart tokens -- frequent words -- are summed in parts first, a wavefront to kPart entries of the sorted list, in 32 bits, and joined in
-// their order.
+// no workgroup waiting for another.  Then the list is cut into parts of equal length, frequent words or not: a wavefront takes 512 elements
+// of the rows of a part's tokens, and writes every sum that begins and ends there.  What reaches over a part's ends is left
+// in the workspace, in 32 bits, and a last launch joins it in its order.
 //
 // What bounds it: memory; few tokens: the launches.
 #include "embed.hpp"
@@ -47,16 +47,16 @@ __global__ __launch_bounds__(kWaveSize * kWaves) void embed_kernel(const EmbedAr
 
 // ---- order of the tokens ------------------------------------------------------------------------------
 
-constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / kWaveSize, kSortRounds = 8;
+constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / kWaveSize, kSortRounds = 16;
 constexpr uint32_t kSortIds = kSortThreads * kSortRounds;  // that a workgroup looks at at once
-constexpr uint32_t kRange = 512;                           // ids of a workgroup
-constexpr uint32_t kPart = 32;                             // entries of the sorted list that are summed by themselves at most
+constexpr uint32_t kRange = 256;                           // ids of a workgroup
 
 struct Sorted {
     uint32_t* begin;  // [vocab + 1] of every id's tokens in the list
     uint32_t* order;  // the list: positions of tokens
     uint32_t* ids;    // and their ids
-    float* parts;     // [2 * parts of the list][width]: sums of long rows' parts
+    float* ends;      // [part of the list][its beginning, its end][width]: sums that reach over it
+    uint32_t part;    // entries of a part
 };
 
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArgs a, const Sorted s)
@@ -77,10 +77,17 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArg
     };
     for (uint32_t i = threadIdx.x; i < kRange; i += kSortThreads) bins[i] = 0;
     __syncthreads();
-    uint32_t below = 0, unused = 0;
-    for (uint64_t t = threadIdx.x; t < n; t += kSortThreads) {
-        const uint32_t b = place(t, below);
-        if (b < kRange) atomicAdd(&bins[b], 1u);
+    // ids of one round: a wavefront's follow each other.  Those of the last round are kept: up to kSortIds tokens are read once
+    uint32_t below = 0, unused = 0, b[kSortRounds];
+    auto look = [&](uint64_t from, uint32_t& low) {
+        const uint64_t t0 = from + wave * (kWaveSize * kSortRounds) + lane;
+        static_for<kSortRounds>([&](auto i) { b[int(i)] = place(t0 + i * kWaveSize, low); });
+    };
+    for (uint64_t from = 0; from < n; from += kSortIds) {
+        look(from, below);
+        static_for<kSortRounds>([&](auto i) {
+            if (b[int(i)] < kRange) atomicAdd(&bins[b[int(i)]], 1u);
+        });
     }
     for (int d = 32; d; d /= 2) below += __shfl_xor(below, d);
     if (lane == 0) below_of[wave] = below;
@@ -105,12 +112,10 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArg
     __syncthreads();
     // the range's tokens, kSortIds ids at a time: in their order into LDS, and from there each behind the last one of its id
     for (uint64_t from = 0; from < n; from += kSortIds) {
-        uint32_t b[kSortRounds], count = 0;
+        uint32_t count = 0;
         const uint64_t t0 = from + wave * (kWaveSize * kSortRounds) + lane;
-        for (uint32_t i = 0; i < kSortRounds; i++) {
-            b[i] = place(t0 + i * kWaveSize, unused);
-            count += __popcll(__ballot(b[i] < kRange));
-        }
+        if (n > kSortIds) look(from, unused);
+        static_for<kSortRounds>([&](auto i) { count += __popcll(__ballot(b[int(i)] < kRange)); });
         if (lane == 0) sums[wave] = count;
         __syncthreads();
         uint32_t at = 0, all = 0;
@@ -118,15 +123,15 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArg
             if (k < wave) at += sums[k];
             all += sums[k];
         }
-        for (uint32_t i = 0; i < kSortRounds; i++) {
-            const uint64_t who = __ballot(b[i] < kRange);
-            if (b[i] < kRange) {
+        static_for<kSortRounds>([&](auto i) {
+            const uint64_t who = __ballot(b[int(i)] < kRange);
+            if (b[int(i)] < kRange) {
                 const uint32_t k = at + __popcll(who & lower);
                 mine_at[k] = static_cast<uint32_t>(t0 + i * kWaveSize);
-                mine_bin[k] = static_cast<uint16_t>(b[i]);
+                mine_bin[k] = static_cast<uint16_t>(b[int(i)]);
             }
             at += __popcll(who);
-        }
+        });
         for (uint32_t first_k = 0; first_k < all; first_k += kSortThreads) {
             for (uint32_t i = threadIdx.x; i < kSortWaves * kRange / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(wave_bins)[i] = 0;
             __syncthreads();  // (and what has been put into LDS is there)
@@ -163,66 +168,117 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArg
 
 // ---- sums -------------------------------------------------------------------------------------------
 
-// The rows of tokens order[from .. to), elements [at, at + 8).
-template <uint32_t DTYPE>
-__device__ __forceinline__ f32x8 sum_of(const EmbedArgs& a, const uint32_t* order, uint32_t from, uint32_t to, uint32_t at)
+// Part c of the list, for a whole wavefront.
+struct Part {
+    const uint32_t *ids, *order;  // of its first entry
+    uint32_t count;
+    bool joins_before, joins_behind;  // its first run begins in front of it, its last one ends behind it
+    __device__ __forceinline__ Part(const Sorted& s, uint32_t c, uint32_t n)
+    {
+        const uint32_t begin = c * s.part;
+        count = n - begin < s.part ? n - begin : s.part;
+        ids = s.ids + begin;
+        order = s.order + begin;
+        joins_before = c && table_entry(s.ids, begin - 1) == id_of(0);
+        joins_behind = begin + count < n && table_entry(s.ids, begin + count) == id_of(count - 1);
+    }
+    __device__ __forceinline__ uint32_t id_of(uint32_t i) const { return table_entry(ids, i); }
+    __device__ __forceinline__ uint32_t token_of(uint32_t i) const { return table_entry(order, i); }
+    // does the run of the last entry begin in the part?
+    __device__ __forceinline__ bool last_begins() const { return !joins_before || id_of(count - 1) != id_of(0); }
+};
+
+// Elements [at, at + 8) of a part's tokens' rows; ADD: sums are added to what is there.
+template <uint32_t DTYPE, bool ADD>
+__device__ __forceinline__ void sum_part(const EmbedArgs& a, const Sorted& s, uint32_t c, uint32_t n, uint32_t at)
 {
     using I = Items<DTYPE>;
     constexpr uint32_t kAhead = 4;
     const uint32_t width = static_cast<uint32_t>(a.width);
+    const Part p(s, c, n);
+    if (at >= width) return;
+    bool begins = !p.joins_before;  // does the run at work begin in this part?
     f32x8 sum = {};
-    auto row = [&](uint32_t k) { return a.rows + static_cast<uint64_t>(order[k]) * a.rows_stride * I::kBytes; };
-    uint32_t k = from;
-    for (; k + kAhead <= to; k += kAhead) {
-        typename I::Held h[kAhead];
-        static_for<kAhead>([&](auto i) { h[int(i)] = I::load(row(k + i), at, width); });
-        static_for<kAhead>([&](auto i) { sum += I::wide(h[int(i)]); });
+    for (uint32_t k = 0; k < p.count; k += kAhead) {
+        typename I::Held h[kAhead], old[kAhead];
+        bool ends[kAhead], whole[kAhead];
+        bool first = begins;
+        static_for<kAhead>([&](auto i) {
+            ends[int(i)] = whole[int(i)] = false;
+            if (k + i >= p.count) return;
+            const uint32_t id = p.id_of(k + i);
+            h[int(i)] = I::load(a.rows + static_cast<uint64_t>(p.token_of(k + i)) * a.rows_stride * I::kBytes, at, width);
+            ends[int(i)] = k + i + 1 == p.count || p.id_of(k + i + 1) != id;
+            whole[int(i)] = ends[int(i)] && first && !(k + i + 1 == p.count && p.joins_behind);
+            if (ADD && whole[int(i)]) old[int(i)] = I::load(a.out + static_cast<uint64_t>(id) * a.out_stride * I::kBytes, at, width);
+            if (ends[int(i)]) first = true;
+        });
+        static_for<kAhead>([&](auto i) {
+            if (k + i >= p.count) return;
+            sum += I::wide(h[int(i)]);
+            if (!ends[int(i)]) return;
+            if (whole[int(i)]) {
+                sum *= a.scale;
+                if (ADD) sum += I::wide(old[int(i)]);
+                I::store(a.out + static_cast<uint64_t>(p.id_of(k + i)) * a.out_stride * I::kBytes, at, width, I::narrow(sum));
+            } else {
+                Items<FF_F32>::store(reinterpret_cast<uint8_t*>(s.ends + (2ull * c + begins) * width), at, width, Items<FF_F32>::narrow(sum));
+            }
+            begins = true;
+            sum = f32x8{};
+        });
     }
-    for (; k < to; k++) sum += I::wide(I::load(row(k), at, width));
-    return sum;
 }
 
-// Entries [kPart * c, kPart * (c + 1)) of the list: what they add to the long rows, of which two at most reach in.
-template <uint32_t DTYPE>
-__global__ __launch_bounds__(kWaveSize* kWaves) void embed_parts_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs)
+// The first `sum_blocks` workgroups: the parts of the list.  The others, unless it is added: zeros into rows without tokens.
+template <uint32_t DTYPE, bool ADD>
+__global__ __launch_bounds__(kWaveSize* kWaves) void embed_sum_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs, const uint32_t sum_blocks)
 {
-    const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width);
-    const uint32_t n = s.begin[vocab], n_parts = (n + kPart - 1) / kPart;
-    const uint64_t total = static_cast<uint64_t>(n_parts) * slabs, step = static_cast<uint64_t>(gridDim.x) * kWaves;
-    for (uint64_t w = static_cast<uint64_t>(blockIdx.x) * kWaves + wave_of(); w < total; w += step) {
-        const uint32_t c = static_cast<uint32_t>(w / slabs), begin = c * kPart, end = begin + kPart < n ? begin + kPart : n;
-        const uint32_t at = static_cast<uint32_t>(w - static_cast<uint64_t>(c) * slabs) * kSlab + threadIdx.x % kWaveSize * kLaneItems;
-        if (at >= width) continue;
-        const uint32_t ids[2] = {s.ids[begin], s.ids[end - 1]};
-        for (int i = 0; i < 2; i++) {
-            if (i && ids[1] == ids[0]) break;
-            const uint32_t from = s.begin[ids[i]], to = s.begin[ids[i] + 1];
-            if (to - from <= kPart) continue;
-            const f32x8 sum = sum_of<DTYPE>(a, s.order, from > begin ? from : begin, to < end ? to : end, at);
-            Items<FF_F32>::store(reinterpret_cast<uint8_t*>(s.parts + (2ull * c + (from >= begin)) * width), at, width, Items<FF_F32>::narrow(sum));
+    using I = Items<DTYPE>;
+    const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width), n = s.begin[vocab];
+    const uint32_t lane_at = threadIdx.x % kWaveSize * kLaneItems;
+    if (blockIdx.x < sum_blocks) {
+        const uint64_t total = static_cast<uint64_t>((n + s.part - 1) / s.part) * slabs, step = static_cast<uint64_t>(sum_blocks) * kWaves;
+        for (uint64_t w = static_cast<uint64_t>(blockIdx.x) * kWaves + wave_of(); w < total; w += step) {
+            const uint32_t c = static_cast<uint32_t>(w / slabs), at = static_cast<uint32_t>(w - static_cast<uint64_t>(c) * slabs) * kSlab + lane_at;
+            sum_part<DTYPE, ADD>(a, s, c, n, at);
+        }
+    } else if (!ADD) {
+        const uint32_t step = (gridDim.x - sum_blocks) * kWaves;
+        for (uint64_t v = (blockIdx.x - sum_blocks) * kWaves + wave_of(); v < vocab; v += step) {
+            if (s.begin[v] != s.begin[v + 1]) continue;
+            for (uint32_t at = lane_at; at < width; at += kSlab) I::store(a.out + v * a.out_stride * I::kBytes, at, width, I::narrow(f32x8{}));
         }
     }
 }
 
-// Rows of the table: all of them, or (ADD) those that tokens have, found at their first entry in the list.
+// Sums that begin in part c and reach over its end.
 template <uint32_t DTYPE, bool ADD>
-__global__ __launch_bounds__(kWaveSize* kWaves) void embed_grad_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs)
+__global__ __launch_bounds__(kWaveSize* kWaves) void embed_join_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs)
 {
     using I = Items<DTYPE>;
     using F = Items<FF_F32>;
-    const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width);
-    const uint64_t total = static_cast<uint64_t>(ADD ? s.begin[vocab] : vocab) * slabs, step = static_cast<uint64_t>(gridDim.x) * kWaves;
+    const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width), n = s.begin[vocab];
+    const uint64_t total = static_cast<uint64_t>((n + s.part - 1) / s.part) * slabs, step = static_cast<uint64_t>(gridDim.x) * kWaves;
     for (uint64_t w = static_cast<uint64_t>(blockIdx.x) * kWaves + wave_of(); w < total; w += step) {
-        const uint32_t which = static_cast<uint32_t>(w / slabs);
-        const uint32_t at = static_cast<uint32_t>(w - static_cast<uint64_t>(which) * slabs) * kSlab + threadIdx.x % kWaveSize * kLaneItems;
-        const uint32_t id = ADD ? s.ids[which] : which, from = s.begin[id], to = s.begin[id + 1];
-        if (at >= width || (ADD && which != from)) continue;
-        f32x8 sum = {};
-        if (to - from <= kPart) {
-            sum = sum_of<DTYPE>(a, s.order, from, to, at);
-        } else {
-            for (uint32_t c = from / kPart; c * kPart < to; c++)
-                sum += F::wide(F::load(reinterpret_cast<const uint8_t*>(s.parts + (2ull * c + (from >= c * kPart)) * width), at, width));
+        const uint32_t c = static_cast<uint32_t>(w / slabs);
+        const uint32_t at = static_cast<uint32_t>(w - static_cast<uint64_t>(c) * slabs) * kSlab + threadIdx.x % kWaveSize * kLaneItems;
+        const Part p(s, c, n);
+        if (!p.joins_behind || !p.last_begins() || at >= width) continue;
+        const uint32_t id = p.id_of(p.count - 1), to = s.begin[id + 1];
+        auto part = [&](uint32_t k, uint32_t which) { return F::wide(F::load(reinterpret_cast<const uint8_t*>(s.ends + (2ull * k + which) * width), at, width)); };
+        f32x8 sum = part(c, 1);
+        const uint32_t last = (to - 1) / s.part;
+        uint32_t k = c + 1;
+        constexpr uint32_t kAhead = 8;
+        for (; k <= last; k += kAhead) {
+            f32x8 x[kAhead];
+            static_for<kAhead>([&](auto i) {
+                if (k + i <= last) x[int(i)] = part(k + i, 0);
+            });
+            static_for<kAhead>([&](auto i) {
+                if (k + i <= last) sum += x[int(i)];
+            });
         }
         sum *= a.scale;
         uint8_t* const out = a.out + static_cast<uint64_t>(id) * a.out_stride * I::kBytes;
@@ -233,35 +289,199 @@ __global__ __launch_bounds__(kWaveSize* kWaves) void embed_grad_kernel(const Emb
 
 uint64_t up(uint64_t x) { return (x + 255) / 256 * 256; }
 
+// ---- few tokens ---------------------------------------------------------------------------------------
+
+// All of it in one launch: a workgroup takes 512 elements of the rows of a range of ids, and finds and sorts the tokens that ask for
+// them in LDS.  A wavefront sums a row's tokens; rows of more than kLong are summed by all wavefronts together.
+constexpr uint32_t kFewThreads = 512, kFewWaves = kFewThreads / kWaveSize, kFewTokens = 4096, kFewRounds = kFewTokens / kFewThreads, kLong = 16, kFewBlocks = 1024;
+
+// Rows of tokens list[from], list[from + step], ... in front of `to`.
+template <uint32_t DTYPE>
+__device__ __forceinline__ f32x8 sum_list(const EmbedArgs& a, const uint16_t* list, uint32_t from, uint32_t to, uint32_t step, uint32_t at)
+{
+    using I = Items<DTYPE>;
+    constexpr uint32_t kAhead = 8;
+    f32x8 sum = {};
+    for (uint32_t k = from; k < to; k += kAhead * step) {
+        typename I::Held h[kAhead];
+        static_for<kAhead>([&](auto i) {
+            if (k + i * step < to) h[int(i)] = I::load(a.rows + list[k + i * step] * a.rows_stride * I::kBytes, at, static_cast<uint32_t>(a.width));
+        });
+        static_for<kAhead>([&](auto i) {
+            if (k + i * step < to) sum += I::wide(h[int(i)]);
+        });
+    }
+    return sum;
+}
+
+template <uint32_t DTYPE, bool ADD>
+__global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs a, const uint32_t slabs, const uint32_t range_ids)
+{
+    using I = Items<DTYPE>;
+    using F = Items<FF_F32>;
+    __shared__ uint32_t begin[kFewThreads + 1], sums[kFewWaves];
+    __shared__ uint16_t token[kFewTokens], bin_of[kFewTokens], order[kFewTokens], wave_bins[kFewWaves][kFewThreads];
+    __shared__ u32x4 joined[kFewWaves][2][kWaveSize];
+    const uint32_t n = static_cast<uint32_t>(a.n_tokens), vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width);
+    const uint32_t wave = wave_of(), lane = threadIdx.x % kWaveSize, block = blockIdx.x / slabs;
+    const uint32_t first = block * range_ids, range = vocab - first < range_ids ? vocab - first : range_ids;
+    const uint32_t at = (blockIdx.x - block * slabs) * kSlab + lane * kLaneItems;
+    const uint64_t lower = (1ull << lane) - 1;
+    // the range's tokens in their order
+    uint32_t b[kFewRounds], count = 0;
+    const uint32_t t0 = wave * (kWaveSize * kFewRounds) + lane;
+    static_for<kFewRounds>([&](auto i) {
+        const uint32_t t = t0 + i * kWaveSize;
+        const uint64_t in = t < n ? static_cast<uint64_t>(a.ids[t]) - first : ~0ull;  // (a negative id is beyond all)
+        b[int(i)] = in < range ? static_cast<uint32_t>(in) : kFewThreads;
+    });
+    static_for<kFewRounds>([&](auto i) { count += __popcll(__ballot(b[int(i)] < kFewThreads)); });
+    if (lane == 0) sums[wave] = count;
+    begin[threadIdx.x] = 0;
+    if (threadIdx.x == 0) begin[kFewThreads] = 0;
+    __syncthreads();
+    uint32_t place = 0, all = 0;
+    for (uint32_t k = 0; k < kFewWaves; k++) {
+        if (k < wave) place += sums[k];
+        all += sums[k];
+    }
+    static_for<kFewRounds>([&](auto i) {
+        const uint64_t who = __ballot(b[int(i)] < kFewThreads);
+        if (b[int(i)] < kFewThreads) {
+            const uint32_t k = place + __popcll(who & lower);
+            token[k] = static_cast<uint16_t>(t0 + i * kWaveSize);
+            bin_of[k] = static_cast<uint16_t>(b[int(i)]);
+            atomicAdd(&begin[b[int(i)]], 1u);
+        }
+        place += __popcll(who);
+    });
+    __syncthreads();
+    // where each id's begin
+    {
+        uint32_t x = begin[threadIdx.x];
+        const uint32_t own = x;
+        for (int d = 1; d < kWaveSize; d *= 2) {
+            const uint32_t y = __shfl_up(x, d);
+            if (lane >= static_cast<uint32_t>(d)) x += y;
+        }
+        if (lane == kWaveSize - 1) sums[wave] = x;
+        __syncthreads();
+        for (uint32_t k = 0; k < wave; k++) x += sums[k];
+        begin[threadIdx.x] = x - own;
+        if (threadIdx.x == kFewThreads - 1) begin[kFewThreads] = x;
+    }
+    // each behind the last one of its id.  (`begin` moves on to the next id's as the list grows)
+    for (uint32_t first_k = 0; first_k < all; first_k += kFewThreads) {
+        for (uint32_t i = threadIdx.x; i < kFewWaves * kFewThreads / 2; i += kFewThreads) reinterpret_cast<uint32_t*>(wave_bins)[i] = 0;
+        __syncthreads();
+        const uint32_t k = first_k + threadIdx.x;
+        const bool on = k < all;
+        const uint32_t bin = on ? bin_of[k] : 0;
+        uint64_t same = __ballot(on);
+        for (uint32_t bit = 1; bit < kFewThreads; bit *= 2) {
+            const uint64_t set = __ballot(bin & bit);
+            same &= bin & bit ? set : ~set;
+        }
+        if (on && (same & lower) == 0) wave_bins[wave][bin] = static_cast<uint16_t>(__popcll(same));
+        __syncthreads();
+        if (on) {
+            uint32_t to = begin[bin] + __popcll(same & lower);
+            for (uint32_t w = 0; w < wave; w++) to += wave_bins[w][bin];
+            order[to] = token[k];
+        }
+        __syncthreads();
+        uint32_t more = 0;
+        for (uint32_t w = 0; w < kFewWaves; w++) more += wave_bins[w][threadIdx.x];
+        begin[threadIdx.x] += more;
+    }
+    __syncthreads();
+    // an id's tokens lie between the end of the one before it and its own
+    auto put = [&](uint32_t id, f32x8 sum, const typename I::Held& old) {
+        sum *= a.scale;
+        if (ADD) sum += I::wide(old);
+        I::store(a.out + static_cast<uint64_t>(first + id) * a.out_stride * I::kBytes, at, width, I::narrow(sum));
+    };
+    auto there = [&](uint32_t id) { return I::load(a.out + static_cast<uint64_t>(first + id) * a.out_stride * I::kBytes, at, width); };
+    bool any_long = false;
+    for (uint32_t id = wave; id < range; id += kFewWaves) {
+        const uint32_t from = id ? begin[id - 1] : 0, to = begin[id];
+        if (to - from > kLong) any_long = true;
+        if (to - from > kLong || (ADD && from == to) || at >= width) continue;
+        typename I::Held old;
+        if (ADD) old = there(id);
+        put(id, sum_list<DTYPE>(a, order, from, to, 1, at), old);
+    }
+    if (!__syncthreads_or(any_long)) return;
+    for (uint32_t id = 0; id < range; id++) {
+        const uint32_t from = id ? begin[id - 1] : 0, to = begin[id];
+        if (to - from <= kLong) continue;
+        f32x8 sum = {};
+        if (at < width) sum = sum_list<DTYPE>(a, order, from + wave, to, kFewWaves, at);
+        const typename F::Held h = F::narrow(sum);
+        joined[wave][0][lane] = h.w[0];
+        joined[wave][1][lane] = h.w[1];
+        __syncthreads();
+        if (wave == 0 && at < width) {
+            typename I::Held old;
+            if (ADD) old = there(id);
+            for (uint32_t k = 1; k < kFewWaves; k++) sum += F::wide(typename F::Held{{joined[k][0][lane], joined[k][1][lane]}});
+            put(id, sum, old);
+        }
+        __syncthreads();
+    }
+}
+
+// Entries of a part: as many as leave work for kPartWaves wavefronts, within limits.
+constexpr uint32_t kPartWaves = 8192, kLeastPart = 8, kMostPart = 32;
+uint32_t part_of(uint64_t n, uint64_t slabs)
+{
+    return static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(n * slabs / kPartWaves, kLeastPart), kMostPart));
+}
+
 struct Places {
-    uint64_t begin, order, ids, parts, bytes;
+    uint64_t begin, order, ids, ends, bytes;
 };
 Places place(uint64_t n, uint64_t vocab, uint64_t width)
 {
     Places p = {};
     p.order = up((vocab + 1) * 4);
     p.ids = p.order + up(n * 4);
-    p.parts = p.ids + up(n * 4);
-    p.bytes = p.parts + (n / kPart + 1) * 2 * width * 4;
+    p.ends = p.ids + up(n * 4);
+    // (both ends of every part; never less for more tokens or elements, whatever the parts come to)
+    const uint64_t parts = (n / kMostPart + 1) * width + std::min<uint64_t>((n / kLeastPart + 1) * width, 2ull * kPartWaves * kSlab);
+    p.bytes = p.ends + parts * 2 * 4;
     return p;
 }
 
 // Workgroups for so many wavefronts' work, several rounds for each where there is much.
 uint32_t groups(uint64_t waves) { return static_cast<uint32_t>(std::max<uint64_t>(1, std::min<uint64_t>((waves + kWaves - 1) / kWaves, 1u << 20))); }
 
+template <uint32_t DTYPE, bool ADD>
+hipError_t launch_grad(const EmbedArgs& a, Sorted s, hipStream_t stream)
+{
+    const uint32_t slabs = static_cast<uint32_t>((a.width + kSlab - 1) / kSlab);
+    if (a.n_tokens <= kFewTokens && (a.vocab / kFewThreads + 1) * slabs <= most_groups(kFewThreads)) {
+        // ranges of 8 to 512 ids, for about kFewBlocks workgroups
+        uint32_t range = 8;
+        while (range < kFewThreads && (a.vocab + range - 1) / range * slabs > kFewBlocks) range *= 2;
+        hipLaunchKernelGGL((embed_few_kernel<DTYPE, ADD>), dim3(static_cast<uint32_t>((a.vocab + range - 1) / range * slabs)), dim3(kFewThreads), 0, stream, a,
+                           slabs, range);
+        return hipGetLastError();
+    }
+    s.part = part_of(a.n_tokens, slabs);
+    const uint64_t n_parts = (a.n_tokens + s.part - 1) / s.part;
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(static_cast<uint32_t>((a.vocab + kRange - 1) / kRange)), dim3(kSortThreads), 0, stream, a, s);
+    const dim3 threads(kWaveSize * kWaves);
+    const uint32_t sum_blocks = groups(n_parts * slabs);
+    hipLaunchKernelGGL((embed_sum_kernel<DTYPE, ADD>), dim3(sum_blocks + (ADD ? 0 : groups(a.vocab))), threads, 0, stream, a, s, slabs, sum_blocks);
+    if (n_parts > 1) hipLaunchKernelGGL((embed_join_kernel<DTYPE, ADD>), dim3(groups(n_parts * slabs)), threads, 0, stream, a, s, slabs);
+    return hipGetLastError();
+}
+
 template <uint32_t DTYPE>
 hipError_t launch_grad(const EmbedArgs& a, bool add, const Sorted& s, hipStream_t stream)
 {
-    const uint32_t slabs = static_cast<uint32_t>((a.width + kSlab - 1) / kSlab);
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(static_cast<uint32_t>((a.vocab + kRange - 1) / kRange)), dim3(kSortThreads), 0, stream, a, s);
-    const dim3 threads(kWaveSize * kWaves);
-    if (a.n_tokens > kPart)
-        hipLaunchKernelGGL(embed_parts_kernel<DTYPE>, dim3(groups((a.n_tokens / kPart + 1) * slabs)), threads, 0, stream, a, s, slabs);
-    if (add)
-        hipLaunchKernelGGL((embed_grad_kernel<DTYPE, true>), dim3(groups(a.n_tokens * slabs)), threads, 0, stream, a, s, slabs);
-    else
-        hipLaunchKernelGGL((embed_grad_kernel<DTYPE, false>), dim3(groups(a.vocab * slabs)), threads, 0, stream, a, s, slabs);
-    return hipGetLastError();
+    return add ? launch_grad<DTYPE, true>(a, s, stream) : launch_grad<DTYPE, false>(a, s, stream);
 }
 
 }  // namespace
@@ -285,7 +505,7 @@ hipError_t launch_embed_grad(const EmbedArgs& a, uint32_t dtype, bool add, void*
     const Places p = place(a.n_tokens, a.vocab, a.width);
     uint8_t* const w = static_cast<uint8_t*>(workspace);
     const Sorted s = {reinterpret_cast<uint32_t*>(w + p.begin), reinterpret_cast<uint32_t*>(w + p.order), reinterpret_cast<uint32_t*>(w + p.ids),
-                      reinterpret_cast<float*>(w + p.parts)};
+                      reinterpret_cast<float*>(w + p.ends), 0};
     if (dtype == FF_BF16) return launch_grad<FF_BF16>(a, add, s, stream);
     if (dtype == FF_F16) return launch_grad<FF_F16>(a, add, s, stream);
     return launch_grad<FF_F32>(a, add, s, stream);

@@ -461,9 +461,17 @@ __global__ __launch_bounds__(256) void head_put_kernel(const HeadArgs A)
     for (uint32_t r = blockIdx.x; r < used; r += gridDim.x) {
         uint8_t* const out = A.dhidden + A.index[r] * A.dhidden_stride * 2;
         for (uint32_t d = 4 * threadIdx.x; d < width; d += 4 * blockDim.x) {
+            constexpr uint32_t kAhead = 8;
             f32x4 s = {0, 0, 0, 0};
-            for (uint32_t k = 0; k < A.slices; k++)
-                s += *(const FF_GLOBAL f32x4*)(A.dh + (static_cast<uint64_t>(k) * A.tokens_up + r) * width_up + d);
+            for (uint32_t k = 0; k < A.slices; k += kAhead) {
+                f32x4 x[kAhead];
+                static_for<kAhead>([&](auto i) {
+                    if (k + i < A.slices) x[int(i)] = *(const FF_GLOBAL f32x4*)(A.dh + (static_cast<uint64_t>(k + i) * A.tokens_up + r) * width_up + d);
+                });
+                static_for<kAhead>([&](auto i) {
+                    if (k + i < A.slices) s += x[int(i)];
+                });
+            }
             put4<BF16>(out, d, width, s * scale);
         }
     }

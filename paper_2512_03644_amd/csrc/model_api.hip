@@ -25,7 +25,7 @@ int check_embed(const void* rows, uint64_t rows_stride, uint32_t dtype, const in
                 float scale, const void* out, uint64_t out_stride, bool add, bool gradient)
 {
     const uint32_t size = element_size(dtype);
-    if (!size || !vocab || vocab > kMost || !width || width > FF_EMBED_MAX_WIDTH || n_tokens > kMost || !std::isfinite(scale)) return FF_ERR_INVALID;
+    if (!size || !vocab || vocab > FF_EMBED_MAX_VOCAB || !width || width > FF_EMBED_MAX_WIDTH || n_tokens > kMost || !std::isfinite(scale)) return FF_ERR_INVALID;
     if (n_tokens && (!rows || !ids)) return FF_ERR_NULL;
     if ((n_tokens || (gradient && !add)) && !out) return FF_ERR_NULL;
     if (!aligned(rows, size) || !aligned(out, size) || !aligned(ids, 8)) return FF_ERR_INVALID;

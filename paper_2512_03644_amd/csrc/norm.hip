@@ -17,7 +17,9 @@ namespace ffsnap {
 namespace {
 
 constexpr int kBlock = 256;             // threads of a workgroup whose wavefronts take rows of their own
-constexpr uint32_t kMostGroups = 1024;  // that leave parts of dw and db
+constexpr uint32_t kForwardBlocks = 2048;
+constexpr uint32_t kMostBlocks = 512;   // of the backward pass, each of which leaves a part of dw and db
+constexpr uint32_t kFewRows = 1024;     // up to so many, dw and db are summed straight from the rows
 
 template <int GROUP>
 constexpr int block_of()
@@ -53,6 +55,16 @@ __device__ __forceinline__ f32x8 cut(f32x8 v, uint32_t at, uint32_t width)
     return v;
 }
 
+// fn(i, at) for the thread's K places in a row.
+template <int GROUP, int K, class Fn>
+__device__ __forceinline__ void places(uint32_t thread, uint32_t width, Fn&& fn)
+{
+    static_for<K>([&](auto i) {
+        const uint32_t at = (i * GROUP + thread) * kLaneItems;
+        if (at < width) fn(i, at);
+    });
+}
+
 template <uint32_t DTYPE, int GROUP, int K>
 __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs a)
 {
@@ -61,39 +73,37 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
     const uint32_t width = static_cast<uint32_t>(a.width), thread = threadIdx.x % GROUP;
     const float each = 1.f / static_cast<float>(width);
     const uint64_t step = static_cast<uint64_t>(gridDim.x) * kPer;
+    typename I::Held w[K], b[K], h[K], next[K];
+    auto fetch = [&](typename I::Held (&to)[K], uint64_t r) {
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) { to[int(i)] = I::load(a.x + r * a.x_stride * I::kBytes, at, width); });
+    };
+    uint64_t r = static_cast<uint64_t>(blockIdx.x) * kPer + threadIdx.x / GROUP;
+    if (r < a.n_rows) fetch(next, r);
+    places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+        w[int(i)] = I::load(a.weight, at, width);
+        if (a.bias) b[int(i)] = I::load(a.bias, at, width);
+    });
     int turn = 0;
-    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * kPer + threadIdx.x / GROUP; r < a.n_rows; r += step) {
-        const uint8_t* const row = a.x + r * a.x_stride * I::kBytes;
-        typename I::Held h[K];
+    for (; r < a.n_rows; r += step) {
+        static_for<K>([&](auto i) { h[int(i)] = next[int(i)]; });
+        if (r + step < a.n_rows) fetch(next, r + step);
         float s[1] = {0.f};
-        static_for<K>([&](auto i) {
-            const uint32_t at = (i * GROUP + thread) * kLaneItems;
-            if (at < width) {
-                h[int(i)] = I::load(row, at, width);
-                s[0] += sum8(I::wide(h[int(i)]));
-            }
-        });
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t) { s[0] += sum8(I::wide(h[int(i)])); });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
         const float mean = s[0] * each;
         s[0] = 0.f;
-        static_for<K>([&](auto i) {
-            const uint32_t at = (i * GROUP + thread) * kLaneItems;
-            if (at < width) {
-                const f32x8 d = cut(I::wide(h[int(i)]) - mean, at, width);
-                s[0] += sum8(d * d);
-            }
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+            const f32x8 d = cut(I::wide(h[int(i)]) - mean, at, width);
+            s[0] += sum8(d * d);
         });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
         const float rstd = 1.f / sqrtf(s[0] * each + a.eps);
-        static_for<K>([&](auto i) {
-            const uint32_t at = (i * GROUP + thread) * kLaneItems;
-            if (at < width) {
-                f32x8 y = (I::wide(h[int(i)]) - mean) * rstd * I::wide(I::load(a.weight, at, width));
-                if (a.bias) y += I::wide(I::load(a.bias, at, width));
-                I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(y));
-            }
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+            f32x8 y = (I::wide(h[int(i)]) - mean) * rstd * I::wide(w[int(i)]);
+            if (a.bias) y += I::wide(b[int(i)]);
+            I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(y));
         });
         if (thread == 0) {
             if (a.mean) a.mean[r] = mean;
@@ -102,81 +112,146 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
     }
 }
 
-template <uint32_t DTYPE, int GROUP, int K>
-__global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const NormArgs a)
+// 32 columns of dw and db, from all rows.
+constexpr uint32_t kColumns = 32;
+template <uint32_t DTYPE, int THREADS>
+__device__ __forceinline__ void columns(const NormArgs& a, const uint32_t block)
 {
     using I = Items<DTYPE>;
+    constexpr uint32_t kAcross = THREADS / kColumns, kAhead = 8;
+    __shared__ float part[2][kAcross][kColumns + 1];
+    const uint32_t width = static_cast<uint32_t>(a.width), n = static_cast<uint32_t>(a.n_rows), c = threadIdx.x % kColumns, k = threadIdx.x / kColumns;
+    const uint32_t at = block * kColumns + c;
+    float dw = 0.f, db = 0.f;
+    if (at < width)
+        for (uint32_t first = k; first < n; first += kAcross * kAhead) {
+            float x[kAhead], dy[kAhead], mean[kAhead], rstd[kAhead];
+            static_for<kAhead>([&](auto i) {
+                const uint64_t r = first + i * kAcross < n ? first + i * kAcross : k;
+                x[int(i)] = I::one(a.x + (r * a.x_stride + at) * I::kBytes);
+                dy[int(i)] = I::one(a.dy + (r * a.dy_stride + at) * I::kBytes);
+                mean[int(i)] = a.mean[r];
+                rstd[int(i)] = a.rstd[r];
+            });
+            static_for<kAhead>([&](auto i) {
+                if (first + i * kAcross >= n) return;
+                dw += dy[int(i)] * ((x[int(i)] - mean[int(i)]) * rstd[int(i)]);
+                db += dy[int(i)];
+            });
+        }
+    part[0][k][c] = dw;
+    part[1][k][c] = db;
+    __syncthreads();
+    if (k >= 2 || at >= width) return;
+    uint8_t* const out = k ? a.dbias : a.dweight;
+    if (!out) return;
+    float s = 0.f;
+    for (uint32_t i = 0; i < kAcross; i++) s += part[k][i][c];
+    I::put(out + static_cast<uint64_t>(at) * I::kBytes, s);
+}
+
+// `column_blocks` workgroups behind the others make dw and db; with none of them, the rows' groups leave their parts.
+template <uint32_t DTYPE, int GROUP, int K>
+__global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const NormArgs a, const uint32_t column_blocks)
+{
+    using I = Items<DTYPE>;
+    const uint32_t blocks = gridDim.x - column_blocks;
+    if (blockIdx.x >= blocks) {
+        columns<DTYPE, block_of<GROUP>()>(a, blockIdx.x - blocks);
+        return;
+    }
     constexpr uint32_t kPer = block_of<GROUP>() / GROUP;
     const uint32_t width = static_cast<uint32_t>(a.width), thread = threadIdx.x % GROUP;
     const float each = 1.f / static_cast<float>(width);
     const uint32_t group = blockIdx.x * kPer + threadIdx.x / GROUP;
-    const uint64_t step = static_cast<uint64_t>(gridDim.x) * kPer;
+    const uint64_t step = static_cast<uint64_t>(blocks) * kPer;
     typename I::Held w[K];
     f32x8 dw[K], db[K];
-    static_for<K>([&](auto i) {
-        const uint32_t at = (i * GROUP + thread) * kLaneItems;
-        if (at < width) w[int(i)] = I::load(a.weight, at, width);
-        dw[int(i)] = db[int(i)] = f32x8{};
-    });
-    int turn = 0;
-    for (uint64_t r = group; r < a.n_rows; r += step) {
-        const uint8_t *const row = a.x + r * a.x_stride * I::kBytes, *const grad = a.dy + r * a.dy_stride * I::kBytes;
-        const float mean = a.mean[r], rstd = a.rstd[r];
+    struct Row {
         typename I::Held x[K], dy[K];
-        static_for<K>([&](auto i) {
-            const uint32_t at = (i * GROUP + thread) * kLaneItems;
-            if (at < width) {
-                x[int(i)] = I::load(row, at, width);
-                dy[int(i)] = I::load(grad, at, width);
-            }
+        float mean, rstd;
+    } next;
+    auto fetch = [&](Row& to, uint64_t r) {
+        to.mean = a.mean[r];
+        to.rstd = a.rstd[r];
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+            to.x[int(i)] = I::load(a.x + r * a.x_stride * I::kBytes, at, width);
+            to.dy[int(i)] = I::load(a.dy + r * a.dy_stride * I::kBytes, at, width);
         });
+    };
+    uint64_t r = group;
+    if (r < a.n_rows) fetch(next, r);
+    places<GROUP, K>(thread, width, [&](auto i, uint32_t at) { w[int(i)] = I::load(a.weight, at, width); });
+    static_for<K>([&](auto i) { dw[int(i)] = db[int(i)] = f32x8{}; });
+    int turn = 0;
+    constexpr bool kAhead = GROUP * K <= 1024;  // the next row while this one is at work, where there are registers for it
+    for (; r < a.n_rows; r += step) {
+        const Row now = next;
+        if (kAhead && r + step < a.n_rows) fetch(next, r + step);
         float s[2] = {0.f, 0.f};
-        static_for<K>([&](auto i) {
-            const uint32_t at = (i * GROUP + thread) * kLaneItems;
-            if (at < width) {
-                const f32x8 normed = (I::wide(x[int(i)]) - mean) * rstd, d = I::wide(dy[int(i)]), g = d * I::wide(w[int(i)]);
-                s[0] += sum8(g);
-                s[1] += sum8(g * normed);
-                dw[int(i)] += d * normed;
-                db[int(i)] += d;
-            }
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t) {
+            const f32x8 normed = (I::wide(now.x[int(i)]) - now.mean) * now.rstd, d = I::wide(now.dy[int(i)]), g = d * I::wide(w[int(i)]);
+            s[0] += sum8(g);
+            s[1] += sum8(g * normed);
+            dw[int(i)] += d * normed;
+            db[int(i)] += d;
         });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
         const float c0 = s[0] * each, c1 = s[1] * each;
-        static_for<K>([&](auto i) {
-            const uint32_t at = (i * GROUP + thread) * kLaneItems;
-            if (at < width) {
-                const f32x8 normed = (I::wide(x[int(i)]) - mean) * rstd, g = I::wide(dy[int(i)]) * I::wide(w[int(i)]);
-                I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(rstd * (g - c0 - normed * c1)));
-            }
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+            const f32x8 normed = (I::wide(now.x[int(i)]) - now.mean) * now.rstd, g = I::wide(now.dy[int(i)]) * I::wide(w[int(i)]);
+            I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(now.rstd * (g - c0 - normed * c1)));
         });
+        if (!kAhead && r + step < a.n_rows) fetch(next, r + step);
     }
-    if (!a.dweight && !a.dbias) return;
-    uint8_t* const out = reinterpret_cast<uint8_t*>(a.parts + 2ull * group * width);
-    static_for<K>([&](auto i) {
-        const uint32_t at = (i * GROUP + thread) * kLaneItems;
-        if (at < width) {
-            Items<FF_F32>::store(out, at, width, Items<FF_F32>::narrow(dw[int(i)]));
-            Items<FF_F32>::store(out + 4ull * width, at, width, Items<FF_F32>::narrow(db[int(i)]));
+    if (column_blocks || (!a.dweight && !a.dbias)) return;
+    if constexpr (kPer > 1) {  // the workgroup's groups into one, in their order
+        __shared__ f32x8 both[2 * K][GROUP];
+        for (uint32_t g = kPer - 1; g > 0; g--) {
+            if (threadIdx.x / GROUP == g)
+                static_for<K>([&](auto i) {
+                    both[2 * i][thread] = dw[int(i)];
+                    both[2 * i + 1][thread] = db[int(i)];
+                });
+            __syncthreads();
+            if (threadIdx.x / GROUP == g - 1)
+                static_for<K>([&](auto i) {
+                    dw[int(i)] += both[2 * i][thread];
+                    db[int(i)] += both[2 * i + 1][thread];
+                });
+            __syncthreads();
         }
+        if (threadIdx.x >= GROUP) return;
+    }
+    uint8_t* const out = reinterpret_cast<uint8_t*>(a.parts + 2ull * blockIdx.x * width);
+    places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+        Items<FF_F32>::store(out, at, width, Items<FF_F32>::narrow(dw[int(i)]));
+        Items<FF_F32>::store(out + 4ull * width, at, width, Items<FF_F32>::narrow(db[int(i)]));
     });
 }
 
-// Columns of dw (blockIdx.y 0) and db (1): the parts of all groups.
-constexpr uint32_t kColumns = 64, kJoinRows = 16;
+// Columns of dw (blockIdx.y 0) and db (1): the parts of all workgroups.
+constexpr uint32_t kJoinRows = 32, kJoinAhead = 8;
 template <uint32_t DTYPE>
-__global__ __launch_bounds__(kColumns* kJoinRows) void norm_join_kernel(const NormArgs a, const uint32_t groups)
+__global__ __launch_bounds__(kColumns* kJoinRows) void norm_join_kernel(const NormArgs a, const uint32_t blocks)
 {
     using I = Items<DTYPE>;
-    __shared__ float part[kJoinRows][kColumns];
+    __shared__ float part[kJoinRows][kColumns + 1];
     uint8_t* const out = blockIdx.y ? a.dbias : a.dweight;
     const uint32_t width = static_cast<uint32_t>(a.width), c = threadIdx.x % kColumns, k = threadIdx.x / kColumns;
     const uint32_t at = blockIdx.x * kColumns + c;
     if (!out) return;
     float s = 0.f;
     if (at < width)
-        for (uint32_t g = k; g < groups; g += kJoinRows) s += as_global(a.parts)[(2ull * g + blockIdx.y) * width + at];
+        for (uint32_t g = k; g < blocks; g += kJoinRows * kJoinAhead) {
+            float x[kJoinAhead];
+            static_for<kJoinAhead>([&](auto i) {
+                const uint32_t row = g + i * kJoinRows;
+                x[int(i)] = row < blocks ? as_global(a.parts)[(2ull * row + blockIdx.y) * width + at] : 0.f;
+            });
+            static_for<kJoinAhead>([&](auto i) { s += x[int(i)]; });
+        }
     part[k][c] = s;
     __syncthreads();
     if (k || at >= width) return;
@@ -190,23 +265,22 @@ void choose(uint64_t width, Fn&& fn)
 {
     using std::integral_constant;
     if (width <= 512) fn(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (width <= 1024) fn(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     else if (width <= 2048) fn(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (width <= 4096) fn(integral_constant<int, 256>{}, integral_constant<int, 2>{});
     else if (width <= 8192) fn(integral_constant<int, 512>{}, integral_constant<int, 2>{});
     else fn(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 
-// Workgroups of the backward pass, and the groups in them.
-uint32_t grad_groups(uint64_t n_rows, uint64_t width, uint32_t* blocks)
+// Workgroups of the backward pass.
+uint32_t grad_blocks(uint64_t n_rows, uint64_t width)
 {
-    uint32_t groups = 0;
+    uint32_t blocks = 0;
     choose(width, [&](auto group, auto) {
         constexpr uint32_t per = block_of<group>() / group;
-        *blocks = static_cast<uint32_t>(std::min<uint64_t>((n_rows + per - 1) / per, kMostGroups / per));
-        *blocks = std::max(*blocks, 1u);
-        groups = *blocks * per;
+        blocks = static_cast<uint32_t>(std::max<uint64_t>(std::min<uint64_t>((n_rows + per - 1) / per, kMostBlocks), 1));
     });
-    return groups;
+    return blocks;
 }
 
 template <uint32_t DTYPE>
@@ -215,7 +289,7 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
     choose(a.width, [&](auto group, auto k) {
         constexpr int threads = block_of<group>();
         constexpr uint32_t per = threads / group;
-        const uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>((a.n_rows + per - 1) / per, 1u << 20));
+        const uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>((a.n_rows + per - 1) / per, kForwardBlocks));
         hipLaunchKernelGGL((norm_kernel<DTYPE, group, k>), dim3(blocks), dim3(threads), 0, stream, a);
     });
     return hipGetLastError();
@@ -224,13 +298,13 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
 template <uint32_t DTYPE>
 hipError_t backward(const NormArgs& a, hipStream_t stream)
 {
-    uint32_t blocks, groups = grad_groups(a.n_rows, a.width, &blocks);
+    const uint32_t blocks = grad_blocks(a.n_rows, a.width);
+    const bool sums = a.dweight || a.dbias, few = a.n_rows <= kFewRows;
+    const uint32_t all = static_cast<uint32_t>((a.width + kColumns - 1) / kColumns), column_blocks = sums && few ? all : 0;
     choose(a.width, [&](auto group, auto k) {
-        hipLaunchKernelGGL((norm_grad_kernel<DTYPE, group, k>), dim3(blocks), dim3(block_of<group>()), 0, stream, a);
+        hipLaunchKernelGGL((norm_grad_kernel<DTYPE, group, k>), dim3(blocks + column_blocks), dim3(block_of<group>()), 0, stream, a, column_blocks);
     });
-    if (a.dweight || a.dbias)
-        hipLaunchKernelGGL(norm_join_kernel<DTYPE>, dim3(static_cast<uint32_t>((a.width + kColumns - 1) / kColumns), 2), dim3(kColumns * kJoinRows), 0, stream,
-                           a, groups);
+    if (sums && !few) hipLaunchKernelGGL(norm_join_kernel<DTYPE>, dim3(all, 2), dim3(kColumns * kJoinRows), 0, stream, a, blocks);
     return hipGetLastError();
 }
 
@@ -238,8 +312,7 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
 
 uint64_t norm_workspace(uint64_t n_rows, uint64_t width)
 {
-    uint32_t blocks;
-    return grad_groups(n_rows, width, &blocks) * 8ull * width;
+    return grad_blocks(n_rows, width) * 8ull * width;
 }
 
 hipError_t launch_norm(const NormArgs& a, uint32_t dtype, hipStream_t stream)

@@ -18,7 +18,7 @@ struct NormArgs {
     const uint8_t* dy;
     uint64_t dy_stride;
     uint8_t *dweight, *dbias;  // or null
-    float* parts;              // [group][dweight, dbias][width]
+    float* parts;              // [workgroup][dweight, dbias][width]
 };
 
 uint64_t norm_workspace(uint64_t n_rows, uint64_t width);

@@ -29,7 +29,7 @@ def test_embedding_refuses_bad_arguments():
     for f, names in ((look, ("table", "ids", "out")), (grad, ("dout", "ids", "dtable", "ws"))):
         for name in names:
             assert f(**{name: None}) == ff.FF_ERR_NULL, name
-        for bad in (dict(dtype=0), dict(dtype=4), dict(vocab=0), dict(vocab=BIG), dict(width=0), dict(width=ff.FF_EMBED_MAX_WIDTH + 1, stride=1 << 30, out_stride=1 << 30),
+        for bad in (dict(dtype=0), dict(dtype=4), dict(vocab=0), dict(vocab=ff.FF_EMBED_MAX_VOCAB + 1), dict(width=0), dict(width=ff.FF_EMBED_MAX_WIDTH + 1, stride=1 << 30, out_stride=1 << 30),
                     dict(n=BIG), dict(stride=7), dict(out_stride=7), dict(stride=(1 << 40) + 1), dict(out_stride=1 << 60), dict(scale=INF), dict(scale=NAN),
                     {names[0]: A16 + 1}, {names[1]: A16 + 4}, {names[2]: A16 + 1}, {names[0]: A16 + 2, "dtype": ff.FF_F32}, {names[2]: A16 + 2, "dtype": ff.FF_F32}):
             assert f(**bad) == ff.FF_ERR_INVALID, bad
