@@ -507,6 +507,7 @@ typedef struct {
  * -- 8 bytes for every token and 256 entries of the vocabulary, 2 to 6 for every element of the hidden states -- and, for a piece of the vocabulary
  * at a time, up to 1.5 GiB, or 0.5 more where rows of `weight` are copied; without gradients those 0.5 alone. */
 #define FF_HEAD_MAX_TOKENS (1u << 22)
+#define FF_HEAD_MAX_VOCAB (1u << 22)
 #define FF_HEAD_MAX_WIDTH 65536u
 uint64_t ff_head_workspace_bytes(const ff_head_batch *b, uint32_t gradient);
 

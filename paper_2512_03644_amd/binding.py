@@ -55,7 +55,7 @@ EXPORTS = ["ff_snapshot_plan", "ff_plan_destroy", "ff_plan_payload_bytes", "ff_p
 
 FF_GRAD_ADD = 1
 FF_EMBED_MAX_VOCAB, FF_EMBED_MAX_WIDTH, FF_NORM_MAX_WIDTH = 1 << 28, 1 << 24, 16384
-FF_HEAD_MAX_TOKENS, FF_HEAD_MAX_WIDTH = 1 << 22, 65536
+FF_HEAD_MAX_TOKENS, FF_HEAD_MAX_VOCAB, FF_HEAD_MAX_WIDTH = 1 << 22, 1 << 22, 65536
 
 
 class ff_segment(ctypes.Structure):

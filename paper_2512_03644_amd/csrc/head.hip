@@ -22,7 +22,8 @@ namespace ffsnap {
 namespace {
 
 constexpr uint32_t kTile = 256;        // vocabulary entries of a tile
-constexpr uint32_t kFewTokens = 64;    // up to so many, tiles are 64 tokens high
+constexpr uint32_t kFewTokens = 64;    // up to so many, G is made of the whole vocabulary at once
+constexpr uint32_t kComputeUnits = 256;
 constexpr float kLog2E = 0x1.715476p+0f;
 
 constexpr uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
@@ -57,16 +58,17 @@ struct HeadArgs {
     Row* rows;
     double* losses;     // of each of them, times its weight
     float* picked;      // logit of the target
-    float2* parts;      // [token][tile]: largest logit, sum of exponentials
+    float2* parts;      // [token][tile]: largest logit times log2(e), sum of exponentials against it
     uint8_t* hidden;    // packed rows of those tokens: `stride` bytes, zeros behind the width and behind the last up to 64 rows
     uint8_t* weight;    // packed rows of a piece, if W's own do not lie as the loads want them; or null
     uint8_t* grad;      // G of a piece: [tokens up to a tile][piece]
     float* logits;      // [token][piece]: of the last piece, if they are kept
     float* dh;          // [slice][token][width up to 64]: dH so far
     uint32_t tokens_up; // tokens, up to a whole tile
-    uint32_t tiles;     // of the vocabulary
+    uint32_t tiles;     // of the vocabulary: parts of a token's sums
     uint32_t stride;    // bytes of a packed row
-    uint32_t piece;     // vocabulary entries of a piece, a multiple of 256
+    uint32_t piece;     // vocabulary entries that G has, a multiple of 256
+    uint32_t step;      // and that the gradients' products take at once
     uint32_t slices;    // of dH's sum over a piece
     float grad_scale;   // loss scale, and what G is too large by
 };
@@ -137,20 +139,20 @@ __device__ __forceinline__ uint32_t select(const HeadArgs& A, uint32_t* index, b
 constexpr int kSelectThreads = 1024;
 __global__ __launch_bounds__(kSelectThreads) void head_select_kernel(const HeadArgs A) { select<kSelectThreads>(A, A.index, true); }
 
-// `width` elements of a row to a packed one; elements behind them are zeros.
+// Elements [at, at + 8) of a row of `width`, zeros behind it.
+__device__ __forceinline__ u32x4 load8(const uint8_t* row, uint32_t at, uint32_t width)
+{
+    if (at + 8 <= width) return *(const FF_GLOBAL u32x4_a2*)(row + 2ull * at);
+    uint32_t x[8] = {};
+    for (uint32_t k = 0; k < 8; k++)
+        if (at + k < width) x[k] = as_global(reinterpret_cast<const uint16_t*>(row))[at + k];
+    return u32x4{x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
+}
+
+// `width` elements of a row to a packed one of `bytes`; elements behind them are zeros.
 __device__ __forceinline__ void copy_row(uint8_t* to, uint32_t bytes, const uint8_t* from, uint32_t width)
 {
-    for (uint32_t i = threadIdx.x; i < bytes / 16; i += blockDim.x) {
-        u32x4 v = {0, 0, 0, 0};
-        if (i * 8 + 8 <= width) {
-            v = *(const FF_GLOBAL u32x4_a2*)(from + 16ull * i);
-        } else {
-            uint16_t x[8] = {};
-            for (uint32_t k = i * 8; k < width; k++) x[k % 8] = as_global(reinterpret_cast<const uint16_t*>(from))[k];
-            v = u32x4{x[0] | uint32_t(x[1]) << 16, x[2] | uint32_t(x[3]) << 16, x[4] | uint32_t(x[5]) << 16, x[6] | uint32_t(x[7]) << 16};
-        }
-        *(FF_GLOBAL u32x4*)(to + 16ull * i) = v;
-    }
+    for (uint32_t i = threadIdx.x; i < bytes / 16; i += blockDim.x) *(FF_GLOBAL u32x4*)(to + 16ull * i) = load8(from, i * 8, width);
 }
 
 // Hidden states of the tokens that count, one behind the other, and zeros up to 64 rows; gradients of the other tokens.
@@ -200,6 +202,54 @@ __device__ __forceinline__ float gradient(float z, uint32_t v, uint32_t vocab, c
 
 // ---- logits ---------------------------------------------------------------------------------------
 
+// For a token's N logits of each of the four lanes that have its row, entries of the vocabulary v + 16 j + e: the target's logit is put down,
+// those behind the vocabulary are left out, and the largest, times log2(e), and the sum of exponentials against it come back to all four.
+template <int N>
+__device__ __forceinline__ float2 join_lanes(const HeadArgs& A, f32x4 (&z)[N], const uint32_t t, const uint32_t v, const int32_t y)
+{
+    const uint32_t vocab = static_cast<uint32_t>(A.b.vocab), in = static_cast<uint32_t>(y) - v;
+    if (__any(in < 16 * N)) {  // (the target is in few of the tiles)
+#pragma unroll
+        for (int j = 0; j < N; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (in == 16u * j + e) A.picked[t] = z[j][e];
+    }
+    if (__any(v + 16 * N > vocab)) {
+#pragma unroll
+        for (int j = 0; j < N; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) z[j][e] = v + 16 * j + e < vocab ? z[j][e] : -INFINITY;
+    }
+    // (a NaN or +inf stays in the sum, as exp(NaN - top) or exp(inf - inf))
+    float top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; j++) top = fmaxf(fmaxf(top, fmaxf(z[j][0], z[j][1])), fmaxf(z[j][2], z[j][3]));
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    // Terms are 2^(z log2(e) - c), c = top log2(e) in 24 bits: one operation in front of the exponential, and c stands for the part from here on.
+    const float c = top * kLog2E, against = top == -INFINITY ? 0.f : c;
+#pragma unroll
+    for (int j = 0; j < N; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) total += __builtin_amdgcn_exp2f(fmaf(z[j][e], kLog2E, -against));
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    return {c, total};
+}
+// Parts of several wavefronts.
+template <int N>
+__device__ __forceinline__ float2 join_parts(const float2 (&p)[N])
+{
+    float c = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; k++) c = fmaxf(c, p[k].x);
+    const float against = c == -INFINITY ? 0.f : c;
+#pragma unroll
+    for (int k = 0; k < N; k++) total += p[k].y * __builtin_amdgcn_exp2f(p[k].x - against);
+    return {c, total};
+}
+
 // The tiles of vocabulary entries [first, first + n): their parts of the sums, with kKeep the logits as well; or G.
 enum Mode { kSums, kKeep, kGrad };
 template <bool BF16, int BM, Mode MODE>
@@ -226,65 +276,119 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;                    // + 16 i
     const uint32_t v = v0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);              // + 16 j + e
     if constexpr (MODE == kGrad) {
-        const uint32_t at = v - first;
-        for (int i = 0; i < S::kM; i++) {
-            const uint32_t t = m + 16 * i;
-            Row r = {0.f, 0.f, 0.f, -1};
-            if (t < used) r = A.rows[t];
-            const bool there = t < used;
-            uint8_t* const out = A.grad + (static_cast<uint64_t>(t) * A.piece + at) * 2;
-            for (int j = 0; j < S::kN; j++) {
+        const uint32_t row0 = m - lane % 16, at = v - 4 * (lane / 16) - first;
+        Row rows[S::kM];
+        static_for<S::kM>([&](auto i) {
+            rows[int(i)] = {0.f, 0.f, 0.f, -1};
+            if (m + 16 * i < used) rows[int(i)] = A.rows[m + 16 * i];
+        });
+        RowsByLds<S::kM, S::kN>::pass(
+            (FF_LDS uint8_t*)lds,
+            [&](auto i, auto j) {
                 f32x4 g;
-                for (int e = 0; e < 4; e++) {
-                    const float x = gradient(z[i][j][e], v + 16 * j + e, vocab, r);
-                    g[e] = there ? x : 0.f;
-                }
-                *(FF_GLOBAL u32x2*)(out + 32 * j) = to_half<BF16>(g);
-            }
-        }
+                static_for<4>([&](auto e) {
+                    const float x = gradient(z[int(i)][int(j)][int(e)], v + 16 * j + e, vocab, rows[int(i)]);
+                    g[int(e)] = m + 16 * i < used ? x : 0.f;
+                });
+                return to_half<BF16>(g);
+            },
+            [&](uint32_t row, uint32_t column, u32x4 x) {
+                *(FF_GLOBAL u32x4*)(A.grad + (static_cast<uint64_t>(row0 + row) * A.piece + at + column) * 2) = x;
+            });
     } else {
-        __shared__ float2 part[S::kAcross][BM];
-        for (int i = 0; i < S::kM; i++) {
+        __shared__ float2 part[BM][S::kAcross];
+        static_for<S::kM>([&](auto i) {
             const uint32_t t = m + 16 * i;
             const int32_t y = t < used ? A.targets[t] : -1;
-            float top = -INFINITY, total = 0.f, target = 0.f;
-            bool mine = false;
             if constexpr (MODE == kKeep) {
                 float* const out = A.logits + static_cast<uint64_t>(t) * A.piece + (v - first);
-                for (int j = 0; j < S::kN; j++)
-                    if (t < used) *(FF_GLOBAL f32x4*)(out + 16 * j) = z[i][j];
+                static_for<S::kN>([&](auto j) {
+                    if (t < used) *(FF_GLOBAL f32x4*)(out + 16 * j) = z[int(i)][int(j)];
+                });
             }
-            for (int j = 0; j < S::kN; j++)
-                for (int e = 0; e < 4; e++) {
-                    const uint32_t vocab_entry = v + 16 * j + e;
-                    if (static_cast<int32_t>(vocab_entry) == y) {
-                        mine = true;
-                        target = z[i][j][e];
-                    }
-                    if (vocab_entry >= vocab) z[i][j][e] = -INFINITY;
-                    // (a NaN or +inf stays in the sum, as exp(NaN - top) or exp(inf - inf))
-                    top = fmaxf(top, z[i][j][e]);
-                }
-            if (mine) A.picked[t] = target;
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float against = top == -INFINITY ? 0.f : top;
-            for (int j = 0; j < S::kN; j++)
-                for (int e = 0; e < 4; e++) total += __builtin_amdgcn_exp2f((z[i][j][e] - against) * kLog2E);
-            total += __shfl_xor(total, 16);
-            total += __shfl_xor(total, 32);
-            if (lane < 16) part[wave % S::kAcross][(wave / S::kAcross) * (16 * S::kM) + 16 * i + lane] = float2{top, total};
-        }
+            const float2 p = join_lanes(A, z[int(i)], t, v, y);
+            if (lane < 16) part[(wave / S::kAcross) * (16 * S::kM) + 16 * i + lane][wave % S::kAcross] = p;
+        });
         __syncthreads();
-        for (uint32_t r = threadIdx.x; r < BM; r += kProductThreads) {
-            if (m0 + r >= used) break;
-            float top = -INFINITY, total = 0.f;
-            for (int k = 0; k < S::kAcross; k++) top = fmaxf(top, part[k][r].x);
-            const float against = top == -INFINITY ? 0.f : top;
-            for (int k = 0; k < S::kAcross; k++) total += part[k][r].y * __builtin_amdgcn_exp2f((part[k][r].x - against) * kLog2E);
-            A.parts[static_cast<uint64_t>(m0 + r) * A.tiles + v0 / kTile] = float2{top, total};
-        }
+        for (uint32_t r = threadIdx.x; r < BM && m0 + r < used; r += kProductThreads)
+            A.parts[static_cast<uint64_t>(m0 + r) * A.tiles + v0 / kTile] = join_parts(part[r]);
     }
+}
+
+// The logits of few tokens, all of the vocabulary: W passes once from memory through registers, rows of any alignment where they lie.  A wavefront
+// takes 16 V rows of it and 16 T tokens, whose hidden states come from the caches; the products of a chunk of K times 32
+// elements are made while the next one is on its way.  At the rate of reading W, where 64 x 256 tiles leave half of the chip idle (see launch).
+constexpr int kStreamThreads = 256, kStreamWaves = kStreamThreads / kWaveSize;
+template <int T>
+struct Stream {
+    static constexpr int V = T == 1 ? 1 : 2, K = 8 / T;
+    static constexpr uint32_t kEntries = 16 * V * kStreamWaves;  // of a workgroup
+};
+template <bool BF16, int T, Mode MODE>
+__global__ __launch_bounds__(kStreamThreads) void head_stream_kernel(const HeadArgs A)
+{
+    using S = Stream<T>;
+    const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width), vocab = static_cast<uint32_t>(A.b.vocab);
+    const uint32_t wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
+    const uint32_t v0 = blockIdx.x * S::kEntries + wave * (16 * S::V);
+    if (used == 0) return;
+    const uint8_t *w[S::V], *h[T];
+    static_for<S::V>([&](auto j) {
+        const uint32_t v = v0 + 16 * j + lane % 16;
+        w[int(j)] = static_cast<const uint8_t*>(A.b.weight) + (v < vocab ? v : vocab - 1) * A.b.weight_stride * 2;
+    });
+    static_for<T>([&](auto i) {
+        const uint32_t t = 16 * i + lane % 16;
+        h[int(i)] = A.hidden + static_cast<uint64_t>(t < used ? t : used - 1) * A.stride;
+    });
+    struct Chunk {
+        s16x8 w[S::K][S::V], h[S::K][T];
+    };
+    const uint32_t steps = (width + 31) / 32, chunks = (steps + S::K - 1) / S::K, whole = width / (32 * S::K);
+    auto fetch = [&](Chunk& c, uint32_t k) {
+        static_for<S::K>([&](auto s) {
+            const uint32_t at = (k * S::K + s) * 32 + lane / 16 * 8;
+            static_for<S::V>([&](auto j) {
+                if (k < whole) c.w[int(s)][int(j)] = __builtin_bit_cast(s16x8, *(const FF_GLOBAL u32x4_a2*)(w[int(j)] + 2 * at));
+                else c.w[int(s)][int(j)] = __builtin_bit_cast(s16x8, load8(w[int(j)], at, width));
+            });
+            static_for<T>([&](auto i) {  // (zeros up to 64 elements)
+                const s16x8 none = {};
+                c.h[int(s)][int(i)] = at < A.stride / 2 ? *(const FF_GLOBAL s16x8*)(h[int(i)] + 2 * at) : none;
+            });
+        });
+    };
+    f32x4 z[T][S::V];
+    static_for<T>([&](auto i) { static_for<S::V>([&](auto j) { z[int(i)][int(j)] = f32x4{0, 0, 0, 0}; }); });
+    auto multiply_all = [&](const Chunk& c) {
+        static_for<S::K>([&](auto s) {
+            static_for<T>([&](auto i) {
+                static_for<S::V>([&](auto j) { z[int(i)][int(j)] = multiply<BF16>(c.w[int(s)][int(j)], c.h[int(s)][int(i)], z[int(i)][int(j)]); });
+            });
+        });
+    };
+    Chunk one, other;
+    fetch(one, 0);
+    for (uint32_t k = 0; k < chunks; k += 2) {
+        if (k + 1 < chunks) fetch(other, k + 1);
+        multiply_all(one);
+        if (k + 2 < chunks) fetch(one, k + 2);
+        if (k + 1 < chunks) multiply_all(other);
+    }
+    __shared__ float2 part[16 * T][kStreamWaves];
+    const uint32_t v = v0 + 4 * (lane / 16);
+    static_for<T>([&](auto i) {
+        const uint32_t t = 16 * i + lane % 16;
+        if constexpr (MODE == kKeep) {
+            static_for<S::V>([&](auto j) {
+                if (t < used && v + 16 * j < A.piece) *(FF_GLOBAL f32x4*)(A.logits + static_cast<uint64_t>(t) * A.piece + v + 16 * j) = z[int(i)][int(j)];
+            });
+        }
+        const float2 p = join_lanes(A, z[int(i)], t, v, t < used ? A.targets[t] : -1);
+        if (lane < 16) part[16 * i + lane][wave] = p;
+    });
+    __syncthreads();
+    if (threadIdx.x < used) A.parts[static_cast<uint64_t>(threadIdx.x) * A.tiles + blockIdx.x] = join_parts(part[threadIdx.x]);
 }
 
 // ---- log-probabilities, G of kept logits ------------------------------------------------------------
@@ -305,19 +409,20 @@ __device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const
 {
     const uint32_t lane = threadIdx.x % kWaveSize;
     const float2* const parts = A.parts + static_cast<uint64_t>(r) * A.tiles;
-    float top = -INFINITY;
-    for (uint32_t k = lane; k < A.tiles; k += kWaveSize) top = fmaxf(top, parts[k].x);
-    for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    const float against = top == -INFINITY ? 0.f : top;
+    float c = -INFINITY;
+    for (uint32_t k = lane; k < A.tiles; k += kWaveSize) c = fmaxf(c, parts[k].x);
+    for (int d = 32; d; d /= 2) c = fmaxf(c, __shfl_xor(c, d));
+    if (c == -INFINITY) c = 0.f;
     double total = 0;
     for (uint32_t k = lane; k < A.tiles; k += kWaveSize) {
         const float2 p = parts[k];
-        total += static_cast<double>(p.y) * exp(static_cast<double>(p.x) - static_cast<double>(against));
+        total += static_cast<double>(p.y) * exp2(static_cast<double>(p.x) - static_cast<double>(c));
     }
     for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
-    const double rest = log(total), logp = (static_cast<double>(A.picked[r]) - static_cast<double>(against)) - rest;
+    const double against = static_cast<double>(c) / static_cast<double>(kLog2E), rest = log(total);
+    const double logp = (static_cast<double>(A.picked[r]) - against) - rest;
     const float w = A.weights[r], f = w / A.state->largest * (BF16 ? 1.f : 0x1p14f);
-    const Row row = {static_cast<float>((static_cast<double>(against) + rest) * 1.4426950408889634), f, f * static_cast<float>(expm1(logp)), A.targets[r]};
+    const Row row = {static_cast<float>((against + rest) * 1.4426950408889634), f, f * static_cast<float>(expm1(logp)), A.targets[r]};
     if (writes && lane == 0) {
         A.logp[A.index[r]] = static_cast<float>(logp);
         A.rows[r] = row;
@@ -357,8 +462,13 @@ __global__ __launch_bounds__(256) void head_kept_kernel(const HeadArgs A, const 
     const uint32_t t = blockIdx.x / wide, part = blockIdx.x - t * wide;  // of `wide` parts of a row
     if (used == 0 && blockIdx.x == 0 && threadIdx.x == 0) put_stats(A, 0.0, 0);
     if (t >= until) return;
-    Row r = {};
-    if (t < used) r = finish<BF16>(A, t, used, part == 0 && threadIdx.x < kWaveSize);
+    __shared__ Row row;
+    if (t < used && threadIdx.x < kWaveSize) {
+        const Row known = finish<BF16>(A, t, used, part == 0);
+        if (threadIdx.x == 0) row = known;
+    }
+    __syncthreads();
+    const Row r = row;
     const uint32_t end = (n + kTile - 1) / kTile * kTile;
     for (uint32_t at = (part * 256 + threadIdx.x) * 8; at < end; at += wide * 2048) {
         u32x4 out = {0, 0, 0, 0};
@@ -392,24 +502,24 @@ __global__ __launch_bounds__(kSelectThreads) void head_sum_kernel(const HeadArgs
 
 // ---- gradients ------------------------------------------------------------------------------------
 
-// Elements [at, at + 4) of a row of `width`, rounded.
-template <bool BF16>
-__device__ __forceinline__ void put4(uint8_t* row, uint32_t at, uint32_t width, f32x4 v)
+// Elements [at, at + 8) of a row of `width`, at < width.
+__device__ __forceinline__ void put8(uint8_t* row, uint32_t at, uint32_t width, u32x4 v)
 {
-    const u32x2 h = to_half<BF16>(v);
     uint8_t* const p = row + 2ull * at;
-    if (at + 4 <= width) {
-        *(FF_GLOBAL u32x2_a2*)p = h;
+    if (at + 8 <= width) {
+        *(FF_GLOBAL u32x4_a2*)p = v;
     } else {
-        for (uint32_t e = 0; at + e < width; e++) as_global(reinterpret_cast<uint16_t*>(p))[e] = static_cast<uint16_t>((e & 2 ? h.y : h.x) >> (e & 1) * 16);
+#pragma unroll
+        for (uint32_t e = 0; e < 7; e++)
+            if (at + e < width) as_global(reinterpret_cast<uint16_t*>(p))[e] = static_cast<uint16_t>(v[e / 2] >> e % 2 * 16);
     }
 }
 
-// dH (+)= G W over a slice of the piece [first, first + n); where that is all of it, in its place.
+// dH (+)= G W over a slice of vocabulary entries [first, first + n), which begin at a column of G; where that is all of it, in its place.
 enum Sum { kOnly, kFirst, kNext };
 template <bool BF16, int BM>
-__device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first, const uint32_t n, const Sum which, const uint32_t block,
-                                        const uint32_t blocks, FF_LDS uint8_t* lds)
+__device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first, const uint32_t n, const uint32_t column, const Sum which,
+                                        const uint32_t block, const uint32_t blocks, FF_LDS uint8_t* lds)
 {
     using S = Share<BM>;
     const uint32_t used = A.state->used, width_up = A.stride / 2;
@@ -423,7 +533,7 @@ __device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first,
     const uint32_t steps = (n + kStepK - 1) / kStepK, each = (steps + A.slices - 1) / A.slices;
     const uint32_t from = slice * each, to = from + each < steps ? from + each : steps;
     if (which == kNext && from >= to) return;
-    const OperandTile a = {A.grad + static_cast<uint64_t>(m0) * A.piece * 2, static_cast<uint64_t>(A.piece) * 2, A.tokens_up - m0, A.piece};
+    const OperandTile a = {A.grad + (static_cast<uint64_t>(m0) * A.piece + column) * 2, static_cast<uint64_t>(A.piece) * 2, A.tokens_up - m0, A.piece};
     OperandTile b;
     b.base = weight_row(A, first, first, &b.stride) + n0 * 2;
     b.valid = (A.weight ? width_up : static_cast<uint32_t>(A.b.width)) - n0;
@@ -433,22 +543,25 @@ __device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first,
     const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
     const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;
     const uint32_t d = n0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);
-    const float scale = A.state->scale;
+    if (which == kOnly) {
+        const float scale = A.state->scale;
+        const uint32_t row0 = m - lane % 16, d0 = d - 4 * (lane / 16), width = static_cast<uint32_t>(A.b.width);
+        RowsByLds<S::kM, S::kN>::pass(
+            lds, [&](auto i, auto j) { return to_half<BF16>(sum[int(i)][int(j)] * scale); },
+            [&](uint32_t row, uint32_t column, u32x4 v) {
+                if (row0 + row < used && d0 + column < width)
+                    put8(A.dhidden + A.index[row0 + row] * A.dhidden_stride * 2, d0 + column, width, v);
+            });
+        return;
+    }
     static_for<S::kM>([&](auto i) {
         const uint32_t t = m + 16 * i;
         if (t >= used) return;
-        if (which == kOnly) {
-            uint8_t* const out = A.dhidden + A.index[t] * A.dhidden_stride * 2;
-            static_for<S::kN>([&](auto j) {
-                if (d + 16 * j < A.b.width) put4<BF16>(out, d + 16 * j, static_cast<uint32_t>(A.b.width), sum[int(i)][int(j)] * scale);
-            });
-        } else {
-            float* const out = A.dh + (static_cast<uint64_t>(slice) * A.tokens_up + t) * width_up + d;
-            static_for<S::kN>([&](auto j) {
-                FF_GLOBAL f32x4* const p = (FF_GLOBAL f32x4*)(out + 16 * j);
-                if (d + 16 * j < width_up) *p = which == kNext ? *p + sum[int(i)][int(j)] : sum[int(i)][int(j)];
-            });
-        }
+        float* const out = A.dh + (static_cast<uint64_t>(slice) * A.tokens_up + t) * width_up + d;
+        static_for<S::kN>([&](auto j) {
+            FF_GLOBAL f32x4* const p = (FF_GLOBAL f32x4*)(out + 16 * j);
+            if (d + 16 * j < width_up) *p = which == kNext ? *p + sum[int(i)][int(j)] : sum[int(i)][int(j)];
+        });
     });
 }
 
@@ -460,26 +573,32 @@ __global__ __launch_bounds__(256) void head_put_kernel(const HeadArgs A)
     const float scale = A.state->scale;
     for (uint32_t r = blockIdx.x; r < used; r += gridDim.x) {
         uint8_t* const out = A.dhidden + A.index[r] * A.dhidden_stride * 2;
-        for (uint32_t d = 4 * threadIdx.x; d < width; d += 4 * blockDim.x) {
+        for (uint32_t d = 8 * threadIdx.x; d < width; d += 8 * blockDim.x) {
             constexpr uint32_t kAhead = 8;
-            f32x4 s = {0, 0, 0, 0};
+            f32x4 s[2] = {};
             for (uint32_t k = 0; k < A.slices; k += kAhead) {
-                f32x4 x[kAhead];
+                f32x4 x[kAhead][2];
                 static_for<kAhead>([&](auto i) {
-                    if (k + i < A.slices) x[int(i)] = *(const FF_GLOBAL f32x4*)(A.dh + (static_cast<uint64_t>(k + i) * A.tokens_up + r) * width_up + d);
+                    if (k + i >= A.slices) return;
+                    const float* const p = A.dh + (static_cast<uint64_t>(k + i) * A.tokens_up + r) * width_up + d;
+                    x[int(i)][0] = *(const FF_GLOBAL f32x4*)p;
+                    x[int(i)][1] = *(const FF_GLOBAL f32x4*)(p + 4);
                 });
                 static_for<kAhead>([&](auto i) {
-                    if (k + i < A.slices) s += x[int(i)];
+                    if (k + i >= A.slices) return;
+                    s[0] += x[int(i)][0];
+                    s[1] += x[int(i)][1];
                 });
             }
-            put4<BF16>(out, d, width, s * scale);
+            const u32x2 a = to_half<BF16>(s[0] * scale), b = to_half<BF16>(s[1] * scale);
+            put8(out, d, width, u32x4{a.x, a.y, b.x, b.y});
         }
     }
 }
 
-// dW = G^T H of the piece [first, first + n).
+// dW = G^T H of vocabulary entries [first, first + n).
 template <bool BF16>
-__device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first, const uint32_t n, const uint32_t block, const uint32_t blocks,
+__device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first, const uint32_t n, const uint32_t column, const uint32_t block, const uint32_t blocks,
                                         FF_LDS uint8_t* lds)
 {
     using S = Share<256>;
@@ -489,32 +608,81 @@ __device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first,
     m0 *= kTile;
     n0 *= kTile;
     const uint32_t steps = (used + kStepK - 1) / kStepK;
-    const OperandTile a = {A.grad + m0 * 2, static_cast<uint64_t>(A.piece) * 2, A.piece - m0, A.tokens_up};
+    const OperandTile a = {A.grad + (static_cast<uint64_t>(column) + m0) * 2, static_cast<uint64_t>(A.piece) * 2, A.piece - column - m0, A.tokens_up};
     const OperandTile b = {A.hidden + n0 * 2, A.stride, A.stride / 2 - n0, A.tokens_up};
     f32x4 sum[S::kM][S::kN];
     product<BF16, 256, kAcrossK, kAcrossK>(a, b, 0, steps, ~0u, lds, sum);
     const float scale = A.state->scale;
-    const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
-    const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;
-    const uint32_t d = n0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);
-    for (int i = 0; i < S::kM; i++) {
-        if (m + 16 * i >= n) continue;
-        uint8_t* const out = A.dweight + (static_cast<uint64_t>(first) + m + 16 * i) * A.dweight_stride * 2;
-        for (int j = 0; j < S::kN; j++)
-            if (d + 16 * j < width) put4<BF16>(out, d + 16 * j, width, used ? sum[i][j] * scale : f32x4{0, 0, 0, 0});
+    const int wave = threadIdx.x / kWaveSize;
+    const uint32_t row0 = m0 + (wave / S::kAcross) * (16 * S::kM), d0 = n0 + (wave % S::kAcross) * (16 * S::kN);
+    RowsByLds<S::kM, S::kN>::pass(
+        lds, [&](auto i, auto j) { return to_half<BF16>(used ? sum[int(i)][int(j)] * scale : f32x4{0, 0, 0, 0}); },
+        [&](uint32_t row, uint32_t column, u32x4 v) {
+            if (row0 + row < n && d0 + column < width)
+                put8(A.dweight + (static_cast<uint64_t>(first) + row0 + row) * A.dweight_stride * 2, d0 + column, width, v);
+        });
+}
+
+// dW of few tokens, whose products are one step: a workgroup holds G of 64 vocabulary entries in registers and goes through the hidden states, 256
+// elements at a time, which lie in the caches; two or more are on a compute unit, so that one's loads run under another's stores.  What bounds it:
+// writing dW.
+constexpr int kFewWaves = 4, kFewEntries = 16 * kFewWaves;
+template <bool BF16>
+__global__ __launch_bounds__(kFewWaves* kWaveSize) void head_few_dweight_kernel(const HeadArgs A, const uint32_t first, const uint32_t n, const uint32_t parts)
+{
+    using H = Operand<kAcrossK, 256, kFewWaves>;
+    using Out = RowsByLds<1, 16>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * H::kBytes + kFewWaves * Out::kBytes];
+    const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width), width_up = A.stride / 2, chunks = (width_up + 255) / 256;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize), lane = threadIdx.x % kWaveSize;
+    const uint32_t block = blockIdx.x / parts, part = blockIdx.x - block * parts;
+    const uint32_t v0 = block * kFewEntries + wave * 16, v = v0 + lane % 16;  // of [first, first + n), as G's columns are here
+    s16x8 g[2] = {};
+    if (used)
+        static_for<2>([&](auto half) {
+            static_for<8>([&](auto e) {
+                const uint32_t t = half * 32 + lane / 16 * 8 + e;  // (rows of zeros up to 64)
+                g[int(half)][int(e)] = ((const FF_GLOBAL short*)A.grad)[static_cast<uint64_t>(t) * A.piece + first + v];
+            });
+        });
+    const float scale = A.state->scale;
+    auto fetch = [&](uint32_t chunk, FF_LDS uint8_t* buffer) {
+        const OperandTile t = {A.hidden + chunk * 512, A.stride, width_up - chunk * 256, 64};
+        H h;
+        h.init(t, wave, lane);
+        static_for<H::kLoads>([&](auto i) { h.fetch(i, 0, buffer, wave); });
+    };
+    uint32_t mine = 0;
+    if (part < chunks) fetch(part, (FF_LDS uint8_t*)lds);
+    for (uint32_t chunk = part; chunk < chunks; chunk += parts) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (chunk + parts < chunks) fetch(chunk + parts, (FF_LDS uint8_t*)lds + (H::kBytes - mine));
+        const FF_LDS uint8_t* const buffer = (FF_LDS uint8_t*)lds + mine;
+        f32x4 sum[16];
+        static_for<16>([&](auto j) {
+            sum[int(j)] = multiply<BF16>(H::fragment(buffer, 16 * j, 0, lane), g[0], f32x4{0, 0, 0, 0});
+            if (used > 32) sum[int(j)] = multiply<BF16>(H::fragment(buffer, 16 * j, 1, lane), g[1], sum[int(j)]);
+        });
+        Out::pass(
+            (FF_LDS uint8_t*)lds + 2 * H::kBytes, [&](auto, auto j) { return to_half<BF16>(used ? sum[int(j)] * scale : f32x4{0, 0, 0, 0}); },
+            [&](uint32_t row, uint32_t column, u32x4 x) {
+                const uint32_t d = chunk * 256 + column;
+                if (v0 + row < n && d < width) put8(A.dweight + (static_cast<uint64_t>(first) + v0 + row) * A.dweight_stride * 2, d, width, x);
+            });
+        mine = H::kBytes - mine;
     }
 }
 
 // Both: the first `dh_blocks` workgroups make dH, whose sums are longer, the others dW.
 template <bool BF16, int BM>
 __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu(2))) void head_grads_kernel(const HeadArgs A, const uint32_t first,
-                                                                                                            const uint32_t n, const Sum which,
-                                                                                                            const uint32_t dh_blocks)
+                                                                                                            const uint32_t n, const uint32_t column,
+                                                                                                            const Sum which, const uint32_t dh_blocks)
 {
     constexpr uint32_t kOne = kProductLds<BM, kAlongK, kAcrossK>, kOther = kProductLds<256, kAcrossK, kAcrossK>;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kOne > kOther ? kOne : kOther];
-    if (blockIdx.x < dh_blocks) dhidden<BF16, BM>(A, first, n, which, blockIdx.x, dh_blocks, (FF_LDS uint8_t*)lds);
-    else dweight<BF16>(A, first, n, blockIdx.x - dh_blocks, gridDim.x - dh_blocks, (FF_LDS uint8_t*)lds);
+    if (blockIdx.x < dh_blocks) dhidden<BF16, BM>(A, first, n, column, which, blockIdx.x, dh_blocks, (FF_LDS uint8_t*)lds);
+    else dweight<BF16>(A, first, n, column, blockIdx.x - dh_blocks, gridDim.x - dh_blocks, (FF_LDS uint8_t*)lds);
 }
 
 __global__ void head_of_nothing_kernel(ff_head_stats* stats) { *stats = {}; }
@@ -522,7 +690,7 @@ __global__ void head_of_nothing_kernel(ff_head_stats* stats) { *stats = {}; }
 // ---- the workspace ----------------------------------------------------------------------------------
 
 constexpr uint64_t kPieceElements = 1ull << 28;  // of G, and of a piece's packed rows
-constexpr uint32_t kSliceTokens = 2048;          // tokens times slices, up to so many
+constexpr uint32_t kFewDweightBlocks = 1024;    // workgroups of head_few_dweight_kernel, about
 constexpr uint32_t kKeptBlocks = 2048;           // workgroups that make G of kept logits, about
 
 bool weight_as_it_is(const ff_head_batch& b)
@@ -530,9 +698,20 @@ bool weight_as_it_is(const ff_head_batch& b)
     return reinterpret_cast<uint64_t>(b.weight) % 16 == 0 && b.weight_stride % 8 == 0 && b.width % 8 == 0 && b.weight_stride <= (1u << 22);
 }
 
+bool few(const ff_head_batch& b) { return b.n_tokens <= kFewTokens; }
 // Is it better to keep the logits of a piece than to make them again?  (Of the last piece, which is all there is for the smaller calls.)
-bool keeps(const ff_head_batch& b) { return b.width >= 1024 || b.n_tokens * 4 <= b.width; }
+bool keeps(const ff_head_batch& b) { return few(b) || b.width >= 1024; }
+// Do the logits come from head_stream_kernel?
+bool streams(const ff_head_batch& b) { return b.n_tokens <= 16 || (few(b) && !weight_as_it_is(b)); }
+// Tiles 256 tokens high, or 64: a round of the latter takes two thirds as long.
+bool high_tiles(const ff_head_batch& b)
+{
+    const uint64_t across = up(b.vocab, kTile) / kTile, rounds = (up(b.n_tokens, kTile) / kTile * across + kComputeUnits - 1) / kComputeUnits;
+    return !few(b) && up(b.n_tokens, 64) / 64 * across * 2 > kComputeUnits * 3 * rounds;
+}
 uint32_t up64(uint64_t n) { return static_cast<uint32_t>(up(std::max<uint64_t>(n, 1), 64)); }
+// Vocabulary entries that a workgroup of head_stream_kernel takes.
+uint32_t stream_entries(uint64_t n_tokens) { return n_tokens <= 16 ? Stream<1>::kEntries : n_tokens <= 32 ? Stream<2>::kEntries : Stream<4>::kEntries; }
 
 struct Places {
     uint64_t state, index, weights, targets, rows, losses, picked, parts, hidden, weight, grad, logits, dh, bytes;
@@ -541,16 +720,23 @@ struct Places {
 Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
 {
     const uint64_t n = b.n_tokens, width_up = up(b.width, kStepK);
-    A->tokens_up = static_cast<uint32_t>(n <= kFewTokens ? kFewTokens : up(n, kTile));
-    A->tiles = static_cast<uint32_t>((b.vocab + kTile - 1) / kTile);
+    const uint32_t high = high_tiles(b) ? kTile : 64, tile = streams(b) ? stream_entries(n) : kTile;
+    A->tokens_up = static_cast<uint32_t>(up(std::max<uint64_t>(n, 1), high));
+    A->tiles = static_cast<uint32_t>((b.vocab + tile - 1) / tile);
     A->stride = static_cast<uint32_t>(width_up * 2);
     const bool packed = !weight_as_it_is(b);
-    const uint32_t tiles_m = A->tokens_up / (n <= kFewTokens ? kFewTokens : kTile);
-    uint64_t piece = std::min<uint64_t>(up(b.vocab, kTile), most_groups(kProductThreads) / tiles_m * kTile);
-    if (grad) piece = std::min(piece, std::max<uint64_t>(kPieceElements / A->tokens_up / kTile, 1) * kTile);
-    if (packed) piece = std::min(piece, std::max<uint64_t>(kPieceElements / width_up / kTile, 1) * kTile);
+    const uint64_t whole = up(b.vocab, kTile), least = kTile;
+    // G is of a piece, rows are copied for a piece: of few tokens it is whole, and they may still be copied in several
+    uint64_t piece = few(b) ? whole : std::min<uint64_t>(whole, most_groups(kProductThreads) / (A->tokens_up / high) * kTile);
+    if (grad && !few(b)) piece = std::min(piece, std::max(kPieceElements / A->tokens_up / kTile * kTile, least));
+    uint64_t step = piece;
+    if (packed) step = std::min(piece, std::max(kPieceElements / width_up / kTile * kTile, least));
+    if (!few(b)) piece = step;
     A->piece = static_cast<uint32_t>(piece);
-    A->slices = std::max(kSliceTokens / A->tokens_up, 1u);
+    A->step = static_cast<uint32_t>(step);
+    // dH's sum over a piece in so many slices that its tiles fill the chip, of four steps at least
+    const uint64_t dh_tiles = A->tokens_up / high * (up(width_up, kTile) / kTile), steps = (step + kStepK - 1) / kStepK;
+    A->slices = static_cast<uint32_t>(std::max<uint64_t>(std::min(kComputeUnits / dh_tiles, steps / 4), 1));
     Places p = {};
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
@@ -565,16 +751,16 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     p.rows = take(n * sizeof(Row));
     p.losses = take(n * 8);
     p.picked = take(n * 4);
-    p.parts = take(n * A->tiles * sizeof(float2));
+    // (never less for more tokens, entries or elements, whatever tiles and pieces come to)
+    p.parts = take(std::max(n * (whole / kTile), std::min<uint64_t>(n, 32) * (whole / 64)) * sizeof(float2));
     p.hidden = take(static_cast<uint64_t>(A->tokens_up) * A->stride);
-    // (never less for more tokens, entries or elements, whatever the pieces come to)
-    const uint64_t whole = up(b.vocab, kTile);
     auto piece_of = [&](uint64_t rows) { return std::max(std::min(rows * whole, kPieceElements), rows * kTile) * 2; };
-    p.weight = take(packed ? piece_of(width_up) : 0);
+    p.weight = take(packed && (grad || !streams(b)) ? piece_of(width_up) : 0);
     if (grad) {
         p.grad = take(piece_of(A->tokens_up));
         p.logits = take(2 * piece_of(A->tokens_up));
-        p.dh = take(static_cast<uint64_t>(std::max(A->tokens_up, kSliceTokens)) * width_up * 4);
+        const uint64_t dh = A->tokens_up * width_up;
+        p.dh = take(std::max(dh, std::min<uint64_t>(dh * (whole / kTile), kComputeUnits * kTile * kTile)) * 4);
     }
     p.bytes = at;
     return p;
@@ -591,27 +777,36 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
         hipLaunchKernelGGL(head_select_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
         hipLaunchKernelGGL(head_gather_kernel, dim3(std::min(A.tokens_up, 4096u)), dim3(256), 0, stream, A);
     }
-    const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.piece - 1) / A.piece);
-    const bool grad = A.dhidden || A.dweight, keep = grad && keeps(A.b);
+    const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.step - 1) / A.step);
+    const bool grad = A.dhidden || A.dweight, keep = grad && keeps(A.b), whole = few(A.b);
     uint32_t first = 0, m = 0, tiles = 0, packed = ~0u;
     // makes piece i the one that the following launches are for
-    auto take = [&](uint32_t i) {
-        first = i * A.piece;
-        m = std::min(A.piece, vocab - first);
+    auto take = [&](uint32_t i, bool rows) {
+        first = i * A.step;
+        m = std::min(A.step, vocab - first);
         tiles = (m + kTile - 1) / kTile;
-        if (A.weight && packed != i) hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, 8192u)), dim3(256), 0, stream, A, first, m);
+        if (!A.weight || !rows || packed == i) return;
+        hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, 8192u)), dim3(256), 0, stream, A, first, m);
         packed = i;
     };
     const dim3 threads(kProductThreads);
-    for (uint32_t i = 0; i < n_pieces; i++) {
-        take(i);
-        const dim3 grid(tiles * tiles_m);
-        if (keep && i == n_pieces - 1) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kKeep>), grid, threads, 0, stream, A, first, m);
-        else hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kSums>), grid, threads, 0, stream, A, first, m);
+    if (streams(A.b)) {
+        const auto kernel = n <= 16   ? (grad ? head_stream_kernel<BF16, 1, kKeep> : head_stream_kernel<BF16, 1, kSums>)
+                            : n <= 32 ? (grad ? head_stream_kernel<BF16, 2, kKeep> : head_stream_kernel<BF16, 2, kSums>)
+                                      : (grad ? head_stream_kernel<BF16, 4, kKeep> : head_stream_kernel<BF16, 4, kSums>);
+        hipLaunchKernelGGL(kernel, dim3(A.tiles), dim3(kStreamThreads), 0, stream, A);
+    } else {
+        for (uint32_t i = 0; i < n_pieces; i++) {
+            take(i, true);
+            const dim3 grid(tiles * tiles_m);
+            if (keep && i == n_pieces - 1) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kKeep>), grid, threads, 0, stream, A, first, m);
+            else hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kSums>), grid, threads, 0, stream, A, first, m);
+        }
     }
     if (keep) {
-        const uint32_t rows = up64(n), wide = std::min((tiles * kTile + 2047) / 2048, (kKeptBlocks + rows - 1) / rows);
-        hipLaunchKernelGGL(head_kept_kernel<BF16>, dim3(rows * wide), dim3(256), 0, stream, A, first, m, wide);
+        const uint32_t from = whole ? 0 : first, of = vocab - from, rows = up64(n);
+        const uint32_t wide = std::min((of + 2047) / 2048, (kKeptBlocks + rows - 1) / rows);
+        hipLaunchKernelGGL(head_kept_kernel<BF16>, dim3(rows * wide), dim3(256), 0, stream, A, from, of, wide);
     } else {
         hipLaunchKernelGGL(head_finish_kernel<BF16>, dim3(n / 4 + 1), dim3(256), 0, stream, A);
     }
@@ -619,11 +814,17 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
     if (!grad) return hipGetLastError();
     const Sum start = n_pieces == 1 && A.slices == 1 ? kOnly : kFirst;
     for (uint32_t i = n_pieces; i-- > 0;) {  // from the last one, whose logits and packed rows are at hand
-        take(i);
-        const bool last = i == n_pieces - 1;
-        if (!keep || !last) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kGrad>), dim3(tiles * tiles_m), threads, 0, stream, A, first, m);
-        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight ? tiles * tiles_d : 0;
-        hipLaunchKernelGGL((head_grads_kernel<BF16, BM>), dim3(dh_blocks + dw_blocks), threads, 0, stream, A, first, m, last ? start : kNext, dh_blocks);
+        const bool last = i == n_pieces - 1, logits = !whole && (!keep || !last);
+        take(i, A.dhidden || logits);
+        if (logits) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kGrad>), dim3(tiles * tiles_m), threads, 0, stream, A, first, m);
+        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight && !whole ? tiles * tiles_d : 0;
+        if (A.dweight && whole) {
+            const uint32_t blocks = (m + kFewEntries - 1) / kFewEntries, parts = std::min(tiles_d, (kFewDweightBlocks + blocks - 1) / blocks);
+            hipLaunchKernelGGL(head_few_dweight_kernel<BF16>, dim3(blocks * parts), dim3(kFewWaves * kWaveSize), 0, stream, A, first, m, parts);
+        }
+        if (dh_blocks + dw_blocks)
+            hipLaunchKernelGGL((head_grads_kernel<BF16, BM>), dim3(dh_blocks + dw_blocks), threads, 0, stream, A, first, m, whole ? first : 0,
+                           last ? start : kNext, dh_blocks);
     }
     if (A.dhidden && start != kOnly) hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(std::min(n + 1, 4096u)), dim3(256), 0, stream, A);
     return hipGetLastError();
@@ -668,8 +869,9 @@ hipError_t launch_head(const ff_head_batch& b, float* logp, void* dhidden, uint6
     A.logits = reinterpret_cast<float*>(w + p.logits);
     A.dh = reinterpret_cast<float*>(w + p.dh);
     A.grad_scale = b.loss_scale * (b.dtype == FF_BF16 ? 1.f : 0x1p-14f);
-    if (b.dtype == FF_BF16) return b.n_tokens <= kFewTokens ? launch<true, 64>(A, stream) : launch<true, 256>(A, stream);
-    return b.n_tokens <= kFewTokens ? launch<false, 64>(A, stream) : launch<false, 256>(A, stream);
+    const bool high = high_tiles(b);
+    if (b.dtype == FF_BF16) return high ? launch<true, 256>(A, stream) : launch<true, 64>(A, stream);
+    return high ? launch<false, 256>(A, stream) : launch<false, 64>(A, stream);
 }
 
 }  // namespace ffsnap

@@ -15,7 +15,7 @@ namespace {
 
 uint32_t element_size(uint32_t dtype) { return dtype == FF_F32 ? 4 : dtype == FF_BF16 || dtype == FF_F16 ? 2 : 0; }
 bool aligned(const void* p, uint64_t a) { return reinterpret_cast<uint64_t>(p) % a == 0; }
-constexpr uint64_t kMost = 0x7FFFFFFFull;                // tokens, rows, entries of a vocabulary
+constexpr uint64_t kMost = 0x7FFFFFFFull;                // tokens, rows
 constexpr uint64_t kMostStride = 1ull << 40;             // elements: addresses of rows fit 64 bits
 bool rows_ok(uint64_t stride, uint64_t width) { return stride >= width && stride <= kMostStride; }
 // A loss scale that is one in 32 bits.
@@ -46,7 +46,7 @@ int check_norm(const void* x, uint64_t n_rows, uint64_t width, uint64_t x_stride
 int check_head(const ff_head_batch* b)
 {
     if (b->dtype != FF_BF16 && b->dtype != FF_F16) return FF_ERR_INVALID;
-    if (b->reserved || !b->vocab || b->vocab > kMost || !b->width || b->width > FF_HEAD_MAX_WIDTH || b->n_tokens > FF_HEAD_MAX_TOKENS)
+    if (b->reserved || !b->vocab || b->vocab > FF_HEAD_MAX_VOCAB || !b->width || b->width > FF_HEAD_MAX_WIDTH || b->n_tokens > FF_HEAD_MAX_TOKENS)
         return FF_ERR_INVALID;
     if (!rows_ok(b->weight_stride, b->width) || !rows_ok(b->hidden_stride, b->width) || !scale_ok(b->loss_scale)) return FF_ERR_INVALID;
     return FF_OK;

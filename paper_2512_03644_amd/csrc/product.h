@@ -36,13 +36,13 @@ struct OperandTile {
     uint32_t k_valid;     // kAlongK: a multiple of 8, zeros stand for what is behind; kAcrossK: rows behind repeat the last
 };
 
-template <Layout LAYOUT, int SIZE>
+template <Layout LAYOUT, int SIZE, int WAVES = kProductWaves>
 struct Operand {
-    static constexpr int kLoads = SIZE / 64;            // of a wavefront a step, 1 KiB each
+    static constexpr int kLoads = SIZE / 8 / WAVES;  // of a wavefront a step, 1 KiB each
     // What a load brings lies together; between those of a kAcrossK tile, two rows each, 64 bytes are left free, and in odd rows the two
     // halves of every 64 bytes are exchanged: the four rows that a transposing read of 16 lanes takes are in different banks.
     static constexpr uint32_t kChunk = LAYOUT == kAlongK ? 1024 : 1024 + 64;
-    static constexpr uint32_t kBytes = kProductWaves * kLoads * kChunk;
+    static constexpr uint32_t kBytes = WAVES * kLoads * kChunk;
     static constexpr uint32_t kRowBytes = LAYOUT == kAlongK ? kStepK * 2 : SIZE * 2;
     static_assert(LAYOUT == kAlongK || SIZE == 256, "a row is 32 pieces of 16 bytes");
 
@@ -53,7 +53,8 @@ struct Operand {
     // A load's row of the tile, and the piece of that row, by lane.
     static __device__ __forceinline__ uint32_t row_of(int i, int wave, int lane)
     {
-        return LAYOUT == kAlongK ? wave * (SIZE / kProductWaves) + 8 * i + lane / 8 : wave * 8 + 2 * i + lane / 32;
+        const int load = wave * kLoads + i;
+        return LAYOUT == kAlongK ? 8 * load + lane / 8 : 2 * load + lane / 32;
     }
     static __device__ __forceinline__ uint32_t piece_of(int i, int wave, int lane)
     {
@@ -95,7 +96,7 @@ struct Operand {
     {
         const uint32_t left = t.k_valid - k * kStepK;
         if (LAYOUT != kAlongK || left >= kStepK) return;
-        for (uint32_t i = threadIdx.x; i < SIZE * 8; i += kProductThreads) {
+        for (uint32_t i = threadIdx.x; i < SIZE * 8; i += WAVES * kWaveSize) {
             const uint32_t row = i / 8, piece = i % 8;
             if (piece * 8 >= left) *(FF_LDS u32x4*)(buffer + row * kRowBytes + (piece ^ (row & 7)) * 16) = u32x4{0, 0, 0, 0};
         }
@@ -230,6 +231,33 @@ __device__ __forceinline__ void product(const OperandTile& a_tile, const Operand
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");  // LDS is free
 }
+
+// A wavefront's part on its way to memory by rows: a lane's elements are four of a row, 16 rows apart in place; through LDS they become 16 bytes of
+// one row, 16 N columns of it side by side.  to16(i, j): the four rounded elements of fragment (i, j); fn(row, column, eight elements).
+// Stores of 32 bytes of 16 rows instead: 1.05 GB of gradient of few tokens took 600 us.
+template <int M, int N>
+struct RowsByLds {
+    static constexpr int kAtOnce = M < 4 ? M : 4, kLanes = 2 * N;
+    static constexpr uint32_t kPitch = 32 * N + 16, kBytes = 16 * kAtOnce * kPitch;  // of a wavefront
+    template <class To16, class Fn>
+    static __device__ __forceinline__ void pass(FF_LDS uint8_t* lds, To16&& to16, Fn&& fn)
+    {
+        const uint32_t lane = threadIdx.x % kWaveSize;
+        FF_LDS uint8_t* const mine = lds + threadIdx.x / kWaveSize * kBytes;
+        static_for<M / kAtOnce>([&](auto h) {
+            static_for<kAtOnce>([&](auto i) {
+                static_for<N>([&](auto j) {
+                    *(FF_LDS u32x2*)(mine + (16 * i + lane % 16) * kPitch + 32 * j + lane / 16 * 8) =
+                        to16(std::integral_constant<int, h * kAtOnce + i>{}, j);
+                });
+            });
+            static_for<kAtOnce * 16 * kLanes / kWaveSize>([&](auto k) {
+                const uint32_t at = k * kWaveSize + lane, row = at / kLanes, piece = at % kLanes;
+                fn(h * kAtOnce * 16 + row, piece * 8, *(const FF_LDS u32x4*)(mine + row * kPitch + piece * 16));
+            });
+        });
+    }
+};
 
 // Tiles in an order in which those that run at one time share operands: bands of 8 tiles along m, within them along n; the
 // workgroups of an XCD take 32 in a row.

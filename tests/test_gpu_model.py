@@ -254,7 +254,7 @@ def check_head(got, want):
 
 
 HEAD_SIZES = [(1, 1, 8), (1, 2, 1), (1, 1000, 64), (2, 257, 72), (3, 300, 65), (37, 4099, 256), (63, 511, 128), (64, 512, 192), (65, 513, 200), (130, 700, 31),
-              (256, 256, 64), (257, 1025, 320), (300, 2000, 264), (600, 999, 100)]
+              (16, 129, 40), (17, 128, 264), (32, 1000, 520), (33, 130, 1001), (64, 3, 2056), (256, 256, 64), (257, 1025, 320), (300, 2000, 264), (600, 999, 100)]
 
 
 @HALVES
@@ -337,9 +337,10 @@ def test_head_with_a_logit_that_is_not_finite():
 
 
 @HALVES
-@pytest.mark.parametrize("n,vocab,width", [(1000, 20011, 512), (2048, 8000, 1000), (16, 50021, 1032)])
-def test_head_at_larger_sizes(dtype, n, vocab, width):
-    """In several workgroups along every axis; the reference on the GPU, in 64 bits."""
-    args = head_inputs(n, vocab, width, dtype, masked=0.1)
+@pytest.mark.parametrize("n,vocab,width,pad,first", [(1000, 20011, 512, 0, 0), (2048, 8000, 1000, 8, 0), (16, 50021, 1032, 0, 0), (60, 50021, 777, 3, 1), (520, 22000, 72, 1, 0),
+                                                     (257, 33000, 1096, 0, 1)])
+def test_head_at_larger_sizes(dtype, n, vocab, width, pad, first):
+    """In several workgroups along every axis, of either height; the reference on the GPU, in 64 bits."""
+    args = head_inputs(n, vocab, width, dtype, pad, first, masked=0.1)
     scale = 1024.0 if dtype == F16 else 1.0
-    check_head(run_head(*args, scale), modelref.head(*args, scale))
+    check_head(run_head(*args, scale, pad=pad, first=first), modelref.head(*args, scale))

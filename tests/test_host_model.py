@@ -86,7 +86,7 @@ def test_head_refuses_bad_arguments():
     for bad in (dict(logp=None), dict(stats=None), dict(ws=None)):
         assert loss(_batch(), **bad) == ff.FF_ERR_NULL, bad
     assert L.ff_head_loss(None, A16, None, 0, None, 0, A16, A16, None) == ff.FF_ERR_NULL
-    for bad in (dict(dtype=0), dict(dtype=ff.FF_F32), dict(reserved=1), dict(vocab=0), dict(vocab=BIG), dict(n_tokens=ff.FF_HEAD_MAX_TOKENS + 1), dict(width=0),
+    for bad in (dict(dtype=0), dict(dtype=ff.FF_F32), dict(reserved=1), dict(vocab=0), dict(vocab=ff.FF_HEAD_MAX_VOCAB + 1), dict(n_tokens=ff.FF_HEAD_MAX_TOKENS + 1), dict(width=0),
                 dict(width=65), dict(hidden_stride=63), dict(weight_stride=63), dict(weight_stride=1 << 60),
                 dict(width=ff.FF_HEAD_MAX_WIDTH + 1, hidden_stride=1 << 20, weight_stride=1 << 20), dict(hidden=A16 + 1), dict(weight=A16 + 1), dict(targets=A16 + 4),
                 dict(weights=A16 + 2), dict(loss_scale=0.0), dict(loss_scale=-1.0), dict(loss_scale=INF), dict(loss_scale=NAN)):
