@@ -515,6 +515,14 @@ __device__ __forceinline__ void put8(uint8_t* row, uint32_t at, uint32_t width, 
     }
 }
 
+// The same, past the caches: a gradient of W is far larger than they are.  (Us, plain / so: dW of 1, 64, 128 tokens on 128,256 x 4096, with all in front of
+// it, 505, 565, 699 and 483, 527, 590.)
+__device__ __forceinline__ void put8_past(uint8_t* row, uint32_t at, uint32_t width, u32x4 v)
+{
+    if (at + 8 <= width) __builtin_nontemporal_store(v, (FF_GLOBAL u32x4_a2*)(row + 2ull * at));
+    else put8(row, at, width, v);
+}
+
 // dH (+)= G W over a slice of vocabulary entries [first, first + n), which begin at a column of G; where that is all of it, in its place.
 enum Sum { kOnly, kFirst, kNext };
 template <bool BF16, int BM>
@@ -565,34 +573,33 @@ __device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first,
     });
 }
 
-// dH of all pieces and slices, in its place.
+// dH of all pieces and slices, in its place: four elements of a row to a thread.
+constexpr uint32_t kPutThreads = 256;
 template <bool BF16>
-__global__ __launch_bounds__(256) void head_put_kernel(const HeadArgs A)
+__global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A, const uint32_t blocks_of_row)
 {
-    const uint32_t used = A.state->used, width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width);
-    const float scale = A.state->scale;
-    for (uint32_t r = blockIdx.x; r < used; r += gridDim.x) {
-        uint8_t* const out = A.dhidden + A.index[r] * A.dhidden_stride * 2;
-        for (uint32_t d = 8 * threadIdx.x; d < width; d += 8 * blockDim.x) {
-            constexpr uint32_t kAhead = 8;
-            f32x4 s[2] = {};
-            for (uint32_t k = 0; k < A.slices; k += kAhead) {
-                f32x4 x[kAhead][2];
-                static_for<kAhead>([&](auto i) {
-                    if (k + i >= A.slices) return;
-                    const float* const p = A.dh + (static_cast<uint64_t>(k + i) * A.tokens_up + r) * width_up + d;
-                    x[int(i)][0] = *(const FF_GLOBAL f32x4*)p;
-                    x[int(i)][1] = *(const FF_GLOBAL f32x4*)(p + 4);
-                });
-                static_for<kAhead>([&](auto i) {
-                    if (k + i >= A.slices) return;
-                    s[0] += x[int(i)][0];
-                    s[1] += x[int(i)][1];
-                });
-            }
-            const u32x2 a = to_half<BF16>(s[0] * scale), b = to_half<BF16>(s[1] * scale);
-            put8(out, d, width, u32x4{a.x, a.y, b.x, b.y});
-        }
+    const uint32_t width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width), r = blockIdx.x / blocks_of_row;
+    const uint32_t d = ((blockIdx.x - r * blocks_of_row) * kPutThreads + threadIdx.x) * 4;
+    if (r >= A.state->used || d >= width) return;
+    constexpr uint32_t kAhead = 8;
+    const float* const from = A.dh + static_cast<uint64_t>(r) * width_up + d;
+    const uint64_t step = static_cast<uint64_t>(A.tokens_up) * width_up;
+    f32x4 s = {0, 0, 0, 0};
+    for (uint32_t k = 0; k < A.slices; k += kAhead) {
+        f32x4 x[kAhead];
+        static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i < A.slices ? k + i : k) * step); });
+        static_for<kAhead>([&](auto i) {
+            if (k + i < A.slices) s += x[int(i)];
+        });
+    }
+    uint8_t* const out = A.dhidden + (A.index[r] * A.dhidden_stride + d) * 2;
+    const u32x2 h = to_half<BF16>(s * A.state->scale);
+    if (d + 4 <= width) {
+        *(FF_GLOBAL u32x2_a2*)out = h;
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 3; e++)
+            if (d + e < width) as_global(reinterpret_cast<uint16_t*>(out))[e] = static_cast<uint16_t>(h[e / 2] >> e % 2 * 16);
     }
 }
 
@@ -619,7 +626,7 @@ __device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first,
         lds, [&](auto i, auto j) { return to_half<BF16>(used ? sum[int(i)][int(j)] * scale : f32x4{0, 0, 0, 0}); },
         [&](uint32_t row, uint32_t column, u32x4 v) {
             if (row0 + row < n && d0 + column < width)
-                put8(A.dweight + (static_cast<uint64_t>(first) + row0 + row) * A.dweight_stride * 2, d0 + column, width, v);
+                put8_past(A.dweight + (static_cast<uint64_t>(first) + row0 + row) * A.dweight_stride * 2, d0 + column, width, v);
         });
 }
 
@@ -631,8 +638,8 @@ template <bool BF16>
 __global__ __launch_bounds__(kFewWaves* kWaveSize) void head_few_dweight_kernel(const HeadArgs A, const uint32_t first, const uint32_t n, const uint32_t parts)
 {
     using H = Operand<kAcrossK, 256, kFewWaves>;
-    using Out = RowsByLds<1, 16>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * H::kBytes + kFewWaves * Out::kBytes];
+    using Out = RowsByLds<1, 4>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[H::kBytes + kFewWaves * Out::kBytes];
     const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width), width_up = A.stride / 2, chunks = (width_up + 255) / 256;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize), lane = threadIdx.x % kWaveSize;
     const uint32_t block = blockIdx.x / parts, part = blockIdx.x - block * parts;
@@ -652,24 +659,24 @@ __global__ __launch_bounds__(kFewWaves* kWaveSize) void head_few_dweight_kernel(
         h.init(t, wave, lane);
         static_for<H::kLoads>([&](auto i) { h.fetch(i, 0, buffer, wave); });
     };
-    uint32_t mine = 0;
-    if (part < chunks) fetch(part, (FF_LDS uint8_t*)lds);
+    FF_LDS uint8_t* const buffer = (FF_LDS uint8_t*)lds;
     for (uint32_t chunk = part; chunk < chunks; chunk += parts) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (chunk + parts < chunks) fetch(chunk + parts, (FF_LDS uint8_t*)lds + (H::kBytes - mine));
-        const FF_LDS uint8_t* const buffer = (FF_LDS uint8_t*)lds + mine;
-        f32x4 sum[16];
-        static_for<16>([&](auto j) {
-            sum[int(j)] = multiply<BF16>(H::fragment(buffer, 16 * j, 0, lane), g[0], f32x4{0, 0, 0, 0});
-            if (used > 32) sum[int(j)] = multiply<BF16>(H::fragment(buffer, 16 * j, 1, lane), g[1], sum[int(j)]);
-        });
-        Out::pass(
-            (FF_LDS uint8_t*)lds + 2 * H::kBytes, [&](auto, auto j) { return to_half<BF16>(used ? sum[int(j)] * scale : f32x4{0, 0, 0, 0}); },
-            [&](uint32_t row, uint32_t column, u32x4 x) {
-                const uint32_t d = chunk * 256 + column;
-                if (v0 + row < n && d < width) put8(A.dweight + (static_cast<uint64_t>(first) + v0 + row) * A.dweight_stride * 2, d, width, x);
+        if (chunk != part) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the last one has been read
+        fetch(chunk, buffer);
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        static_for<4>([&](auto q) {
+            f32x4 sum[4];
+            static_for<4>([&](auto j) {
+                sum[int(j)] = multiply<BF16>(H::fragment(buffer, 64 * q + 16 * j, 0, lane), g[0], f32x4{0, 0, 0, 0});
+                if (used > 32) sum[int(j)] = multiply<BF16>(H::fragment(buffer, 64 * q + 16 * j, 1, lane), g[1], sum[int(j)]);
             });
-        mine = H::kBytes - mine;
+            Out::pass(
+                buffer + H::kBytes, [&](auto, auto j) { return to_half<BF16>(used ? sum[int(j)] * scale : f32x4{0, 0, 0, 0}); },
+                [&](uint32_t row, uint32_t column, u32x4 x) {
+                    const uint32_t d = chunk * 256 + 64 * q + column;
+                    if (v0 + row < n && d < width) put8_past(A.dweight + (static_cast<uint64_t>(first) + v0 + row) * A.dweight_stride * 2, d, width, x);
+                });
+        });
     }
 }
 
@@ -690,6 +697,7 @@ __global__ void head_of_nothing_kernel(ff_head_stats* stats) { *stats = {}; }
 // ---- the workspace ----------------------------------------------------------------------------------
 
 constexpr uint64_t kPieceElements = 1ull << 28;  // of G, and of a piece's packed rows
+constexpr uint64_t kFewDweightFrom = 1 << 23;    // elements of W, from which on dW of few tokens has its own launch
 constexpr uint32_t kFewDweightBlocks = 1024;    // workgroups of head_few_dweight_kernel, about
 constexpr uint32_t kKeptBlocks = 2048;           // workgroups that make G of kept logits, about
 
@@ -779,6 +787,7 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
     }
     const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.step - 1) / A.step);
     const bool grad = A.dhidden || A.dweight, keep = grad && keeps(A.b), whole = few(A.b);
+    const bool few_dweight = whole && static_cast<uint64_t>(vocab) * A.b.width >= kFewDweightFrom;
     uint32_t first = 0, m = 0, tiles = 0, packed = ~0u;
     // makes piece i the one that the following launches are for
     auto take = [&](uint32_t i, bool rows) {
@@ -817,8 +826,8 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
         const bool last = i == n_pieces - 1, logits = !whole && (!keep || !last);
         take(i, A.dhidden || logits);
         if (logits) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kGrad>), dim3(tiles * tiles_m), threads, 0, stream, A, first, m);
-        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight && !whole ? tiles * tiles_d : 0;
-        if (A.dweight && whole) {
+        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight && !few_dweight ? tiles * tiles_d : 0;
+        if (A.dweight && few_dweight) {
             const uint32_t blocks = (m + kFewEntries - 1) / kFewEntries, parts = std::min(tiles_d, (kFewDweightBlocks + blocks - 1) / blocks);
             hipLaunchKernelGGL(head_few_dweight_kernel<BF16>, dim3(blocks * parts), dim3(kFewWaves * kWaveSize), 0, stream, A, first, m, parts);
         }
@@ -826,7 +835,10 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
             hipLaunchKernelGGL((head_grads_kernel<BF16, BM>), dim3(dh_blocks + dw_blocks), threads, 0, stream, A, first, m, whole ? first : 0,
                            last ? start : kNext, dh_blocks);
     }
-    if (A.dhidden && start != kOnly) hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(std::min(n + 1, 4096u)), dim3(256), 0, stream, A);
+    if (A.dhidden && start != kOnly && n) {
+        const uint32_t blocks_of_row = static_cast<uint32_t>((A.b.width + 4 * kPutThreads - 1) / (4 * kPutThreads));
+        hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(n * blocks_of_row), dim3(kPutThreads), 0, stream, A, blocks_of_row);
+    }
     return hipGetLastError();
 }
 
