@@ -84,7 +84,7 @@ class ff_policy_batch(ctypes.Structure):
 
 
 class ff_head_batch(ctypes.Structure):
-    tensors = ()  # those that it points at (head_batch), kept alive
+    tensors, shapes = (), ()  # those that it points at (head_batch), kept alive; of hidden states, W, one a token
 
     _fields_ = [("hidden", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
                 ("vocab", ctypes.c_uint64), ("width", ctypes.c_uint64), ("hidden_stride", ctypes.c_uint64),
@@ -592,24 +592,28 @@ def ff_policy_loss(batch, logp, token_loss, stats, workspace, dlogits=None, stre
 
 # ---- the two ends of a model ----------------------------------------------------------------------
 
+_I64, _F32 = torch.int64, torch.float32
+
+
+def _refuse(t, name, shape, dtype):
+    raise ValueError("%s is a %s tensor %s of contiguous %s" % (name, dtype, tuple(shape), "rows" if len(shape) == 2 else "entries"))
+
+
 def _rows(t, name, shape, dtype):
     """Elements between a matrix's rows; the rows themselves are contiguous."""
-    if t.dim() != 2 or t.dtype is not dtype or tuple(t.shape) != shape:
-        raise ValueError("%s is a tensor %s of %s" % (name, shape, dtype))
+    if t.dtype is not dtype or t.shape != shape:
+        _refuse(t, name, shape, dtype)
     stride, inner = t.stride()
     if inner != 1 and shape[1] != 1:
-        raise ValueError("%s are rows of contiguous elements" % name)
+        _refuse(t, name, shape, dtype)
     return stride if shape[0] > 1 else max(stride, shape[1])
 
 
-def _vector(t, name, n, dtype):
-    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError("%s is a contiguous tensor of %d entries of %s" % (name, n, dtype))
+def _vector(t, name, shape, dtype):
+    """The address of a vector's entries."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(t, name, shape, dtype)
     return t.data_ptr()
-
-
-def _optional(t, name, n, dtype):
-    return None if t is None else _vector(t, name, n, dtype)
 
 
 def _matrix(t, name):
@@ -621,11 +625,13 @@ def _matrix(t, name):
 def ff_embed(table, ids, out, scale=1.0, stream=None):
     """out[t] = scale * table[ids[t]]; table [vocab, width] of bf16, fp16 or fp32, ids int64 [tokens], out [tokens, width] in
     the table's format.  Rows may lie apart.  An id outside the table (padding) gives a row of zeros."""
-    vocab, width = _matrix(table, "table")
-    n, dtype = ids.numel(), table.dtype
-    _check(lib().ff_embed(table.data_ptr(), vocab, width, _rows(table, "table", (vocab, width), dtype), _DTYPES[dtype],
-                          _vector(ids, "ids", n, torch.int64), n, scale, out.data_ptr(), _rows(out, "out", (n, width), dtype),
-                          _stream_ptr(stream)))
+    shape, n, dtype = _matrix(table, "table"), ids.numel(), table.dtype
+    vocab, width = shape
+    status = lib().ff_embed(table.data_ptr(), vocab, width, _rows(table, "table", shape, dtype), _DTYPES[dtype],
+                            _vector(ids, "ids", (n,), _I64), n, scale, out.data_ptr(), _rows(out, "out", (n, width), dtype),
+                            _stream_ptr(stream))
+    if status:
+        _check(status)
 
 
 def alloc_embed_workspace(n_tokens, vocab, width, device):
@@ -635,25 +641,31 @@ def alloc_embed_workspace(n_tokens, vocab, width, device):
 def ff_embed_grad(dout, ids, dtable, workspace, scale=1.0, add=False, stream=None):
     """dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] == v); add: added to what is there, rows that no
     token asks for left alone."""
-    vocab, width = _matrix(dtable, "dtable")
-    n, dtype = ids.numel(), dtable.dtype
-    if workspace.nbytes < lib().ff_embed_workspace_bytes(n, vocab, width):
+    shape, n, dtype, L = _matrix(dtable, "dtable"), ids.numel(), dtable.dtype, lib()
+    vocab, width = shape
+    if workspace.nbytes < L.ff_embed_workspace_bytes(n, vocab, width):
         raise ValueError("the workspace is smaller than ff_embed_workspace_bytes()")
-    _check(lib().ff_embed_grad(dout.data_ptr(), _rows(dout, "dout", (n, width), dtype), _DTYPES[dtype],
-                               _vector(ids, "ids", n, torch.int64), n, vocab, width, scale, dtable.data_ptr(),
-                               _rows(dtable, "dtable", (vocab, width), dtype), FF_GRAD_ADD if add else 0, workspace.data_ptr(),
-                               _stream_ptr(stream)))
+    status = L.ff_embed_grad(dout.data_ptr(), _rows(dout, "dout", (n, width), dtype), _DTYPES[dtype],
+                             _vector(ids, "ids", (n,), _I64), n, vocab, width, scale, dtable.data_ptr(),
+                             _rows(dtable, "dtable", shape, dtype), FF_GRAD_ADD if add else 0, workspace.data_ptr(),
+                             _stream_ptr(stream))
+    if status:
+        _check(status)
 
 
 def ff_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, stream=None):
     """y = (x - mean) * rstd * weight + bias over the rows of x [rows, width]; bias may be None; y may be x.  mean, rstd: fp32
     [rows], for the gradient, or None."""
-    n, width = _matrix(x, "x")
-    dtype, f32 = x.dtype, torch.float32
-    _check(lib().ff_layer_norm(x.data_ptr(), n, width, _rows(x, "x", (n, width), dtype), _DTYPES[dtype],
-                               _vector(weight, "weight", width, dtype), _optional(bias, "bias", width, dtype), eps, y.data_ptr(),
-                               _rows(y, "y", (n, width), dtype), _optional(mean, "mean", n, f32), _optional(rstd, "rstd", n, f32),
-                               _stream_ptr(stream)))
+    shape, dtype = _matrix(x, "x"), x.dtype
+    n, width = shape
+    one, each = (width,), (n,)
+    status = lib().ff_layer_norm(x.data_ptr(), n, width, _rows(x, "x", shape, dtype), _DTYPES[dtype],
+                                 _vector(weight, "weight", one, dtype), None if bias is None else _vector(bias, "bias", one, dtype),
+                                 eps, y.data_ptr(), _rows(y, "y", shape, dtype),
+                                 None if mean is None else _vector(mean, "mean", each, _F32),
+                                 None if rstd is None else _vector(rstd, "rstd", each, _F32), _stream_ptr(stream))
+    if status:
+        _check(status)
 
 
 def alloc_norm_workspace(n_rows, width, device):
@@ -662,16 +674,20 @@ def alloc_norm_workspace(n_rows, width, device):
 
 def ff_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight=None, dbias=None, workspace=None, stream=None):
     """Gradients of ff_layer_norm from dy; dx may be dy or x; dweight and dbias [width], or None."""
-    n, width = _matrix(x, "x")
-    dtype, f32 = x.dtype, torch.float32
+    shape, dtype, L = _matrix(x, "x"), x.dtype, lib()
+    n, width = shape
+    one, each = (width,), (n,)
     if dweight is not None or dbias is not None:
-        if workspace is None or workspace.nbytes < lib().ff_layer_norm_workspace_bytes(n, width):
+        if workspace is None or workspace.nbytes < L.ff_layer_norm_workspace_bytes(n, width):
             raise ValueError("the workspace is smaller than ff_layer_norm_workspace_bytes()")
-    _check(lib().ff_layer_norm_grad(
-        x.data_ptr(), n, width, _rows(x, "x", (n, width), dtype), _DTYPES[dtype], _vector(weight, "weight", width, dtype),
-        _vector(mean, "mean", n, f32), _vector(rstd, "rstd", n, f32), dy.data_ptr(), _rows(dy, "dy", (n, width), dtype),
-        dx.data_ptr(), _rows(dx, "dx", (n, width), dtype), _optional(dweight, "dweight", width, dtype),
-        _optional(dbias, "dbias", width, dtype), None if workspace is None else workspace.data_ptr(), _stream_ptr(stream)))
+    status = L.ff_layer_norm_grad(
+        x.data_ptr(), n, width, _rows(x, "x", shape, dtype), _DTYPES[dtype], _vector(weight, "weight", one, dtype),
+        _vector(mean, "mean", each, _F32), _vector(rstd, "rstd", each, _F32), dy.data_ptr(), _rows(dy, "dy", shape, dtype),
+        dx.data_ptr(), _rows(dx, "dx", shape, dtype), None if dweight is None else _vector(dweight, "dweight", one, dtype),
+        None if dbias is None else _vector(dbias, "dbias", one, dtype), None if workspace is None else workspace.data_ptr(),
+        _stream_ptr(stream))
+    if status:
+        _check(status)
 
 
 class HeadStats:
@@ -692,13 +708,15 @@ _HEAD = struct.Struct("7Q2I2QfI")
 def head_batch(hidden, weight, targets, weights, loss_scale=1.0):
     """ff_head_batch of device tensors: hidden [tokens, width], weight [vocab, width] (bf16 or fp16, rows may lie apart), targets
     int64 and weights fp32 [tokens].  It keeps the tensors alive (see policy_batch)."""
-    n, width = _matrix(hidden, "hidden")
-    vocab, dtype = _matrix(weight, "weight")[0], hidden.dtype
+    shape, dtype = _matrix(hidden, "hidden"), hidden.dtype
+    n, width = shape
+    table = (_matrix(weight, "weight")[0], width)
     batch = ff_head_batch.from_buffer_copy(_HEAD.pack(
-        hidden.data_ptr(), weight.data_ptr(), n, vocab, width, _rows(hidden, "hidden", (n, width), dtype),
-        _rows(weight, "weight", (vocab, width), dtype), _DTYPES[dtype], 0, _vector(targets, "targets", n, torch.int64),
-        _vector(weights, "weights", n, torch.float32), loss_scale, 0))
+        hidden.data_ptr(), weight.data_ptr(), n, table[0], width, _rows(hidden, "hidden", shape, dtype),
+        _rows(weight, "weight", table, dtype), _DTYPES[dtype], 0, _vector(targets, "targets", (n,), _I64),
+        _vector(weights, "weights", (n,), _F32), loss_scale, 0))
     batch.tensors = (hidden, weight, targets, weights)
+    batch.shapes = shape, table, (n,)
     return batch
 
 
@@ -711,14 +729,17 @@ def alloc_head_workspace(batch, device, grad=True):
 def ff_head_loss(batch, logp, stats, workspace, dhidden=None, dweight=None, stream=None):
     """Cross entropy of the batch's targets: log-probabilities into logp [tokens], the loss into stats (HeadStats); dhidden
     [tokens, width] (may be the hidden states), dweight [vocab, width], or None."""
-    n, width, vocab, dtype = batch.n_tokens, batch.width, batch.vocab, batch.tensors[0].dtype
-    grad = dhidden is not None or dweight is not None
-    dh = dw = (None, 0)
+    L, ref, dtype = lib(), ctypes.byref(batch), batch.tensors[0].dtype
+    tokens, table, one = batch.shapes
+    dh = dw = None
+    dh_stride = dw_stride = 0
     if dhidden is not None:
-        dh = dhidden.data_ptr(), _rows(dhidden, "dhidden", (n, width), dtype)
+        dh, dh_stride = dhidden.data_ptr(), _rows(dhidden, "dhidden", tokens, dtype)
     if dweight is not None:
-        dw = dweight.data_ptr(), _rows(dweight, "dweight", (vocab, width), dtype)
-    if workspace.nbytes < lib().ff_head_workspace_bytes(ctypes.byref(batch), 1 if grad else 0):
+        dw, dw_stride = dweight.data_ptr(), _rows(dweight, "dweight", table, dtype)
+    if workspace.nbytes < L.ff_head_workspace_bytes(ref, 0 if dhidden is None and dweight is None else 1):
         raise ValueError("the workspace is smaller than ff_head_workspace_bytes()")
-    _check(lib().ff_head_loss(ctypes.byref(batch), _vector(logp, "logp", n, torch.float32), *dh, *dw, stats.data_ptr(),
-                              workspace.data_ptr(), _stream_ptr(stream)))
+    status = L.ff_head_loss(ref, _vector(logp, "logp", one, _F32), dh, dh_stride, dw, dw_stride, stats.data_ptr(),
+                            workspace.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status)

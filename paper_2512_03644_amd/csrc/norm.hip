@@ -165,32 +165,43 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
     const float each = 1.f / static_cast<float>(width);
     const uint32_t group = blockIdx.x * kPer + threadIdx.x / GROUP;
     const uint64_t step = static_cast<uint64_t>(blocks) * kPer;
+    // The widest rows leave no registers for the next row, nor for this one while its sums are made: it is read again, from the caches.
+    constexpr bool kHold = GROUP * K <= 1024;
     typename I::Held w[K];
     f32x8 dw[K], db[K];
     struct Row {
         typename I::Held x[K], dy[K];
         float mean, rstd;
     } next;
+    auto load_x = [&](uint64_t r, uint32_t at) { return I::load(a.x + r * a.x_stride * I::kBytes, at, width); };
+    auto load_dy = [&](uint64_t r, uint32_t at) { return I::load(a.dy + r * a.dy_stride * I::kBytes, at, width); };
+    auto load_w = [&](uint32_t at) { return I::load(a.weight, at, width); };
     auto fetch = [&](Row& to, uint64_t r) {
         to.mean = a.mean[r];
         to.rstd = a.rstd[r];
-        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
-            to.x[int(i)] = I::load(a.x + r * a.x_stride * I::kBytes, at, width);
-            to.dy[int(i)] = I::load(a.dy + r * a.dy_stride * I::kBytes, at, width);
-        });
+        if constexpr (kHold)
+            places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+                to.x[int(i)] = load_x(r, at);
+                to.dy[int(i)] = load_dy(r, at);
+            });
     };
     uint64_t r = group;
     if (r < a.n_rows) fetch(next, r);
-    places<GROUP, K>(thread, width, [&](auto i, uint32_t at) { w[int(i)] = I::load(a.weight, at, width); });
+    if constexpr (kHold) places<GROUP, K>(thread, width, [&](auto i, uint32_t at) { w[int(i)] = load_w(at); });
     static_for<K>([&](auto i) { dw[int(i)] = db[int(i)] = f32x8{}; });
     int turn = 0;
-    constexpr bool kAhead = GROUP * K <= 1024;  // the next row while this one is at work, where there are registers for it
     for (; r < a.n_rows; r += step) {
         const Row now = next;
-        if (kAhead && r + step < a.n_rows) fetch(next, r + step);
+        if (r + step < a.n_rows) fetch(next, r + step);
+        // fn(i, at, x normed, dy, dy * weight)
+        auto each_place = [&](auto&& fn) {
+            places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
+                const f32x8 x = I::wide(kHold ? now.x[int(i)] : load_x(r, at)), d = I::wide(kHold ? now.dy[int(i)] : load_dy(r, at));
+                fn(i, at, (x - now.mean) * now.rstd, d, d * I::wide(kHold ? w[int(i)] : load_w(at)));
+            });
+        };
         float s[2] = {0.f, 0.f};
-        places<GROUP, K>(thread, width, [&](auto i, uint32_t) {
-            const f32x8 normed = (I::wide(now.x[int(i)]) - now.mean) * now.rstd, d = I::wide(now.dy[int(i)]), g = d * I::wide(w[int(i)]);
+        each_place([&](auto i, uint32_t, f32x8 normed, f32x8 d, f32x8 g) {
             s[0] += sum8(g);
             s[1] += sum8(g * normed);
             dw[int(i)] += d * normed;
@@ -199,11 +210,9 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
         sum_over<GROUP>(s, turn);
         turn ^= 1;
         const float c0 = s[0] * each, c1 = s[1] * each;
-        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
-            const f32x8 normed = (I::wide(now.x[int(i)]) - now.mean) * now.rstd, g = I::wide(now.dy[int(i)]) * I::wide(w[int(i)]);
+        each_place([&](auto, uint32_t at, f32x8 normed, f32x8, f32x8 g) {
             I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(now.rstd * (g - c0 - normed * c1)));
         });
-        if (!kAhead && r + step < a.n_rows) fetch(next, r + step);
     }
     if (column_blocks || (!a.dweight && !a.dbias)) return;
     if constexpr (kPer > 1) {  // the workgroup's groups into one, in their order
