@@ -45,6 +45,22 @@ __global__ __launch_bounds__(kWaveSize * kWaves) void embed_kernel(const EmbedAr
     }
 }
 
+// Rows [0, n) of the table's gradient from `out` on, elements [from, to): zeros in those that `which(row)` names.  `waves` wavefronts, of which this
+// is number `wave`; as many rows at a time as a wavefront has lanes for.
+template <uint32_t DTYPE, class Which>
+__device__ __forceinline__ void clear_rows(uint8_t* out, uint64_t stride, uint64_t n, uint32_t from, uint32_t to, uint64_t wave, uint64_t waves, Which&& which)
+{
+    using I = Items<DTYPE>;
+    const uint32_t lane = threadIdx.x % kWaveSize;
+    uint32_t lanes = 1;  // of a row
+    while (lanes < kWaveSize && lanes * kLaneItems < to - from) lanes *= 2;
+    const uint32_t rows = kWaveSize / lanes;
+    for (uint64_t r = wave * rows + lane / lanes; r < n; r += waves * rows)
+        if (which(r))
+            for (uint32_t at = from + lane % lanes * kLaneItems; at < to; at += lanes * kLaneItems)
+                I::store(out + r * stride * I::kBytes, at, to, I::narrow(f32x8{}));
+}
+
 // ---- order of the tokens ------------------------------------------------------------------------------
 
 constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / kWaveSize, kSortRounds = 16;
@@ -57,7 +73,10 @@ struct Sorted {
     uint32_t* ids;    // and their ids
     float* ends;      // [part of the list][its beginning, its end][width]: sums that reach over it
     uint32_t part;    // entries of a part
+    uint32_t* counts; // of runs that reach over parts' ends: over few parts, over many
+    uint2* runs[2];   // the part that each begins in, and its last one, in any order
 };
+constexpr uint32_t kManyParts = 8;  // more than these
 
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArgs a, const Sorted s)
 {
@@ -76,6 +95,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedArg
         return id >= 0 && in < range ? static_cast<uint32_t>(in) : kRange;
     };
     for (uint32_t i = threadIdx.x; i < kRange; i += kSortThreads) bins[i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) s.counts[threadIdx.x] = 0;
     __syncthreads();
     // ids of one round: a wavefront's follow each other.  Those of the last round are kept: up to kSortIds tokens are read once
     uint32_t below = 0, unused = 0, b[kSortRounds];
@@ -196,6 +216,11 @@ __device__ __forceinline__ void sum_part(const EmbedArgs& a, const Sorted& s, ui
     constexpr uint32_t kAhead = 4;
     const uint32_t width = static_cast<uint32_t>(a.width);
     const Part p(s, c, n);
+    if (p.joins_behind && p.last_begins() && at < kLaneItems) {  // (one lane, of one wavefront to a part)
+        const uint32_t last = (s.begin[p.id_of(p.count - 1) + 1] - 1) / s.part;
+        const uint32_t many = last - c >= kManyParts;
+        s.runs[many][atomicAdd(s.counts + many, 1u)] = uint2{c, last};
+    }
     if (at >= width) return;
     bool begins = !p.joins_before;  // does the run at work begin in this part?
     f32x8 sum = {};
@@ -234,7 +259,6 @@ __device__ __forceinline__ void sum_part(const EmbedArgs& a, const Sorted& s, ui
 template <uint32_t DTYPE, bool ADD>
 __global__ __launch_bounds__(kWaveSize* kWaves) void embed_sum_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs, const uint32_t sum_blocks)
 {
-    using I = Items<DTYPE>;
     const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width), n = s.begin[vocab];
     const uint32_t lane_at = threadIdx.x % kWaveSize * kLaneItems;
     if (blockIdx.x < sum_blocks) {
@@ -244,56 +268,78 @@ __global__ __launch_bounds__(kWaveSize* kWaves) void embed_sum_kernel(const Embe
             sum_part<DTYPE, ADD>(a, s, c, n, at);
         }
     } else if (!ADD) {
-        const uint32_t step = (gridDim.x - sum_blocks) * kWaves;
-        for (uint64_t v = (blockIdx.x - sum_blocks) * kWaves + wave_of(); v < vocab; v += step) {
-            if (s.begin[v] != s.begin[v + 1]) continue;
-            for (uint32_t at = lane_at; at < width; at += kSlab) I::store(a.out + v * a.out_stride * I::kBytes, at, width, I::narrow(f32x8{}));
-        }
+        clear_rows<DTYPE>(a.out, a.out_stride, vocab, 0, width, static_cast<uint64_t>(blockIdx.x - sum_blocks) * kWaves + wave_of(),
+                          static_cast<uint64_t>(gridDim.x - sum_blocks) * kWaves, [&](uint64_t v) { return s.begin[v] == s.begin[v + 1]; });
     }
 }
 
-// Sums that begin in part c and reach over its end.
+// Sums that reach over the ends of parts.  Over few parts: a wavefront to 512 elements of one; over many: a workgroup, whose wavefronts take its parts in
+// turn.  `few_blocks` workgroups take the former.
+constexpr uint32_t kJoinWaves = 8, kJoinFewBlocks = 1024, kJoinManyBlocks = 512;
 template <uint32_t DTYPE, bool ADD>
-__global__ __launch_bounds__(kWaveSize* kWaves) void embed_join_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs)
+__global__ __launch_bounds__(kWaveSize* kJoinWaves) void embed_join_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs, const uint32_t few_blocks)
 {
     using I = Items<DTYPE>;
     using F = Items<FF_F32>;
-    const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width), n = s.begin[vocab];
-    const uint64_t total = static_cast<uint64_t>((n + s.part - 1) / s.part) * slabs, step = static_cast<uint64_t>(gridDim.x) * kWaves;
-    for (uint64_t w = static_cast<uint64_t>(blockIdx.x) * kWaves + wave_of(); w < total; w += step) {
-        const uint32_t c = static_cast<uint32_t>(w / slabs);
-        const uint32_t at = static_cast<uint32_t>(w - static_cast<uint64_t>(c) * slabs) * kSlab + threadIdx.x % kWaveSize * kLaneItems;
-        const Part p(s, c, n);
-        if (!p.joins_behind || !p.last_begins() || at >= width) continue;
-        const uint32_t id = p.id_of(p.count - 1), to = s.begin[id + 1];
-        auto part = [&](uint32_t k, uint32_t which) { return F::wide(F::load(reinterpret_cast<const uint8_t*>(s.ends + (2ull * k + which) * width), at, width)); };
-        f32x8 sum = part(c, 1);
-        const uint32_t last = (to - 1) / s.part;
-        uint32_t k = c + 1;
+    __shared__ u32x4 joined[kJoinWaves][2][kWaveSize];
+    const uint32_t width = static_cast<uint32_t>(a.width), wave = wave_of(), lane = threadIdx.x % kWaveSize;
+    auto end_of = [&](uint32_t k, uint32_t which, uint32_t at) {
+        return F::wide(F::load(reinterpret_cast<const uint8_t*>(s.ends + (2ull * k + which) * width), at, width));
+    };
+    // parts from, from + step, ... up to last: their beginnings
+    auto sum_of = [&](f32x8 sum, uint32_t from, uint32_t last, uint32_t step, uint32_t at) {
         constexpr uint32_t kAhead = 8;
-        for (; k <= last; k += kAhead) {
+        for (uint32_t k = from; k <= last; k += kAhead * step) {
             f32x8 x[kAhead];
             static_for<kAhead>([&](auto i) {
-                if (k + i <= last) x[int(i)] = part(k + i, 0);
+                if (k + i * step <= last) x[int(i)] = end_of(k + i * step, 0, at);
             });
             static_for<kAhead>([&](auto i) {
-                if (k + i <= last) sum += x[int(i)];
+                if (k + i * step <= last) sum += x[int(i)];
             });
         }
-        sum *= a.scale;
+        return sum;
+    };
+    auto put = [&](uint32_t part, f32x8 sum, uint32_t at) {
+        const uint32_t id = s.ids[(part + 1) * s.part - 1];
         uint8_t* const out = a.out + static_cast<uint64_t>(id) * a.out_stride * I::kBytes;
+        sum *= a.scale;
         if (ADD) sum += I::wide(I::load(out, at, width));
         I::store(out, at, width, I::narrow(sum));
+    };
+    if (blockIdx.x < few_blocks) {
+        const uint64_t total = static_cast<uint64_t>(s.counts[0]) * slabs;
+        for (uint64_t w = static_cast<uint64_t>(blockIdx.x) * kJoinWaves + wave; w < total; w += static_cast<uint64_t>(few_blocks) * kJoinWaves) {
+            const uint32_t k = static_cast<uint32_t>(w / slabs), at = static_cast<uint32_t>(w - static_cast<uint64_t>(k) * slabs) * kSlab + lane * kLaneItems;
+            const uint2 run = s.runs[0][k];
+            if (at < width) put(run.x, sum_of(end_of(run.x, 1, at), run.x + 1, run.y, 1, at), at);
+        }
+        return;
+    }
+    const uint64_t total = static_cast<uint64_t>(s.counts[1]) * slabs;
+    for (uint64_t w = blockIdx.x - few_blocks; w < total; w += gridDim.x - few_blocks) {
+        const uint32_t k = static_cast<uint32_t>(w / slabs), at = static_cast<uint32_t>(w - static_cast<uint64_t>(k) * slabs) * kSlab + lane * kLaneItems;
+        const uint2 run = s.runs[1][k];
+        f32x8 sum = {};
+        if (at < width) sum = sum_of(wave == 0 ? end_of(run.x, 1, at) : sum, run.x + 1 + wave, run.y, kJoinWaves, at);
+        const typename F::Held h = F::narrow(sum);
+        joined[wave][0][lane] = h.w[0];
+        joined[wave][1][lane] = h.w[1];
+        __syncthreads();
+        if (wave == 0 && at < width) {
+            for (uint32_t i = 1; i < kJoinWaves; i++) sum += F::wide(typename F::Held{{joined[i][0][lane], joined[i][1][lane]}});
+            put(run.x, sum, at);
+        }
+        __syncthreads();
     }
 }
-
-uint64_t up(uint64_t x) { return (x + 255) / 256 * 256; }
 
 // ---- few tokens ---------------------------------------------------------------------------------------
 
 // All of it in one launch: a workgroup takes 512 elements of the rows of a range of ids, and finds and sorts the tokens that ask for
-// them in LDS.  A wavefront sums a row's tokens; rows of more than kLong are summed by all wavefronts together.
-constexpr uint32_t kFewThreads = 512, kFewWaves = kFewThreads / kWaveSize, kFewTokens = 4096, kFewRounds = kFewTokens / kFewThreads, kLong = 16, kFewBlocks = 1024;
+// them in LDS.  A wavefront sums a row's tokens, several at a time where its lanes are more than a row takes; rows of more than kLong are summed by all
+// wavefronts together.
+constexpr uint32_t kFewThreads = 512, kFewWaves = kFewThreads / kWaveSize, kFewTokens = 4096, kFewRounds = kFewTokens / kFewThreads, kLong = 16, kFewBlocks = 768, kFewWork = 8192;
 
 // Rows of tokens list[from], list[from + step], ... in front of `to`.
 template <uint32_t DTYPE>
@@ -325,8 +371,23 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
     const uint32_t n = static_cast<uint32_t>(a.n_tokens), vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width);
     const uint32_t wave = wave_of(), lane = threadIdx.x % kWaveSize, block = blockIdx.x / slabs;
     const uint32_t first = block * range_ids, range = vocab - first < range_ids ? vocab - first : range_ids;
-    const uint32_t at = (blockIdx.x - block * slabs) * kSlab + lane * kLaneItems;
+    const uint32_t slab = (blockIdx.x - block * slabs) * kSlab, slab_end = width - slab < kSlab ? width : slab + kSlab;
+    uint32_t lanes = 1;  // that a row takes
+    while (lanes < kWaveSize && lanes * kLaneItems < slab_end - slab) lanes *= 2;
+    const uint32_t at = slab + lane % lanes * kLaneItems, turn = lane / lanes, turns = kWaveSize / lanes;
+    const bool mine = at < width, puts = mine && turn == 0;
     const uint64_t lower = (1ull << lane) - 1;
+    // of a wavefront's lanes that have the same elements, in the first of them
+    auto join = [&](f32x8 sum) {
+        for (uint32_t d = kWaveSize / 2; d >= lanes; d /= 2)
+            static_for<8>([&](auto i) { sum[int(i)] += __shfl_down(sum[int(i)], d); });
+        return sum;
+    };
+    // The whole range is cleared first, while the ids are on their way; sums overwrite it, behind the barriers.
+    if (!ADD) {
+        clear_rows<DTYPE>(a.out + static_cast<uint64_t>(first) * a.out_stride * I::kBytes, a.out_stride, range, slab, slab_end, wave, kFewWaves,
+                          [](uint64_t) { return true; });
+    }
     // the range's tokens in their order
     uint32_t b[kFewRounds], count = 0;
     const uint32_t t0 = wave * (kWaveSize * kFewRounds) + lane;
@@ -406,22 +467,26 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
     for (uint32_t id = wave; id < range; id += kFewWaves) {
         const uint32_t from = id ? begin[id - 1] : 0, to = begin[id];
         if (to - from > kLong) any_long = true;
-        if (to - from > kLong || (ADD && from == to) || at >= width) continue;
+        if (to - from > kLong || from == to) continue;
         typename I::Held old;
-        if (ADD) old = there(id);
-        put(id, sum_list<DTYPE>(a, order, from, to, 1, at), old);
+        if (ADD && puts) old = there(id);
+        f32x8 sum = {};
+        if (mine) sum = sum_list<DTYPE>(a, order, from + turn, to, turns, at);
+        sum = join(sum);
+        if (puts) put(id, sum, old);
     }
     if (!__syncthreads_or(any_long)) return;
     for (uint32_t id = 0; id < range; id++) {
         const uint32_t from = id ? begin[id - 1] : 0, to = begin[id];
         if (to - from <= kLong) continue;
         f32x8 sum = {};
-        if (at < width) sum = sum_list<DTYPE>(a, order, from + wave, to, kFewWaves, at);
+        if (mine) sum = sum_list<DTYPE>(a, order, from + wave * turns + turn, to, kFewWaves * turns, at);
+        sum = join(sum);
         const typename F::Held h = F::narrow(sum);
         joined[wave][0][lane] = h.w[0];
         joined[wave][1][lane] = h.w[1];
         __syncthreads();
-        if (wave == 0 && at < width) {
+        if (wave == 0 && puts) {
             typename I::Held old;
             if (ADD) old = there(id);
             for (uint32_t k = 1; k < kFewWaves; k++) sum += F::wide(typename F::Held{{joined[k][0][lane], joined[k][1][lane]}});
@@ -431,6 +496,8 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
     }
 }
 
+uint64_t up(uint64_t x) { return (x + 255) / 256 * 256; }
+
 // Entries of a part: as many as leave work for kPartWaves wavefronts, within limits.
 constexpr uint32_t kPartWaves = 8192, kLeastPart = 8, kMostPart = 32;
 uint32_t part_of(uint64_t n, uint64_t slabs)
@@ -439,14 +506,16 @@ uint32_t part_of(uint64_t n, uint64_t slabs)
 }
 
 struct Places {
-    uint64_t begin, order, ids, ends, bytes;
+    uint64_t begin, order, ids, counts, runs, ends, bytes;
 };
 Places place(uint64_t n, uint64_t vocab, uint64_t width)
 {
     Places p = {};
     p.order = up((vocab + 1) * 4);
     p.ids = p.order + up(n * 4);
-    p.ends = p.ids + up(n * 4);
+    p.counts = p.ids + up(n * 4);
+    p.runs = p.counts + 256;
+    p.ends = p.runs + 2 * up((n / kLeastPart + 1) * sizeof(uint2));
     // (both ends of every part; never less for more tokens or elements, whatever the parts come to)
     const uint64_t parts = (n / kMostPart + 1) * width + std::min<uint64_t>((n / kLeastPart + 1) * width, 2ull * kPartWaves * kSlab);
     p.bytes = p.ends + parts * 2 * 4;
@@ -460,7 +529,7 @@ template <uint32_t DTYPE, bool ADD>
 hipError_t launch_grad(const EmbedArgs& a, Sorted s, hipStream_t stream)
 {
     const uint32_t slabs = static_cast<uint32_t>((a.width + kSlab - 1) / kSlab);
-    if (a.n_tokens <= kFewTokens && (a.vocab / kFewThreads + 1) * slabs <= most_groups(kFewThreads)) {
+    if (a.n_tokens <= kFewTokens && a.n_tokens * slabs <= kFewWork && (a.vocab / kFewThreads + 1) * slabs <= most_groups(kFewThreads)) {
         // ranges of 8 to 512 ids, for about kFewBlocks workgroups
         uint32_t range = 8;
         while (range < kFewThreads && (a.vocab + range - 1) / range * slabs > kFewBlocks) range *= 2;
@@ -472,9 +541,13 @@ hipError_t launch_grad(const EmbedArgs& a, Sorted s, hipStream_t stream)
     const uint64_t n_parts = (a.n_tokens + s.part - 1) / s.part;
     hipLaunchKernelGGL(embed_sort_kernel, dim3(static_cast<uint32_t>((a.vocab + kRange - 1) / kRange)), dim3(kSortThreads), 0, stream, a, s);
     const dim3 threads(kWaveSize * kWaves);
-    const uint32_t sum_blocks = groups(n_parts * slabs);
-    hipLaunchKernelGGL((embed_sum_kernel<DTYPE, ADD>), dim3(sum_blocks + (ADD ? 0 : groups(a.vocab))), threads, 0, stream, a, s, slabs, sum_blocks);
-    if (n_parts > 1) hipLaunchKernelGGL((embed_join_kernel<DTYPE, ADD>), dim3(groups(n_parts * slabs)), threads, 0, stream, a, s, slabs);
+    const uint32_t sum_blocks = groups(n_parts * slabs), rows_at_once = static_cast<uint32_t>(std::max<uint64_t>(kSlab / a.width, 1));
+    hipLaunchKernelGGL((embed_sum_kernel<DTYPE, ADD>), dim3(sum_blocks + (ADD ? 0 : groups((a.vocab + rows_at_once - 1) / rows_at_once))), threads, 0, stream, a, s, slabs, sum_blocks);
+    if (n_parts > 1) {
+        const uint32_t few_blocks = static_cast<uint32_t>(std::min<uint64_t>((n_parts * slabs + kJoinWaves - 1) / kJoinWaves, kJoinFewBlocks));
+        const uint32_t many_blocks = static_cast<uint32_t>(std::min<uint64_t>(n_parts / kManyParts * slabs, kJoinManyBlocks));
+        hipLaunchKernelGGL((embed_join_kernel<DTYPE, ADD>), dim3(few_blocks + many_blocks), dim3(kWaveSize * kJoinWaves), 0, stream, a, s, slabs, few_blocks);
+    }
     return hipGetLastError();
 }
 
@@ -505,7 +578,8 @@ hipError_t launch_embed_grad(const EmbedArgs& a, uint32_t dtype, bool add, void*
     const Places p = place(a.n_tokens, a.vocab, a.width);
     uint8_t* const w = static_cast<uint8_t*>(workspace);
     const Sorted s = {reinterpret_cast<uint32_t*>(w + p.begin), reinterpret_cast<uint32_t*>(w + p.order), reinterpret_cast<uint32_t*>(w + p.ids),
-                      reinterpret_cast<float*>(w + p.ends), 0};
+                      reinterpret_cast<float*>(w + p.ends), 0, reinterpret_cast<uint32_t*>(w + p.counts),
+                      {reinterpret_cast<uint2*>(w + p.runs), reinterpret_cast<uint2*>(w + p.runs) + (a.n_tokens / kLeastPart + 1)}};
     if (dtype == FF_BF16) return launch_grad<FF_BF16>(a, add, s, stream);
     if (dtype == FF_F16) return launch_grad<FF_F16>(a, add, s, stream);
     return launch_grad<FF_F32>(a, add, s, stream);
