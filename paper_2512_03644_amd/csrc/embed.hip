@@ -27,7 +27,7 @@ __device__ __forceinline__ uint32_t wave_of() { return __builtin_amdgcn_readfirs
 
 // ---- lookup -----------------------------------------------------------------------------------------
 
-template <uint32_t DTYPE>
+template <uint32_t DTYPE, bool PAST>
 __global__ __launch_bounds__(kWaveSize * kWaves) void embed_kernel(const EmbedArgs a, const uint32_t slabs)
 {
     using I = Items<DTYPE>;
@@ -41,13 +41,13 @@ __global__ __launch_bounds__(kWaveSize * kWaves) void embed_kernel(const EmbedAr
         f32x8 v = {};
         if (id >= 0 && static_cast<uint64_t>(id) < a.vocab)
             v = I::wide(I::load(a.rows + static_cast<uint64_t>(id) * a.rows_stride * I::kBytes, at, width)) * a.scale;
-        I::store(a.out + t * a.out_stride * I::kBytes, at, width, I::narrow(v));
+        I::template store<PAST>(a.out + t * a.out_stride * I::kBytes, at, width, I::narrow(v));
     }
 }
 
 // Rows [0, n) of the table's gradient from `out` on, elements [from, to): zeros in those that `which(row)` names.  `waves` wavefronts, of which this
 // is number `wave`; as many rows at a time as a wavefront has lanes for.
-template <uint32_t DTYPE, class Which>
+template <uint32_t DTYPE, bool PAST, class Which>
 __device__ __forceinline__ void clear_rows(uint8_t* out, uint64_t stride, uint64_t n, uint32_t from, uint32_t to, uint64_t wave, uint64_t waves, Which&& which)
 {
     using I = Items<DTYPE>;
@@ -58,7 +58,7 @@ __device__ __forceinline__ void clear_rows(uint8_t* out, uint64_t stride, uint64
     for (uint64_t r = wave * rows + lane / lanes; r < n; r += waves * rows)
         if (which(r))
             for (uint32_t at = from + lane % lanes * kLaneItems; at < to; at += lanes * kLaneItems)
-                I::store(out + r * stride * I::kBytes, at, to, I::narrow(f32x8{}));
+                I::template store<PAST>(out + r * stride * I::kBytes, at, to, I::narrow(f32x8{}));
 }
 
 // ---- order of the tokens ------------------------------------------------------------------------------
@@ -209,7 +209,7 @@ struct Part {
 };
 
 // Elements [at, at + 8) of a part's tokens' rows; ADD: sums are added to what is there.
-template <uint32_t DTYPE, bool ADD>
+template <uint32_t DTYPE, bool ADD, bool PAST>
 __device__ __forceinline__ void sum_part(const EmbedArgs& a, const Sorted& s, uint32_t c, uint32_t n, uint32_t at)
 {
     using I = Items<DTYPE>;
@@ -245,7 +245,7 @@ __device__ __forceinline__ void sum_part(const EmbedArgs& a, const Sorted& s, ui
             if (whole[int(i)]) {
                 sum *= a.scale;
                 if (ADD) sum += I::wide(old[int(i)]);
-                I::store(a.out + static_cast<uint64_t>(p.id_of(k + i)) * a.out_stride * I::kBytes, at, width, I::narrow(sum));
+                I::template store<PAST>(a.out + static_cast<uint64_t>(p.id_of(k + i)) * a.out_stride * I::kBytes, at, width, I::narrow(sum));
             } else {
                 Items<FF_F32>::store(reinterpret_cast<uint8_t*>(s.ends + (2ull * c + begins) * width), at, width, Items<FF_F32>::narrow(sum));
             }
@@ -256,7 +256,7 @@ __device__ __forceinline__ void sum_part(const EmbedArgs& a, const Sorted& s, ui
 }
 
 // The first `sum_blocks` workgroups: the parts of the list.  The others, unless it is added: zeros into rows without tokens.
-template <uint32_t DTYPE, bool ADD>
+template <uint32_t DTYPE, bool ADD, bool PAST>
 __global__ __launch_bounds__(kWaveSize* kWaves) void embed_sum_kernel(const EmbedArgs a, const Sorted s, const uint32_t slabs, const uint32_t sum_blocks)
 {
     const uint32_t vocab = static_cast<uint32_t>(a.vocab), width = static_cast<uint32_t>(a.width), n = s.begin[vocab];
@@ -265,10 +265,10 @@ __global__ __launch_bounds__(kWaveSize* kWaves) void embed_sum_kernel(const Embe
         const uint64_t total = static_cast<uint64_t>((n + s.part - 1) / s.part) * slabs, step = static_cast<uint64_t>(sum_blocks) * kWaves;
         for (uint64_t w = static_cast<uint64_t>(blockIdx.x) * kWaves + wave_of(); w < total; w += step) {
             const uint32_t c = static_cast<uint32_t>(w / slabs), at = static_cast<uint32_t>(w - static_cast<uint64_t>(c) * slabs) * kSlab + lane_at;
-            sum_part<DTYPE, ADD>(a, s, c, n, at);
+            sum_part<DTYPE, ADD, PAST>(a, s, c, n, at);
         }
     } else if (!ADD) {
-        clear_rows<DTYPE>(a.out, a.out_stride, vocab, 0, width, static_cast<uint64_t>(blockIdx.x - sum_blocks) * kWaves + wave_of(),
+        clear_rows<DTYPE, PAST>(a.out, a.out_stride, vocab, 0, width, static_cast<uint64_t>(blockIdx.x - sum_blocks) * kWaves + wave_of(),
                           static_cast<uint64_t>(gridDim.x - sum_blocks) * kWaves, [&](uint64_t v) { return s.begin[v] == s.begin[v + 1]; });
     }
 }
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
     };
     // The whole range is cleared first, while the ids are on their way; sums overwrite it, behind the barriers.
     if (!ADD) {
-        clear_rows<DTYPE>(a.out + static_cast<uint64_t>(first) * a.out_stride * I::kBytes, a.out_stride, range, slab, slab_end, wave, kFewWaves,
+        clear_rows<DTYPE, false>(a.out + static_cast<uint64_t>(first) * a.out_stride * I::kBytes, a.out_stride, range, slab, slab_end, wave, kFewWaves,
                           [](uint64_t) { return true; });
     }
     // the range's tokens in their order
@@ -499,6 +499,10 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
 uint64_t up(uint64_t x) { return (x + 255) / 256 * 256; }
 
 // Entries of a part: as many as leave work for kPartWaves wavefronts, within limits.
+// A new gradient goes past the caches where it and the tokens' rows together are beyond the 256 MiB that lie in front of memory: zeros would drive those
+// out.  (Us, through the caches / past them: tables of 32,000 x 4096 bf16 elements, 4096 tokens 60 and 65, 16,384 115 and 83; of 128,256 x 8192, 16,384 tokens
+// 475 and 447.)
+constexpr uint64_t kPastGradBytes = 320ull << 20;
 constexpr uint32_t kPartWaves = 8192, kLeastPart = 8, kMostPart = 32;
 uint32_t part_of(uint64_t n, uint64_t slabs)
 {
@@ -542,7 +546,9 @@ hipError_t launch_grad(const EmbedArgs& a, Sorted s, hipStream_t stream)
     hipLaunchKernelGGL(embed_sort_kernel, dim3(static_cast<uint32_t>((a.vocab + kRange - 1) / kRange)), dim3(kSortThreads), 0, stream, a, s);
     const dim3 threads(kWaveSize * kWaves);
     const uint32_t sum_blocks = groups(n_parts * slabs), rows_at_once = static_cast<uint32_t>(std::max<uint64_t>(kSlab / a.width, 1));
-    hipLaunchKernelGGL((embed_sum_kernel<DTYPE, ADD>), dim3(sum_blocks + (ADD ? 0 : groups((a.vocab + rows_at_once - 1) / rows_at_once))), threads, 0, stream, a, s, slabs, sum_blocks);
+    const bool past = !ADD && (a.n_tokens + a.vocab) * a.width * Items<DTYPE>::kBytes >= kPastGradBytes;
+    const auto sums = past ? embed_sum_kernel<DTYPE, ADD, !ADD> : embed_sum_kernel<DTYPE, ADD, false>;
+    hipLaunchKernelGGL(sums, dim3(sum_blocks + (ADD ? 0 : groups((a.vocab + rows_at_once - 1) / rows_at_once))), threads, 0, stream, a, s, slabs, sum_blocks);
     if (n_parts > 1) {
         const uint32_t few_blocks = static_cast<uint32_t>(std::min<uint64_t>((n_parts * slabs + kJoinWaves - 1) / kJoinWaves, kJoinFewBlocks));
         const uint32_t many_blocks = static_cast<uint32_t>(std::min<uint64_t>(n_parts / kManyParts * slabs, kJoinManyBlocks));
@@ -566,9 +572,11 @@ hipError_t launch_embed(const EmbedArgs& a, uint32_t dtype, hipStream_t stream)
     if (!a.n_tokens) return hipSuccess;
     const uint32_t slabs = static_cast<uint32_t>((a.width + kSlab - 1) / kSlab);
     const dim3 grid(groups(a.n_tokens * slabs)), threads(kWaveSize * kWaves);
-    if (dtype == FF_BF16) hipLaunchKernelGGL(embed_kernel<FF_BF16>, grid, threads, 0, stream, a, slabs);
-    else if (dtype == FF_F16) hipLaunchKernelGGL(embed_kernel<FF_F16>, grid, threads, 0, stream, a, slabs);
-    else hipLaunchKernelGGL(embed_kernel<FF_F32>, grid, threads, 0, stream, a, slabs);
+    const bool past = a.n_tokens * a.width * (dtype == FF_F32 ? 4 : 2) >= kPastBytes;
+    const auto kernel = dtype == FF_BF16  ? (past ? embed_kernel<FF_BF16, true> : embed_kernel<FF_BF16, false>)
+                        : dtype == FF_F16 ? (past ? embed_kernel<FF_F16, true> : embed_kernel<FF_F16, false>)
+                                          : (past ? embed_kernel<FF_F32, true> : embed_kernel<FF_F32, false>);
+    hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a, slabs);
     return hipGetLastError();
 }
 

@@ -18,7 +18,8 @@ namespace {
 
 constexpr int kBlock = 256;             // threads of a workgroup whose wavefronts take rows of their own
 constexpr uint32_t kForwardBlocks = 2048;
-constexpr uint32_t kMostBlocks = 512;   // of the backward pass, each of which leaves a part of dw and db
+// Workgroups of the backward pass, each of which leaves a part of dw and db: those of 512 threads and more have a compute unit to themselves.
+constexpr uint32_t kMostBlocks = 512, kMostWideBlocks = 256;
 constexpr uint32_t kFewRows = 1024;     // up to so many, dw and db are summed straight from the rows
 
 template <int GROUP>
@@ -65,7 +66,7 @@ __device__ __forceinline__ void places(uint32_t thread, uint32_t width, Fn&& fn)
     });
 }
 
-template <uint32_t DTYPE, int GROUP, int K>
+template <uint32_t DTYPE, int GROUP, int K, bool PAST>
 __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs a)
 {
     using I = Items<DTYPE>;
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
         places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
             f32x8 y = (I::wide(h[int(i)]) - mean) * rstd * I::wide(w[int(i)]);
             if (a.bias) y += I::wide(b[int(i)]);
-            I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(y));
+            I::template store<PAST>(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(y));
         });
         if (thread == 0) {
             if (a.mean) a.mean[r] = mean;
@@ -151,7 +152,7 @@ __device__ __forceinline__ void columns(const NormArgs& a, const uint32_t block)
 }
 
 // `column_blocks` workgroups behind the others make dw and db; with none of them, the rows' groups leave their parts.
-template <uint32_t DTYPE, int GROUP, int K>
+template <uint32_t DTYPE, int GROUP, int K, bool PAST>
 __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const NormArgs a, const uint32_t column_blocks)
 {
     using I = Items<DTYPE>;
@@ -173,8 +174,8 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
         typename I::Held x[K], dy[K];
         float mean, rstd;
     } next;
-    auto load_x = [&](uint64_t r, uint32_t at) { return I::load(a.x + r * a.x_stride * I::kBytes, at, width); };
-    auto load_dy = [&](uint64_t r, uint32_t at) { return I::load(a.dy + r * a.dy_stride * I::kBytes, at, width); };
+    auto load_x = [&](uint64_t r, uint32_t at) { return I::template load<PAST>(a.x + r * a.x_stride * I::kBytes, at, width); };
+    auto load_dy = [&](uint64_t r, uint32_t at) { return I::template load<PAST>(a.dy + r * a.dy_stride * I::kBytes, at, width); };
     auto load_w = [&](uint32_t at) { return I::load(a.weight, at, width); };
     auto fetch = [&](Row& to, uint64_t r) {
         to.mean = a.mean[r];
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
         turn ^= 1;
         const float c0 = s[0] * each, c1 = s[1] * each;
         each_place([&](auto, uint32_t at, f32x8 normed, f32x8, f32x8 g) {
-            I::store(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(now.rstd * (g - c0 - normed * c1)));
+            I::template store<PAST>(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(now.rstd * (g - c0 - normed * c1)));
         });
     }
     if (column_blocks || (!a.dweight && !a.dbias)) return;
@@ -287,9 +288,15 @@ uint32_t grad_blocks(uint64_t n_rows, uint64_t width)
     uint32_t blocks = 0;
     choose(width, [&](auto group, auto) {
         constexpr uint32_t per = block_of<group>() / group;
-        blocks = static_cast<uint32_t>(std::max<uint64_t>(std::min<uint64_t>((n_rows + per - 1) / per, kMostBlocks), 1));
+        blocks = static_cast<uint32_t>(std::max<uint64_t>(std::min<uint64_t>((n_rows + per - 1) / per, group >= 512 ? kMostWideBlocks : kMostBlocks), 1));
     });
     return blocks;
+}
+
+template <uint32_t DTYPE>
+bool past(const NormArgs& a)
+{
+    return a.n_rows * a.width * Items<DTYPE>::kBytes >= kPastBytes;
 }
 
 template <uint32_t DTYPE>
@@ -299,7 +306,8 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
         constexpr int threads = block_of<group>();
         constexpr uint32_t per = threads / group;
         const uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>((a.n_rows + per - 1) / per, kForwardBlocks));
-        hipLaunchKernelGGL((norm_kernel<DTYPE, group, k>), dim3(blocks), dim3(threads), 0, stream, a);
+        const auto kernel = past<DTYPE>(a) ? norm_kernel<DTYPE, group, k, true> : norm_kernel<DTYPE, group, k, false>;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a);
     });
     return hipGetLastError();
 }
@@ -311,7 +319,8 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
     const bool sums = a.dweight || a.dbias, few = a.n_rows <= kFewRows;
     const uint32_t all = static_cast<uint32_t>((a.width + kColumns - 1) / kColumns), column_blocks = sums && few ? all : 0;
     choose(a.width, [&](auto group, auto k) {
-        hipLaunchKernelGGL((norm_grad_kernel<DTYPE, group, k>), dim3(blocks + column_blocks), dim3(block_of<group>()), 0, stream, a, column_blocks);
+        const auto kernel = past<DTYPE>(a) ? norm_grad_kernel<DTYPE, group, k, true> : norm_grad_kernel<DTYPE, group, k, false>;
+        hipLaunchKernelGGL(kernel, dim3(blocks + column_blocks), dim3(block_of<group>()), 0, stream, a, column_blocks);
     });
     if (sums && !few) hipLaunchKernelGGL(norm_join_kernel<DTYPE>, dim3(all, 2), dim3(kColumns * kJoinRows), 0, stream, a, blocks);
     return hipGetLastError();

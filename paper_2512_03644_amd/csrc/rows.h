@@ -11,6 +11,11 @@ typedef _Float16 f16x8v __attribute__((ext_vector_type(8)));
 
 constexpr int kLaneItems = 8;
 
+// Outputs of so many bytes go past the caches: of what is larger than all L2s together little is there when it is read next.  (Us, through them / past
+// them: layer norm of 16,384 rows of 8192 bf16 elements, forward and backward, 256 and 238, with the inputs of the latter past them too 233; 16,384 embedded tokens of
+// 8192 92 and 84.  Inputs of 3001 rows of 1003 fp32 elements past them 24.2 where 21.7 are taken.)
+constexpr uint64_t kPastBytes = 32ull << 20;
+
 template <uint32_t DTYPE>
 struct Items {
     static constexpr uint32_t kBytes = DTYPE == FF_F32 ? 4 : 2;
@@ -31,12 +36,6 @@ struct Items {
     struct Held {
         u32x4 w[kBytes / 2];
     };
-    static __device__ __forceinline__ Held load8(const uint8_t* p)
-    {
-        Held h;
-        for (uint32_t i = 0; i < kBytes / 2; i++) h.w[i] = ((const FF_GLOBAL u32x4_a2*)p)[i];
-        return h;
-    }
     static __device__ __forceinline__ f32x8 wide(const Held& h)
     {
         f32x8 v;
@@ -64,20 +63,33 @@ struct Items {
         }
         return h;
     }
-    // Elements [at, at + 8) of a row of `width`, at < width; those behind it are zeros.
+    // Elements [at, at + 8) of a row of `width`, at < width; those behind it are zeros.  PAST: not to be kept in the caches.
+    template <bool PAST = false>
     static __device__ __forceinline__ Held load(const uint8_t* row, uint32_t at, uint32_t width)
     {
         const uint8_t* const p = row + static_cast<uint64_t>(at) * kBytes;
-        if (at + kLaneItems <= width) return load8(p);
+        if (at + kLaneItems <= width) {
+            Held h;
+            for (uint32_t i = 0; i < kBytes / 2; i++) {
+                const auto* const q = (const FF_GLOBAL u32x4_a2*)p + i;
+                h.w[i] = PAST ? __builtin_nontemporal_load(q) : *q;
+            }
+            return h;
+        }
         f32x8 v;
         for (uint32_t i = 0; i < kLaneItems; i++) v[i] = at + i < width ? one(p + i * kBytes) : 0.f;
         return narrow(v);
     }
+    template <bool PAST = false>
     static __device__ __forceinline__ void store(uint8_t* row, uint32_t at, uint32_t width, const Held& h)
     {
         uint8_t* const p = row + static_cast<uint64_t>(at) * kBytes;
         if (at + kLaneItems <= width) {
-            for (uint32_t i = 0; i < kBytes / 2; i++) ((FF_GLOBAL u32x4_a2*)p)[i] = h.w[i];
+            for (uint32_t i = 0; i < kBytes / 2; i++) {
+                auto* const q = (FF_GLOBAL u32x4_a2*)p + i;
+                if (PAST) __builtin_nontemporal_store(h.w[i], q);
+                else *q = h.w[i];
+            }
             return;
         }
         const f32x8 v = wide(h);
