@@ -316,7 +316,8 @@ template <uint32_t DTYPE>
 hipError_t backward(const NormArgs& a, hipStream_t stream)
 {
     const uint32_t blocks = grad_blocks(a.n_rows, a.width);
-    const bool sums = a.dweight || a.dbias, few = a.n_rows <= kFewRows;
+    // (not from rows that the launch replaces)
+    const bool sums = a.dweight || a.dbias, few = a.n_rows <= kFewRows && a.out != a.x && a.out != a.dy;
     const uint32_t all = static_cast<uint32_t>((a.width + kColumns - 1) / kColumns), column_blocks = sums && few ? all : 0;
     choose(a.width, [&](auto group, auto k) {
         const auto kernel = past<DTYPE>(a) ? norm_grad_kernel<DTYPE, group, k, true> : norm_grad_kernel<DTYPE, group, k, false>;

@@ -187,6 +187,19 @@ def test_layer_norm_in_place_and_without_statistics():
     assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("n,width", [(1, 8), (50, 1000), (1024, 4096), (700, 16384), (1500, 300)])
+@pytest.mark.parametrize("over", ["x", "dy"])
+def test_layer_norm_gradients_of_weights_where_dx_replaces_its_inputs(over, n, width):
+    x, weight, bias, dy, _ = norm_inputs(n, width, BF16, 0, 0)
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    ff.ff_layer_norm(x, weight, bias, y, mean, rstd)
+    want = modelref.norm_grad(x, weight, mean, rstd, dy)
+    dx, dw, db = (x if over == "x" else dy), torch.empty_like(weight), torch.empty_like(weight)
+    ff.ff_layer_norm_grad(x, weight, mean, rstd, dy, dx, dw, db, ff.alloc_norm_workspace(n, width, DEV))
+    for name, got in (("dx", dx), ("dweight", dw), ("dbias", db)):
+        modelref.check(got, want[name], want["tol_" + name], name)
+
+
 @pytest.mark.parametrize("n,width", [(3000, 64), (5000, 300), (2100, 2048)])
 def test_layer_norm_of_many_rows_and_none(n, width):
     x, weight, bias, dy, _ = norm_inputs(n, width, F32, 0, 0)
