@@ -430,6 +430,9 @@ int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss,
 
 /* ---- the two ends of a model: embedding, layer norm, head with cross entropy -------------------- */
 
+/* Nothing is allocated, and calls only launch kernels: they can be recorded into a HIP graph.  Calls that may be in flight at the same time
+ * take a workspace each; graphs that are replayed one behind the other may share one.  Outputs must not overlap inputs or each other but where this is said. */
+
 /*
  * Embedding: out[t] = scale * table[ids[t]], one fp32 product rounded to the format.  table: DEVICE, vocab rows of `width` elements of
  * dtype (FF_BF16, FF_F16 or FF_F32), table_stride >= width elements apart; ids: DEVICE int64; out: DEVICE, n_tokens rows,
@@ -478,7 +481,7 @@ int ff_layer_norm_grad(const void *x, uint64_t n_rows, uint64_t width, uint64_t 
                        void *dweight, void *dbias, void *workspace, void *hip_stream);
 
 /*
- * Head: the cross entropy of targets over a vocabulary, from the hidden states, without logits in memory.  hidden: n_tokens rows of `width`
+ * Head: the cross entropy of targets over a vocabulary, from the hidden states, with the logits of one piece of the vocabulary in memory at most.  hidden: n_tokens rows of `width`
  * elements of dtype (FF_BF16 or FF_F16), hidden_stride >= width elements apart; weight: vocab such rows.  All arrays DEVICE and
  * aligned to their elements; rows of `weight` that are 16-byte aligned, of a width that is a multiple of 8, are read where they lie,
  * others are copied piece by piece first.  targets int64; weights fp32: what a token counts in the loss, its share of the mean included; 0
@@ -517,7 +520,7 @@ uint64_t ff_head_workspace_bytes(const ff_head_batch *b, uint32_t gradient);
  * dhidden, dweight: DEVICE, either may be NULL; rows of `width` elements of dtype, their strides apart: with g[t][v] = weights[t] * loss_scale *
  * (softmax(z[t])[v] - [v is the target]), rounded to dtype relative to the largest weight, dhidden = g . weight (rows of zeros for
  * tokens that are left out) and dweight = g^T . hidden, summed in fp32 in an order that the sizes give and rounded once.
- * dhidden may be hidden (of the same stride).  Without either, scoring: one product in place of four.
+ * dhidden may be hidden (of the same stride).  Without either, scoring: one product in place of three or four.
  * workspace: DEVICE, 256-byte aligned, ff_head_workspace_bytes() bytes; its content does not matter.
  */
 int ff_head_loss(const ff_head_batch *b, float *logp, void *dhidden, uint64_t dhidden_stride,

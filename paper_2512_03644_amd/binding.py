@@ -84,7 +84,8 @@ class ff_policy_batch(ctypes.Structure):
 
 
 class ff_head_batch(ctypes.Structure):
-    tensors, shapes = (), ()  # those that it points at (head_batch), kept alive; of hidden states, W, one a token
+    tensors = ()  # those that it points at (head_batch), kept alive
+    shapes = ()   # of hidden states, W, what there is of for every token; format; device
 
     _fields_ = [("hidden", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
                 ("vocab", ctypes.c_uint64), ("width", ctypes.c_uint64), ("hidden_stride", ctypes.c_uint64),
@@ -595,24 +596,24 @@ def ff_policy_loss(batch, logp, token_loss, stats, workspace, dlogits=None, stre
 _I64, _F32 = torch.int64, torch.float32
 
 
-def _refuse(t, name, shape, dtype):
-    raise ValueError("%s is a %s tensor %s of contiguous %s" % (name, dtype, tuple(shape), "rows" if len(shape) == 2 else "entries"))
+def _refuse(t, name, shape, dtype, dev):
+    raise ValueError("%s is a %s tensor %s of contiguous %s on device %d" % (name, dtype, tuple(shape), "rows" if len(shape) == 2 else "entries", dev))
 
 
-def _rows(t, name, shape, dtype):
+def _rows(t, name, shape, dtype, dev):
     """Elements between a matrix's rows; the rows themselves are contiguous."""
-    if t.dtype is not dtype or t.shape != shape:
-        _refuse(t, name, shape, dtype)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _refuse(t, name, shape, dtype, dev)
     stride, inner = t.stride()
     if inner != 1 and shape[1] != 1:
-        _refuse(t, name, shape, dtype)
+        _refuse(t, name, shape, dtype, dev)
     return stride if shape[0] > 1 else max(stride, shape[1])
 
 
-def _vector(t, name, shape, dtype):
+def _vector(t, name, shape, dtype, dev):
     """The address of a vector's entries."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        _refuse(t, name, shape, dtype)
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        _refuse(t, name, shape, dtype, dev)
     return t.data_ptr()
 
 
@@ -622,13 +623,20 @@ def _matrix(t, name):
     return t.shape
 
 
+def _current(dev):
+    """The device of a call's tensors is the one that it is made on."""
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError("the tensors are on device %d, which is not the current one" % dev)
+
+
 def ff_embed(table, ids, out, scale=1.0, stream=None):
     """out[t] = scale * table[ids[t]]; table [vocab, width] of bf16, fp16 or fp32, ids int64 [tokens], out [tokens, width] in
     the table's format.  Rows may lie apart.  An id outside the table (padding) gives a row of zeros."""
-    shape, n, dtype = _matrix(table, "table"), ids.numel(), table.dtype
+    shape, n, dtype, dev = _matrix(table, "table"), ids.numel(), table.dtype, table.get_device()
     vocab, width = shape
-    status = lib().ff_embed(table.data_ptr(), vocab, width, _rows(table, "table", shape, dtype), _DTYPES[dtype],
-                            _vector(ids, "ids", (n,), _I64), n, scale, out.data_ptr(), _rows(out, "out", (n, width), dtype),
+    stride, at, out_stride = _rows(table, "table", shape, dtype, dev), _vector(ids, "ids", (n,), _I64, dev), _rows(out, "out", (n, width), dtype, dev)
+    _current(dev)
+    status = lib().ff_embed(table.data_ptr(), vocab, width, stride, _DTYPES[dtype], at, n, scale, out.data_ptr(), out_stride,
                             _stream_ptr(stream))
     if status:
         _check(status)
@@ -641,29 +649,34 @@ def alloc_embed_workspace(n_tokens, vocab, width, device):
 def ff_embed_grad(dout, ids, dtable, workspace, scale=1.0, add=False, stream=None):
     """dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] == v); add: added to what is there, rows that no
     token asks for left alone."""
-    shape, n, dtype, L = _matrix(dtable, "dtable"), ids.numel(), dtable.dtype, lib()
+    shape, n, dtype, dev, L = _matrix(dtable, "dtable"), ids.numel(), dtable.dtype, dtable.get_device(), lib()
     vocab, width = shape
-    if workspace.nbytes < L.ff_embed_workspace_bytes(n, vocab, width):
-        raise ValueError("the workspace is smaller than ff_embed_workspace_bytes()")
-    status = L.ff_embed_grad(dout.data_ptr(), _rows(dout, "dout", (n, width), dtype), _DTYPES[dtype],
-                             _vector(ids, "ids", (n,), _I64), n, vocab, width, scale, dtable.data_ptr(),
-                             _rows(dtable, "dtable", shape, dtype), FF_GRAD_ADD if add else 0, workspace.data_ptr(),
-                             _stream_ptr(stream))
+    stride, at, out_stride = _rows(dout, "dout", (n, width), dtype, dev), _vector(ids, "ids", (n,), _I64, dev), _rows(dtable, "dtable", shape, dtype, dev)
+    _space(workspace, L.ff_embed_workspace_bytes(n, vocab, width), "ff_embed_workspace_bytes()", dev)
+    status = L.ff_embed_grad(dout.data_ptr(), stride, _DTYPES[dtype], at, n, vocab, width, scale, dtable.data_ptr(), out_stride,
+                             FF_GRAD_ADD if add else 0, workspace.data_ptr(), _stream_ptr(stream))
     if status:
         _check(status)
+
+
+def _space(workspace, least, name, dev):
+    if workspace is None or workspace.nbytes < least or workspace.get_device() != dev:
+        raise ValueError("the workspace is smaller than %s, or elsewhere" % name)
+    _current(dev)
 
 
 def ff_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, stream=None):
     """y = (x - mean) * rstd * weight + bias over the rows of x [rows, width]; bias may be None; y may be x.  mean, rstd: fp32
     [rows], for the gradient, or None."""
-    shape, dtype = _matrix(x, "x"), x.dtype
+    shape, dtype, dev = _matrix(x, "x"), x.dtype, x.get_device()
     n, width = shape
     one, each = (width,), (n,)
-    status = lib().ff_layer_norm(x.data_ptr(), n, width, _rows(x, "x", shape, dtype), _DTYPES[dtype],
-                                 _vector(weight, "weight", one, dtype), None if bias is None else _vector(bias, "bias", one, dtype),
-                                 eps, y.data_ptr(), _rows(y, "y", shape, dtype),
-                                 None if mean is None else _vector(mean, "mean", each, _F32),
-                                 None if rstd is None else _vector(rstd, "rstd", each, _F32), _stream_ptr(stream))
+    args = (x.data_ptr(), n, width, _rows(x, "x", shape, dtype, dev), _DTYPES[dtype], _vector(weight, "weight", one, dtype, dev),
+            None if bias is None else _vector(bias, "bias", one, dtype, dev), eps, y.data_ptr(), _rows(y, "y", shape, dtype, dev),
+            None if mean is None else _vector(mean, "mean", each, _F32, dev),
+            None if rstd is None else _vector(rstd, "rstd", each, _F32, dev))
+    _current(dev)
+    status = lib().ff_layer_norm(*args, _stream_ptr(stream))
     if status:
         _check(status)
 
@@ -674,18 +687,21 @@ def alloc_norm_workspace(n_rows, width, device):
 
 def ff_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight=None, dbias=None, workspace=None, stream=None):
     """Gradients of ff_layer_norm from dy; dx may be dy or x; dweight and dbias [width], or None."""
-    shape, dtype, L = _matrix(x, "x"), x.dtype, lib()
+    shape, dtype, dev, L = _matrix(x, "x"), x.dtype, x.get_device(), lib()
     n, width = shape
     one, each = (width,), (n,)
-    if dweight is not None or dbias is not None:
-        if workspace is None or workspace.nbytes < L.ff_layer_norm_workspace_bytes(n, width):
-            raise ValueError("the workspace is smaller than ff_layer_norm_workspace_bytes()")
-    status = L.ff_layer_norm_grad(
-        x.data_ptr(), n, width, _rows(x, "x", shape, dtype), _DTYPES[dtype], _vector(weight, "weight", one, dtype),
-        _vector(mean, "mean", each, _F32), _vector(rstd, "rstd", each, _F32), dy.data_ptr(), _rows(dy, "dy", shape, dtype),
-        dx.data_ptr(), _rows(dx, "dx", shape, dtype), None if dweight is None else _vector(dweight, "dweight", one, dtype),
-        None if dbias is None else _vector(dbias, "dbias", one, dtype), None if workspace is None else workspace.data_ptr(),
-        _stream_ptr(stream))
+    args = (x.data_ptr(), n, width, _rows(x, "x", shape, dtype, dev), _DTYPES[dtype], _vector(weight, "weight", one, dtype, dev),
+            _vector(mean, "mean", each, _F32, dev), _vector(rstd, "rstd", each, _F32, dev), dy.data_ptr(),
+            _rows(dy, "dy", shape, dtype, dev), dx.data_ptr(), _rows(dx, "dx", shape, dtype, dev),
+            None if dweight is None else _vector(dweight, "dweight", one, dtype, dev),
+            None if dbias is None else _vector(dbias, "dbias", one, dtype, dev))
+    if dweight is None and dbias is None:
+        _current(dev)
+        space = None
+    else:
+        _space(workspace, L.ff_layer_norm_workspace_bytes(n, width), "ff_layer_norm_workspace_bytes()", dev)
+        space = workspace.data_ptr()
+    status = L.ff_layer_norm_grad(*args, space, _stream_ptr(stream))
     if status:
         _check(status)
 
@@ -708,15 +724,15 @@ _HEAD = struct.Struct("7Q2I2QfI")
 def head_batch(hidden, weight, targets, weights, loss_scale=1.0):
     """ff_head_batch of device tensors: hidden [tokens, width], weight [vocab, width] (bf16 or fp16, rows may lie apart), targets
     int64 and weights fp32 [tokens].  It keeps the tensors alive (see policy_batch)."""
-    shape, dtype = _matrix(hidden, "hidden"), hidden.dtype
+    shape, dtype, dev = _matrix(hidden, "hidden"), hidden.dtype, hidden.get_device()
     n, width = shape
     table = (_matrix(weight, "weight")[0], width)
     batch = ff_head_batch.from_buffer_copy(_HEAD.pack(
-        hidden.data_ptr(), weight.data_ptr(), n, table[0], width, _rows(hidden, "hidden", shape, dtype),
-        _rows(weight, "weight", table, dtype), _DTYPES[dtype], 0, _vector(targets, "targets", (n,), _I64),
-        _vector(weights, "weights", (n,), _F32), loss_scale, 0))
+        hidden.data_ptr(), weight.data_ptr(), n, table[0], width, _rows(hidden, "hidden", shape, dtype, dev),
+        _rows(weight, "weight", table, dtype, dev), _DTYPES[dtype], 0, _vector(targets, "targets", (n,), _I64, dev),
+        _vector(weights, "weights", (n,), _F32, dev), loss_scale, 0))
     batch.tensors = (hidden, weight, targets, weights)
-    batch.shapes = shape, table, (n,)
+    batch.shapes = shape, table, (n,), dtype, dev
     return batch
 
 
@@ -729,17 +745,16 @@ def alloc_head_workspace(batch, device, grad=True):
 def ff_head_loss(batch, logp, stats, workspace, dhidden=None, dweight=None, stream=None):
     """Cross entropy of the batch's targets: log-probabilities into logp [tokens], the loss into stats (HeadStats); dhidden
     [tokens, width] (may be the hidden states), dweight [vocab, width], or None."""
-    L, ref, dtype = lib(), ctypes.byref(batch), batch.tensors[0].dtype
-    tokens, table, one = batch.shapes
+    L, ref = lib(), ctypes.byref(batch)
+    tokens, table, one, dtype, dev = batch.shapes
     dh = dw = None
     dh_stride = dw_stride = 0
     if dhidden is not None:
-        dh, dh_stride = dhidden.data_ptr(), _rows(dhidden, "dhidden", tokens, dtype)
+        dh, dh_stride = dhidden.data_ptr(), _rows(dhidden, "dhidden", tokens, dtype, dev)
     if dweight is not None:
-        dw, dw_stride = dweight.data_ptr(), _rows(dweight, "dweight", table, dtype)
-    if workspace.nbytes < L.ff_head_workspace_bytes(ref, 0 if dhidden is None and dweight is None else 1):
-        raise ValueError("the workspace is smaller than ff_head_workspace_bytes()")
-    status = L.ff_head_loss(ref, _vector(logp, "logp", one, _F32), dh, dh_stride, dw, dw_stride, stats.data_ptr(),
-                            workspace.data_ptr(), _stream_ptr(stream))
+        dw, dw_stride = dweight.data_ptr(), _rows(dweight, "dweight", table, dtype, dev)
+    logp = _vector(logp, "logp", one, _F32, dev)
+    _space(workspace, L.ff_head_workspace_bytes(ref, 0 if dhidden is None and dweight is None else 1), "ff_head_workspace_bytes()", dev)
+    status = L.ff_head_loss(ref, logp, dh, dh_stride, dw, dw_stride, stats.data_ptr(), workspace.data_ptr(), _stream_ptr(stream))
     if status:
         _check(status)

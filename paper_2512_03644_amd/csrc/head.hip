@@ -1,15 +1,22 @@
 // Cross entropy over a large vocabulary from hidden states, and its gradients, for gfx950.
 //
-// z = H W^T is made in tiles of 256 vocabulary entries and never stored: a tile leaves, for each token, its largest logit, the sum of
+// z = H W^T is made in tiles of 256 vocabulary entries: a tile leaves, for each token, its largest logit and the sum of
 // exponentials against it, and the target's logit.  Joined over the tiles these give the log-probability.  For the
-// gradients the vocabulary is taken in pieces: a piece's logits are made once more, become G = (softmax - [target]) * weight in 16 bits, and two
-// products take G: dH += G W, in 32 bits over the pieces, and dW = G^T H.  Four products of 2 * tokens * vocab * width operations in all, where
-// three would do if all logits were kept.
+// gradients the vocabulary is taken in pieces, of up to 2^28 logits.  A piece's logits become G = (softmax - [target]) * weight in 16 bits, and two
+// products take G: dH += G W, in 32 bits over the pieces, and dW = G^T H.  The last piece, with which they begin, is still there from
+// the first time (kKeep); the others' logits are made once more: three products of 2 * tokens * vocab * width operations for the last piece, four for the
+// others.  (Head of 8192 x 128,256, 4096 tokens, a tenth masked, us, pieces of 2^25 / 2^26 / 2^27 / 2^28 logits 25188 / 24666 / 23290 / 21682, of 4096 x
+// 32,000, which the last two take in one, 3204 / 3103 / 2698 / 2698: what is kept for a fixed 1 GiB.)
 //
 // G is rounded to 16 bits, for the matrix instructions; nothing else is, in front of the outputs.  Weights are divided
 // by the largest one first, so that tokens of equal weight have exact factors of 1 (a factor rounded with G would
 // be the same error in every token); it comes back, with the loss scale, on 32-bit sums.  For fp16, G is 2^14 times that: a
 // softmax of 2^-28 is still a normal number.
+//
+// What bounds it: many tokens, the matrix instructions (product.h); few, reading W once for the logits and once for dH, and writing dW: 64 tokens and
+// fewer take kernels of their own for the logits (head_stream_kernel) and dW (head_few_dweight_kernel); small heads, the chain of five
+// launches.  Us, logits / all with both gradients, width 4096, 1 / 16 / 64 / 128 / 256 tokens on 32,000 65 / 77 / 102 / 101 / 120 and 175 / 190 / 223 / 250 / 317,
+// on 128,256 225 / 275 / 249 / 273 / 280 and 678 / 733 / 731 / 896 / 1049.
 #include "head.hpp"
 
 #include <algorithm>
@@ -317,7 +324,9 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
 
 // The logits of few tokens, all of the vocabulary: W passes once from memory through registers, rows of any alignment where they lie.  A wavefront
 // takes 16 V rows of it and 16 T tokens, whose hidden states come from the caches; the products of a chunk of K times 32
-// elements are made while the next one is on its way.  At the rate of reading W, where 64 x 256 tiles leave half of the chip idle (see launch).
+// elements are made while the next one is on its way.  What bounds it: reading W, up to 16 tokens; more read their hidden states from the caches as often,
+// and 64 x 256 tiles are better where W lies as those want it.  Us, scoring, this / tiles: 1 token on 32,000 x 4096 65 / 89; 17, 32, 64 tokens 80, 88, 114 / 92, 93, 102; on
+// 128,256 x 4096 266, 323, 425 / 242, 245, 249.
 constexpr int kStreamThreads = 256, kStreamWaves = kStreamThreads / kWaveSize;
 template <int T>
 struct Stream {
@@ -574,32 +583,35 @@ __device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first,
 }
 
 // dH of all pieces and slices, in its place: four elements of a row to a thread.
-constexpr uint32_t kPutThreads = 256;
+constexpr uint32_t kPutThreads = 256, kPutRows = 1 << 16;
 template <bool BF16>
-__global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A, const uint32_t blocks_of_row)
+__global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A)
 {
-    const uint32_t width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width), r = blockIdx.x / blocks_of_row;
-    const uint32_t d = ((blockIdx.x - r * blocks_of_row) * kPutThreads + threadIdx.x) * 4;
-    if (r >= A.state->used || d >= width) return;
+    const uint32_t width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width), used = A.state->used;
+    const uint32_t d = (blockIdx.y * kPutThreads + threadIdx.x) * 4;
+    if (d >= width) return;
     constexpr uint32_t kAhead = 8;
-    const float* const from = A.dh + static_cast<uint64_t>(r) * width_up + d;
     const uint64_t step = static_cast<uint64_t>(A.tokens_up) * width_up;
-    f32x4 s = {0, 0, 0, 0};
-    for (uint32_t k = 0; k < A.slices; k += kAhead) {
-        f32x4 x[kAhead];
-        static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i < A.slices ? k + i : k) * step); });
-        static_for<kAhead>([&](auto i) {
-            if (k + i < A.slices) s += x[int(i)];
-        });
-    }
-    uint8_t* const out = A.dhidden + (A.index[r] * A.dhidden_stride + d) * 2;
-    const u32x2 h = to_half<BF16>(s * A.state->scale);
-    if (d + 4 <= width) {
-        *(FF_GLOBAL u32x2_a2*)out = h;
-    } else {
+    const float scale = A.state->scale;
+    for (uint32_t r = blockIdx.x; r < used; r += gridDim.x) {
+        const float* const from = A.dh + static_cast<uint64_t>(r) * width_up + d;
+        f32x4 s = {0, 0, 0, 0};
+        for (uint32_t k = 0; k < A.slices; k += kAhead) {
+            f32x4 x[kAhead];
+            static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i < A.slices ? k + i : k) * step); });
+            static_for<kAhead>([&](auto i) {
+                if (k + i < A.slices) s += x[int(i)];
+            });
+        }
+        uint8_t* const out = A.dhidden + (A.index[r] * A.dhidden_stride + d) * 2;
+        const u32x2 h = to_half<BF16>(s * scale);
+        if (d + 4 <= width) {
+            *(FF_GLOBAL u32x2_a2*)out = h;
+        } else {
 #pragma unroll
-        for (uint32_t e = 0; e < 3; e++)
-            if (d + e < width) as_global(reinterpret_cast<uint16_t*>(out))[e] = static_cast<uint16_t>(h[e / 2] >> e % 2 * 16);
+            for (uint32_t e = 0; e < 3; e++)
+                if (d + e < width) as_global(reinterpret_cast<uint16_t*>(out))[e] = static_cast<uint16_t>(h[e / 2] >> e % 2 * 16);
+        }
     }
 }
 
@@ -631,8 +643,8 @@ __device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first,
 }
 
 // dW of few tokens, whose products are one step: a workgroup holds G of 64 vocabulary entries in registers and goes through the hidden states, 256
-// elements at a time, which lie in the caches; two or more are on a compute unit, so that one's loads run under another's stores.  What bounds it:
-// writing dW.
+// elements at a time, which lie in the caches; three are on a compute unit, so that one's loads run under another's stores.  What bounds it:
+// writing dW.  (260 us for the 1.05 GB of 128,256 x 4096, where 256 x 256 tiles, alone on a compute unit, took 460; with two buffers for the hidden states, and one workgroup, 340.)
 constexpr int kFewWaves = 4, kFewEntries = 16 * kFewWaves;
 template <bool BF16>
 __global__ __launch_bounds__(kFewWaves* kWaveSize) void head_few_dweight_kernel(const HeadArgs A, const uint32_t first, const uint32_t n, const uint32_t parts)
@@ -707,11 +719,13 @@ bool weight_as_it_is(const ff_head_batch& b)
 }
 
 bool few(const ff_head_batch& b) { return b.n_tokens <= kFewTokens; }
-// Is it better to keep the logits of a piece than to make them again?  (Of the last piece, which is all there is for the smaller calls.)
+// Is it better to keep the logits of the last piece than to make them again?  Eight bytes of memory to and fro stand against 2 * width operations: equal at a
+// width of about 1000.
 bool keeps(const ff_head_batch& b) { return few(b) || b.width >= 1024; }
 // Do the logits come from head_stream_kernel?
 bool streams(const ff_head_batch& b) { return b.n_tokens <= 16 || (few(b) && !weight_as_it_is(b)); }
-// Tiles 256 tokens high, or 64: a round of the latter takes two thirds as long.
+// Tiles 256 tokens high, or 64: a round of the latter takes two thirds as long.  (Us, 256 / 64: scoring 256, 300, 512 tokens on 32,000 x 4096 121, 126, 129 / 162, 220,
+// 287; 128 tokens 119 / 101.)
 bool high_tiles(const ff_head_batch& b)
 {
     const uint64_t across = up(b.vocab, kTile) / kTile, rounds = (up(b.n_tokens, kTile) / kTile * across + kComputeUnits - 1) / kComputeUnits;
@@ -766,7 +780,7 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     p.weight = take(packed && (grad || !streams(b)) ? piece_of(width_up) : 0);
     if (grad) {
         p.grad = take(piece_of(A->tokens_up));
-        p.logits = take(2 * piece_of(A->tokens_up));
+        p.logits = take(2 * (keeps(b) ? piece_of(A->tokens_up) : kFewTokens * whole * 2));
         const uint64_t dh = A->tokens_up * width_up;
         p.dh = take(std::max(dh, std::min<uint64_t>(dh * (whole / kTile), kComputeUnits * kTile * kTile)) * 4);
     }
@@ -837,7 +851,7 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
     }
     if (A.dhidden && start != kOnly && n) {
         const uint32_t blocks_of_row = static_cast<uint32_t>((A.b.width + 4 * kPutThreads - 1) / (4 * kPutThreads));
-        hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(n * blocks_of_row), dim3(kPutThreads), 0, stream, A, blocks_of_row);
+        hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(std::min(n, kPutRows), blocks_of_row), dim3(kPutThreads), 0, stream, A);
     }
     return hipGetLastError();
 }

@@ -29,7 +29,7 @@ int check_embed(const void* rows, uint64_t rows_stride, uint32_t dtype, const in
     if (n_tokens && (!rows || !ids)) return FF_ERR_NULL;
     if ((n_tokens || (gradient && !add)) && !out) return FF_ERR_NULL;
     if (!aligned(rows, size) || !aligned(out, size) || !aligned(ids, 8)) return FF_ERR_INVALID;
-    if (!rows_ok(rows_stride, width) || !rows_ok(out_stride, width)) return FF_ERR_INVALID;
+    if (!rows_ok(rows_stride, width) || !rows_ok(out_stride, width) || (n_tokens && rows == out)) return FF_ERR_INVALID;
     return FF_OK;
 }
 
@@ -119,7 +119,7 @@ int ff_layer_norm_grad(const void* x, uint64_t n_rows, uint64_t width, uint64_t 
     if ((dweight || dbias) && !workspace) return FF_ERR_NULL;
     const uint32_t size = element_size(dtype);
     if (!rows_ok(dy_stride, width) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, size) || !aligned(dbias, size) ||
-        !aligned(workspace, 16) || (dx == dy && dx_stride != dy_stride) || (dx == x && dx_stride != x_stride))
+        !aligned(workspace, 16) || dweight == weight || dbias == weight || (dx == dy && dx_stride != dy_stride) || (dx == x && dx_stride != x_stride))
         return FF_ERR_INVALID;
     NormArgs a = {};
     a.x = static_cast<const uint8_t*>(x);
@@ -163,7 +163,7 @@ int ff_head_loss(const ff_head_batch* b, float* logp, void* dhidden, uint64_t dh
         if (!workspace) return FF_ERR_NULL;
         if (!aligned(workspace, 256)) return FF_ERR_INVALID;
     }
-    if (dweight && (!aligned(dweight, 2) || !rows_ok(dweight_stride, b->width))) return FF_ERR_INVALID;
+    if (dweight && (!aligned(dweight, 2) || !rows_ok(dweight_stride, b->width) || dweight == b->weight)) return FF_ERR_INVALID;
     FF_HIP_TRY(launch_head(*b, logp, dhidden, dhidden_stride, dweight, dweight_stride, stats, workspace, static_cast<hipStream_t>(hip_stream)));
     return FF_OK;
 }

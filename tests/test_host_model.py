@@ -14,16 +14,17 @@ from paper_2512_03644_amd import binding as ff
 INF, NAN = float("inf"), float("nan")
 A16 = 1 << 20  # an address that is aligned to everything and never used
 BIG = 1 << 31
-NOWHERE = types.SimpleNamespace(cuda_stream=0)  # calls that get so far fail without a device
+NOWHERE = types.SimpleNamespace(cuda_stream=0)
+SHAPE = "is a |smaller"
 
 
 def test_embedding_refuses_bad_arguments():
     L = ff.lib()
 
-    def look(table=A16, vocab=10, width=8, stride=8, dtype=ff.FF_BF16, ids=A16, n=4, scale=1.0, out=A16, out_stride=8):
+    def look(table=A16, vocab=10, width=8, stride=8, dtype=ff.FF_BF16, ids=A16, n=4, scale=1.0, out=3 * A16, out_stride=8):
         return L.ff_embed(table, vocab, width, stride, dtype, ids, n, scale, out, out_stride, None)
 
-    def grad(dout=A16, stride=8, dtype=ff.FF_BF16, ids=A16, n=4, vocab=10, width=8, scale=1.0, dtable=A16, out_stride=8, flags=0, ws=A16):
+    def grad(dout=A16, stride=8, dtype=ff.FF_BF16, ids=A16, n=4, vocab=10, width=8, scale=1.0, dtable=3 * A16, out_stride=8, flags=0, ws=A16):
         return L.ff_embed_grad(dout, stride, dtype, ids, n, vocab, width, scale, dtable, out_stride, flags, ws, None)
 
     for f, names in ((look, ("table", "ids", "out")), (grad, ("dout", "ids", "dtable", "ws"))):
@@ -31,7 +32,7 @@ def test_embedding_refuses_bad_arguments():
             assert f(**{name: None}) == ff.FF_ERR_NULL, name
         for bad in (dict(dtype=0), dict(dtype=4), dict(vocab=0), dict(vocab=ff.FF_EMBED_MAX_VOCAB + 1), dict(width=0), dict(width=ff.FF_EMBED_MAX_WIDTH + 1, stride=1 << 30, out_stride=1 << 30),
                     dict(n=BIG), dict(stride=7), dict(out_stride=7), dict(stride=(1 << 40) + 1), dict(out_stride=1 << 60), dict(scale=INF), dict(scale=NAN),
-                    {names[0]: A16 + 1}, {names[1]: A16 + 4}, {names[2]: A16 + 1}, {names[0]: A16 + 2, "dtype": ff.FF_F32}, {names[2]: A16 + 2, "dtype": ff.FF_F32}):
+                    {names[0]: A16 + 1}, {names[1]: A16 + 4}, {names[2]: A16 + 1}, {names[0]: 2 * A16, names[2]: 2 * A16}, {names[0]: A16 + 2, "dtype": ff.FF_F32}, {names[2]: A16 + 2, "dtype": ff.FF_F32}):
             assert f(**bad) == ff.FF_ERR_INVALID, bad
     assert grad(flags=2) == grad(ws=A16 + 8) == ff.FF_ERR_INVALID
     assert look(table=None, ids=None, out=None, n=0) == ff.FF_OK  # nothing to do
@@ -45,7 +46,7 @@ def test_layer_norm_refuses_bad_arguments():
     def norm(x=A16, n=4, width=8, stride=8, dtype=ff.FF_BF16, weight=A16, bias=A16, eps=1e-5, out=2 * A16, out_stride=8, mean=A16, rstd=A16):
         return L.ff_layer_norm(x, n, width, stride, dtype, weight, bias, eps, out, out_stride, mean, rstd, None)
 
-    def grad(x=A16, n=4, width=8, stride=8, dtype=ff.FF_BF16, weight=A16, mean=A16, rstd=A16, dy=3 * A16, dy_stride=8, out=2 * A16, out_stride=8, dw=A16, db=A16,
+    def grad(x=A16, n=4, width=8, stride=8, dtype=ff.FF_BF16, weight=A16, mean=A16, rstd=A16, dy=3 * A16, dy_stride=8, out=2 * A16, out_stride=8, dw=4 * A16, db=5 * A16,
              ws=A16):
         return L.ff_layer_norm_grad(x, n, width, stride, dtype, weight, mean, rstd, dy, dy_stride, out, out_stride, dw, db, ws, None)
 
@@ -63,7 +64,7 @@ def test_layer_norm_refuses_bad_arguments():
     for bad in (dict(eps=-1e-5), dict(eps=NAN), dict(eps=INF), dict(bias=A16 + 1), dict(out=A16, out_stride=16)):
         assert norm(**bad) == ff.FF_ERR_INVALID, bad
     for bad in (dict(dy_stride=7), dict(dy=A16 + 1), dict(dw=A16 + 1), dict(db=A16 + 1), dict(ws=A16 + 8), dict(out=3 * A16, out_stride=16),
-                dict(out=A16, out_stride=16)):
+                dict(out=A16, out_stride=16), dict(dw=A16), dict(db=A16)):
         assert grad(**bad) == ff.FF_ERR_INVALID, bad
     assert norm(x=None, out=None, n=0, mean=None, rstd=None) == ff.FF_OK
 
@@ -92,7 +93,7 @@ def test_head_refuses_bad_arguments():
                 dict(weights=A16 + 2), dict(loss_scale=0.0), dict(loss_scale=-1.0), dict(loss_scale=INF), dict(loss_scale=NAN)):
         assert loss(_batch(**bad)) == ff.FF_ERR_INVALID, bad
     for bad in (dict(logp=A16 + 2), dict(stats=A16 + 4), dict(ws=A16 + 16), dict(dh=A16 + 1, dh_stride=64), dict(dh=2 * A16, dh_stride=63),
-                dict(dh=A16, dh_stride=72), dict(dw=A16 + 1, dw_stride=64), dict(dw=A16, dw_stride=63)):
+                dict(dh=A16, dh_stride=72), dict(dw=2 * A16 + 1, dw_stride=64), dict(dw=2 * A16, dw_stride=63), dict(dw=A16, dw_stride=64)):
         assert loss(_batch(), **bad) == ff.FF_ERR_INVALID, bad
     assert L.ff_head_workspace_bytes(None, 1) == 0 and L.ff_head_workspace_bytes(ctypes.byref(_batch(dtype=ff.FF_F32)), 1) == 0
 
@@ -135,30 +136,41 @@ def test_binding_refuses_shapes_types_and_small_workspaces():
     table, out = torch.zeros(10, 8, dtype=bf), torch.zeros(4, 8, dtype=bf)
     for args in ((table, ids.int(), out), (table, ids[::2], out), (table, ids, out.float()), (table, ids, out[:3]), (table.t(), ids, out), (table, ids, out[:, :7]),
                  (table[0], ids, out)):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=SHAPE):
             ff.ff_embed(*args, stream=NOWHERE)
+    with pytest.raises(ValueError, match="current"):  # the machine's own memory
+        ff.ff_embed(table, ids, out, stream=NOWHERE)
     ws = ff.alloc_embed_workspace(4, 10, 8, "cpu")
     for args in ((out, ids, table, ws[:-1]), (out.float(), ids, table, ws), (out, ids[:3], table, ws), (out, ids, table.t(), ws)):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=SHAPE):
             ff.ff_embed_grad(*args, stream=NOWHERE)
+    with pytest.raises(ValueError, match="current"):
+        ff.ff_embed_grad(out, ids, table, ws, stream=NOWHERE)
     w8 = torch.zeros(8, dtype=bf)
     for change in (dict(weight=w8.float()), dict(weight=w8[:7]), dict(bias=w8[:7]), dict(y=out.float()), dict(y=out[:3]), dict(mean=f.double()), dict(rstd=f[:3]), dict(x=out[0])):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=SHAPE):
             ff.ff_layer_norm(**dict(dict(x=out, weight=w8, bias=w8, y=out), **change), stream=NOWHERE)
+    with pytest.raises(ValueError, match="current"):
+        ff.ff_layer_norm(out, w8, w8, out, stream=NOWHERE)
     ws = ff.alloc_norm_workspace(4, 8, "cpu")
     ok = dict(x=out, weight=w8, mean=f, rstd=f, dy=out, dx=out, dweight=w8, dbias=w8, workspace=ws)
     for change in (dict(workspace=ws[:-1]), dict(workspace=None), dict(dweight=w8.float()), dict(dbias=w8[:3]), dict(dy=out[:2]), dict(dx=out.float()), dict(mean=f[:3])):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=SHAPE):
+            ff.ff_layer_norm_grad(**dict(ok, **change), stream=NOWHERE)
+    for change in (dict(), dict(dweight=None, dbias=None, workspace=None)):
+        with pytest.raises(ValueError, match="current"):
             ff.ff_layer_norm_grad(**dict(ok, **change), stream=NOWHERE)
     b = ff.head_batch(out, table, ids, f, 2.0)
     assert (b.n_tokens, b.vocab, b.width, b.hidden_stride, b.weight_stride, b.dtype, b.loss_scale) == (4, 10, 8, 8, 8, ff.FF_BF16, 2.0)
     for args in ((out.t(), table, ids, f), (out, table.float(), ids, f), (out, table[:, :7], ids, f), (out, table, ids.int(), f), (out, table, ids, f[:3]), (out, table, ids, f.double())):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=SHAPE):
             ff.head_batch(*args)
     stats, ws = ff.HeadStats("cpu"), ff.alloc_head_workspace(b, "cpu")
     for change in (dict(workspace=ws[:-1]), dict(logp=f[:3]), dict(dhidden=out.float()), dict(dhidden=out[:3]), dict(dweight=out), dict(dweight=table.t())):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=SHAPE):
             ff.ff_head_loss(**dict(dict(batch=b, logp=f, stats=stats, workspace=ws, dhidden=out, dweight=table), **change), stream=NOWHERE)
+    with pytest.raises(ValueError, match="current"):
+        ff.ff_head_loss(b, f, stats, ws, stream=NOWHERE)
 
 
 def test_a_head_batch_keeps_its_tensors_alive():
