@@ -508,7 +508,7 @@ typedef struct {
 
 /* What ff_head_loss is given; gradient: whether either is wanted.  0 for a batch that is refused.  What the tokens need
  * -- 8 bytes for every token and 256 entries of the vocabulary, 2 to 6 for every element of the hidden states -- and, for a piece of the vocabulary
- * at a time, up to 1.5 GiB, or 0.5 more where rows of `weight` are copied; without gradients those 0.5 alone. */
+ * at a time, up to 3 GiB, or 1 more where rows of `weight` are copied; without gradients that one alone. */
 #define FF_HEAD_MAX_TOKENS (1u << 22)
 #define FF_HEAD_MAX_VOCAB (1u << 22)
 #define FF_HEAD_MAX_WIDTH 65536u

@@ -2,11 +2,12 @@
 //
 // z = H W^T is made in tiles of 256 vocabulary entries: a tile leaves, for each token, its largest logit and the sum of
 // exponentials against it, and the target's logit.  Joined over the tiles these give the log-probability.  For the
-// gradients the vocabulary is taken in pieces, of up to 2^28 logits.  A piece's logits become G = (softmax - [target]) * weight in 16 bits, and two
-// products take G: dH += G W, in 32 bits over the pieces, and dW = G^T H.  The last piece, with which they begin, is still there from
-// the first time (kKeep); the others' logits are made once more: three products of 2 * tokens * vocab * width operations for the last piece, four for the
-// others.  (Head of 8192 x 128,256, 4096 tokens, a tenth masked, us, pieces of 2^25 / 2^26 / 2^27 / 2^28 logits 25188 / 24666 / 23290 / 21682, of 4096 x
-// 32,000, which the last two take in one, 3204 / 3103 / 2698 / 2698: what is kept for a fixed 1 GiB.)
+// gradients the vocabulary is taken in pieces, of up to 2^29 logits.  A piece's logits become G = (softmax - [target]) * weight in
+// 16 bits, and two products take G: dH += G W, in 32 bits over the pieces, and dW = G^T H.  The last piece, with which they
+// begin, is still there from the first time (kKeep); the others' logits are made once more: three products of 2 * tokens * vocab *
+// width operations for the last piece, four for the others.  What is kept goes by the card's 288 GB, of which 3 GiB are one hundredth.  (Pieces
+// of 2^25 / 2^26 / 2^27 / 2^28 / 2^29 / 2^30 logits: 4096 tokens, a tenth of them masked, 8192 x 128,256 25.2 / 24.7 / 23.3 / 21.7 /
+// 18.7 / 18.8 ms, 4096 x 32,000, which lies in one from 2^27 on, 3.20 / 3.10 / 2.70 / 2.70 / 2.62 / 2.64.)
 //
 // G is rounded to 16 bits, for the matrix instructions; nothing else is, in front of the outputs.  Weights are divided
 // by the largest one first, so that tokens of equal weight have exact factors of 1 (a factor rounded with G would
@@ -708,7 +709,7 @@ __global__ void head_of_nothing_kernel(ff_head_stats* stats) { *stats = {}; }
 
 // ---- the workspace ----------------------------------------------------------------------------------
 
-constexpr uint64_t kPieceElements = 1ull << 28;  // of G, and of a piece's packed rows
+constexpr uint64_t kPieceElements = 1ull << 29;  // of G, and of a piece's packed rows
 constexpr uint64_t kFewDweightFrom = 1 << 23;    // elements of W, from which on dW of few tokens has its own launch
 constexpr uint32_t kFewDweightBlocks = 1024;    // workgroups of head_few_dweight_kernel, about
 constexpr uint32_t kKeptBlocks = 2048;           // workgroups that make G of kept logits, about

@@ -357,3 +357,12 @@ def test_head_at_larger_sizes(dtype, n, vocab, width, pad, first):
     args = head_inputs(n, vocab, width, dtype, pad, first, masked=0.1)
     scale = 1024.0 if dtype == F16 else 1.0
     check_head(run_head(*args, scale, pad=pad, first=first), modelref.head(*args, scale))
+
+
+@HALVES
+@pytest.mark.parametrize("n,vocab,width,pad,first", [(40000, 14000, 1032, 0, 0), (30011, 18000, 136, 8, 0), (70, 9000, 65528, 3, 1), (20, 9000, 65528, 3, 1)])
+def test_head_in_several_pieces_of_the_vocabulary(dtype, n, vocab, width, pad, first):
+    """Of logits, the last of which are kept or not, and of copied rows."""
+    args = head_inputs(n, vocab, width, dtype, pad, first, masked=0.1)
+    scale = 1024.0 if dtype == F16 else 1.0
+    check_head(run_head(*args, scale, pad=pad, first=first), modelref.head(*args, scale))
