@@ -419,15 +419,23 @@ __device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const
 {
     const uint32_t lane = threadIdx.x % kWaveSize;
     const float2* const parts = A.parts + static_cast<uint64_t>(r) * A.tiles;
+    // fn(part), several on their way at once
+    auto each_part = [&](auto&& fn) {
+        constexpr uint32_t kAhead = 8;
+        for (uint32_t k = lane; k < A.tiles; k += kAhead * kWaveSize) {
+            float2 p[kAhead];
+            static_for<kAhead>([&](auto i) { p[int(i)] = k + i * kWaveSize < A.tiles ? parts[k + i * kWaveSize] : float2{-INFINITY, 0.f}; });
+            static_for<kAhead>([&](auto i) { fn(p[int(i)]); });
+        }
+    };
     float c = -INFINITY;
-    for (uint32_t k = lane; k < A.tiles; k += kWaveSize) c = fmaxf(c, parts[k].x);
+    each_part([&](float2 p) { c = fmaxf(c, p.x); });
     for (int d = 32; d; d /= 2) c = fmaxf(c, __shfl_xor(c, d));
     if (c == -INFINITY) c = 0.f;
     double total = 0;
-    for (uint32_t k = lane; k < A.tiles; k += kWaveSize) {
-        const float2 p = parts[k];
-        total += static_cast<double>(p.y) * exp2(static_cast<double>(p.x) - static_cast<double>(c));
-    }
+    each_part([&](float2 p) {
+        if (p.y != 0.f) total += static_cast<double>(p.y) * exp2(static_cast<double>(p.x) - static_cast<double>(c));
+    });
     for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
     const double against = static_cast<double>(c) / static_cast<double>(kLog2E), rest = log(total);
     const double logp = (static_cast<double>(A.picked[r]) - against) - rest;

@@ -48,14 +48,6 @@ __device__ __forceinline__ void sum_over(float (&v)[N], int turn)
 
 __device__ __forceinline__ float sum8(f32x8 v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 
-// Of the eight elements from `at` on, those that the row has.
-__device__ __forceinline__ f32x8 cut(f32x8 v, uint32_t at, uint32_t width)
-{
-    if (at + kLaneItems > width)
-        for (uint32_t i = 0; i < kLaneItems; i++) v[i] = at + i < width ? v[i] : 0.f;
-    return v;
-}
-
 // fn(i, at) for the thread's K places in a row.
 template <int GROUP, int K, class Fn>
 __device__ __forceinline__ void places(uint32_t thread, uint32_t width, Fn&& fn)
@@ -66,10 +58,9 @@ __device__ __forceinline__ void places(uint32_t thread, uint32_t width, Fn&& fn)
     });
 }
 
-template <uint32_t DTYPE, int GROUP, int K, bool PAST>
+template <class I, int GROUP, int K, bool PAST>
 __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs a)
 {
-    using I = Items<DTYPE>;
     constexpr uint32_t kPer = block_of<GROUP>() / GROUP;
     const uint32_t width = static_cast<uint32_t>(a.width), thread = threadIdx.x % GROUP;
     const float each = 1.f / static_cast<float>(width);
@@ -89,13 +80,13 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
         static_for<K>([&](auto i) { h[int(i)] = next[int(i)]; });
         if (r + step < a.n_rows) fetch(next, r + step);
         float s[1] = {0.f};
-        places<GROUP, K>(thread, width, [&](auto i, uint32_t) { s[0] += sum8(I::wide(h[int(i)])); });
+        places<GROUP, K>(thread, width, [&](auto i, uint32_t at) { s[0] += sum8(I::cut(I::wide(h[int(i)]), at, width)); });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
         const float mean = s[0] * each;
         s[0] = 0.f;
         places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
-            const f32x8 d = cut(I::wide(h[int(i)]) - mean, at, width);
+            const f32x8 d = I::cut(I::wide(h[int(i)]) - mean, at, width);
             s[0] += sum8(d * d);
         });
         sum_over<GROUP>(s, turn);
@@ -115,10 +106,9 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
 
 // 32 columns of dw and db, from all rows.
 constexpr uint32_t kColumns = 32;
-template <uint32_t DTYPE, int THREADS>
+template <class I, int THREADS>
 __device__ __forceinline__ void columns(const NormArgs& a, const uint32_t block)
 {
-    using I = Items<DTYPE>;
     constexpr uint32_t kAcross = THREADS / kColumns, kAhead = 8;
     __shared__ float part[2][kAcross][kColumns + 1];
     const uint32_t width = static_cast<uint32_t>(a.width), n = static_cast<uint32_t>(a.n_rows), c = threadIdx.x % kColumns, k = threadIdx.x / kColumns;
@@ -152,13 +142,12 @@ __device__ __forceinline__ void columns(const NormArgs& a, const uint32_t block)
 }
 
 // `column_blocks` workgroups behind the others make dw and db; with none of them, the rows' groups leave their parts.
-template <uint32_t DTYPE, int GROUP, int K, bool PAST>
+template <class I, int GROUP, int K, bool PAST>
 __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const NormArgs a, const uint32_t column_blocks)
 {
-    using I = Items<DTYPE>;
     const uint32_t blocks = gridDim.x - column_blocks;
     if (blockIdx.x >= blocks) {
-        columns<DTYPE, block_of<GROUP>()>(a, blockIdx.x - blocks);
+        columns<I, block_of<GROUP>()>(a, blockIdx.x - blocks);
         return;
     }
     constexpr uint32_t kPer = block_of<GROUP>() / GROUP;
@@ -197,7 +186,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
         // fn(i, at, x normed, dy, dy * weight)
         auto each_place = [&](auto&& fn) {
             places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
-                const f32x8 x = I::wide(kHold ? now.x[int(i)] : load_x(r, at)), d = I::wide(kHold ? now.dy[int(i)] : load_dy(r, at));
+                const f32x8 x = I::wide(kHold ? now.x[int(i)] : load_x(r, at)), d = I::cut(I::wide(kHold ? now.dy[int(i)] : load_dy(r, at)), at, width);
                 fn(i, at, (x - now.mean) * now.rstd, d, d * I::wide(kHold ? w[int(i)] : load_w(at)));
             });
         };
@@ -236,17 +225,16 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
     }
     uint8_t* const out = reinterpret_cast<uint8_t*>(a.parts + 2ull * blockIdx.x * width);
     places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
-        Items<FF_F32>::store(out, at, width, Items<FF_F32>::narrow(dw[int(i)]));
-        Items<FF_F32>::store(out + 4ull * width, at, width, Items<FF_F32>::narrow(db[int(i)]));
+        I::Wide::store(out, at, width, I::Wide::narrow(dw[int(i)]));
+        I::Wide::store(out + 4ull * width, at, width, I::Wide::narrow(db[int(i)]));
     });
 }
 
 // Columns of dw (blockIdx.y 0) and db (1): the parts of all workgroups.
 constexpr uint32_t kJoinRows = 32, kJoinAhead = 8;
-template <uint32_t DTYPE>
+template <class I>
 __global__ __launch_bounds__(kColumns* kJoinRows) void norm_join_kernel(const NormArgs a, const uint32_t blocks)
 {
-    using I = Items<DTYPE>;
     __shared__ float part[kJoinRows][kColumns + 1];
     uint8_t* const out = blockIdx.y ? a.dbias : a.dweight;
     const uint32_t width = static_cast<uint32_t>(a.width), c = threadIdx.x % kColumns, k = threadIdx.x / kColumns;
@@ -293,26 +281,26 @@ uint32_t grad_blocks(uint64_t n_rows, uint64_t width)
     return blocks;
 }
 
-template <uint32_t DTYPE>
+template <class I>
 bool past(const NormArgs& a)
 {
-    return a.n_rows * a.width * Items<DTYPE>::kBytes >= kPastBytes;
+    return a.n_rows * a.width * I::kBytes >= kPastBytes;
 }
 
-template <uint32_t DTYPE>
+template <class I>
 hipError_t forward(const NormArgs& a, hipStream_t stream)
 {
     choose(a.width, [&](auto group, auto k) {
         constexpr int threads = block_of<group>();
         constexpr uint32_t per = threads / group;
         const uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>((a.n_rows + per - 1) / per, kForwardBlocks));
-        const auto kernel = past<DTYPE>(a) ? norm_kernel<DTYPE, group, k, true> : norm_kernel<DTYPE, group, k, false>;
+        const auto kernel = past<I>(a) ? norm_kernel<I, group, k, true> : norm_kernel<I, group, k, false>;
         hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a);
     });
     return hipGetLastError();
 }
 
-template <uint32_t DTYPE>
+template <class I>
 hipError_t backward(const NormArgs& a, hipStream_t stream)
 {
     const uint32_t blocks = grad_blocks(a.n_rows, a.width);
@@ -320,10 +308,10 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
     const bool sums = a.dweight || a.dbias, few = a.n_rows <= kFewRows && a.out != a.x && a.out != a.dy;
     const uint32_t all = static_cast<uint32_t>((a.width + kColumns - 1) / kColumns), column_blocks = sums && few ? all : 0;
     choose(a.width, [&](auto group, auto k) {
-        const auto kernel = past<DTYPE>(a) ? norm_grad_kernel<DTYPE, group, k, true> : norm_grad_kernel<DTYPE, group, k, false>;
+        const auto kernel = past<I>(a) ? norm_grad_kernel<I, group, k, true> : norm_grad_kernel<I, group, k, false>;
         hipLaunchKernelGGL(kernel, dim3(blocks + column_blocks), dim3(block_of<group>()), 0, stream, a, column_blocks);
     });
-    if (sums && !few) hipLaunchKernelGGL(norm_join_kernel<DTYPE>, dim3(all, 2), dim3(kColumns * kJoinRows), 0, stream, a, blocks);
+    if (sums && !few) hipLaunchKernelGGL(norm_join_kernel<I>, dim3(all, 2), dim3(kColumns * kJoinRows), 0, stream, a, blocks);
     return hipGetLastError();
 }
 
@@ -336,13 +324,16 @@ uint64_t norm_workspace(uint64_t n_rows, uint64_t width)
 
 hipError_t launch_norm(const NormArgs& a, uint32_t dtype, hipStream_t stream)
 {
-    if (!a.n_rows) return hipSuccess;
-    return dtype == FF_BF16 ? forward<FF_BF16>(a, stream) : dtype == FF_F16 ? forward<FF_F16>(a, stream) : forward<FF_F32>(a, stream);
+    hipError_t err = hipSuccess;
+    if (a.n_rows) with_items(dtype, a.width, [&](auto items) { err = forward<decltype(items)>(a, stream); });
+    return err;
 }
 
 hipError_t launch_norm_grad(const NormArgs& a, uint32_t dtype, hipStream_t stream)
 {
-    return dtype == FF_BF16 ? backward<FF_BF16>(a, stream) : dtype == FF_F16 ? backward<FF_F16>(a, stream) : backward<FF_F32>(a, stream);
+    hipError_t err = hipSuccess;
+    with_items(dtype, a.width, [&](auto items) { err = backward<decltype(items)>(a, stream); });
+    return err;
 }
 
 }  // namespace ffsnap

@@ -16,9 +16,32 @@ constexpr int kLaneItems = 8;
 // 8192 92 and 84.  Inputs of 3001 rows of 1003 fp32 elements past them 24.2 where 21.7 are taken.)
 constexpr uint64_t kPastBytes = 32ull << 20;
 
-template <uint32_t DTYPE>
+// WHOLE: rows are multiples of eight elements.  (What others need at their ends costs all rows registers: layer norm of 16,384 x 8192 bf16 elements, forward
+// and backward, 248 us where they are treated like the others, 231 so; 16,384 embedded tokens of 8192 85 and 82.)
+template <uint32_t DTYPE, bool WHOLE>
 struct Items {
     static constexpr uint32_t kBytes = DTYPE == FF_F32 ? 4 : 2;
+    using Wide = Items<FF_F32, WHOLE>;  // of sums
+
+    // Where the eight elements lie that a lane holds for its [at, at + 8) of a row of `width`, at < width: those, or, where the row has fewer, its last
+    // eight, which it holds in part for another lane.  (Element by element, a lane would wait for each row's in turn, and its wavefront with it: 3001 rows of
+    // 257 fp32 elements added to a table's gradient 17.4 us, so 12.5.)  A row of less than eight is filled up with its last one.
+    static __device__ __forceinline__ uint32_t window(uint32_t at, uint32_t width)
+    {
+        return WHOLE || at + kLaneItems <= width || width < kLaneItems ? at : width - kLaneItems;
+    }
+    // Is element i of those the lane's own?
+    static __device__ __forceinline__ bool owns(uint32_t i, uint32_t at, uint32_t width)
+    {
+        return WHOLE || (window(at, width) + i >= at && window(at, width) + i < width);
+    }
+    // Zeros for those that are not.
+    static __device__ __forceinline__ f32x8 cut(f32x8 v, uint32_t at, uint32_t width)
+    {
+        if (!WHOLE && at + kLaneItems > width)
+            for (uint32_t i = 0; i < kLaneItems; i++) v[i] = owns(i, at, width) ? v[i] : 0.f;
+        return v;
+    }
 
     static __device__ __forceinline__ float one(const uint8_t* p)
     {
@@ -63,12 +86,12 @@ struct Items {
         }
         return h;
     }
-    // Elements [at, at + 8) of a row of `width`, at < width; those behind it are zeros.  PAST: not to be kept in the caches.
+    // A lane's elements [at, at + 8) of a row of `width`, at < width.  PAST: not to be kept in the caches.
     template <bool PAST = false>
     static __device__ __forceinline__ Held load(const uint8_t* row, uint32_t at, uint32_t width)
     {
-        const uint8_t* const p = row + static_cast<uint64_t>(at) * kBytes;
-        if (at + kLaneItems <= width) {
+        const uint8_t* const p = row + static_cast<uint64_t>(window(at, width)) * kBytes;
+        if (WHOLE || width >= kLaneItems) {
             Held h;
             for (uint32_t i = 0; i < kBytes / 2; i++) {
                 const auto* const q = (const FF_GLOBAL u32x4_a2*)p + i;
@@ -77,14 +100,14 @@ struct Items {
             return h;
         }
         f32x8 v;
-        for (uint32_t i = 0; i < kLaneItems; i++) v[i] = at + i < width ? one(p + i * kBytes) : 0.f;
+        for (uint32_t i = 0; i < kLaneItems; i++) v[i] = one(p + (i < width ? i : width - 1) * kBytes);
         return narrow(v);
     }
     template <bool PAST = false>
     static __device__ __forceinline__ void store(uint8_t* row, uint32_t at, uint32_t width, const Held& h)
     {
-        uint8_t* const p = row + static_cast<uint64_t>(at) * kBytes;
-        if (at + kLaneItems <= width) {
+        uint8_t* const p = row + static_cast<uint64_t>(window(at, width)) * kBytes;
+        if (WHOLE || at + kLaneItems <= width) {
             for (uint32_t i = 0; i < kBytes / 2; i++) {
                 auto* const q = (FF_GLOBAL u32x4_a2*)p + i;
                 if (PAST) __builtin_nontemporal_store(h.w[i], q);
@@ -94,8 +117,18 @@ struct Items {
         }
         const f32x8 v = wide(h);
         for (uint32_t i = 0; i < kLaneItems; i++)
-            if (at + i < width) put(p + i * kBytes, v[i]);
+            if (owns(i, at, width)) put(p + i * kBytes, v[i]);
     }
 };
+
+// fn(the items) of rows of this width.
+template <class Fn>
+void with_items(uint32_t dtype, uint64_t width, Fn&& fn)
+{
+    const bool whole = width % kLaneItems == 0;
+    if (dtype == FF_BF16) whole ? fn(Items<FF_BF16, true>{}) : fn(Items<FF_BF16, false>{});
+    else if (dtype == FF_F16) whole ? fn(Items<FF_F16, true>{}) : fn(Items<FF_F16, false>{});
+    else whole ? fn(Items<FF_F32, true>{}) : fn(Items<FF_F32, false>{});
+}
 
 }  // namespace ffsnap
