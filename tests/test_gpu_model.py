@@ -96,6 +96,14 @@ def test_gradient_by_sorted_tokens(dtype, kind, n, vocab, width, pad, first):
         assert torch.equal(dtable, first_bits)  # the same bits every time
 
 
+@TYPES
+@pytest.mark.parametrize("kind", ["even", "text", "same"])
+@pytest.mark.parametrize("n,vocab,width,pad,first", [(300, 40, 513, 0, 0), (9001, 300, 517, 1, 1), (5000, 64, 13, 0, 0), (4200, 33, 5, 0, 3), (6000, 2000, 1025, 0, 0)])
+def test_gradient_of_rows_that_end_inside_a_lane(dtype, kind, n, vocab, width, pad, first):
+    """The last elements lie with others in a lane, of the same wavefront or of another's."""
+    test_gradient_by_sorted_tokens(dtype, kind, n, vocab, width, pad, first)
+
+
 def test_embedding_of_nothing():
     table = torch.ones(4, 8, device=DEV)
     ids = torch.zeros(0, dtype=torch.int64, device=DEV)
@@ -187,7 +195,7 @@ def test_layer_norm_in_place_and_without_statistics():
     assert torch.equal(x, y)
 
 
-@pytest.mark.parametrize("n,width", [(1, 8), (50, 1000), (1024, 4096), (700, 16384), (1500, 300)])
+@pytest.mark.parametrize("n,width", [(1, 8), (50, 1000), (1024, 4096), (700, 16384), (1500, 300), (300, 9), (40, 1027), (2000, 513), (600, 8193), (1100, 8199), (20, 16383)])
 @pytest.mark.parametrize("over", ["x", "dy"])
 def test_layer_norm_gradients_of_weights_where_dx_replaces_its_inputs(over, n, width):
     x, weight, bias, dy, _ = norm_inputs(n, width, BF16, 0, 0)
