@@ -59,6 +59,14 @@ __device__ __forceinline__ void clear_rows(uint8_t* out, uint64_t stride, uint64
                 I::template store<PAST>(out + r * stride * I::kBytes, at, to, I::narrow(f32x8{}));
 }
 
+// The sum over a wavefront's lanes that have the same elements, every `lanes`-th, in the first of them.
+__device__ __forceinline__ f32x8 join_turns(f32x8 sum, uint32_t lanes)
+{
+    for (uint32_t d = kWaveSize / 2; d >= lanes; d /= 2)
+        static_for<8>([&](auto i) { sum[int(i)] += __shfl_down(sum[int(i)], d); });
+    return sum;
+}
+
 // ---- order of the tokens ------------------------------------------------------------------------------
 
 constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / kWaveSize, kSortRounds = 16;
@@ -312,17 +320,22 @@ __global__ __launch_bounds__(kWaveSize* kJoinWaves) void embed_join_kernel(const
         }
         return;
     }
+    // (narrow rows: several parts to a wavefront at a time)
+    uint32_t lanes = 1;
+    while (lanes < kWaveSize && lanes * kLaneItems < width) lanes *= 2;
+    const uint32_t turn = lane / lanes, turns = kWaveSize / lanes;
     const uint64_t total = static_cast<uint64_t>(s.counts[1]) * slabs;
     for (uint64_t w = blockIdx.x - few_blocks; w < total; w += gridDim.x - few_blocks) {
-        const uint32_t k = static_cast<uint32_t>(w / slabs), at = static_cast<uint32_t>(w - static_cast<uint64_t>(k) * slabs) * kSlab + lane * kLaneItems;
+        const uint32_t k = static_cast<uint32_t>(w / slabs), at = static_cast<uint32_t>(w - static_cast<uint64_t>(k) * slabs) * kSlab + lane % lanes * kLaneItems;
         const uint2 run = s.runs[1][k];
         f32x8 sum = {};
-        if (at < width) sum = sum_of(wave == 0 ? end_of(run.x, 1, at) : sum, run.x + 1 + wave, run.y, kJoinWaves, at);
+        if (at < width) sum = sum_of(wave == 0 && turn == 0 ? end_of(run.x, 1, at) : sum, run.x + 1 + wave * turns + turn, run.y, kJoinWaves * turns, at);
+        sum = join_turns(sum, lanes);
         const typename F::Held h = F::narrow(sum);
         joined[wave][0][lane] = h.w[0];
         joined[wave][1][lane] = h.w[1];
         __syncthreads();
-        if (wave == 0 && at < width) {
+        if (wave == 0 && turn == 0 && at < width) {
             for (uint32_t i = 1; i < kJoinWaves; i++) sum += F::wide(typename F::Held{{joined[i][0][lane], joined[i][1][lane]}});
             put(run.x, sum, at);
         }
@@ -372,12 +385,6 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
     const uint32_t at = slab + lane % lanes * kLaneItems, turn = lane / lanes, turns = kWaveSize / lanes;
     const bool mine = at < width, puts = mine && turn == 0;
     const uint64_t lower = (1ull << lane) - 1;
-    // of a wavefront's lanes that have the same elements, in the first of them
-    auto join = [&](f32x8 sum) {
-        for (uint32_t d = kWaveSize / 2; d >= lanes; d /= 2)
-            static_for<8>([&](auto i) { sum[int(i)] += __shfl_down(sum[int(i)], d); });
-        return sum;
-    };
     // The whole range is cleared first, while the ids are on their way; sums overwrite it, behind the barriers.
     if (!ADD) {
         clear_rows<I, false>(a.out + static_cast<uint64_t>(first) * a.out_stride * I::kBytes, a.out_stride, range, slab, slab_end, wave, kFewWaves,
@@ -482,14 +489,14 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
         if (ADD && puts) old = there(id);
         f32x8 sum = {};
         if (mine) sum = sum_list<I>(a, order, from + turn, to, turns, at);
-        sum = join(sum);
+        sum = join_turns(sum, lanes);
         if (puts) put(id, sum, old);
     }
     for (uint32_t k = 0; k < many; k++) {
         const uint32_t id = bin_of[kFewThreads + k], from = id ? begin[id - 1] : 0, to = begin[id];
         f32x8 sum = {};
         if (mine) sum = sum_list<I>(a, order, from + wave * turns + turn, to, kFewWaves * turns, at);
-        sum = join(sum);
+        sum = join_turns(sum, lanes);
         const typename F::Held h = F::narrow(sum);
         joined[wave][0][lane] = h.w[0];
         joined[wave][1][lane] = h.w[1];
