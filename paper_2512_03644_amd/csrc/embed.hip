@@ -346,10 +346,15 @@ __global__ __launch_bounds__(kWaveSize* kJoinWaves) void embed_join_kernel(const
 // ---- few tokens ---------------------------------------------------------------------------------------
 
 // All of it in one launch: a workgroup takes 512 elements of the rows of a range of ids, and finds and sorts the tokens that ask for
-// them in LDS.  A wavefront sums a row's tokens, several at a time where its lanes are more than a row takes; rows of more than kLong are summed by all
-// wavefronts together.  Of the range's ids only those that have any are looked at again: 128 tokens added to 32,000 x 4096 bf16 elements 13.1 us where
-// wavefronts go through all, 7.0 so.
-constexpr uint32_t kFewThreads = 512, kFewWaves = kFewThreads / kWaveSize, kFewTokens = 4096, kFewRounds = kFewTokens / kFewThreads, kLong = 16, kFewBlocks = 768, kFewWork = 8192;
+// them in LDS.  A wavefront sums a row's tokens, several at a time where its lanes are more than a row takes; rows of more than kLong are
+// summed by all wavefronts together.  Of the range's ids only those that have any are looked at again: 128 tokens added to 32,000 x 4096
+// bf16 elements 13.1 us where wavefronts go through all, 7.0 so.
+//
+// For up to kFewTokens, unless the table is so large that kMostFewBlocks workgroups are too few for it.  (Us, this / sort, sums, join; bf16, words as
+// frequent as in text, added: 1000 tokens on 32,000 x 4096 11 / 19, 4096 20 / 29, 4000 on 128,256 x 4096 (2008 workgroups) 26 / 36, x 6144 (3012) 36 / 42, 500
+// on 128,256 x 8192 (4016) 32 / 23.  All of 4096 tokens the same word: 80 / 44, what one compute unit reads.)
+constexpr uint32_t kFewThreads = 512, kFewWaves = kFewThreads / kWaveSize, kFewTokens = 4096, kFewRounds = kFewTokens / kFewThreads;
+constexpr uint32_t kLong = 16, kFewBlocks = 768, kMostFewBlocks = 3072;
 
 // Rows of tokens list[from], list[from + step], ... in front of `to`.
 template <class I>
@@ -548,7 +553,7 @@ template <class I, bool ADD>
 hipError_t launch_grad(const EmbedArgs& a, Sorted s, hipStream_t stream)
 {
     const uint32_t slabs = static_cast<uint32_t>((a.width + kSlab - 1) / kSlab);
-    if (a.n_tokens <= kFewTokens && a.n_tokens * slabs <= kFewWork && (a.vocab / kFewThreads + 1) * slabs <= most_groups(kFewThreads)) {
+    if (a.n_tokens <= kFewTokens && (a.vocab + kFewThreads - 1) / kFewThreads * slabs <= kMostFewBlocks) {
         // ranges of 8 to 512 ids, for about kFewBlocks workgroups
         uint32_t range = 8;
         while (range < kFewThreads && (a.vocab + range - 1) / range * slabs > kFewBlocks) range *= 2;
