@@ -79,6 +79,7 @@ struct HeadArgs {
     uint32_t step;      // and that the gradients' products take at once
     uint32_t slices;    // of dH's sum over a piece
     float grad_scale;   // loss scale, and what G is too large by
+    uint32_t past;      // dW's rows are whole pieces of 16 bytes
 };
 
 __device__ __forceinline__ OperandTile hidden_tile(const HeadArgs& A, uint32_t m0, uint32_t used)
@@ -164,16 +165,16 @@ __device__ __forceinline__ void copy_row(uint8_t* to, uint32_t bytes, const uint
 }
 
 // Hidden states of the tokens that count, one behind the other, and zeros up to 64 rows; gradients of the other tokens.
-__device__ __forceinline__ void gather(const HeadArgs& A, const uint32_t used, const uint32_t* index)
+__device__ __forceinline__ void gather(const HeadArgs& A, const uint32_t used, const uint32_t* index, const uint32_t blocks)
 {
     const uint32_t until = (used + 63) / 64 * 64, n = static_cast<uint32_t>(A.b.n_tokens);
-    for (uint32_t r = blockIdx.x; r < until; r += gridDim.x) {
+    for (uint32_t r = blockIdx.x; r < until; r += blocks) {
         const uint64_t t = r < used ? index[r] : 0;
         copy_row(A.hidden + static_cast<uint64_t>(r) * A.stride, A.stride,
                  static_cast<const uint8_t*>(A.b.hidden) + t * A.b.hidden_stride * 2, r < used ? static_cast<uint32_t>(A.b.width) : 0);
     }
     if (!A.dhidden) return;
-    for (uint64_t t = blockIdx.x; t < n; t += gridDim.x) {
+    for (uint64_t t = blockIdx.x; t < n; t += blocks) {
         const float w = A.b.weights[t];
         const int64_t y = A.b.targets[t];
         if (!(w == 0.f) && y >= 0 && static_cast<uint64_t>(y) < A.b.vocab) continue;
@@ -181,24 +182,31 @@ __device__ __forceinline__ void gather(const HeadArgs& A, const uint32_t used, c
         for (uint32_t i = threadIdx.x; i < A.b.width; i += blockDim.x) as_global(to)[i] = 0;
     }
 }
-__global__ __launch_bounds__(256) void head_gather_kernel(const HeadArgs A) { gather(A, A.state->used, A.index); }
+__global__ __launch_bounds__(256) void head_gather_kernel(const HeadArgs A) { gather(A, A.state->used, A.index, gridDim.x); }
 
-// Both, where every workgroup can look at all tokens by itself.
-constexpr uint32_t kSelectFew = 1024;
-__global__ __launch_bounds__(256) void head_few_kernel(const HeadArgs A)
+// Rows [first, first + n) of W, packed, by `blocks` workgroups.
+__device__ __forceinline__ void pack(const HeadArgs& A, const uint32_t first, const uint32_t n, const uint32_t block, const uint32_t blocks)
 {
+    for (uint32_t r = block; r < n; r += blocks)
+        copy_row(A.weight + static_cast<uint64_t>(r) * A.stride, A.stride,
+                 static_cast<const uint8_t*>(A.b.weight) + (static_cast<uint64_t>(first) + r) * A.b.weight_stride * 2, static_cast<uint32_t>(A.b.width));
+}
+constexpr uint32_t kPackBlocks = 8192;
+__global__ __launch_bounds__(256) void head_pack_kernel(const HeadArgs A, const uint32_t first, const uint32_t n) { pack(A, first, n, blockIdx.x, gridDim.x); }
+
+// Tokens and hidden states in one launch, where every workgroup can look at all tokens by itself; the workgroups behind the first `blocks` pack the
+// first n rows of W.
+constexpr uint32_t kSelectFew = 1024;
+__global__ __launch_bounds__(256) void head_few_kernel(const HeadArgs A, const uint32_t blocks, const uint32_t n)
+{
+    if (blockIdx.x >= blocks) {
+        pack(A, 0, n, blockIdx.x - blocks, gridDim.x - blocks);
+        return;
+    }
     __shared__ uint32_t index[kSelectFew];
     const uint32_t used = select<256>(A, index, blockIdx.x == 0);
     __syncthreads();
-    gather(A, used, index);
-}
-
-// Rows [first, first + n) of W, packed.
-__global__ __launch_bounds__(256) void head_pack_kernel(const HeadArgs A, const uint32_t first, const uint32_t n)
-{
-    for (uint32_t r = blockIdx.x; r < n; r += gridDim.x)
-        copy_row(A.weight + static_cast<uint64_t>(r) * A.stride, A.stride,
-                 static_cast<const uint8_t*>(A.b.weight) + (static_cast<uint64_t>(first) + r) * A.b.weight_stride * 2, static_cast<uint32_t>(A.b.width));
+    gather(A, used, index, blocks);
 }
 
 // An element of G.
@@ -305,11 +313,12 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
             });
     } else {
         __shared__ float2 part[BM][S::kAcross];
+        const uint32_t kept_from = A.piece < vocab ? first : 0;  // of few tokens all are kept
         static_for<S::kM>([&](auto i) {
             const uint32_t t = m + 16 * i;
             const int32_t y = t < used ? A.targets[t] : -1;
             if constexpr (MODE == kKeep) {
-                float* const out = A.logits + static_cast<uint64_t>(t) * A.piece + (v - first);
+                float* const out = A.logits + static_cast<uint64_t>(t) * A.piece + (v - kept_from);
                 static_for<S::kN>([&](auto j) {
                     if (t < used) *(FF_GLOBAL f32x4*)(out + 16 * j) = z[int(i)][int(j)];
                 });
@@ -323,15 +332,16 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     }
 }
 
-// The logits of few tokens, all of the vocabulary: W passes once from memory through registers, rows of any alignment where they lie.  A wavefront
-// takes 16 V rows of it and 16 T tokens, whose hidden states come from the caches; the products of a chunk of K times 32
-// elements are made while the next one is on its way.  What bounds it: reading W, up to 16 tokens; more read their hidden states from the caches as often,
-// and 64 x 256 tiles are better where W lies as those want it.  Us, scoring, this / tiles: 1 token on 32,000 x 4096 65 / 89; 17, 32, 64 tokens 80, 88, 114 / 92, 93, 102; on
-// 128,256 x 4096 266, 323, 425 / 242, 245, 249.
+// The logits of few tokens, all of the vocabulary: W passes once from memory through registers, rows of any alignment where they lie.  A
+// wavefront takes 16 V rows of it and 16 T tokens, whose hidden states come from the caches; the products of a chunk of K times 32 elements
+// are made while the next one is on its way.  What bounds it: reading W; of 17 tokens and more hidden states as well, and 64 x 256
+// tiles are better, also where rows have to be copied for them, but for up to 32 tokens that are only scored.  (Us, scoring, this / tiles: 1
+// token on 32,000 x 4096 64 / 89, 17 80 / 92, 32 88 / 93, 64 114 / 102, on 128,256 x 4096 17 266 / 242; copied for tiles, 22 tokens on 67,725 x 1491 108 / 154, 51 on
+// 10,863 x 2651 87 / 61; with both gradients, which have rows copied anyway, 2 tokens on 49,835 x 2189 360 / 307.)
 constexpr int kStreamThreads = 256, kStreamWaves = kStreamThreads / kWaveSize;
 template <int T>
 struct Stream {
-    static constexpr int V = T == 1 ? 1 : 2, K = 8 / T;
+    static constexpr int V = T, K = 8 / T;
     static constexpr uint32_t kEntries = 16 * V * kStreamWaves;  // of a workgroup
 };
 template <bool BF16, int T, Mode MODE>
@@ -412,8 +422,9 @@ __device__ __forceinline__ void put_stats(const HeadArgs& A, double loss, const 
     A.stats->n_invalid = A.state->invalid;
 }
 
+constexpr uint32_t kCountFew = 256;
 // A wavefront joins the tiles' parts of row r, in 64 bits from the exponentials on.  The one that writes leaves the results; of few rows
-// (kFewTokens) the last one to do so adds their losses up.
+// (kCountFew: they count one another at one address, 10 ns each) the last one to do so adds their losses up, of others a launch.
 template <bool BF16>
 __device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const uint32_t used, const bool writes)
 {
@@ -446,7 +457,7 @@ __device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const
         A.rows[r] = row;
         __hip_atomic_store(A.losses + r, -static_cast<double>(w) * logp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (writes && A.b.n_tokens <= kFewTokens) {
+    if (writes && A.b.n_tokens <= kCountFew) {
         bool last = false;
         if (lane == 0) {
             // (the loss has arrived when the store is done; a release would write the caches back)
@@ -455,7 +466,8 @@ __device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const
             last = __hip_atomic_fetch_add(&A.state->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == used;
         }
         if (__any(last)) {
-            double s = lane < used ? __hip_atomic_load(A.losses + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+            double s = 0;
+            for (uint32_t k = lane; k < used; k += kWaveSize) s += __hip_atomic_load(A.losses + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             for (int d = 32; d; d /= 2) s += __shfl_xor(s, d);
             if (lane == 0) put_stats(A, s, used);
         }
@@ -534,10 +546,11 @@ __device__ __forceinline__ void put8(uint8_t* row, uint32_t at, uint32_t width, 
 }
 
 // The same, past the caches: a gradient of W is far larger than they are.  (Us, plain / so: dW of 1, 64, 128 tokens on 128,256 x 4096, with all in front of
-// it, 505, 565, 699 and 483, 527, 590.)
-__device__ __forceinline__ void put8_past(uint8_t* row, uint32_t at, uint32_t width, u32x4 v)
+// it, 505, 565, 699 and 483, 527, 590.)  Not where rows begin between 16-byte steps: pieces of lines would go to memory one by one (2 tokens on 49,835 x 2189,
+// dW 168 us past the caches, 60 through them).
+__device__ __forceinline__ void put8_past(bool past, uint8_t* row, uint32_t at, uint32_t width, u32x4 v)
 {
-    if (at + 8 <= width) __builtin_nontemporal_store(v, (FF_GLOBAL u32x4_a2*)(row + 2ull * at));
+    if (past && at + 8 <= width) __builtin_nontemporal_store(v, (FF_GLOBAL u32x4_a2*)(row + 2ull * at));
     else put8(row, at, width, v);
 }
 
@@ -591,27 +604,40 @@ __device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first,
     });
 }
 
-// dH of all pieces and slices, in its place: four elements of a row to a thread.
+// dH of all pieces and slices, in its place: four elements of a row to a thread; of narrow rows the threads that are left over take slices in turn
+// (85 of them, 189 tokens, 120 wide: 13.5 us one behind the other, 5 so).
 constexpr uint32_t kPutThreads = 256, kPutRows = 1 << 16;
 template <bool BF16>
 __global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A)
 {
+    __shared__ f32x4 joined[kPutThreads];
     const uint32_t width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width), used = A.state->used;
-    const uint32_t d = (blockIdx.y * kPutThreads + threadIdx.x) * 4;
-    if (d >= width) return;
+    uint32_t across = kPutThreads;  // threads of a row
+    while (across > kWaveSize / 4 && across * 2 >= width_up) across /= 2;
+    const uint32_t turn = threadIdx.x / across, turns = kPutThreads / across;
+    const uint32_t d = (blockIdx.y * across + threadIdx.x % across) * 4;
     constexpr uint32_t kAhead = 8;
     const uint64_t step = static_cast<uint64_t>(A.tokens_up) * width_up;
     const float scale = A.state->scale;
     for (uint32_t r = blockIdx.x; r < used; r += gridDim.x) {
         const float* const from = A.dh + static_cast<uint64_t>(r) * width_up + d;
         f32x4 s = {0, 0, 0, 0};
-        for (uint32_t k = 0; k < A.slices; k += kAhead) {
-            f32x4 x[kAhead];
-            static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i < A.slices ? k + i : k) * step); });
-            static_for<kAhead>([&](auto i) {
-                if (k + i < A.slices) s += x[int(i)];
-            });
+        if (d < width)
+            for (uint32_t k = turn; k < A.slices; k += kAhead * turns) {
+                f32x4 x[kAhead];
+                static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i * turns < A.slices ? k + i * turns : k) * step); });
+                static_for<kAhead>([&](auto i) {
+                    if (k + i * turns < A.slices) s += x[int(i)];
+                });
+            }
+        if (turns > 1) {
+            __syncthreads();
+            joined[threadIdx.x] = s;
+            __syncthreads();
+            if (turn) continue;
+            for (uint32_t k = 1; k < turns; k++) s += joined[k * across + threadIdx.x];
         }
+        if (d >= width) continue;
         uint8_t* const out = A.dhidden + (A.index[r] * A.dhidden_stride + d) * 2;
         const u32x2 h = to_half<BF16>(s * scale);
         if (d + 4 <= width) {
@@ -647,7 +673,7 @@ __device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first,
         lds, [&](auto i, auto j) { return to_half<BF16>(used ? sum[int(i)][int(j)] * scale : f32x4{0, 0, 0, 0}); },
         [&](uint32_t row, uint32_t column, u32x4 v) {
             if (row0 + row < n && d0 + column < width)
-                put8_past(A.dweight + (static_cast<uint64_t>(first) + row0 + row) * A.dweight_stride * 2, d0 + column, width, v);
+                put8_past(A.past, A.dweight + (static_cast<uint64_t>(first) + row0 + row) * A.dweight_stride * 2, d0 + column, width, v);
         });
 }
 
@@ -695,7 +721,7 @@ __global__ __launch_bounds__(kFewWaves* kWaveSize) void head_few_dweight_kernel(
                 buffer + H::kBytes, [&](auto, auto j) { return to_half<BF16>(used ? sum[int(j)] * scale : f32x4{0, 0, 0, 0}); },
                 [&](uint32_t row, uint32_t column, u32x4 x) {
                     const uint32_t d = chunk * 256 + 64 * q + column;
-                    if (v0 + row < n && d < width) put8_past(A.dweight + (static_cast<uint64_t>(first) + v0 + row) * A.dweight_stride * 2, d, width, x);
+                    if (v0 + row < n && d < width) put8_past(A.past, A.dweight + (static_cast<uint64_t>(first) + v0 + row) * A.dweight_stride * 2, d, width, x);
                 });
         });
     }
@@ -728,11 +754,13 @@ bool weight_as_it_is(const ff_head_batch& b)
 }
 
 bool few(const ff_head_batch& b) { return b.n_tokens <= kFewTokens; }
-// Is it better to keep the logits of the last piece than to make them again?  Eight bytes of memory to and fro stand against 2 * width operations: equal at a
-// width of about 1000.
-bool keeps(const ff_head_batch& b) { return few(b) || b.width >= 1024; }
-// Do the logits come from head_stream_kernel?
-bool streams(const ff_head_batch& b) { return b.n_tokens <= 16 || (few(b) && !weight_as_it_is(b)); }
+// Is it better to keep the logits of the last piece than to make them again?  Eight bytes of memory to and fro stand against 2 * width
+// operations: equal at a width of about 1000.  (Us, kept / made again: 1492 tokens on 34,257 x 1016 452 / 478, 4096 on 32,000 x 512 654 / 597, 2870 on 109,803 x
+// 128 1115 / 823.)  Up to kKeptElements lie in the caches, and a launch is saved: 374 on 1922 x 185 42 / 48.
+constexpr uint64_t kKeptElements = 1 << 22;
+bool keeps(const ff_head_batch& b) { return few(b) || b.width >= 1024 || b.n_tokens * b.vocab <= kKeptElements; }
+// Do the logits come from head_stream_kernel?  (Figures there.)
+bool streams(const ff_head_batch& b, bool grad) { return weight_as_it_is(b) ? b.n_tokens <= 16 : !grad && b.n_tokens <= 32; }
 // Tiles 256 tokens high, or 64: a round of the latter takes two thirds as long.  (Us, 256 / 64: scoring 256, 300, 512 tokens on 32,000 x 4096 121, 126, 129 / 162, 220,
 // 287; 128 tokens 119 / 101.)
 bool high_tiles(const ff_head_batch& b)
@@ -742,7 +770,7 @@ bool high_tiles(const ff_head_batch& b)
 }
 uint32_t up64(uint64_t n) { return static_cast<uint32_t>(up(std::max<uint64_t>(n, 1), 64)); }
 // Vocabulary entries that a workgroup of head_stream_kernel takes.
-uint32_t stream_entries(uint64_t n_tokens) { return n_tokens <= 16 ? Stream<1>::kEntries : n_tokens <= 32 ? Stream<2>::kEntries : Stream<4>::kEntries; }
+uint32_t stream_entries(uint64_t n_tokens) { return n_tokens <= 16 ? Stream<1>::kEntries : Stream<2>::kEntries; }
 
 struct Places {
     uint64_t state, index, weights, targets, rows, losses, picked, parts, hidden, weight, grad, logits, dh, bytes;
@@ -751,7 +779,7 @@ struct Places {
 Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
 {
     const uint64_t n = b.n_tokens, width_up = up(b.width, kStepK);
-    const uint32_t high = high_tiles(b) ? kTile : 64, tile = streams(b) ? stream_entries(n) : kTile;
+    const uint32_t high = high_tiles(b) ? kTile : 64, tile = streams(b, grad) ? stream_entries(n) : kTile;
     A->tokens_up = static_cast<uint32_t>(up(std::max<uint64_t>(n, 1), high));
     A->tiles = static_cast<uint32_t>((b.vocab + tile - 1) / tile);
     A->stride = static_cast<uint32_t>(width_up * 2);
@@ -784,13 +812,15 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     p.picked = take(n * 4);
     // (never less for more tokens, entries or elements, whatever tiles and pieces come to)
     p.parts = take(std::max(n * (whole / kTile), std::min<uint64_t>(n, 32) * (whole / 64)) * sizeof(float2));
-    p.hidden = take(static_cast<uint64_t>(A->tokens_up) * A->stride);
-    auto piece_of = [&](uint64_t rows) { return std::max(std::min(rows * whole, kPieceElements), rows * kTile) * 2; };
-    p.weight = take(packed && (grad || !streams(b)) ? piece_of(width_up) : 0);
+    const uint64_t rows = few(b) ? kFewTokens : up(n, kTile);
+    p.hidden = take(rows * A->stride);
+    auto piece_of = [&](uint64_t r) { return std::max(std::min(r * whole, kPieceElements), r * kTile) * 2; };
+    p.weight = take(packed && (grad || !streams(b, grad)) ? piece_of(width_up) : 0);
     if (grad) {
-        p.grad = take(piece_of(A->tokens_up));
-        p.logits = take(2 * (keeps(b) ? piece_of(A->tokens_up) : kFewTokens * whole * 2));
-        const uint64_t dh = A->tokens_up * width_up;
+        const uint64_t all = piece_of(rows), smaller = std::max(kFewTokens * whole, kKeptElements + kTile * (rows + whole + kTile)) * 4;
+        p.grad = take(all);
+        p.logits = take(keeps(b) ? 2 * all : std::min(2 * all, smaller));
+        const uint64_t dh = rows * width_up;
         p.dh = take(std::max(dh, std::min<uint64_t>(dh * (whole / kTile), kComputeUnits * kTile * kTile)) * 4);
     }
     p.bytes = at;
@@ -802,36 +832,36 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
 {
     const uint32_t n = static_cast<uint32_t>(A.b.n_tokens), vocab = static_cast<uint32_t>(A.b.vocab), tiles_m = A.tokens_up / BM;
     const uint32_t tiles_d = (A.stride / 2 + kTile - 1) / kTile;
-    if (n <= kSelectFew) {
-        hipLaunchKernelGGL(head_few_kernel, dim3(up64(n)), dim3(256), 0, stream, A);
-    } else {
-        hipLaunchKernelGGL(head_select_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
-        hipLaunchKernelGGL(head_gather_kernel, dim3(std::min(A.tokens_up, 4096u)), dim3(256), 0, stream, A);
-    }
     const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.step - 1) / A.step);
     const bool grad = A.dhidden || A.dweight, keep = grad && keeps(A.b), whole = few(A.b);
     const bool few_dweight = whole && static_cast<uint64_t>(vocab) * A.b.width >= kFewDweightFrom;
     uint32_t first = 0, m = 0, tiles = 0, packed = ~0u;
+    if (n <= kSelectFew) {
+        const uint32_t rows = A.weight && !streams(A.b, grad) ? std::min(A.step, vocab) : 0, blocks = up64(n);
+        hipLaunchKernelGGL(head_few_kernel, dim3(blocks + std::min(rows, kPackBlocks)), dim3(256), 0, stream, A, blocks, rows);
+        if (rows) packed = 0;
+    } else {
+        hipLaunchKernelGGL(head_select_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
+        hipLaunchKernelGGL(head_gather_kernel, dim3(std::min(A.tokens_up, 4096u)), dim3(256), 0, stream, A);
+    }
     // makes piece i the one that the following launches are for
     auto take = [&](uint32_t i, bool rows) {
         first = i * A.step;
         m = std::min(A.step, vocab - first);
         tiles = (m + kTile - 1) / kTile;
         if (!A.weight || !rows || packed == i) return;
-        hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, 8192u)), dim3(256), 0, stream, A, first, m);
+        hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, kPackBlocks)), dim3(256), 0, stream, A, first, m);
         packed = i;
     };
     const dim3 threads(kProductThreads);
-    if (streams(A.b)) {
-        const auto kernel = n <= 16   ? (grad ? head_stream_kernel<BF16, 1, kKeep> : head_stream_kernel<BF16, 1, kSums>)
-                            : n <= 32 ? (grad ? head_stream_kernel<BF16, 2, kKeep> : head_stream_kernel<BF16, 2, kSums>)
-                                      : (grad ? head_stream_kernel<BF16, 4, kKeep> : head_stream_kernel<BF16, 4, kSums>);
+    if (streams(A.b, grad)) {
+        const auto kernel = grad ? head_stream_kernel<BF16, 1, kKeep> : n <= 16 ? head_stream_kernel<BF16, 1, kSums> : head_stream_kernel<BF16, 2, kSums>;
         hipLaunchKernelGGL(kernel, dim3(A.tiles), dim3(kStreamThreads), 0, stream, A);
     } else {
         for (uint32_t i = 0; i < n_pieces; i++) {
             take(i, true);
             const dim3 grid(tiles * tiles_m);
-            if (keep && i == n_pieces - 1) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kKeep>), grid, threads, 0, stream, A, first, m);
+            if (keep && (whole || i == n_pieces - 1)) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kKeep>), grid, threads, 0, stream, A, first, m);
             else hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kSums>), grid, threads, 0, stream, A, first, m);
         }
     }
@@ -842,7 +872,7 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
     } else {
         hipLaunchKernelGGL(head_finish_kernel<BF16>, dim3(n / 4 + 1), dim3(256), 0, stream, A);
     }
-    if (n > kFewTokens) hipLaunchKernelGGL(head_sum_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
+    if (n > kCountFew) hipLaunchKernelGGL(head_sum_kernel, dim3(1), dim3(kSelectThreads), 0, stream, A);
     if (!grad) return hipGetLastError();
     const Sum start = n_pieces == 1 && A.slices == 1 ? kOnly : kFirst;
     for (uint32_t i = n_pieces; i-- > 0;) {  // from the last one, whose logits and packed rows are at hand
@@ -904,6 +934,7 @@ hipError_t launch_head(const ff_head_batch& b, float* logp, void* dhidden, uint6
     A.logits = reinterpret_cast<float*>(w + p.logits);
     A.dh = reinterpret_cast<float*>(w + p.dh);
     A.grad_scale = b.loss_scale * (b.dtype == FF_BF16 ? 1.f : 0x1p-14f);
+    A.past = reinterpret_cast<uint64_t>(dweight) % 16 == 0 && dweight_stride % 8 == 0;
     const bool high = high_tiles(b);
     if (b.dtype == FF_BF16) return high ? launch<true, 256>(A, stream) : launch<true, 64>(A, stream);
     return high ? launch<false, 256>(A, stream) : launch<false, 64>(A, stream);
