@@ -78,6 +78,7 @@ struct HeadArgs {
     uint32_t piece;     // vocabulary entries that G has, a multiple of 256
     uint32_t step;      // and that the gradients' products take at once
     uint32_t slices;    // of dH's sum over a piece
+    uint32_t splits;    // of the logits' sums, of few tiles
     float grad_scale;   // loss scale, and what G is too large by
     uint32_t past;      // dW's rows are whole pieces of 16 bytes
 };
@@ -267,7 +268,8 @@ __device__ __forceinline__ float2 join_parts(const float2 (&p)[N])
 }
 
 // The tiles of vocabulary entries [first, first + n): their parts of the sums, with kKeep the logits as well; or G.
-enum Mode { kSums, kKeep, kGrad };
+// kSplit: nothing but a slice of their sums.
+enum Mode { kSums, kKeep, kGrad, kSplit };
 template <bool BF16, int BM, Mode MODE>
 __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu(2))) void head_logits_kernel(const HeadArgs A, const uint32_t first,
                                                                                                              const uint32_t n)
@@ -276,7 +278,8 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kProductLds<BM, kAlongK, kAlongK>];
     const uint32_t used = A.state->used;
     uint32_t m0, n0;
-    tile_at(xcd_order(blockIdx.x, gridDim.x, kXcdTiles), A.tokens_up / BM, (n + kTile - 1) / kTile, &m0, &n0);
+    const uint32_t tiles = gridDim.x / (MODE == kSplit ? A.splits : 1), slice = MODE == kSplit ? blockIdx.x / tiles : 0;
+    tile_at(xcd_order(blockIdx.x - slice * tiles, tiles, kXcdTiles), A.tokens_up / BM, (n + kTile - 1) / kTile, &m0, &n0);
     m0 *= BM;
     n0 *= kTile;
     if (m0 >= used) return;
@@ -285,13 +288,21 @@ __global__ __launch_bounds__(kProductThreads) __attribute__((amdgpu_waves_per_eu
     b.base = weight_row(A, first, v0, &b.stride);
     b.valid = n - n0;
     b.k_valid = A.weight ? A.stride / 2 : static_cast<uint32_t>(A.b.width);
-    const uint32_t steps = A.stride / (2 * kStepK);
+    const uint32_t steps = A.stride / (2 * kStepK), from = MODE == kSplit ? steps * slice / A.splits : 0;
     f32x4 z[S::kM][S::kN];
-    product<BF16, BM, kAlongK, kAlongK>(hidden_tile(A, m0, used), b, 0, steps, b.k_valid % kStepK ? steps - 1 : ~0u, (FF_LDS uint8_t*)lds, z);
+    product<BF16, BM, kAlongK, kAlongK>(hidden_tile(A, m0, used), b, from, MODE == kSplit ? steps * (slice + 1) / A.splits : steps, b.k_valid % kStepK ? steps - 1 : ~0u, (FF_LDS uint8_t*)lds, z);
     const int wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
     const uint32_t m = m0 + (wave / S::kAcross) * (16 * S::kM) + lane % 16;                    // + 16 i
     const uint32_t v = v0 + (wave % S::kAcross) * (16 * S::kN) + 4 * (lane / 16);              // + 16 j + e
-    if constexpr (MODE == kGrad) {
+    if constexpr (MODE == kSplit) {
+        static_for<S::kM>([&](auto i) {
+            const uint32_t t = m + 16 * i;
+            float* const out = A.logits + (static_cast<uint64_t>(slice) * A.tokens_up + t) * A.piece + v;
+            static_for<S::kN>([&](auto j) {
+                if (t < used) *(FF_GLOBAL f32x4*)(out + 16 * j) = z[int(i)][int(j)];
+            });
+        });
+    } else if constexpr (MODE == kGrad) {
         const uint32_t row0 = m - lane % 16, at = v - 4 * (lane / 16) - first;
         Row rows[S::kM];
         static_for<S::kM>([&](auto i) {
@@ -423,33 +434,14 @@ __device__ __forceinline__ void put_stats(const HeadArgs& A, double loss, const 
 }
 
 constexpr uint32_t kCountFew = 256;
-// A wavefront joins the tiles' parts of row r, in 64 bits from the exponentials on.  The one that writes leaves the results; of few rows
+// What is known of row r from its sum of exponentials `total` against c and its target's logit.  The wavefront that writes leaves the results; of few rows
 // (kCountFew: they count one another at one address, 10 ns each) the last one to do so adds their losses up, of others a launch.
 template <bool BF16>
-__device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const uint32_t used, const bool writes)
+__device__ __forceinline__ Row outcome(const HeadArgs& A, const uint32_t r, const uint32_t used, const float c, const double total, const float picked, const bool writes)
 {
     const uint32_t lane = threadIdx.x % kWaveSize;
-    const float2* const parts = A.parts + static_cast<uint64_t>(r) * A.tiles;
-    // fn(part), several on their way at once
-    auto each_part = [&](auto&& fn) {
-        constexpr uint32_t kAhead = 8;
-        for (uint32_t k = lane; k < A.tiles; k += kAhead * kWaveSize) {
-            float2 p[kAhead];
-            static_for<kAhead>([&](auto i) { p[int(i)] = k + i * kWaveSize < A.tiles ? parts[k + i * kWaveSize] : float2{-INFINITY, 0.f}; });
-            static_for<kAhead>([&](auto i) { fn(p[int(i)]); });
-        }
-    };
-    float c = -INFINITY;
-    each_part([&](float2 p) { c = fmaxf(c, p.x); });
-    for (int d = 32; d; d /= 2) c = fmaxf(c, __shfl_xor(c, d));
-    if (c == -INFINITY) c = 0.f;
-    double total = 0;
-    each_part([&](float2 p) {
-        if (p.y != 0.f) total += static_cast<double>(p.y) * exp2(static_cast<double>(p.x) - static_cast<double>(c));
-    });
-    for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
     const double against = static_cast<double>(c) / static_cast<double>(kLog2E), rest = log(total);
-    const double logp = (static_cast<double>(A.picked[r]) - against) - rest;
+    const double logp = (static_cast<double>(picked) - against) - rest;
     const float w = A.weights[r], f = w / A.state->largest * (BF16 ? 1.f : 0x1p14f);
     const Row row = {static_cast<float>((against + rest) * 1.4426950408889634), f, f * static_cast<float>(expm1(logp)), A.targets[r]};
     if (writes && lane == 0) {
@@ -473,6 +465,33 @@ __device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const
         }
     }
     return row;
+}
+
+// A wavefront joins the tiles' parts of row r, in 64 bits from the exponentials on.
+template <bool BF16>
+__device__ __forceinline__ Row finish(const HeadArgs& A, const uint32_t r, const uint32_t used, const bool writes)
+{
+    const uint32_t lane = threadIdx.x % kWaveSize;
+    const float2* const parts = A.parts + static_cast<uint64_t>(r) * A.tiles;
+    // fn(part), several on their way at once
+    auto each_part = [&](auto&& fn) {
+        constexpr uint32_t kAhead = 8;
+        for (uint32_t k = lane; k < A.tiles; k += kAhead * kWaveSize) {
+            float2 p[kAhead];
+            static_for<kAhead>([&](auto i) { p[int(i)] = k + i * kWaveSize < A.tiles ? parts[k + i * kWaveSize] : float2{-INFINITY, 0.f}; });
+            static_for<kAhead>([&](auto i) { fn(p[int(i)]); });
+        }
+    };
+    float c = -INFINITY;
+    each_part([&](float2 p) { c = fmaxf(c, p.x); });
+    for (int d = 32; d; d /= 2) c = fmaxf(c, __shfl_xor(c, d));
+    if (c == -INFINITY) c = 0.f;
+    double total = 0;
+    each_part([&](float2 p) {
+        if (p.y != 0.f) total += static_cast<double>(p.y) * exp2(static_cast<double>(p.x) - static_cast<double>(c));
+    });
+    for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
+    return outcome<BF16>(A, r, used, c, total, A.picked[r], writes);
 }
 
 // A wavefront to a row.
@@ -512,6 +531,75 @@ __global__ __launch_bounds__(256) void head_kept_kernel(const HeadArgs A, const 
         }
         *(FF_GLOBAL u32x4*)(A.grad + (static_cast<uint64_t>(t) * A.piece + at) * 2) = out;
     }
+}
+
+// Both, and the sums of the logits' slices before, for a row of few tiles: a workgroup.  A thread's elements are its own from one pass to the next.  What bounds
+// it: three passes over the caches, one behind the other.
+template <bool BF16>
+__global__ __launch_bounds__(256) void head_row_kernel(const HeadArgs A, const bool grad)
+{
+    __shared__ float top[256 / kWaveSize], target;
+    __shared__ double sum[256 / kWaveSize];
+    __shared__ Row row;
+    const uint32_t used = A.state->used, vocab = static_cast<uint32_t>(A.b.vocab), t = blockIdx.x, wave = threadIdx.x / kWaveSize, lane = threadIdx.x % kWaveSize;
+    if (used == 0 && t == 0 && threadIdx.x == 0) put_stats(A, 0.0, 0);
+    if (t >= (grad ? (used + 63) / 64 * 64 : used)) return;
+    float* const z = A.logits + static_cast<uint64_t>(t) * A.piece;
+    auto each = [&](auto&& fn) {
+        for (uint32_t v = threadIdx.x * 4; v < A.piece; v += 256 * 4) fn(v);
+    };
+    if (t < used) {
+        const uint64_t step = static_cast<uint64_t>(A.tokens_up) * A.piece;
+        const uint32_t y = static_cast<uint32_t>(A.targets[t]);
+        float most = -INFINITY;
+        each([&](uint32_t v) {
+            constexpr uint32_t kAhead = 8;
+            f32x4 s = {0, 0, 0, 0};
+            for (uint32_t k = 0; k < A.splits; k += kAhead) {
+                f32x4 x[kAhead];
+                static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(z + v + (k + i < A.splits ? k + i : k) * step); });
+                static_for<kAhead>([&](auto i) {
+                    if (k + i < A.splits) s += x[int(i)];
+                });
+            }
+            for (int e = 0; e < 4; e++) {
+                if (v + e == y) target = s[e];
+                s[e] = v + e < vocab ? s[e] : -INFINITY;
+                most = fmaxf(most, s[e]);
+            }
+            *(FF_GLOBAL f32x4*)(z + v) = s;
+        });
+        for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
+        if (lane == 0) top[wave] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float c = most == -INFINITY ? 0.f : most * kLog2E;
+        double total = 0;
+        each([&](uint32_t v) {
+            const f32x4 x = *(const FF_GLOBAL f32x4*)(z + v);
+            float s = 0;
+            for (int e = 0; e < 4; e++) s += __builtin_amdgcn_exp2f(fmaf(x[e], kLog2E, -c));
+            total += static_cast<double>(s);
+        });
+        for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
+        if (lane == 0) sum[wave] = total;
+        __syncthreads();
+        if (wave == 0) {
+            const Row known = outcome<BF16>(A, t, used, c, (sum[0] + sum[1]) + (sum[2] + sum[3]), target, true);
+            if (lane == 0) row = known;
+        }
+        if (!grad) return;
+        __syncthreads();
+    }
+    const Row r = row;
+    each([&](uint32_t v) {
+        f32x4 g = {0, 0, 0, 0};
+        if (t < used) {
+            g = *(const FF_GLOBAL f32x4*)(z + v);
+            for (int e = 0; e < 4; e++) g[e] = gradient(g[e], v + e, vocab, r);
+        }
+        *(FF_GLOBAL u32x2*)(A.grad + (static_cast<uint64_t>(t) * A.piece + v) * 2) = to_half<BF16>(g);
+    });
 }
 
 // The loss of many rows.
@@ -796,6 +884,13 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     // dH's sum over a piece in so many slices that its tiles fill the chip, of four steps at least
     const uint64_t dh_tiles = A->tokens_up / high * (up(width_up, kTile) / kTile), steps = (step + kStepK - 1) / kStepK;
     A->slices = static_cast<uint32_t>(std::max<uint64_t>(std::min(kComputeUnits / dh_tiles, steps / 4), 1));
+    // The logits' sums in so many slices that their tiles fill the chip, of four steps at least, where that saves more than a row's workgroup takes:
+    // a step, 0.9 us, for every 512 entries.  (Us, without / with: 21 tokens on 1240 x 8128 126 / 50, 256 on 256 x 4096 73 / 36, 64 on 8000 x 4096, scored,
+    // 61 / 41; 120 on 9023 x 768 would take 58 instead of 52.)
+    const uint64_t z_tiles = A->tokens_up / high * (whole / kTile), z_steps = width_up / kStepK;
+    uint64_t splits = high == 64 && !streams(b, grad) && step >= b.vocab ? std::max<uint64_t>(std::min(kComputeUnits / z_tiles, z_steps / 4), 1) : 1;
+    if ((z_steps - z_steps / splits) * 512 < b.vocab) splits = 1;
+    A->splits = static_cast<uint32_t>(splits);
     Places p = {};
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
@@ -816,10 +911,12 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     p.hidden = take(rows * A->stride);
     auto piece_of = [&](uint64_t r) { return std::max(std::min(r * whole, kPieceElements), r * kTile) * 2; };
     p.weight = take(packed && (grad || !streams(b, grad)) ? piece_of(width_up) : 0);
+    const uint64_t split = std::min<uint64_t>(rows * whole * z_steps, kComputeUnits * 64 * kTile) * 4;  // of any slices
+    if (!grad) p.logits = take(split);
     if (grad) {
         const uint64_t all = piece_of(rows), smaller = std::max(kFewTokens * whole, kKeptElements + kTile * (rows + whole + kTile)) * 4;
         p.grad = take(all);
-        p.logits = take(keeps(b) ? 2 * all : std::min(2 * all, smaller));
+        p.logits = take(std::max(split, keeps(b) ? 2 * all : std::min(2 * all, smaller)));
         const uint64_t dh = rows * width_up;
         p.dh = take(std::max(dh, std::min<uint64_t>(dh * (whole / kTile), kComputeUnits * kTile * kTile)) * 4);
     }
@@ -833,7 +930,7 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
     const uint32_t n = static_cast<uint32_t>(A.b.n_tokens), vocab = static_cast<uint32_t>(A.b.vocab), tiles_m = A.tokens_up / BM;
     const uint32_t tiles_d = (A.stride / 2 + kTile - 1) / kTile;
     const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.step - 1) / A.step);
-    const bool grad = A.dhidden || A.dweight, keep = grad && keeps(A.b), whole = few(A.b);
+    const bool grad = A.dhidden || A.dweight, keep = grad && (A.splits > 1 || keeps(A.b)), whole = few(A.b);
     const bool few_dweight = whole && static_cast<uint64_t>(vocab) * A.b.width >= kFewDweightFrom;
     uint32_t first = 0, m = 0, tiles = 0, packed = ~0u;
     if (n <= kSelectFew) {
@@ -854,7 +951,10 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
         packed = i;
     };
     const dim3 threads(kProductThreads);
-    if (streams(A.b, grad)) {
+    if (A.splits > 1) {
+        take(0, true);
+        if constexpr (BM == 64) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kSplit>), dim3(tiles * tiles_m * A.splits), threads, 0, stream, A, first, m);
+    } else if (streams(A.b, grad)) {
         const auto kernel = grad ? head_stream_kernel<BF16, 1, kKeep> : n <= 16 ? head_stream_kernel<BF16, 1, kSums> : head_stream_kernel<BF16, 2, kSums>;
         hipLaunchKernelGGL(kernel, dim3(A.tiles), dim3(kStreamThreads), 0, stream, A);
     } else {
@@ -865,7 +965,9 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
             else hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kSums>), grid, threads, 0, stream, A, first, m);
         }
     }
-    if (keep) {
+    if (A.splits > 1) {
+        hipLaunchKernelGGL(head_row_kernel<BF16>, dim3(up64(n)), dim3(256), 0, stream, A, grad);
+    } else if (keep) {
         const uint32_t from = whole ? 0 : first, of = vocab - from, rows = up64(n);
         const uint32_t wide = std::min((of + 2047) / 2048, (kKeptBlocks + rows - 1) / rows);
         hipLaunchKernelGGL(head_kept_kernel<BF16>, dim3(rows * wide), dim3(256), 0, stream, A, from, of, wide);

@@ -374,3 +374,40 @@ def test_head_in_several_pieces_of_the_vocabulary(dtype, n, vocab, width, pad, f
     args = head_inputs(n, vocab, width, dtype, pad, first, masked=0.1)
     scale = 1024.0 if dtype == F16 else 1.0
     check_head(run_head(*args, scale, pad=pad, first=first), modelref.head(*args, scale))
+
+
+FEW_TILES = [(21, 1240, 8128, 0, 0), (130, 700, 4096, 8, 0), (300, 256, 2000, 3, 1), (1500, 300, 1100, 0, 0), (2, 1689, 2578, 0, 0), (64, 4099, 2056, 0, 3), (17, 1, 1024, 0, 0)]
+
+
+@HALVES
+@pytest.mark.parametrize("n,vocab,width,pad,first", FEW_TILES)
+def test_head_of_few_tiles_and_long_sums(dtype, n, vocab, width, pad, first):
+    """The logits' sums in slices; with gradients and scored, masks that leave no token in."""
+    args = head_inputs(n, vocab, width, dtype, pad, first, masked=0.2)
+    scale = 1024.0 if dtype == F16 else 1.0
+    want = modelref.head(*args, scale)
+    both = run_head(*args, scale, pad=pad, first=first)
+    check_head(both, want)
+    scored = run_head(*args, scale, dh=False, dw=False)
+    modelref.check(scored["logp"], want["logp"], want["tol_logp"], "logp")
+    modelref.check(scored["stats"].loss, want["loss"], want["tol_loss"], "loss")
+    again = run_head(*args, scale, pad=pad, first=first)
+    assert all(torch.equal(both[k], again[k]) for k in ("logp", "dhidden", "dweight"))
+    args[3].zero_()
+    for grad in (True, False):
+        got = run_head(*args, scale, dh=grad, dw=grad)
+        assert bool((got["logp"] == 0).all()) and got["stats"].words.tolist() == [0, 0, 0]
+        assert not grad or bool((got["dhidden"] == 0).all() and (got["dweight"] == 0).all())
+
+
+def test_head_of_few_tiles_with_a_logit_that_is_not_finite_and_large_ones():
+    hidden, weight, targets, weights = head_inputs(40, 600, 2048, BF16)
+    hidden[5, 0] = INF
+    hidden[6] = weight[targets[6]] * 200.0
+    hidden[7] = weight[targets[7]] * -200.0
+    clean = torch.arange(40, device=DEV) != 5
+    got = run_head(hidden, weight, targets, weights)
+    assert bool(torch.isnan(got["logp"][5])) and not bool(torch.isfinite(got["dhidden"][5]).any()) and math.isnan(float(got["stats"].loss))
+    want = modelref.head(hidden[clean], weight, targets[clean], weights[clean])
+    for name in ("logp", "dhidden"):
+        modelref.check(got[name][clean], want[name], want["tol_" + name], name)

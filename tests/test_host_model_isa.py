@@ -45,7 +45,7 @@ def test_nothing_is_kept_in_scratch_memory(kernels):
 
 def test_products_leave_room_for_two_wavefronts_on_a_simd_and_their_tiles_in_lds(kernels):
     found = {k: v for k, v in kernels.items() if re.search(r"head_(logits|grads)_kernel", k)}
-    assert len(found) == 16
+    assert len(found) == 18
     for k, v in found.items():
         assert v["vgpr_count"] <= 256 and v["group_segment_fixed_size"] <= 160 * 1024, (k, v)
         if re.search(r"logits_kernelILb\dELi64E", k):  # two workgroups on a compute unit
