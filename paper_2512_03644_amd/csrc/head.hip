@@ -79,6 +79,8 @@ struct HeadArgs {
     uint32_t step;      // and that the gradients' products take at once
     uint32_t slices;    // of dH's sum over a piece
     uint32_t splits;    // of the logits' sums, of few tiles
+    float* dw;          // [slice][piece][width up to 64]: dW so far, of few tiles
+    uint32_t dw_slices; // of dW's sum over the tokens
     float grad_scale;   // loss scale, and what G is too large by
     uint32_t past;      // dW's rows are whole pieces of 16 bytes
 };
@@ -692,42 +694,49 @@ __device__ __forceinline__ void dhidden(const HeadArgs& A, const uint32_t first,
     });
 }
 
-// dH of all pieces and slices, in its place: four elements of a row to a thread; of narrow rows the threads that are left over take slices in turn
-// (85 of them, 189 tokens, 120 wide: 13.5 us one behind the other, 5 so).
+// Sums of slices, rounded, in their place: four elements of a row to a thread; of narrow rows the threads that are left over take slices in turn
+// (85 of them, dH of 189 tokens, 120 wide: 13.5 us one behind the other, 5 so).
 constexpr uint32_t kPutThreads = 256, kPutRows = 1 << 16;
+struct Slices {
+    const float* from;
+    uint64_t step;  // elements from one slice to the next
+    uint32_t count, rows;
+    uint8_t* out;
+    uint64_t stride;  // elements
+    const uint32_t* index;  // of the rows in their place, or null
+};
 template <bool BF16>
-__global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A)
+__device__ __forceinline__ void put_rows(const HeadArgs& A, const Slices& s, const uint32_t block, const uint32_t blocks)
 {
     __shared__ f32x4 joined[kPutThreads];
-    const uint32_t width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width), used = A.state->used;
+    const uint32_t width_up = A.stride / 2, width = static_cast<uint32_t>(A.b.width);
     uint32_t across = kPutThreads;  // threads of a row
     while (across > kWaveSize / 4 && across * 2 >= width_up) across /= 2;
     const uint32_t turn = threadIdx.x / across, turns = kPutThreads / across;
     const uint32_t d = (blockIdx.y * across + threadIdx.x % across) * 4;
     constexpr uint32_t kAhead = 8;
-    const uint64_t step = static_cast<uint64_t>(A.tokens_up) * width_up;
     const float scale = A.state->scale;
-    for (uint32_t r = blockIdx.x; r < used; r += gridDim.x) {
-        const float* const from = A.dh + static_cast<uint64_t>(r) * width_up + d;
-        f32x4 s = {0, 0, 0, 0};
+    for (uint32_t r = block; r < s.rows; r += blocks) {
+        const float* const from = s.from + static_cast<uint64_t>(r) * width_up + d;
+        f32x4 sum = {0, 0, 0, 0};
         if (d < width)
-            for (uint32_t k = turn; k < A.slices; k += kAhead * turns) {
+            for (uint32_t k = turn; k < s.count; k += kAhead * turns) {
                 f32x4 x[kAhead];
-                static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i * turns < A.slices ? k + i * turns : k) * step); });
+                static_for<kAhead>([&](auto i) { x[int(i)] = *(const FF_GLOBAL f32x4*)(from + (k + i * turns < s.count ? k + i * turns : k) * s.step); });
                 static_for<kAhead>([&](auto i) {
-                    if (k + i * turns < A.slices) s += x[int(i)];
+                    if (k + i * turns < s.count) sum += x[int(i)];
                 });
             }
         if (turns > 1) {
             __syncthreads();
-            joined[threadIdx.x] = s;
+            joined[threadIdx.x] = sum;
             __syncthreads();
             if (turn) continue;
-            for (uint32_t k = 1; k < turns; k++) s += joined[k * across + threadIdx.x];
+            for (uint32_t k = 1; k < turns; k++) sum += joined[k * across + threadIdx.x];
         }
         if (d >= width) continue;
-        uint8_t* const out = A.dhidden + (A.index[r] * A.dhidden_stride + d) * 2;
-        const u32x2 h = to_half<BF16>(s * scale);
+        uint8_t* const out = s.out + ((s.index ? s.index[r] : r) * s.stride + d) * 2;
+        const u32x2 h = to_half<BF16>(sum * scale);
         if (d + 4 <= width) {
             *(FF_GLOBAL u32x2_a2*)out = h;
         } else {
@@ -737,6 +746,16 @@ __global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A)
         }
     }
 }
+// dH of all pieces and slices by the first `dh_blocks` workgroups, dW by the others.
+template <bool BF16>
+__global__ __launch_bounds__(kPutThreads) void head_put_kernel(const HeadArgs A, const uint32_t dh_blocks)
+{
+    const uint32_t width_up = A.stride / 2;
+    const bool dh = blockIdx.x < dh_blocks;
+    const Slices s = dh ? Slices{A.dh, static_cast<uint64_t>(A.tokens_up) * width_up, A.slices, A.state->used, A.dhidden, A.dhidden_stride, A.index}
+                        : Slices{A.dw, static_cast<uint64_t>(A.piece) * width_up, A.dw_slices, static_cast<uint32_t>(A.b.vocab), A.dweight, A.dweight_stride, nullptr};
+    put_rows<BF16>(A, s, dh ? blockIdx.x : blockIdx.x - dh_blocks, dh ? dh_blocks : gridDim.x - dh_blocks);
+}
 
 // dW = G^T H of vocabulary entries [first, first + n).
 template <bool BF16>
@@ -744,19 +763,31 @@ __device__ __forceinline__ void dweight(const HeadArgs& A, const uint32_t first,
                                         FF_LDS uint8_t* lds)
 {
     using S = Share<256>;
-    const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width);
+    const uint32_t used = A.state->used, width = static_cast<uint32_t>(A.b.width), width_up = A.stride / 2;
+    const uint32_t tiles = blocks / A.dw_slices, slice = block / tiles;
     uint32_t m0, n0;
-    tile_at(xcd_order(block, blocks, kXcdTiles), (n + kTile - 1) / kTile, (A.stride / 2 + kTile - 1) / kTile, &m0, &n0);
+    tile_at(xcd_order(block - slice * tiles, tiles, kXcdTiles), (n + kTile - 1) / kTile, (width_up + kTile - 1) / kTile, &m0, &n0);
     m0 *= kTile;
     n0 *= kTile;
     const uint32_t steps = (used + kStepK - 1) / kStepK;
     const OperandTile a = {A.grad + (static_cast<uint64_t>(column) + m0) * 2, static_cast<uint64_t>(A.piece) * 2, A.piece - column - m0, A.tokens_up};
     const OperandTile b = {A.hidden + n0 * 2, A.stride, A.stride / 2 - n0, A.tokens_up};
     f32x4 sum[S::kM][S::kN];
-    product<BF16, 256, kAcrossK, kAcrossK>(a, b, 0, steps, ~0u, lds, sum);
+    product<BF16, 256, kAcrossK, kAcrossK>(a, b, steps * slice / A.dw_slices, steps * (slice + 1) / A.dw_slices, ~0u, lds, sum);
     const float scale = A.state->scale;
     const int wave = threadIdx.x / kWaveSize;
     const uint32_t row0 = m0 + (wave / S::kAcross) * (16 * S::kM), d0 = n0 + (wave % S::kAcross) * (16 * S::kN);
+    if (A.dw_slices > 1) {
+        const uint32_t lane = threadIdx.x % kWaveSize;
+        static_for<S::kM>([&](auto i) {
+            const uint32_t row = row0 + 16 * i + lane % 16, d = d0 + lane / 16 * 4;
+            float* const out = A.dw + (static_cast<uint64_t>(slice) * A.piece + row) * width_up + d;
+            static_for<S::kN>([&](auto j) {
+                if (row < n && d + 16 * j < width_up) *(FF_GLOBAL f32x4*)(out + 16 * j) = sum[int(i)][int(j)];
+            });
+        });
+        return;
+    }
     RowsByLds<S::kM, S::kN>::pass(
         lds, [&](auto i, auto j) { return to_half<BF16>(used ? sum[int(i)][int(j)] * scale : f32x4{0, 0, 0, 0}); },
         [&](uint32_t row, uint32_t column, u32x4 v) {
@@ -861,7 +892,7 @@ uint32_t up64(uint64_t n) { return static_cast<uint32_t>(up(std::max<uint64_t>(n
 uint32_t stream_entries(uint64_t n_tokens) { return n_tokens <= 16 ? Stream<1>::kEntries : Stream<2>::kEntries; }
 
 struct Places {
-    uint64_t state, index, weights, targets, rows, losses, picked, parts, hidden, weight, grad, logits, dh, bytes;
+    uint64_t state, index, weights, targets, rows, losses, picked, parts, hidden, weight, grad, logits, dh, dw, bytes;
 };
 
 Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
@@ -891,6 +922,12 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
     uint64_t splits = high == 64 && !streams(b, grad) && step >= b.vocab ? std::max<uint64_t>(std::min(kComputeUnits / z_tiles, z_steps / 4), 1) : 1;
     if ((z_steps - z_steps / splits) * 512 < b.vocab) splits = 1;
     A->splits = static_cast<uint32_t>(splits);
+    // dW's over the tokens likewise, where the steps that it saves take longer than what writing and reading the slices does, at 5 TB/s.  (Us, without / with: 3185
+    // tokens on 1332 x 384 119 / 92, 4096 on 256 x 4096 150 / 114, on 4099 x 768 228 / 200; 1000 on 4099 x 768 would take 96 instead of 90.)
+    const uint64_t dw_tiles = whole / kTile * (up(width_up, kTile) / kTile), dw_steps = up(n, kStepK) / kStepK;
+    uint64_t dw_slices = !few(b) && step >= b.vocab ? std::max<uint64_t>(std::min(kComputeUnits / dw_tiles, dw_steps / 4), 1) : 1;
+    if ((dw_steps - dw_steps / dw_slices) << 22 < whole * width_up * (8 * dw_slices + 2)) dw_slices = 1;
+    A->dw_slices = static_cast<uint32_t>(dw_slices);
     Places p = {};
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
@@ -918,6 +955,7 @@ Places place(const ff_head_batch& b, bool grad, HeadArgs* A)
         p.grad = take(all);
         p.logits = take(std::max(split, keeps(b) ? 2 * all : std::min(2 * all, smaller)));
         const uint64_t dh = rows * width_up;
+        p.dw = take(std::min<uint64_t>(whole * width_up * (rows / kStepK), kComputeUnits * kTile * kTile) * 4);
         p.dh = take(std::max(dh, std::min<uint64_t>(dh * (whole / kTile), kComputeUnits * kTile * kTile)) * 4);
     }
     p.bytes = at;
@@ -981,7 +1019,7 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
         const bool last = i == n_pieces - 1, logits = !whole && (!keep || !last);
         take(i, A.dhidden || logits);
         if (logits) hipLaunchKernelGGL((head_logits_kernel<BF16, BM, kGrad>), dim3(tiles * tiles_m), threads, 0, stream, A, first, m);
-        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight && !few_dweight ? tiles * tiles_d : 0;
+        const uint32_t dh_blocks = A.dhidden ? tiles_m * tiles_d * A.slices : 0, dw_blocks = A.dweight && !few_dweight ? tiles * tiles_d * A.dw_slices : 0;
         if (A.dweight && few_dweight) {
             const uint32_t blocks = (m + kFewEntries - 1) / kFewEntries, parts = std::min(tiles_d, (kFewDweightBlocks + blocks - 1) / blocks);
             hipLaunchKernelGGL(head_few_dweight_kernel<BF16>, dim3(blocks * parts), dim3(kFewWaves * kWaveSize), 0, stream, A, first, m, parts);
@@ -990,9 +1028,10 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
             hipLaunchKernelGGL((head_grads_kernel<BF16, BM>), dim3(dh_blocks + dw_blocks), threads, 0, stream, A, first, m, whole ? first : 0,
                            last ? start : kNext, dh_blocks);
     }
-    if (A.dhidden && start != kOnly && n) {
+    const uint32_t dh_rows = A.dhidden && start != kOnly ? std::min(n, kPutRows) : 0, dw_rows = A.dweight && A.dw_slices > 1 ? std::min(vocab, kPutRows) : 0;
+    if (dh_rows + dw_rows) {
         const uint32_t blocks_of_row = static_cast<uint32_t>((A.b.width + 4 * kPutThreads - 1) / (4 * kPutThreads));
-        hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(std::min(n, kPutRows), blocks_of_row), dim3(kPutThreads), 0, stream, A);
+        hipLaunchKernelGGL(head_put_kernel<BF16>, dim3(dh_rows + dw_rows, blocks_of_row), dim3(kPutThreads), 0, stream, A, dh_rows);
     }
     return hipGetLastError();
 }
@@ -1035,6 +1074,7 @@ hipError_t launch_head(const ff_head_batch& b, float* logp, void* dhidden, uint6
     A.grad = w + p.grad;
     A.logits = reinterpret_cast<float*>(w + p.logits);
     A.dh = reinterpret_cast<float*>(w + p.dh);
+    A.dw = reinterpret_cast<float*>(w + p.dw);
     A.grad_scale = b.loss_scale * (b.dtype == FF_BF16 ? 1.f : 0x1p-14f);
     A.past = reinterpret_cast<uint64_t>(dweight) % 16 == 0 && dweight_stride % 8 == 0;
     const bool high = high_tiles(b);

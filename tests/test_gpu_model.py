@@ -376,7 +376,7 @@ def test_head_in_several_pieces_of_the_vocabulary(dtype, n, vocab, width, pad, f
     check_head(run_head(*args, scale, pad=pad, first=first), modelref.head(*args, scale))
 
 
-FEW_TILES = [(21, 1240, 8128, 0, 0), (130, 700, 4096, 8, 0), (300, 256, 2000, 3, 1), (1500, 300, 1100, 0, 0), (2, 1689, 2578, 0, 0), (64, 4099, 2056, 0, 3), (17, 1, 1024, 0, 0)]
+FEW_TILES = [(21, 1240, 8128, 0, 0), (130, 700, 4096, 8, 0), (300, 256, 2000, 3, 1), (1500, 300, 1100, 0, 0), (2, 1689, 2578, 0, 0), (64, 4099, 2056, 0, 3), (17, 1, 1024, 0, 0), (1300, 500, 333, 3, 1)]
 
 
 @HALVES
