@@ -430,8 +430,9 @@ int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss,
 
 /* ---- the two ends of a model: embedding, layer norm, head with cross entropy -------------------- */
 
-/* Nothing is allocated, and calls only launch kernels: they can be recorded into a HIP graph.  Calls that may be in flight at the same time
- * take a workspace each; graphs that are replayed one behind the other may share one.  Outputs must not overlap inputs or each other but where this is said. */
+/* Nothing is allocated, and calls only launch kernels: they can be recorded into a HIP graph.  Calls that may be in
+ * flight at the same time take a workspace each; graphs that are replayed one behind the other may share one.  Outputs
+ * must not overlap inputs or each other but where this is said. */
 
 /*
  * Embedding: out[t] = scale * table[ids[t]], one fp32 product rounded to the format.  table: DEVICE, vocab rows of `width` elements of
@@ -481,8 +482,8 @@ int ff_layer_norm_grad(const void *x, uint64_t n_rows, uint64_t width, uint64_t 
                        void *dweight, void *dbias, void *workspace, void *hip_stream);
 
 /*
- * Head: the cross entropy of targets over a vocabulary, from the hidden states, with the logits of one piece of the vocabulary in memory at most.  hidden: n_tokens rows of `width`
- * elements of dtype (FF_BF16 or FF_F16), hidden_stride >= width elements apart; weight: vocab such rows.  All arrays DEVICE and
+ * Head: the cross entropy of targets over a vocabulary, from the hidden states, with the logits of one piece of the
+ * vocabulary in memory at most.  hidden: n_tokens rows of `width` elements of dtype (FF_BF16 or FF_F16), hidden_stride >= width elements apart; weight: vocab such rows.  All arrays DEVICE and
  * aligned to their elements; rows of `weight` that are 16-byte aligned, of a width that is a multiple of 8, are read where they lie,
  * others are copied piece by piece first.  targets int64; weights fp32: what a token counts in the loss, its share of the mean included; 0
  * leaves it out (prompts, padding): its row is not read.
@@ -506,9 +507,10 @@ typedef struct {
     uint64_t n_invalid; /* weight not 0 and yet left out: target outside the vocabulary */
 } ff_head_stats;
 
-/* What ff_head_loss is given; gradient: whether either is wanted.  0 for a batch that is refused.  What the tokens need
- * -- 8 bytes for every token and 256 entries of the vocabulary, 2 to 6 for every element of the hidden states -- and, for a piece of the vocabulary
- * at a time, up to 3 GiB, or 1 more where rows of `weight` are copied; without gradients that one alone. */
+/* What ff_head_loss is given; gradient: whether either is wanted.  0 for a batch that is refused.  8 bytes for every token
+ * and 256 entries of the vocabulary, 2 for every element of the hidden states (6 with gradients; tokens rounded up to 256),
+ * up to 16 MiB of logits of small calls; and with gradients up to 128 MiB of slices of sums and, for a piece of the vocabulary at
+ * a time, up to 3 GiB.  Where rows of `weight` are copied, up to 1 GiB more.  Never less for more tokens or entries. */
 #define FF_HEAD_MAX_TOKENS (1u << 22)
 #define FF_HEAD_MAX_VOCAB (1u << 22)
 #define FF_HEAD_MAX_WIDTH 65536u
