@@ -16,8 +16,8 @@
 //
 // What bounds it: many tokens, the matrix instructions (product.h); few, reading W once for the logits and once for dH, and writing dW: 64 tokens and
 // fewer take kernels of their own for the logits (head_stream_kernel) and dW (head_few_dweight_kernel); small heads, the chain of five
-// launches.  Us, logits / all with both gradients, width 4096, 1 / 16 / 64 / 128 / 256 tokens on 32,000 65 / 77 / 102 / 101 / 120 and 175 / 190 / 223 / 250 / 317,
-// on 128,256 225 / 275 / 249 / 273 / 280 and 678 / 733 / 731 / 896 / 1049.
+// launches.  Us, scoring / with both gradients, width 4096, 1 / 16 / 64 / 128 / 256 tokens on 32,000 (which lie in the caches from the call before, in part) 52 / 71 /
+// 70 / 84 / 109 and 158 / 177 / 202 / 240 / 322, on 128,256 216 / 266 / 249 / 276 / 286 and 661 / 723 / 721 / 888 / 1053.
 #include "head.hpp"
 
 #include <algorithm>
