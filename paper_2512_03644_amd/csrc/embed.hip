@@ -462,6 +462,7 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(const EmbedArgs 
         uint32_t more = 0;
         for (uint32_t w = 0; w < kFewWaves; w++) more += wave_bins[w][threadIdx.x];
         begin[threadIdx.x] += more;
+        __syncthreads();  // the next round clears what the others read here
     }
     __syncthreads();
     // an id's tokens lie between the end of the one before it and its own
