@@ -523,6 +523,7 @@ uint64_t ff_head_workspace_bytes(const ff_head_batch *b, uint32_t gradient);
  * (softmax(z[t])[v] - [v is the target]), rounded to dtype relative to the largest weight, dhidden = g . weight (rows of zeros for
  * tokens that are left out) and dweight = g^T . hidden, summed in fp32 in an order that the sizes give and rounded once.
  * dhidden may be hidden (of the same stride).  Without either, scoring: one product in place of three or four.
+ * n_tokens 0: dweight of zeros and the stats alone; hidden, weight and the arrays of tokens are not read and may be NULL.
  * workspace: DEVICE, 256-byte aligned, ff_head_workspace_bytes() bytes; its content does not matter.
  */
 int ff_head_loss(const ff_head_batch *b, float *logp, void *dhidden, uint64_t dhidden_stride,

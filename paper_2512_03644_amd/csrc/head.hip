@@ -970,9 +970,10 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
     const uint32_t n_pieces = static_cast<uint32_t>((static_cast<uint64_t>(vocab) + A.step - 1) / A.step);
     const bool grad = A.dhidden || A.dweight, keep = grad && (A.splits > 1 || keeps(A.b)), whole = few(A.b);
     const bool few_dweight = whole && static_cast<uint64_t>(vocab) * A.b.width >= kFewDweightFrom;
+    const bool copies = A.weight && n;  // (without tokens W is not read: there may be none)
     uint32_t first = 0, m = 0, tiles = 0, packed = ~0u;
     if (n <= kSelectFew) {
-        const uint32_t rows = A.weight && !streams(A.b, grad) ? std::min(A.step, vocab) : 0, blocks = up64(n);
+        const uint32_t rows = copies && !streams(A.b, grad) ? std::min(A.step, vocab) : 0, blocks = up64(n);
         hipLaunchKernelGGL(head_few_kernel, dim3(blocks + std::min(rows, kPackBlocks)), dim3(256), 0, stream, A, blocks, rows);
         if (rows) packed = 0;
     } else {
@@ -984,7 +985,7 @@ hipError_t launch(const HeadArgs& A, hipStream_t stream)
         first = i * A.step;
         m = std::min(A.step, vocab - first);
         tiles = (m + kTile - 1) / kTile;
-        if (!A.weight || !rows || packed == i) return;
+        if (!copies || !rows || packed == i) return;
         hipLaunchKernelGGL(head_pack_kernel, dim3(std::min(m, kPackBlocks)), dim3(256), 0, stream, A, first, m);
         packed = i;
     };

@@ -411,3 +411,23 @@ def test_head_of_few_tiles_with_a_logit_that_is_not_finite_and_large_ones():
     want = modelref.head(hidden[clean], weight, targets[clean], weights[clean])
     for name in ("logp", "dhidden"):
         modelref.check(got[name][clean], want[name], want["tol_" + name], name)
+
+
+@HALVES
+@pytest.mark.parametrize("vocab,width,pad,first", [(300, 65, 0, 0), (4099, 64, 3, 1), (1, 1, 0, 0), (9000, 65521, 0, 0)])
+def test_head_of_nothing_on_rows_that_would_be_copied(dtype, vocab, width, pad, first):
+    """Of widths and strides at which W's rows are copied for tokens; W may be absent."""
+    weight, _ = rows(vocab, width, dtype, gen(8), 1.0, pad, first)
+    none = torch.empty(0, width, dtype=dtype, device=DEV)
+    ids, weights = torch.empty(0, dtype=torch.int64, device=DEV), torch.empty(0, device=DEV)
+    got = run_head(none, weight, ids, weights, pad=pad, first=first)
+    assert bool((got["dweight"] == 0).all()) and got["stats"].words.tolist() == [0, 0, 0]
+    batch = ff.head_batch(none, weight, ids, weights)
+    batch.weight = None
+    dweight, arena = rows(vocab, width, dtype, None, 0, pad, first)
+    stats = ff.HeadStats(DEV)
+    stats.words.fill_(-1)
+    ff.ff_head_loss(batch, weights, stats, ff.alloc_head_workspace(batch, DEV), dweight=dweight)
+    torch.cuda.synchronize()
+    assert bool((dweight == 0).all()) and stats.words.tolist() == [0, 0, 0]
+    untouched(dweight, arena)
