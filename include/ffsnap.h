@@ -432,7 +432,7 @@ int ff_policy_loss(const ff_policy_batch *batch, float *logp, float *token_loss,
 
 /* Nothing is allocated, and calls only launch kernels: they can be recorded into a HIP graph.  Calls that may be in
  * flight at the same time take a workspace each; graphs that are replayed one behind the other may share one.  Outputs
- * must not overlap inputs or each other but where this is said. */
+ * must not overlap inputs or each other but where this is said; where they begin at the same address, the call is refused. */
 
 /*
  * Embedding: out[t] = scale * table[ids[t]], one fp32 product rounded to the format.  table: DEVICE, vocab rows of `width` elements of

@@ -1,7 +1,9 @@
 // extern "C" entry points of the operators at a model's two ends (see include/ffsnap.h for the contract).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "../../include/ffsnap.h"
 #include "embed.hpp"
@@ -21,6 +23,14 @@ bool rows_ok(uint64_t stride, uint64_t width) { return stride >= width && stride
 // A loss scale that is one in 32 bits.
 bool scale_ok(float v) { return v > 0.f && std::isfinite(v); }
 
+// Is an output's address, unless it is null, another output's or an input's?
+bool shared(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs)
+{
+    for (auto o = outputs.begin(); o != outputs.end(); o++)
+        if (*o && (std::find(o + 1, outputs.end(), *o) != outputs.end() || std::find(inputs.begin(), inputs.end(), *o) != inputs.end())) return true;
+    return false;
+}
+
 int check_embed(const void* rows, uint64_t rows_stride, uint32_t dtype, const int64_t* ids, uint64_t n_tokens, uint64_t vocab, uint64_t width,
                 float scale, const void* out, uint64_t out_stride, bool add, bool gradient)
 {
@@ -29,7 +39,8 @@ int check_embed(const void* rows, uint64_t rows_stride, uint32_t dtype, const in
     if (n_tokens && (!rows || !ids)) return FF_ERR_NULL;
     if ((n_tokens || (gradient && !add)) && !out) return FF_ERR_NULL;
     if (!aligned(rows, size) || !aligned(out, size) || !aligned(ids, 8)) return FF_ERR_INVALID;
-    if (!rows_ok(rows_stride, width) || !rows_ok(out_stride, width) || (n_tokens && rows == out)) return FF_ERR_INVALID;
+    if (!rows_ok(rows_stride, width) || !rows_ok(out_stride, width)) return FF_ERR_INVALID;
+    if (n_tokens && shared({out}, {rows, ids})) return FF_ERR_INVALID;
     return FF_OK;
 }
 
@@ -88,6 +99,7 @@ int ff_layer_norm(const void* x, uint64_t n_rows, uint64_t width, uint64_t x_str
     const int rc = check_norm(x, n_rows, width, x_stride, dtype, weight, y, y_stride, bias);
     if (rc != FF_OK) return rc;
     if (!(eps >= 0.f) || !std::isfinite(eps) || !aligned(mean, 4) || !aligned(rstd, 4) || (x == y && x_stride != y_stride)) return FF_ERR_INVALID;
+    if (n_rows && (shared({y, mean, rstd}, {weight, bias}) || shared({mean, rstd}, {x}))) return FF_ERR_INVALID;
     NormArgs a = {};
     a.x = static_cast<const uint8_t*>(x);
     a.n_rows = n_rows;
@@ -119,8 +131,9 @@ int ff_layer_norm_grad(const void* x, uint64_t n_rows, uint64_t width, uint64_t 
     if ((dweight || dbias) && !workspace) return FF_ERR_NULL;
     const uint32_t size = element_size(dtype);
     if (!rows_ok(dy_stride, width) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, size) || !aligned(dbias, size) ||
-        !aligned(workspace, 16) || dweight == weight || dbias == weight || (dx == dy && dx_stride != dy_stride) || (dx == x && dx_stride != x_stride))
+        !aligned(workspace, 16) || (dx == dy && dx_stride != dy_stride) || (dx == x && dx_stride != x_stride))
         return FF_ERR_INVALID;
+    if (shared({dweight, dbias}, {weight}) || (n_rows && (shared({dx, dweight, dbias}, {weight, mean, rstd}) || shared({dweight, dbias}, {x, dy})))) return FF_ERR_INVALID;
     NormArgs a = {};
     a.x = static_cast<const uint8_t*>(x);
     a.n_rows = n_rows;
@@ -163,7 +176,10 @@ int ff_head_loss(const ff_head_batch* b, float* logp, void* dhidden, uint64_t dh
         if (!workspace) return FF_ERR_NULL;
         if (!aligned(workspace, 256)) return FF_ERR_INVALID;
     }
-    if (dweight && (!aligned(dweight, 2) || !rows_ok(dweight_stride, b->width) || dweight == b->weight)) return FF_ERR_INVALID;
+    if (dweight && (!aligned(dweight, 2) || !rows_ok(dweight_stride, b->width))) return FF_ERR_INVALID;
+    if (shared({dweight, stats}, {b->weight}) ||
+        (b->n_tokens && (shared({dhidden, dweight, logp, stats}, {b->weight, b->targets, b->weights}) || shared({dweight, logp, stats}, {b->hidden}))))
+        return FF_ERR_INVALID;
     FF_HIP_TRY(launch_head(*b, logp, dhidden, dhidden_stride, dweight, dweight_stride, stats, workspace, static_cast<hipStream_t>(hip_stream)));
     return FF_OK;
 }

@@ -238,3 +238,37 @@ def test_plain_embedding():
     total, tol = modelref.embed_grad(torch.ones(5, 3), ids, 4, 2.0, table)
     assert total.tolist() == [[2.0, 3.0, 4.0], [3.0, 4.0, 5.0], [6.0, 7.0, 8.0], [13.0, 14.0, 15.0]]
     assert float(tol.max()) < 1e-5 and math.isfinite(float(tol.min()))
+
+
+# ---- addresses that are an output's and another's ----------------------------------------------------
+
+def _pairs(call, outputs, inputs, allowed):
+    """Every output at every other output's and input's address, but for what is allowed; every other address its own."""
+    names = outputs + inputs
+    at = {name: (k + 2) * A16 for k, name in enumerate(names)}
+    for k, out in enumerate(outputs):
+        for other in outputs[k + 1:] + inputs:
+            if (out, other) not in allowed:
+                assert call(**dict(at, **{out: at[other]})) == ff.FF_ERR_INVALID, (out, other)
+
+
+def test_outputs_at_the_addresses_of_others_are_refused():
+    L = ff.lib()
+    for dtype in (ff.FF_BF16, ff.FF_F32):
+        _pairs(lambda table, ids, out: L.ff_embed(table, 10, 8, 8, dtype, ids, 4, 1.0, out, 8, None), ["out"], ["table", "ids"], ())
+        for flags in (0, ff.FF_GRAD_ADD):
+            _pairs(lambda dout, ids, dtable: L.ff_embed_grad(dout, 8, dtype, ids, 4, 10, 8, 1.0, dtable, 8, flags, A16, None), ["dtable"], ["dout", "ids"], ())
+        _pairs(lambda x, weight, bias, y, mean, rstd: L.ff_layer_norm(x, 4, 8, 8, dtype, weight, bias, 1e-5, y, 8, mean, rstd, None),
+               ["y", "mean", "rstd"], ["x", "weight", "bias"], [("y", "x")])
+        _pairs(lambda x, weight, mean, rstd, dy, dx, dweight, dbias: L.ff_layer_norm_grad(x, 4, 8, 8, dtype, weight, mean, rstd, dy, 8, dx, 8, dweight, dbias, A16, None),
+               ["dx", "dweight", "dbias"], ["x", "dy", "weight", "mean", "rstd"], [("dx", "x"), ("dx", "dy")])
+
+    def loss(hidden, weight, targets, weights, logp, dhidden, dweight, stats):
+        b = _batch(hidden=hidden, weight=weight, targets=targets, weights=weights)
+        return L.ff_head_loss(ctypes.byref(b), logp, dhidden, 64, dweight, 64, stats, A16, None)
+
+    _pairs(loss, ["dhidden", "dweight", "logp", "stats"], ["hidden", "weight", "targets", "weights"], [("dhidden", "hidden")])
+    # what is not there is at no address, and arrays of no rows are nowhere either
+    assert L.ff_layer_norm(None, 0, 8, 8, ff.FF_BF16, A16, A16, 1e-5, None, 8, None, None, None) == ff.FF_OK
+    assert L.ff_layer_norm(A16, 0, 8, 8, ff.FF_BF16, A16, A16, 1e-5, A16, 8, A16, A16, None) == ff.FF_OK
+    assert L.ff_embed(A16, 10, 8, 8, ff.FF_BF16, A16, 0, 1.0, A16, 8, None) == ff.FF_OK
