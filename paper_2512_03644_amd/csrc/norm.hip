@@ -1,7 +1,8 @@
 // Layer norm, forward and backward, for gfx950.
 //
 // y = (x - mean) rstd w + b, rstd = 1 / sqrt(var + eps).  A group of threads -- a wavefront, or a workgroup -- holds a row in registers: the mean
-// first, then the squares of what is left of it, so that a large mean costs the variance nothing.  Backward, with xh = (x - mean) rstd and g =
+// first, then the squares of what is left of it, so that a large mean costs the variance nothing.  Quotients by the width are exact where they can be (Divisor):
+// of a row of one value of few bits nothing is left, whatever the value.  Backward, with xh = (x - mean) rstd and g =
 // dy w: dx = rstd (g - mean(g) - xh mean(g xh)); dw = sum of dy xh, db = sum of dy over the rows: a group keeps
 // them in registers over the rows that it takes, and leaves its part in the workspace; a second launch joins the parts in their order.
 //
@@ -51,6 +52,18 @@ __device__ __forceinline__ void sum_over(float (&v)[N], int turn)
 
 __device__ __forceinline__ float sum8(f32x8 v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 
+// Quotients by the width: the product with its reciprocal, and what that leaves of the sum divided likewise.  A quotient that 32 bits hold comes out
+// exactly.  (The division that the compiler makes takes ten operations, and 155 us of 16,384 rows of 8192 bf16 elements backward instead of 143.)
+struct Divisor {
+    float of, each;
+    __device__ explicit Divisor(uint32_t width) : of(static_cast<float>(width)), each(1.f / of) {}
+    __device__ __forceinline__ float quotient(float s) const
+    {
+        const float q = s * each;
+        return __builtin_isfinite(q) ? fmaf(fmaf(-q, of, s), each, q) : q;
+    }
+};
+
 // fn(i, at) for the thread's K places in a row.
 template <int GROUP, int K, class Fn>
 __device__ __forceinline__ void places(uint32_t thread, uint32_t width, Fn&& fn)
@@ -66,7 +79,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
 {
     constexpr uint32_t kPer = block_of<GROUP>() / GROUP;
     const uint32_t width = static_cast<uint32_t>(a.width), thread = threadIdx.x % GROUP;
-    const float each = 1.f / static_cast<float>(width);
+    const Divisor of(width);
     const uint64_t step = static_cast<uint64_t>(gridDim.x) * kPer;
     typename I::Held w[K], b[K], h[K], next[K];
     auto fetch = [&](typename I::Held (&to)[K], uint64_t r) {
@@ -86,7 +99,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
         places<GROUP, K>(thread, width, [&](auto i, uint32_t at) { s[0] += sum8(I::cut(I::wide(h[int(i)]), at, width)); });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
-        const float mean = s[0] * each;
+        const float mean = of.quotient(s[0]);
         s[0] = 0.f;
         places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
             const f32x8 d = I::cut(I::wide(h[int(i)]) - mean, at, width);
@@ -94,7 +107,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_kernel(const NormArgs 
         });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
-        const float rstd = 1.f / sqrtf(s[0] * each + a.eps);
+        const float rstd = 1.f / sqrtf(of.quotient(s[0]) + a.eps);
         places<GROUP, K>(thread, width, [&](auto i, uint32_t at) {
             f32x8 y = (I::wide(h[int(i)]) - mean) * rstd * I::wide(w[int(i)]);
             if (a.bias) y += I::wide(b[int(i)]);
@@ -155,7 +168,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
     }
     constexpr uint32_t kPer = block_of<GROUP>() / GROUP;
     const uint32_t width = static_cast<uint32_t>(a.width), thread = threadIdx.x % GROUP;
-    const float each = 1.f / static_cast<float>(width);
+    const Divisor of(width);
     const uint32_t group = blockIdx.x * kPer + threadIdx.x / GROUP;
     const uint64_t step = static_cast<uint64_t>(blocks) * kPer;
     // The widest rows leave no registers for the next row, nor for this one while its sums are made: it is read again, from the caches.
@@ -202,7 +215,7 @@ __global__ __launch_bounds__(block_of<GROUP>()) void norm_grad_kernel(const Norm
         });
         sum_over<GROUP>(s, turn);
         turn ^= 1;
-        const float c0 = s[0] * each, c1 = s[1] * each;
+        const float c0 = of.quotient(s[0]), c1 = of.quotient(s[1]);
         each_place([&](auto, uint32_t at, f32x8 normed, f32x8, f32x8 g) {
             I::template store<PAST>(a.out + r * a.out_stride * I::kBytes, at, width, I::narrow(now.rstd * (g - c0 - normed * c1)));
         });

@@ -431,3 +431,18 @@ def test_head_of_nothing_on_rows_that_would_be_copied(dtype, vocab, width, pad, 
     torch.cuda.synchronize()
     assert bool((dweight == 0).all()) and stats.words.tolist() == [0, 0, 0]
     untouched(dweight, arena)
+
+
+@TYPES
+@pytest.mark.parametrize("width", [15, 41, 107, 777, 1003, 2049, 4097, 5000, 8191, 16383])
+def test_rows_of_one_value_are_the_bias_and_have_no_gradient(dtype, width):
+    """Of few bits: their sum is exact, and so is its quotient.  rstd is eps's alone, 316."""
+    values = torch.tensor([5.0, 300.0, 1000.0, 20000.0], device=DEV)
+    assert bool((values.to(dtype) == values.to(torch.float32)).all()) or dtype == BF16
+    x = values.to(dtype)[:, None].repeat(1, width)
+    weight, bias = torch.ones(width, dtype=dtype, device=DEV), torch.randn(width, generator=gen(9), device=DEV).to(dtype)
+    y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(4, device=DEV), torch.empty(4, device=DEV)
+    ff.ff_layer_norm(x, weight, bias, y, mean, rstd)
+    assert torch.equal(y, bias[None].repeat(4, 1)) and torch.equal(mean, x[:, 0].float())
+    ff.ff_layer_norm_grad(x, weight, mean, rstd, x, dx)
+    assert bool((dx == 0).all())

@@ -32,3 +32,7 @@ def _run(check, tmp_path):
 
 def test_gradients_of_an_embedding_in_any_order_of_wavefronts(tmp_path):
     _run("embed_order_check", tmp_path)
+
+
+def test_layer_norms_in_any_order_of_wavefronts_and_rows_of_one_value(tmp_path):
+    _run("norm_order_check", tmp_path)
