@@ -507,10 +507,11 @@ typedef struct {
     uint64_t n_invalid; /* weight not 0 and yet left out: target outside the vocabulary */
 } ff_head_stats;
 
-/* What ff_head_loss is given; gradient: whether either is wanted.  0 for a batch that is refused.  8 bytes for every token
- * and 256 entries of the vocabulary, 2 for every element of the hidden states (6 with gradients; tokens rounded up to 256),
- * up to 16 MiB of logits of small calls; and with gradients up to 128 MiB of slices of sums and, for a piece of the vocabulary at
- * a time, up to 3 GiB.  Where rows of `weight` are copied, up to 1 GiB more.  Never less for more tokens or entries. */
+/* What ff_head_loss is given; gradient: whether either is wanted.  0 for a batch that is refused.  No more bytes than: 40 for every
+ * token, and 8 for each and 256 entries of the vocabulary (for 64 entries of the first 32 tokens); 2 for every element of the hidden
+ * states, 6 with gradients, tokens rounded up to 256, the width to 64; 16 MiB of logits of small calls; with gradients 128 MiB of slices
+ * of sums and, for a piece of the vocabulary at a time, 3 GiB, or 1536 for every token if that is more.  Where rows of `weight` are copied, 1 GiB more; and 4
+ * KiB for alignment.  Never less for more tokens or entries. */
 #define FF_HEAD_MAX_TOKENS (1u << 22)
 #define FF_HEAD_MAX_VOCAB (1u << 22)
 #define FF_HEAD_MAX_WIDTH 65536u

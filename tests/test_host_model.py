@@ -272,3 +272,27 @@ def test_outputs_at_the_addresses_of_others_are_refused():
     assert L.ff_layer_norm(None, 0, 8, 8, ff.FF_BF16, A16, A16, 1e-5, None, 8, None, None, None) == ff.FF_OK
     assert L.ff_layer_norm(A16, 0, 8, 8, ff.FF_BF16, A16, A16, 1e-5, A16, 8, A16, A16, None) == ff.FF_OK
     assert L.ff_embed(A16, 10, 8, 8, ff.FF_BF16, A16, 0, 1.0, A16, 8, None) == ff.FF_OK
+
+
+def test_head_workspaces_are_within_what_is_documented():
+    """The bound that ffsnap.h states, over all of the allowed range, corners included."""
+    L, up = ff.lib(), lambda x, to: (x + to - 1) // to * to
+    gib, mib = 1 << 30, 1 << 20
+    nearest = 1.0
+    for n in (0, 1, 16, 17, 20, 32, 33, 64, 65, 256, 300, 4096, 30000, 1 << 20, 1 << 21, (1 << 21) + 1, 3000000, 1 << 22):
+        for vocab in (1, 300, 4099, 128256, 1 << 20, ff.FF_HEAD_MAX_VOCAB):
+            for width in (1, 64, 72, 1000, 4096, 8192, ff.FF_HEAD_MAX_WIDTH):
+                for grad in (0, 1):
+                    for copied in (False, True):
+                        b = _batch(n_tokens=n, vocab=vocab, width=width, hidden_stride=width, weight_stride=width + 1 if copied else up(width, 8))
+                        copied = copied or width % 8 != 0
+                        tiles, rows = up(vocab, 256) // 256, up(max(n, 1), 256)
+                        bound = 40 * n + 8 * max(n * tiles, min(n, 32) * 4 * tiles) + (6 if grad else 2) * rows * up(width, 64) + 16 * mib + 4096
+                        if grad:
+                            bound += 128 * mib + max(3 * gib, 1536 * rows)
+                        if copied:
+                            bound += gib
+                        size = L.ff_head_workspace_bytes(ctypes.byref(b), grad)
+                        assert 0 < size <= bound, (n, vocab, width, grad, copied, size, bound)
+                        nearest = min(nearest, 1 - size / bound)
+    assert nearest < 0.01  # (it is no idle bound)
