@@ -447,8 +447,8 @@ int ff_embed(const void *table, uint64_t vocab, uint64_t width, uint64_t table_s
              void *hip_stream);
 
 /*
- * Its gradient: dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] == v), in fp32 and in the tokens' order, whatever else
- * runs, rounded once.  Every row is written, those without tokens with zeros.  With FF_GRAD_ADD the sum is added to
+ * Its gradient: dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] == v), in fp32, in an order that the sizes and the
+ * ids give (not always the tokens' own), the same at every call, rounded once.  Every row is written, those without tokens with zeros.  With FF_GRAD_ADD the sum is added to
  * what is there (a table that is the head's too has the head's gradient there), and rows without tokens are neither read nor
  * written.  Ids outside the vocabulary count nowhere.  workspace: DEVICE, 16-byte aligned, ff_embed_workspace_bytes(), which never
  * falls with any argument; its content does not matter.
