@@ -660,8 +660,8 @@ def ff_embed_grad(dout, ids, dtable, workspace, scale=1.0, add=False, stream=Non
 
 
 def _space(workspace, least, name, dev):
-    if workspace is None or workspace.nbytes < least or workspace.get_device() != dev:
-        raise ValueError("the workspace is smaller than %s, or elsewhere" % name)
+    if workspace is None or workspace.nbytes < least or not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError("the workspace is smaller than %s, not contiguous, or elsewhere" % name)
     _current(dev)
 
 
@@ -753,8 +753,8 @@ def ff_head_loss(batch, logp, stats, workspace, dhidden=None, dweight=None, stre
         dh, dh_stride = dhidden.data_ptr(), _rows(dhidden, "dhidden", tokens, dtype, dev)
     if dweight is not None:
         dw, dw_stride = dweight.data_ptr(), _rows(dweight, "dweight", table, dtype, dev)
-    logp = _vector(logp, "logp", one, _F32, dev)
+    logp, stats = _vector(logp, "logp", one, _F32, dev), _vector(stats.words, "stats", (3,), _I64, dev)
     _space(workspace, L.ff_head_workspace_bytes(ref, 0 if dhidden is None and dweight is None else 1), "ff_head_workspace_bytes()", dev)
-    status = L.ff_head_loss(ref, logp, dh, dh_stride, dw, dw_stride, stats.data_ptr(), workspace.data_ptr(), _stream_ptr(stream))
+    status = L.ff_head_loss(ref, logp, dh, dh_stride, dw, dw_stride, stats, workspace.data_ptr(), _stream_ptr(stream))
     if status:
         _check(status)

@@ -296,3 +296,34 @@ def test_head_workspaces_are_within_what_is_documented():
                         assert 0 < size <= bound, (n, vocab, width, grad, copied, size, bound)
                         nearest = min(nearest, 1 - size / bound)
     assert nearest < 0.01  # (it is no idle bound)
+
+
+class _Elsewhere:
+    """Stands for a tensor on a device: what the binding asks of one."""
+
+    def __init__(self, *shape, dtype=torch.float32):
+        self.dtype, self.shape, self.nbytes = dtype, shape, 1 << 40
+
+    def get_device(self):
+        return 5
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return A16
+
+
+def test_binding_refuses_stats_in_host_memory_and_workspaces_that_only_look_large():
+    bf = torch.bfloat16
+    b = ff.head_batch(torch.zeros(4, 8, dtype=bf), torch.zeros(10, 8, dtype=bf), torch.zeros(4, dtype=torch.int64), torch.zeros(4))
+    b.shapes = b.shapes[:-1] + (5,)
+    with pytest.raises(ValueError, match="stats is a"):  # the kernel would write there
+        ff.ff_head_loss(b, _Elsewhere(4), ff.HeadStats("cpu"), _Elsewhere(1 << 40), stream=NOWHERE)
+    table, out, ids, w8, f = torch.zeros(10, 8, dtype=bf), torch.zeros(4, 8, dtype=bf), torch.zeros(4, dtype=torch.int64), torch.zeros(8, dtype=bf), torch.zeros(4)
+    b = ff.head_batch(out, table, ids, f)
+    one = torch.zeros(1, dtype=torch.uint8).expand(1 << 30)  # one byte
+    for call in (lambda: ff.ff_embed_grad(out, ids, table, one, stream=NOWHERE), lambda: ff.ff_layer_norm_grad(out, w8, f, f, out, out, w8, None, one, stream=NOWHERE),
+                 lambda: ff.ff_head_loss(b, f, ff.HeadStats("cpu"), one, stream=NOWHERE)):
+        with pytest.raises(ValueError, match="workspace"):
+            call()
