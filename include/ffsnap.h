@@ -483,7 +483,7 @@ int ff_layer_norm_grad(const void *x, uint64_t n_rows, uint64_t width, uint64_t 
 
 /*
  * Head: the cross entropy of targets over a vocabulary, from the hidden states, with the logits of one piece of the
- * vocabulary in memory at most.  hidden: n_tokens rows of `width` elements of dtype (FF_BF16 or FF_F16), hidden_stride >= width elements apart; weight: vocab such rows.  All arrays DEVICE and
+ * vocabulary in memory at most (a piece has up to 2^29: 4096 tokens of 128,256 entries are one).  hidden: n_tokens rows of `width` elements of dtype (FF_BF16 or FF_F16), hidden_stride >= width elements apart; weight: vocab such rows.  All arrays DEVICE and
  * aligned to their elements; rows of `weight` that are 16-byte aligned, of a width that is a multiple of 8, are read where they lie,
  * others are copied piece by piece first.  targets int64; weights fp32: what a token counts in the loss, its share of the mean included; 0
  * leaves it out (prompts, padding): its row is not read.

@@ -9,8 +9,8 @@
 // of the rows of a part's tokens, and writes every sum that begins and ends there.  What reaches over a part's ends is left
 // in the workspace, in 32 bits, and a last launch joins it in its order.
 //
-// What bounds it: memory; few tokens: the launches.  Lookup of 16,384 tokens of 8192 bf16 elements 84 us; gradient of 16,384 tokens of 4096 added to 32,000 rows 75 us: the
-// list 14, sums 37 (of 134 MB and 89 MB of rows read and written, 6.0 TB/s), joins 7.
+// What bounds it: memory; few tokens: the steps of a workgroup, which hang on one another.  Lookup of 16,384 tokens of 8192 bf16 elements 84 us; gradient of 16,384 tokens of 4096 added to 32,000 rows 75 us: the
+// list 14, sums 36 (of 134 MB and 89 MB of rows read and written, 6.0 TB/s), joins 7.
 #include "embed.hpp"
 
 #include <algorithm>

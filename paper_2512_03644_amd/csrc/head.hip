@@ -15,8 +15,8 @@
 // softmax of 2^-28 is still a normal number.
 //
 // What bounds it: many tokens, the matrix instructions (product.h); few, reading W once for the logits and once for dH, and writing dW: 64 tokens and
-// fewer take kernels of their own for the logits (head_stream_kernel) and dW (head_few_dweight_kernel); small heads, the chain of five
-// launches.  Us, scoring / with both gradients, width 4096, 1 / 16 / 64 / 128 / 256 tokens on 32,000 (which lie in the caches from the call before, in part) 52 / 71 /
+// fewer take kernels of their own for the logits (head_stream_kernel) and dW (head_few_dweight_kernel); small heads, five
+// kernels one behind the other on few compute units.  Us, scoring / with both gradients, width 4096, 1 / 16 / 64 / 128 / 256 tokens on 32,000 (which lie in the caches from the call before, in part) 52 / 71 /
 // 70 / 84 / 109 and 158 / 177 / 202 / 240 / 322, on 128,256 216 / 266 / 249 / 276 / 286 and 661 / 723 / 721 / 888 / 1053.
 #include "head.hpp"
 

@@ -6,7 +6,7 @@
 // dy w: dx = rstd (g - mean(g) - xh mean(g xh)); dw = sum of dy xh, db = sum of dy over the rows: a group keeps
 // them in registers over the rows that it takes, and leaves its part in the workspace; a second launch joins the parts in their order.
 //
-// What bounds it: memory.  Forward, 16,384 rows of 8192 bf16 elements 80 us (6.7 TB/s), backward 138 (5.8 TB/s); a row of 4096 2.7 us, launch included.
+// What bounds it: memory.  Forward, 16,384 rows of 8192 bf16 elements 80 to 82 us (6.6 TB/s), backward 138 to 143 (5.7 TB/s); a row of 4096 2.7 us, launch included.
 #include "norm.hpp"
 
 #include <algorithm>

@@ -12,9 +12,9 @@
 // and LDS for the first fragments of the next, and multiplies the second half's: one barrier a step, and always 32 products
 // between a read and its use.
 //
-// What bounds it: power, and the matrix instructions.  In logits of 3840 x 65,536 x 8192 (bf16, 3.2 ms with their epilogue, 1.30 PFLOP/s; both gradients' products 1.35; a library's product of
-// that form reaches 1.55 alone, of the gradients' forms 1.40 and 1.20) the matrix units are at work for 65 % of the cycles, at 1.9 GHz; without loads 77 % at 2.06,
-// without reads of LDS or loads 83 % at 2.37.  Four wavefronts with parts of 128 x 128 (a third fewer reads of LDS) 2 % slower; loads earlier or later among the
+// What bounds it: power, and the matrix instructions.  In logits of 3686 x 128,256 x 8192 (bf16, 6.6 ms with their epilogue, 1.18 PFLOP/s; both gradients' products 1.30; a library's product of
+// that form reaches 1.55 alone, of the gradients' forms 1.35 and 1.17) the matrix units are at work for 62 % of the cycles, at 1.88 GHz, in the gradients for 68 % at 1.84; there LDS
+// works for 44 % of the cycles, 17 % of them all in conflicts between banks (logits: 24 and 0.1).  Four wavefronts with parts of 128 x 128 (a third fewer reads of LDS) 2 % slower; loads earlier or later among the
 // products, bands of 4 or 16 tiles, strides off the powers of two, a raised priority, reads sooner: within 2 % either way, or worse.
 #pragma once
 #include "fold.h"
@@ -45,7 +45,7 @@ template <Layout LAYOUT, int SIZE, int WAVES = kProductWaves>
 struct Operand {
     static constexpr int kLoads = SIZE / 8 / WAVES;  // of a wavefront a step, 1 KiB each
     // What a load brings lies together; between those of a kAcrossK tile, two rows each, 64 bytes are left free, and in odd rows the two
-    // halves of every 64 bytes are exchanged: the four rows that a transposing read of 16 lanes takes are in different banks.
+    // halves of every 64 bytes are exchanged: the four rows that a transposing read of 16 lanes takes are in different banks (not those of all 64 lanes).
     static constexpr uint32_t kChunk = LAYOUT == kAlongK ? 1024 : 1024 + 64;
     static constexpr uint32_t kBytes = WAVES * kLoads * kChunk;
     static constexpr uint32_t kRowBytes = LAYOUT == kAlongK ? kStepK * 2 : SIZE * 2;
