@@ -327,3 +327,34 @@ def test_binding_refuses_stats_in_host_memory_and_workspaces_that_only_look_larg
                  lambda: ff.ff_head_loss(b, f, ff.HeadStats("cpu"), one, stream=NOWHERE)):
         with pytest.raises(ValueError, match="workspace"):
             call()
+
+
+def test_every_refusal_with_addresses_of_their_own():
+    """One bad argument at a time, every array elsewhere."""
+    L, null, bad = ff.lib(), ff.FF_ERR_NULL, ff.FF_ERR_INVALID
+    P = [(k + 2) * A16 for k in range(10)]
+
+    def check(call, ok, nulls, invalid):
+        for name in nulls:
+            assert call(**dict(ok, **{name: None})) == null, name
+        for change in invalid:
+            assert call(**dict(ok, **change)) == bad, change
+
+    check(lambda x, n, width, stride, dtype, weight, bias, eps, y, y_stride, mean, rstd: L.ff_layer_norm(x, n, width, stride, dtype, weight, bias, eps, y, y_stride, mean, rstd, None),
+          dict(x=P[0], n=4, width=8, stride=8, dtype=ff.FF_F32, weight=P[1], bias=P[2], eps=1e-5, y=P[3], y_stride=8, mean=P[4], rstd=P[5]), ["x", "weight", "y"],
+          [dict(n=BIG), dict(width=0), dict(width=9), dict(width=ff.FF_NORM_MAX_WIDTH + 1, stride=1 << 20, y_stride=1 << 20), dict(stride=7), dict(y_stride=7), dict(dtype=0), dict(dtype=9),
+           dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(x=P[0], y=P[0], y_stride=16)] + [{k: P[9] + 2} for k in ("x", "weight", "bias", "y", "mean", "rstd")])
+    check(lambda x, n, width, stride, dtype, weight, mean, rstd, dy, dy_stride, dx, dx_stride, dw, db, ws:
+          L.ff_layer_norm_grad(x, n, width, stride, dtype, weight, mean, rstd, dy, dy_stride, dx, dx_stride, dw, db, ws, None),
+          dict(x=P[0], n=4, width=8, stride=8, dtype=ff.FF_F32, weight=P[1], mean=P[2], rstd=P[3], dy=P[4], dy_stride=8, dx=P[5], dx_stride=8, dw=P[6], db=P[7], ws=P[8]),
+          ["x", "weight", "mean", "rstd", "dy", "dx", "ws"],
+          [dict(n=BIG), dict(width=0), dict(stride=7), dict(dy_stride=7), dict(dx_stride=7), dict(dtype=3, width=9), dict(dx=P[0], dx_stride=16), dict(dx=P[4], dx_stride=16), dict(ws=P[8] + 8)] +
+          [{k: P[9] + 2} for k in ("x", "weight", "mean", "rstd", "dy", "dx", "dw", "db")])
+
+    def loss(logp, dh, dh_stride, dw, dw_stride, stats, ws, **batch):
+        return L.ff_head_loss(ctypes.byref(_batch(**dict(dict(hidden=P[0], weight=P[1], targets=P[2], weights=P[3]), **batch))), logp, dh, dh_stride, dw, dw_stride, stats, ws, None)
+
+    check(loss, dict(logp=P[4], dh=P[5], dh_stride=64, dw=P[6], dw_stride=64, stats=P[7], ws=P[8]), ["hidden", "weight", "targets", "weights", "logp", "stats", "ws"],
+          [dict(hidden=P[9] + 1), dict(weight=P[9] + 1), dict(targets=P[9] + 4), dict(weights=P[9] + 2), dict(logp=P[9] + 2), dict(dh=P[9] + 1), dict(dw=P[9] + 1), dict(stats=P[9] + 4),
+           dict(ws=P[9] + 128), dict(dh_stride=63), dict(dw_stride=63), dict(dh=P[0], dh_stride=72), dict(hidden_stride=63), dict(weight_stride=63), dict(reserved=1), dict(loss_scale=0.0),
+           dict(loss_scale=NAN), dict(dtype=ff.FF_F32), dict(vocab=0), dict(width=0), dict(n_tokens=ff.FF_HEAD_MAX_TOKENS + 1), dict(vocab=ff.FF_HEAD_MAX_VOCAB + 1)])
